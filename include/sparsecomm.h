@@ -209,6 +209,68 @@ int sc_step_apply(sc_ctx* ctx, int scheme, int W, const float* grads, float* res
 int sc_step_host(sc_ctx* ctx, int scheme, int W, const float* h_grads, float* residuals, size_t n,
                  const sc_segment* segs, int nseg, const uint64_t* h_seeds, float* h_out, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------
+ * Layer operators: a linear layer whose activations are kept in 8 bits between its forward and its backward
+ * pass.  They produce the gradient rows that the calls above compress: the weight and bias gradients are fp32
+ * and are written (or added) straight into a worker's row, at any element offset.
+ *
+ *     forward        z = x W^T + b,  y = act(z) + residual        x [M, K], W [N, K], z and y [M, N]
+ *     checkpoints    8 bits an element of x and z, instead of 16
+ *     backward       dz = dy * act'(z^),  db = column sums of dz
+ *                    dx = dz W,           dW = dz^T x^            ^: the value that the checkpoint holds
+ *
+ * Matrices are rows of the stated length, `ld` elements apart (ld >= the row's length; any value, any base
+ * aligned to its element; 16-byte aligned rows are the fast case).  Everything is computed in fp32 from the 16-bit
+ * inputs and rounded once, to the type of the output.  Empty sizes are allowed: no rows or columns, nothing is
+ * written; an empty sum is 0.  Sizes are below 2^31.  Unless a call says otherwise outputs alias no input.
+ *
+ * Checkpoint of a matrix [rows, cols]: q, rows * cols int8, and scales, rows * ceil(cols / 32) bytes, both dense.
+ * Each run of 32 elements of a row has one scale 2^e, stored as e + 127: e is the least exponent with
+ * m <= 127 * 2^e for the largest finite magnitude m of the run, within [-126, 122] (SC_F16: [-24, 10]);
+ * q = x 2^-e rounded to the nearest integer, ties to even, and within +-127 (+-63 where e is the largest of its range).
+ * An element that is not finite is kept as q = -128, which reads as NaN.  The value q * 2^e is exactly a value of
+ * the type, so what reads a checkpoint adds no rounding of its own.
+ * --------------------------------------------------------------------------------------------------------- */
+enum { SC_BF16 = 0, SC_F16 = 1, SC_F32 = 2 /* checkpoints only */ };
+enum { SC_ACT_NONE = 0, SC_ACT_RELU = 1, SC_ACT_GELU = 2 /* z Phi(z) */,
+       SC_ACT_GELU_TANH = 3 /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */, SC_ACT_SILU = 4 /* z / (1 + e^-z) */ };
+
+/* The layer operators keep their workspace in the context.  A call that needs more than it has allocates
+ * (synchronous), or returns SC_ERR_WORKSPACE while its stream is being captured.  sc_layer_reserve allocates
+ * ahead what any layer call of at most these sizes needs. */
+int sc_layer_reserve(sc_ctx* ctx, size_t M, size_t N, size_t K);
+
+/* Checkpoint of x, and the values of a checkpoint (rounded to `type` where the checkpoint was made from another). */
+int sc_checkpoint_pack(sc_ctx* ctx, int type, const void* x, size_t ldx, size_t rows, size_t cols,
+                       int8_t* q, uint8_t* scales, void* stream);
+int sc_checkpoint_unpack(sc_ctx* ctx, int type, const int8_t* q, const uint8_t* scales, size_t rows, size_t cols,
+                         void* out, size_t ldo, void* stream);
+
+/* dz = dy * act'(z^) with z^ the checkpoint (q, scales) of the pre-activation, and db[cols] = column sums of dz
+ * before its rounding (accumulate: added to db).  dz or db may be NULL; dz may be dy.  With SC_ACT_NONE the
+ * checkpoint is not read: the call gives the bias gradient of dy. */
+int sc_activation_grad(sc_ctx* ctx, int type, int act, const void* dy, size_t lddy, const int8_t* q, const uint8_t* scales,
+                       size_t rows, size_t cols, void* dz, size_t lddz, float* db, int accumulate, void* stream);
+
+/* y = act(x W^T + bias) + residual.  bias[N] and residual [M, N] are of the type and may be NULL; y may be residual
+ * (same ld).  With q and scales the checkpoint of z = x W^T + bias, taken from its fp32 values, is written too. */
+int sc_linear(sc_ctx* ctx, int type, int act, const void* x, size_t ldx, const void* w, size_t ldw, const void* bias,
+              const void* residual, size_t ldr, size_t M, size_t N, size_t K, void* y, size_t ldy,
+              int8_t* q, uint8_t* scales, void* stream);
+
+/* dx = (dz W + residual) * act'(z^): the gradient of the layer's input, plus a residual branch's gradient [M, K]
+ * (NULL: none), through the activation that made that input (SC_ACT_NONE, or z^ [M, K] as q and scales).  dx may be
+ * residual (same ld). */
+int sc_linear_grad_input(sc_ctx* ctx, int type, int act, const void* dz, size_t lddz, const void* w, size_t ldw,
+                         const void* residual, size_t ldr, const int8_t* q, const uint8_t* scales,
+                         size_t M, size_t N, size_t K, void* dx, size_t lddx, void* stream);
+
+/* dW = dz^T x in fp32, rows of lddw (accumulate: added to dW).  The layer's input is given once: as x, or as its
+ * checkpoint (q, scales) with x NULL. */
+int sc_linear_grad_weight(sc_ctx* ctx, int type, const void* dz, size_t lddz, const void* x, size_t ldx,
+                          const int8_t* q, const uint8_t* scales, size_t M, size_t N, size_t K,
+                          float* dw, size_t lddw, int accumulate, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -15,13 +15,21 @@ import torch
 SC_TOPK, SC_RANDK, SC_RANDBLOCK, SC_RANDBLOCK_WRAP = 0, 1, 2, 3
 SCHEMES = {"topk": SC_TOPK, "randk": SC_RANDK, "randblock": SC_RANDBLOCK, "randblock_wrap": SC_RANDBLOCK_WRAP}
 
+SC_BF16, SC_F16, SC_F32 = 0, 1, 2
+SC_ACT_NONE, SC_ACT_RELU, SC_ACT_GELU, SC_ACT_GELU_TANH, SC_ACT_SILU = 0, 1, 2, 3, 4
+ACTIVATIONS = {"none": SC_ACT_NONE, "relu": SC_ACT_RELU, "gelu": SC_ACT_GELU, "gelu_tanh": SC_ACT_GELU_TANH, "silu": SC_ACT_SILU}
+CHECKPOINT_GROUP = 32
+_TYPES = {torch.bfloat16: SC_BF16, torch.float16: SC_F16, torch.float32: SC_F32}
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsparsecomm.so")
 
 EXPORTS = ["sc_create", "sc_destroy", "sc_strerror", "sc_sync_status", "sc_set_gamma", "sc_scratch_bytes", "sc_launch_count",
            "sc_topk_path_counts", "sc_topk_path_detail", "sc_debug_set_poll_limits", "sc_debug_wait_probe", "sc_profile", "sc_profile_kinds", "sc_profile_name", "sc_profile_read",
            "sc_compress", "sc_compress_batch", "sc_aggregate", "sc_aggregate_shared", "sc_aggregate_static", "sc_aggregate_apply",
-           "sc_aggregate_apply_shared", "sc_step", "sc_step_apply", "sc_step_host"]
+           "sc_aggregate_apply_shared", "sc_step", "sc_step_apply", "sc_step_host",
+           "sc_layer_reserve", "sc_checkpoint_pack", "sc_checkpoint_unpack", "sc_activation_grad", "sc_linear", "sc_linear_grad_input",
+           "sc_linear_grad_weight"]
 
 
 class ScSegment(ctypes.Structure):
@@ -99,6 +107,16 @@ def load_library() -> ctypes.CDLL:
     lib.sc_step_host.argtypes = [vp, ci, ci, vp, vp, sz, ctypes.POINTER(ScSegment), ci, ctypes.POINTER(u64),
                                  vp, vp]
     lib.sc_step_host.restype = ci
+    lib.sc_layer_reserve.argtypes = [vp, sz, sz, sz]
+    lib.sc_checkpoint_pack.argtypes = [vp, ci, vp, sz, sz, sz, vp, vp, vp]
+    lib.sc_checkpoint_unpack.argtypes = [vp, ci, vp, vp, sz, sz, vp, sz, vp]
+    lib.sc_activation_grad.argtypes = [vp, ci, ci, vp, sz, vp, vp, sz, sz, vp, sz, vp, ci, vp]
+    lib.sc_linear.argtypes = [vp, ci, ci, vp, sz, vp, sz, vp, vp, sz, sz, sz, sz, vp, sz, vp, vp, vp]
+    lib.sc_linear_grad_input.argtypes = [vp, ci, ci, vp, sz, vp, sz, vp, sz, vp, vp, sz, sz, sz, vp, sz, vp]
+    lib.sc_linear_grad_weight.argtypes = [vp, ci, vp, sz, vp, sz, vp, vp, sz, sz, sz, vp, sz, ci, vp]
+    for name in ("sc_layer_reserve", "sc_checkpoint_pack", "sc_checkpoint_unpack", "sc_activation_grad", "sc_linear",
+                 "sc_linear_grad_input", "sc_linear_grad_weight"):
+        getattr(lib, name).restype = ci
     _lib = lib
     return lib
 
@@ -137,6 +155,46 @@ def _check(code: int, what: str) -> None:
 def _want(t: torch.Tensor, dtype, name: str, cuda: bool = True) -> None:
     if t.dtype != dtype or not t.is_contiguous() or (cuda and not t.is_cuda):
         raise TypeError(f"{name}: expected a contiguous {'CUDA ' if cuda else ''}{dtype} tensor")
+
+
+def _matrix(t: torch.Tensor, rows: int, cols: int, dtype, name: str) -> int:
+    """Checks a CUDA matrix [rows, cols] whose rows are contiguous; returns the distance between rows in elements."""
+    if t.dtype != dtype or not t.is_cuda or t.dim() != 2:
+        raise TypeError(f"{name}: expected a 2-D CUDA {dtype} tensor")
+    if t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name}: expected shape {(rows, cols)}, got {tuple(t.shape)}")
+    ld, step = t.stride()
+    if (step != 1 and cols > 1) or (ld < cols and rows > 1):
+        raise TypeError(f"{name}: the last dimension must be contiguous and rows must not overlap")
+    return max(ld, cols)
+
+
+def _vector(t: torch.Tensor, n: int, dtype, name: str) -> None:
+    _want(t, dtype, name)
+    if t.numel() != n:
+        raise ValueError(f"{name}: expected {n} elements, got {t.numel()}")
+
+
+def _kept(q, scales, rows: int, cols: int) -> None:
+    """Checks a checkpoint of a [rows, cols] matrix."""
+    if q is None or scales is None:
+        raise ValueError("q and scales: a checkpoint is both or neither")
+    _vector(q, rows * cols, torch.int8, "q")
+    _vector(scales, rows * -(-cols // CHECKPOINT_GROUP), torch.uint8, "scales")
+
+
+def _layer_type(t: torch.Tensor, name: str, f32: bool = False) -> int:
+    if t.dtype not in _TYPES or (t.dtype == torch.float32 and not f32):
+        raise TypeError(f"{name}: expected bfloat16 or float16{' or float32' if f32 else ''}, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected a matrix, got shape {tuple(t.shape)}")
+    return _TYPES[t.dtype]
+
+
+def checkpoint_buffers(rows: int, cols: int, device="cuda"):
+    """(q, scales) for the 8-bit checkpoint of a [rows, cols] matrix."""
+    return (torch.empty(rows, cols, dtype=torch.int8, device=device),
+            torch.empty(rows, -(-cols // CHECKPOINT_GROUP), dtype=torch.uint8, device=device))
 
 
 STATIC_MAX_N, STATIC_MAX_W = 1 << 24, 64
@@ -304,3 +362,93 @@ class Context:
             raise ValueError("buffer sizes do not match W and n")
         _check(self._lib.sc_step_host(self._h, scheme, W, _ptr(h_grads), _ptr(residuals), n, _segments(segs),
                                       len(segs), _seeds(seeds), _ptr(h_out), _stream(stream)), "sc_step_host")
+
+    # -- layer operators ---------------------------------------------------------
+    def sc_layer_reserve(self, M: int, N: int, K: int) -> None:
+        """Allocates ahead the workspace of layer calls of at most these sizes (before a stream capture, for instance)."""
+        _check(self._lib.sc_layer_reserve(self._h, M, N, K), "sc_layer_reserve")
+
+    def sc_checkpoint_pack(self, x, q, scales, stream=None) -> None:
+        """q, scales <- the 8-bit checkpoint of x [rows, cols] (bfloat16, float16 or float32)."""
+        kind = _layer_type(x, "x", f32=True)
+        rows, cols = x.shape
+        ldx = _matrix(x, rows, cols, x.dtype, "x")
+        _kept(q, scales, rows, cols)
+        _check(self._lib.sc_checkpoint_pack(self._h, kind, _ptr(x), ldx, rows, cols, _ptr(q), _ptr(scales), _stream(stream)),
+               "sc_checkpoint_pack")
+
+    def sc_checkpoint_unpack(self, q, scales, out, stream=None) -> None:
+        """out [rows, cols] <- the values that a checkpoint holds."""
+        kind = _layer_type(out, "out", f32=True)
+        rows, cols = out.shape
+        ldo = _matrix(out, rows, cols, out.dtype, "out")
+        _kept(q, scales, rows, cols)
+        _check(self._lib.sc_checkpoint_unpack(self._h, kind, _ptr(q), _ptr(scales), rows, cols, _ptr(out), ldo, _stream(stream)),
+               "sc_checkpoint_unpack")
+
+    def sc_activation_grad(self, act: int, dy, q, scales, dz, db=None, accumulate: bool = False, stream=None) -> None:
+        """dz <- dy * act'(z^), db <- (db +) column sums of dz; z^ is the checkpoint (q, scales), unused for SC_ACT_NONE.
+        dz or db may be None; dz may be dy."""
+        kind = _layer_type(dy, "dy")
+        rows, cols = dy.shape
+        lddy = _matrix(dy, rows, cols, dy.dtype, "dy")
+        if act != SC_ACT_NONE:
+            _kept(q, scales, rows, cols)
+        lddz = cols if dz is None else _matrix(dz, rows, cols, dy.dtype, "dz")
+        if db is not None:
+            _vector(db, cols, torch.float32, "db")
+        _check(self._lib.sc_activation_grad(self._h, kind, act, _ptr(dy), lddy, _ptr(q), _ptr(scales), rows, cols, _ptr(dz), lddz,
+                                            _ptr(db), 1 if accumulate else 0, _stream(stream)), "sc_activation_grad")
+
+    def sc_linear(self, act: int, x, w, y, bias=None, residual=None, q=None, scales=None, stream=None) -> None:
+        """y [M, N] <- act(x W^T + bias) + residual, x [M, K], w [N, K]; q, scales <- the checkpoint of x W^T + bias."""
+        kind = _layer_type(x, "x")
+        M, K = x.shape
+        ldx = _matrix(x, M, K, x.dtype, "x")
+        if w.dim() != 2:
+            raise ValueError("w: expected a matrix")
+        N = w.shape[0]
+        ldw = _matrix(w, N, K, x.dtype, "w")
+        ldy = _matrix(y, M, N, x.dtype, "y")
+        if bias is not None:
+            _vector(bias, N, x.dtype, "bias")
+        ldr = N if residual is None else _matrix(residual, M, N, x.dtype, "residual")
+        if q is not None or scales is not None:
+            _kept(q, scales, M, N)
+        _check(self._lib.sc_linear(self._h, kind, act, _ptr(x), ldx, _ptr(w), ldw, _ptr(bias), _ptr(residual), ldr, M, N, K,
+                                   _ptr(y), ldy, _ptr(q), _ptr(scales), _stream(stream)), "sc_linear")
+
+    def sc_linear_grad_input(self, dz, w, dx, residual=None, act: int = SC_ACT_NONE, q=None, scales=None, stream=None) -> None:
+        """dx [M, K] <- (dz W + residual) * act'(z^), dz [M, N], w [N, K], z^ [M, K] the checkpoint below the layer."""
+        kind = _layer_type(dz, "dz")
+        M, N = dz.shape
+        lddz = _matrix(dz, M, N, dz.dtype, "dz")
+        if w.dim() != 2:
+            raise ValueError("w: expected a matrix")
+        K = w.shape[1]
+        ldw = _matrix(w, N, K, dz.dtype, "w")
+        lddx = _matrix(dx, M, K, dz.dtype, "dx")
+        ldr = K if residual is None else _matrix(residual, M, K, dz.dtype, "residual")
+        if act != SC_ACT_NONE:
+            _kept(q, scales, M, K)
+        _check(self._lib.sc_linear_grad_input(self._h, kind, act, _ptr(dz), lddz, _ptr(w), ldw, _ptr(residual), ldr, _ptr(q), _ptr(scales),
+                                              M, N, K, _ptr(dx), lddx, _stream(stream)), "sc_linear_grad_input")
+
+    def sc_linear_grad_weight(self, dz, dw, x=None, q=None, scales=None, accumulate: bool = False, stream=None) -> None:
+        """dw [N, K] fp32 <- (dw +) dz^T x, dz [M, N]; the layer's input is given as x [M, K] or as its checkpoint (q, scales)."""
+        kind = _layer_type(dz, "dz")
+        M, N = dz.shape
+        lddz = _matrix(dz, M, N, dz.dtype, "dz")
+        if dw.dim() != 2:
+            raise ValueError("dw: expected a matrix")
+        K = dw.shape[1]
+        lddw = _matrix(dw, N, K, torch.float32, "dw")
+        if (x is None) == (q is None):
+            raise ValueError("the layer's input is given once: as x, or as a checkpoint")
+        ldx = K
+        if x is not None:
+            ldx = _matrix(x, M, K, dz.dtype, "x")
+        else:
+            _kept(q, scales, M, K)
+        _check(self._lib.sc_linear_grad_weight(self._h, kind, _ptr(dz), lddz, _ptr(x), ldx, _ptr(q), _ptr(scales), M, N, K,
+                                               _ptr(dw), lddw, 1 if accumulate else 0, _stream(stream)), "sc_linear_grad_weight")

@@ -5,11 +5,12 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparsecomm.so")
-SOURCES = ["sc_api.cu"]
+SOURCES = ["sc_api.cu", "sc_layer.cu"]
 
 
 def _dependencies():
@@ -23,7 +24,7 @@ def _dependencies():
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-lineinfo",
     "-gencode", "arch=compute_100a,code=sm_100a",
-    "-Xcompiler", "-fPIC", "-shared",
+    "-Xcompiler", "-fPIC",
     # bit-exact fp32: no fast-math, denormals kept, IEEE division and square root
     "-ftz=false", "-prec-div=true", "-prec-sqrt=true",
 ]
@@ -46,14 +47,23 @@ def needs_build() -> bool:
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB
-    cmd = [_nvcc()] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + \
-          ["-o", LIB] + [os.path.join(CSRC, s) for s in SOURCES]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
+    # one nvcc per translation unit, side by side, then the link
+    with tempfile.TemporaryDirectory(prefix="sparsecomm_build_") as tmp:
+        objects = [os.path.join(tmp, os.path.splitext(src)[0] + ".o") for src in SOURCES]
+        flags = [_nvcc()] + NVCC_FLAGS
+        jobs = [subprocess.Popen(flags + (["-Xptxas", "-v"] if verbose else []) + ["-c", "-o", obj, os.path.join(CSRC, src)],
+                                 stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+                for src, obj in zip(SOURCES, objects)]
+        said = [job.communicate()[0] for job in jobs]
+        failed = any(job.returncode != 0 for job in jobs)
+        if not failed:
+            link = subprocess.run(flags + ["-shared", "-o", LIB] + objects, capture_output=True, text=True)
+            said.append(link.stdout + link.stderr)
+            failed = link.returncode != 0
+    if failed or verbose:
+        sys.stderr.write("".join(said))
+    if failed:
         raise RuntimeError("nvcc failed building libsparsecomm.so")
-    if verbose:
-        sys.stderr.write(res.stdout + res.stderr)
     return LIB
 
 

@@ -8,97 +8,11 @@
 #include <new>
 #include <vector>
 
-#include "../../include/sparsecomm.h"
 #include "sc_aggregate.cuh"
-#include "sc_common.cuh"
+#include "sc_context.cuh"
 #include "sc_random.cuh"
 #include "sc_topk_fallback.cuh"
 #include "sc_topk_tiny.cuh"
-
-using namespace sc;
-
-struct sc_ctx {
-    int device = 0;
-    int sm_count = 0;
-    size_t max_n = 0;
-    int max_W = 0, max_seg = 0;
-    size_t max_tiles_per_worker = 0;
-    size_t max_mask_words = 0;      // per seed group
-    size_t max_atiles = 0;
-    size_t scratch_bytes = 0;
-
-    SegEntry* d_segs = nullptr;
-    uint32_t* d_fast_list = nullptr;
-    uint32_t* d_tiny_list = nullptr;      // [max_segments]: short segments, the <= TINY_SMALL_MAX ones first
-    uint32_t tiny_small = 0, tiny_large = 0, tiny_large_max_n = 0;
-    int occ_tiny_small = 1;
-    uint32_t* d_lists = nullptr;     // tiles of the large segments | their pack groups (each max_tiles long)
-    uint32_t n_fast_tiles = 0, n_fast_groups = 0;
-    uint32_t* d_hist = nullptr;      // radix histograms of the fall-back (cleared by the fall-back kernel itself)
-    TopkState* d_state = nullptr;
-    unsigned long long* d_desc = nullptr;
-    unsigned long long* d_ticket = nullptr;
-    uint32_t* d_mask = nullptr;
-    uint32_t* d_bounds = nullptr;
-    uint32_t* d_offsets = nullptr;   // per seed group / worker: exclusive kept-count prefix over tiles
-    // sampled-bracket top-k path.  Everything that must start at zero in a top-k call lies in one block
-    // (one memset): counters and the barrier word, then the per-problem states, then the candidate histograms.
-    unsigned char* d_zero = nullptr;
-    size_t zero_bytes = 0;
-    FastState* d_fstate = nullptr;   // inside d_zero
-    uint32_t* d_sample = nullptr;
-    uint2* d_cand = nullptr;
-    uint2* d_list2 = nullptr;
-    uint32_t* d_tile_sure = nullptr;
-    uint32_t* d_tile_csum = nullptr;
-    uint32_t* d_tile_cbase = nullptr;
-    uint32_t* d_tile_ccnt = nullptr;
-    uint32_t* d_tile_fbase = nullptr;
-    uint32_t* d_tile_fcnt = nullptr;
-    uint32_t* d_tile_tie = nullptr;
-    size_t max_main_grid = 0;            // CTAs of the top-k pass in the build chosen for the current table
-    size_t main_grid_v[2] = {0, 0};      // [0]: three CTAs per SM, [1]: the two-CTA build
-    int main_wide = 0;                   // 1: the current table uses the two-CTA build
-    uint2* d_flagged = nullptr;      // grown on demand: its size depends on k
-    size_t flagged_slots = 0;
-    size_t max_fast_per_worker = 0, max_cand_per_worker = 0;
-    uint32_t last_topk_problems = 0; // (worker, segment) pairs of the most recent top-k call
-    uint32_t max_sample_m = 0, fast_big = 0, fast_huge = 0;   // of the fast list: the first fast_huge are long segments, the first fast_big have large samples
-    float gamma = 1.0f;                  // step size of the accumulate line (sc_set_gamma)
-    int occ_main = 1, occ_main_wide = 1, occ_emit_v[4] = {1, 1, 1, 1}, occ_fallback = 1, occ_filter = 1;
-    uint32_t lookback_poll_limit = LOOKBACK_POLL_LIMIT, barrier_poll_limit = BARRIER_POLL_LIMIT;
-    uint64_t* d_seeds = nullptr;
-    int* d_status = nullptr;
-
-    std::vector<sc_segment> cached_segs;
-    size_t cached_n = 0;
-    bool layout_valid = false;
-    Layout layout{};
-
-    uint32_t epoch = 0;
-    uint64_t launches = 0;
-
-    int occ_pack_mask = 1, occ_block = 1, occ_agg = 1, occ_agg_big = 1, occ_agg_warp = 1;
-    int occ_agg_fine[5] = {1, 1, 1, 1, 1};
-
-    // optional per-kernel timing (sc_profile)
-    bool prof_on = false;
-    struct ProfRec { int kind; cudaEvent_t a, b; };
-    std::vector<ProfRec> prof_recs;
-    std::vector<cudaEvent_t> prof_free;
-
-    // host-buffer entry point
-    float* d_stage_grads = nullptr;
-    float* d_stage_vals = nullptr;
-    uint32_t* d_stage_idx = nullptr;
-    float* d_stage_out = nullptr;
-    size_t stage_grads_elems = 0, stage_msg_elems = 0, stage_out_elems = 0;
-    cudaStream_t copy_stream = nullptr;
-    cudaStream_t aux_stream = nullptr;   // short top-k segments run here, beside the large ones
-    cudaEvent_t ev_fork = nullptr, ev_join = nullptr;
-    cudaEvent_t ev_start = nullptr;
-    std::vector<cudaEvent_t> ev_worker;
-};
 
 // Top-k of segments below FAST_MIN_N elements runs with the segment in shared memory: one CTA per (worker,
 // segment) up to TINY_SMALL_MAX elements (the many very short tensors of a network keep several CTAs per SM),
@@ -110,66 +24,6 @@ constexpr uint32_t TINY_SMALL_MAX = 4096;        // elements: 16 KB of shared me
 constexpr double EMIT_MAX_8 = 12.0, EMIT_MAX_16 = 80.0, EMIT_MAX_32 = 200.0;
 
 namespace {
-
-#define SC_CUDA(call)                                   \
-    do {                                                \
-        cudaError_t err__ = (call);                     \
-        if (err__ != cudaSuccess) return SC_ERR_CUDA;   \
-    } while (0)
-
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-template <typename T>
-int dev_alloc(sc_ctx* c, T** p, size_t count) {
-    size_t bytes = std::max<size_t>(count, 1) * sizeof(T);
-    if (cudaMalloc(reinterpret_cast<void**>(p), bytes) != cudaSuccess) { *p = nullptr; return SC_ERR_WORKSPACE; }
-    c->scratch_bytes += bytes;
-    return SC_OK;
-}
-
-class DeviceGuard {
-  public:
-    explicit DeviceGuard(int dev) { cudaGetDevice(&prev_); if (prev_ != dev) { cudaSetDevice(dev); set_ = true; } }
-    ~DeviceGuard() { if (set_) cudaSetDevice(prev_); }
-  private:
-    int prev_ = 0;
-    bool set_ = false;
-};
-
-enum { KIND_SCATTER = 0, KIND_MASK_COUNT, KIND_ROW_SCAN, KIND_RANDK_PACK, KIND_RANDBLOCK, KIND_AGG_BOUNDS, KIND_AGG_TILES,
-       KIND_AGG_WARP, KIND_AGG_FINE, KIND_AGG_APPLY, KIND_TINY, KIND_BRACKET, KIND_MAIN, KIND_FILTER, KIND_FINISH, KIND_RESOLVE_SMALL, KIND_EMIT,
-       KIND_FALLBACK, KIND_COUNT };
-const char* const kKindNames[KIND_COUNT] = {"randk_scatter", "mask_count", "row_scan", "randk_pack", "randblock", "agg_bounds",
-                                            "agg_tiles", "agg_warp", "agg_fine", "agg_apply", "topk_tiny", "topk_bracket",
-                                            "topk_main", "topk_filter", "topk_finish", "topk_resolve_small", "topk_emit", "topk_fallback"};
-
-// Counts a kernel launch and, when profiling is on, brackets it with two events.
-class Launch {
-  public:
-    Launch(sc_ctx* c, int kind, cudaStream_t st) : c_(c), st_(st) {
-        ++c->launches;
-        if (!c->prof_on) return;
-        rec_.kind = kind;
-        rec_.a = take(); rec_.b = take();
-        if (rec_.a && rec_.b) { cudaEventRecord(rec_.a, st_); on_ = true; }
-    }
-    ~Launch() {
-        if (!on_) return;
-        cudaEventRecord(rec_.b, st_);
-        c_->prof_recs.push_back(rec_);
-    }
-  private:
-    cudaEvent_t take() {
-        if (!c_->prof_free.empty()) { cudaEvent_t e = c_->prof_free.back(); c_->prof_free.pop_back(); return e; }
-        cudaEvent_t e = nullptr;
-        if (cudaEventCreate(&e) != cudaSuccess) return nullptr;
-        return e;
-    }
-    sc_ctx* c_;
-    cudaStream_t st_;
-    sc_ctx::ProfRec rec_{};
-    bool on_ = false;
-};
 
 // Validates the segment table and (re)builds the device copy when it changed.
 int prepare_layout(sc_ctx* c, size_t n, const sc_segment* segs, int nseg, cudaStream_t stream) {
@@ -727,6 +581,7 @@ int sc_create(sc_ctx** out, size_t max_n, int max_W, int max_segments) {
         return SC_ERR_CUDA;
     }
     c->max_n = max_n; c->max_W = max_W; c->max_seg = max_segments;
+    c->lookback_poll_limit = LOOKBACK_POLL_LIMIT; c->barrier_poll_limit = BARRIER_POLL_LIMIT;
     c->max_tiles_per_worker = (max_n + 31 + TILE - 1) / TILE + (size_t)max_segments + 1;
     c->max_mask_words = (max_n + 31) / 32 + (size_t)max_segments;
     c->max_atiles = (max_n + ATILE - 1) / ATILE;
@@ -816,6 +671,7 @@ void sc_destroy(sc_ctx* c) {
     cudaFree(c->d_tile_ccnt); cudaFree(c->d_tile_fbase); cudaFree(c->d_tile_fcnt); cudaFree(c->d_tile_tie);
     cudaFree(c->d_flagged); cudaFree(c->d_seeds); cudaFree(c->d_status);
     cudaFree(c->d_stage_grads); cudaFree(c->d_stage_vals); cudaFree(c->d_stage_idx); cudaFree(c->d_stage_out);
+    cudaFree(c->d_layer);
     for (cudaEvent_t e : c->ev_worker) cudaEventDestroy(e);
     for (auto& r : c->prof_recs) { cudaEventDestroy(r.a); cudaEventDestroy(r.b); }
     for (cudaEvent_t e : c->prof_free) cudaEventDestroy(e);
