@@ -1,5 +1,6 @@
 // Host side of the layer operators declared in include/sparsecomm.h: argument checks, scratch, launches.
 #include <algorithm>
+#include <mutex>
 
 #include "sc_checkpoint.cuh"
 #include "sc_context.cuh"
@@ -91,17 +92,140 @@ GradPlan grad_plan(const sc_ctx* c, size_t rows, size_t cols) {
     return p;
 }
 
-template <typename T>
-void launch_product(int mode, const Operand& A, const Operand& B, size_t red, const Epilogue& ep, cudaStream_t st) {
-    const dim3 grid((uint32_t)ceil_div(ep.cols, 64), (uint32_t)ceil_div(ep.rows, 64));
-    if (mode == PRODUCT_FORWARD) product_plain_kernel<T, PRODUCT_FORWARD><<<grid, 256, 0, st>>>(A, B, red, ep);
-    else if (mode == PRODUCT_INPUT) product_plain_kernel<T, PRODUCT_INPUT><<<grid, 256, 0, st>>>(A, B, red, ep);
-    else product_plain_kernel<T, PRODUCT_WEIGHT><<<grid, 256, 0, st>>>(A, B, red, ep);
+// ---------------------------------------------------------------------------
+// matrix products
+// ---------------------------------------------------------------------------
+// A stored 16-bit matrix: `rows` rows of `cols` elements, `ld` apart.
+struct Stored { const void* p; uint64_t rows, cols, ld; };
+
+inline uint64_t round8(uint64_t n) { return (n + 7) & ~7ull; }
+inline bool tma_ready(const Stored& m) { return aligned(m.p, 16) && m.ld % 8 == 0; }
+inline size_t layout_bytes(uint64_t rows, uint64_t cols) { return (rows * round8(cols) * 2 + 255) & ~(size_t)255; }
+
+decltype(&cuTensorMapEncodeTiled) encode_fn() {
+    static decltype(&cuTensorMapEncodeTiled) fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) p = nullptr;
+        return reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(p);
+    }();
+    return fn;
 }
 
-void launch_product(int type, int mode, const Operand& A, const Operand& B, size_t red, const Epilogue& ep, cudaStream_t st) {
-    if (type == SC_BF16) launch_product<__nv_bfloat16>(mode, A, B, red, ep, st);
-    else launch_product<__half>(mode, A, B, red, ep, st);
+// Boxes of 64 elements (one 128-byte swizzled row) by `box_rows` rows; what lies outside the matrix reads as zero.
+bool tile_map(CUtensorMap* map, int type, const Stored& m, uint32_t box_rows) {
+    const auto fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {m.cols, m.rows}, strides[1] = {m.ld * 2};
+    const cuuint32_t box[2] = {64, box_rows}, steps[2] = {1, 1};
+    return fn(map, type == SC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(m.p), dims, strides, box,
+              steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+constexpr size_t PARTIAL_CAP = 64u << 20;      // bytes of partial sums a split product may use
+
+struct ProductPlan { int bn, cg; uint32_t splits; uint64_t part_ld; size_t bytes; };
+
+// Tile shape and number of parts by an estimate in SM cycles: waves of tiles, each a fixed cost plus its blocks of 64
+// reduction steps, and the partial sums' way to HBM and back.
+ProductPlan product_plan(const sc_ctx* c, uint64_t rows, uint64_t cols, uint64_t red) {
+    ProductPlan best{256, 1, 1, (cols + 31) & ~31ull, 0};
+    const uint64_t blocks = ceil_div(red, TC_STEP);
+    double best_cost = 0;
+    const uint32_t box = (uint32_t)std::min<uint64_t>(rows, TC_ROWS);
+    for (int shape = 0; shape < 4; ++shape) {                 // 256 x 256 by pairs, then 128 x 256, 128, 64
+        const int cg = shape == 0 ? 2 : 1, bn = shape == 0 ? 256 : 512 >> shape;
+        if (cg == 2 && rows <= TC_ROWS) continue;
+        const uint64_t tiles = ceil_div(rows, TC_ROWS * cg) * ceil_div(cols, bn), units = c->sm_count / cg;
+        const double block_cost = std::max((cg == 2 ? 2.0 : 2.3) * bn, (box + bn) * 128 / 40.0);
+        for (uint32_t s = 1; s <= blocks && s <= 64; ++s) {
+            const size_t bytes = s > 1 ? s * rows * best.part_ld * sizeof(float) : 0;
+            if (bytes > PARTIAL_CAP || (s > 1 && tiles * s > units * 2)) break;
+            const double cost = (double)ceil_div(tiles * s, units) * (1500.0 + bn * 6.0 + (double)ceil_div(blocks, s) * block_cost) +
+                                (s > 1 ? 4000.0 + 2.0 * bytes / 3400.0 : 0.0);
+            if (best_cost == 0 || cost < best_cost) { best_cost = cost; best.bn = bn; best.cg = cg; best.splits = s; best.bytes = bytes; }
+        }
+    }
+    return best;
+}
+
+template <typename T, int MODE, int BN, int CG>
+int launch_tiles(sc_ctx* c, const CUtensorMap& ma, const CUtensorMap& mb, const TcArgs& a, const Epilogue& ep, cudaStream_t st) {
+    static std::once_flag once;
+    static cudaError_t rc;
+    std::call_once(once, [] { rc = cudaFuncSetAttribute(product_kernel<T, MODE, BN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<BN, CG>::SMEM); });
+    if (rc != cudaSuccess) return SC_ERR_CUDA;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(CG * (uint32_t)std::min<uint64_t>((uint64_t)a.tiles * a.splits, c->sm_count / CG));
+    cfg.blockDim = dim3(TC_THREADS);
+    cfg.dynamicSmemBytes = TcShape<BN, CG>::SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim = {CG, 1, 1};
+    cfg.attrs = &attr;
+    cfg.numAttrs = CG == 2 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, product_kernel<T, MODE, BN, CG>, ma, mb, a, ep) == cudaSuccess ? SC_OK : SC_ERR_CUDA;
+}
+
+template <typename T, int MODE>
+int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red, const Epilogue& ep, size_t used, cudaStream_t st) {
+    constexpr bool A_MN = MODE == PRODUCT_WEIGHT, B_MN = MODE != PRODUCT_FORWARD;
+    const uint64_t chunks = 4 * ckpt_groups(ep.cols);
+    const uint32_t join_grid = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(ep.rows * chunks, 256), (uint64_t)c->sm_count * 8));
+    if (red == 0) {
+        Launch l(c, KIND_LAYER_JOIN, st);
+        product_join_kernel<T, MODE><<<join_grid, 256, 0, st>>>(nullptr, 0, 0, 0, ep);
+        return SC_OK;
+    }
+    const ProductPlan p = product_plan(c, ep.rows, ep.cols, red);
+    const uint64_t tiles = ceil_div(ep.rows, TC_ROWS * p.cg) * ceil_div(ep.cols, p.bn);
+    if (tiles * p.splits > 0x7FFFFFFFull) return SC_ERR_RANGE;
+    const size_t copy_a = tma_ready(A) ? 0 : layout_bytes(A.rows, A.cols), copy_b = tma_ready(B) ? 0 : layout_bytes(B.rows, B.cols);
+    if (const int rc = layer_scratch(c, used + p.bytes + copy_a + copy_b, st)) return rc;
+    unsigned char* at = c->d_layer ? c->d_layer + TICKET_BYTES + used : nullptr;
+    float* partial = reinterpret_cast<float*>(at);
+    at += p.bytes;
+    for (Stored* m : {&A, &B}) {
+        if (tma_ready(*m)) continue;
+        const uint32_t ldd = (uint32_t)round8(m->cols);
+        Launch l(c, KIND_LAYER_LAYOUT, st);
+        layout_kernel<<<(uint32_t)std::min<uint64_t>(ceil_div(m->rows * (ldd / 8), 256), (uint64_t)c->sm_count * 8), 256, 0, st>>>(
+            static_cast<const uint16_t*>(m->p), m->ld, m->rows, (uint32_t)m->cols, reinterpret_cast<uint16_t*>(at), ldd);
+        m->p = at; m->ld = ldd;
+        at += layout_bytes(m->rows, m->cols);
+    }
+    TcArgs a{};
+    a.tiles_i = (uint32_t)ceil_div(ep.rows, TC_ROWS * p.cg); a.tiles_j = (uint32_t)ceil_div(ep.cols, p.bn); a.tiles = (uint32_t)tiles;
+    a.splits = p.splits; a.blocks = (uint32_t)ceil_div(red, TC_STEP);
+    a.idesc = mma_idesc(TC_ROWS * p.cg, p.bn, type == SC_BF16, A_MN, B_MN);
+    a.a_box_rows = A_MN ? 64u : (uint32_t)std::min<uint64_t>(TC_ROWS, round8(ep.rows));
+    a.part_ld = (uint32_t)p.part_ld; a.part_stride = ep.rows * p.part_ld; a.partial = partial; a.status = c->d_status;
+    CUtensorMap ma, mb;
+    if (!tile_map(&ma, type, A, a.a_box_rows) || !tile_map(&mb, type, B, B_MN ? 64u : (uint32_t)(p.bn / p.cg))) return SC_ERR_CUDA;
+    {
+        Launch l(c, kind, st);
+        int rc;
+        if (p.cg == 2) rc = launch_tiles<T, MODE, 256, 2>(c, ma, mb, a, ep, st);
+        else if (p.bn == 256) rc = launch_tiles<T, MODE, 256, 1>(c, ma, mb, a, ep, st);
+        else if (p.bn == 128) rc = launch_tiles<T, MODE, 128, 1>(c, ma, mb, a, ep, st);
+        else rc = launch_tiles<T, MODE, 64, 1>(c, ma, mb, a, ep, st);
+        if (rc) return rc;
+    }
+    if (p.splits > 1) {
+        Launch l(c, KIND_LAYER_JOIN, st);
+        product_join_kernel<T, MODE><<<join_grid, 256, 0, st>>>(partial, p.splits, a.part_stride, a.part_ld, ep);
+    }
+    return SC_OK;
+}
+
+template <int MODE>
+int run_product(sc_ctx* c, int kind, int type, const Stored& A, const Stored& B, uint64_t red, const Epilogue& ep, size_t used, cudaStream_t st) {
+    // the weight gradient is fp32 whatever the operands are: one build serves both types
+    if constexpr (MODE != PRODUCT_WEIGHT)
+        if (type == SC_F16) return run_product<__half, MODE>(c, kind, type, A, B, red, ep, used, st);
+    return run_product<__nv_bfloat16, MODE>(c, kind, type, A, B, red, ep, used, st);
 }
 
 }  // namespace
@@ -112,7 +236,9 @@ int sc_layer_reserve(sc_ctx* ctx, size_t M, size_t N, size_t K) {
     if (!ctx) return SC_ERR_INVALID;
     if (M >= MAX_DIM || N >= MAX_DIM || K >= MAX_DIM) return SC_ERR_RANGE;
     DeviceGuard guard(ctx->device);
-    const size_t bytes = 2 * M * K + std::max(grad_plan(ctx, std::max<size_t>(M, 1), std::max<size_t>(N, 1)).bytes, grad_plan(ctx, std::max<size_t>(M, 1), std::max<size_t>(K, 1)).bytes);
+    const size_t grad = M && N && K ? std::max(grad_plan(ctx, M, N).bytes, grad_plan(ctx, M, K).bytes) : 0;
+    const size_t x = layout_bytes(M, K), w = K % 8 ? layout_bytes(N, K) : 0, z = N % 8 ? layout_bytes(M, N) : 0;
+    const size_t bytes = std::max(grad, PARTIAL_CAP + x + w + z);
     return layer_scratch(ctx, bytes, nullptr);
 }
 
@@ -204,8 +330,9 @@ int sc_linear(sc_ctx* ctx, int type, int act, const void* x, size_t ldx, const v
     Epilogue ep{};
     ep.bias = bias; ep.residual = residual; ep.ldr = ldr; ep.out = y; ep.ldo = ldy; ep.rows = M; ep.cols = (uint32_t)N;
     ep.q = reinterpret_cast<uint8_t*>(q); ep.scales = scales; ep.groups = (uint32_t)ckpt_groups(N); ep.act = act;
-    { Launch l(ctx, KIND_LINEAR, st);
-      launch_product(type, PRODUCT_FORWARD, Operand{x, ldx, 1}, Operand{w, ldw, 1}, K, ep, st); }
+    ep.vec_out = N % 8 == 0 && aligned(y, 16) && ldy % 8 == 0; ep.vec_res = N % 8 == 0 && aligned(residual, 16) && ldr % 8 == 0;
+    ep.vec_q = N % 8 == 0 && aligned(q, 8);
+    if (const int rc = run_product<PRODUCT_FORWARD>(ctx, KIND_LINEAR, type, Stored{x, M, K, ldx}, Stored{w, N, K, ldw}, K, ep, 0, st)) return rc;
     SC_CUDA(cudaGetLastError());
     return SC_OK;
 }
@@ -230,8 +357,9 @@ int sc_linear_grad_input(sc_ctx* ctx, int type, int act, const void* dz, size_t 
         ep.scales = const_cast<uint8_t*>(scales);
         ep.groups = (uint32_t)ckpt_groups(K);
     }
-    { Launch l(ctx, KIND_LINEAR_DX, st);
-      launch_product(type, PRODUCT_INPUT, Operand{dz, lddz, 1}, Operand{w, 1, ldw}, N, ep, st); }
+    ep.vec_out = K % 8 == 0 && aligned(dx, 16) && lddx % 8 == 0; ep.vec_res = K % 8 == 0 && aligned(residual, 16) && ldr % 8 == 0;
+    ep.vec_q = K % 8 == 0 && aligned(q, 8);
+    if (const int rc = run_product<PRODUCT_INPUT>(ctx, KIND_LINEAR_DX, type, Stored{dz, M, N, lddz}, Stored{w, N, K, ldw}, N, ep, 0, st)) return rc;
     SC_CUDA(cudaGetLastError());
     return SC_OK;
 }
@@ -248,18 +376,21 @@ int sc_linear_grad_weight(sc_ctx* ctx, int type, const void* dz, size_t lddz, co
     if (q && !scales) return SC_ERR_INVALID;
     DeviceGuard guard(ctx->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (q && M) {
-        if (const int rc = layer_scratch(ctx, 2 * M * K, st)) return rc;
-        void* wide = ctx->d_layer + TICKET_BYTES;
-        const uint8_t* qb = reinterpret_cast<const uint8_t*>(q);
-        if (type == SC_BF16) launch_unpack<__nv_bfloat16>(ctx, qb, scales, M, K, wide, K, st);
-        else launch_unpack<__half>(ctx, qb, scales, M, K, wide, K, st);
-        x = wide; ldx = K;
-    }
     Epilogue ep{};
     ep.out = dw; ep.ldo = lddw; ep.rows = N; ep.cols = (uint32_t)K; ep.accumulate = accumulate ? 1u : 0u;
-    { Launch l(ctx, KIND_LINEAR_DW, st);
-      launch_product(type, PRODUCT_WEIGHT, Operand{dz, 1, lddz}, Operand{x, 1, ldx}, M, ep, st); }
+    ep.vec_out = K % 8 == 0 && aligned(dw, 16) && lddw % 4 == 0;
+    size_t used = 0;
+    if (q && M) {                                  // the checkpoint's values, rows 16-byte aligned
+        used = layout_bytes(M, K);
+        const Stored dzs{dz, M, N, lddz};
+        if (const int rc = layer_scratch(ctx, used + product_plan(ctx, N, K, M).bytes + (tma_ready(dzs) ? 0 : layout_bytes(M, N)), st)) return rc;
+        void* wide = ctx->d_layer + TICKET_BYTES;
+        const uint8_t* qb = reinterpret_cast<const uint8_t*>(q);
+        if (type == SC_BF16) launch_unpack<__nv_bfloat16>(ctx, qb, scales, M, K, wide, round8(K), st);
+        else launch_unpack<__half>(ctx, qb, scales, M, K, wide, round8(K), st);
+        x = wide; ldx = round8(K);
+    }
+    if (const int rc = run_product<PRODUCT_WEIGHT>(ctx, KIND_LINEAR_DW, type, Stored{dz, M, N, lddz}, Stored{x, M, K, ldx}, M, ep, used, st)) return rc;
     SC_CUDA(cudaGetLastError());
     return SC_OK;
 }

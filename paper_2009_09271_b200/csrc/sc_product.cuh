@@ -3,7 +3,9 @@
 //   input grad    dx = (dz W + residual) * act'(z^)       A = dz [M, N],  B = W^T [K, N],  r over N
 //   weight grad   dW (+)= dz^T x^                         A = dz^T [N, M], B = x^T [K, M], r over M
 #pragma once
+#include "sc_checkpoint.cuh"
 #include "sc_layer_common.cuh"
+#include "sc_tcgen05.cuh"
 
 namespace sc {
 
@@ -19,101 +21,376 @@ struct Epilogue {
     uint32_t cols, groups;
     int act;
     uint32_t accumulate;
+    uint32_t vec_out, vec_res, vec_q;      // 16-byte (q: 8-byte) accesses are aligned and 8 columns never straddle a row's end
 };
 
-// Operand with any strides, element (i, r) at i * si + r * sr.
-struct Operand {
-    const void* p;
-    uint64_t si, sr;
-};
-
+// What follows the product for 8 columns from c0 of one row.  All 32 lanes of a warp call it; four neighbouring lanes hold
+// 32 consecutive columns of one row, from a multiple of 32, so they share a checkpoint group.
 template <typename T, int MODE>
-__global__ void __launch_bounds__(256) product_plain_kernel(Operand A, Operand B, uint64_t red, Epilogue ep) {
-    constexpr int TILE_I = 64, TILE_J = 64, STEP = 16;
-    __shared__ float sa[STEP][TILE_I + 4], sb[STEP][TILE_J + 4];
-    const uint64_t i0 = (uint64_t)blockIdx.y * TILE_I;
-    const uint32_t j0 = blockIdx.x * TILE_J;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const T* a = static_cast<const T*>(A.p);
-    const T* b = static_cast<const T*>(B.p);
-    float acc[4][4] = {}, sum[4][4] = {};                // a long sum is kept as a sum of sums of 256 products
-    for (uint64_t r0 = 0; r0 < red; r0 += STEP) {
-        for (int t = threadIdx.x; t < TILE_I * STEP; t += 256) {
-            // the index that is contiguous in memory runs fastest over the threads
-            const int i = A.sr == 1 ? t / STEP : t % TILE_I, r = A.sr == 1 ? t % STEP : t / TILE_I;
-            const int j = B.sr == 1 ? t / STEP : t % TILE_J, s = B.sr == 1 ? t % STEP : t / TILE_J;
-            sa[r][i] = i0 + i < ep.rows && r0 + r < red ? Elem<T>::to_float(a[(i0 + i) * A.si + (r0 + r) * A.sr]) : 0.0f;
-            sb[s][j] = j0 + j < ep.cols && r0 + s < red ? Elem<T>::to_float(b[(uint64_t)(j0 + j) * B.si + (r0 + s) * B.sr]) : 0.0f;
+__device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint32_t c0, float v[8]) {
+    const bool in = row < ep.rows && c0 < ep.cols;
+    if constexpr (MODE == PRODUCT_WEIGHT) {
+        if (!in) return;
+        float* out = static_cast<float*>(ep.out) + row * ep.ldo + c0;
+        if (ep.vec_out) {
+            float4* o = reinterpret_cast<float4*>(out);
+            float4 a = make_float4(v[0], v[1], v[2], v[3]), b = make_float4(v[4], v[5], v[6], v[7]);
+            if (ep.accumulate) {
+                const float4 x = o[0], y = o[1];
+                a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+                b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
+            }
+            o[0] = a; o[1] = b;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c0 + i < ep.cols) out[i] = ep.accumulate ? out[i] + v[i] : v[i];
         }
-        __syncthreads();
+    } else {
+        float res[8] = {};
+        if (in && ep.residual) to_floats(load8(static_cast<const T*>(ep.residual) + row * ep.ldr, c0, ep.cols, ep.vec_res), res);
+        if constexpr (MODE == PRODUCT_FORWARD) {
+            if (in && ep.bias) {
+                float b[8];
+                to_floats(load8(static_cast<const T*>(ep.bias), c0, ep.cols, 0u), b);
 #pragma unroll
-        for (int r = 0; r < STEP; ++r) {
-            float va[4], vb[4];
+                for (int i = 0; i < 8; ++i) v[i] += b[i];
+            }
+            if (ep.q) {
+                uint32_t m = 0;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) { va[u] = sa[r][ty * 4 + u]; vb[u] = sb[r][tx * 4 + u]; }
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t a = __float_as_uint(v[i]) & 0x7FFFFFFFu;
+                    if (c0 + i < ep.cols && a < 0x7F800000u) m = max(m, a);
+                }
+                m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+                m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+                const int e = ckpt_exponent<T>(m);
+                const float inv = pow2(-e), most = e == Elem<T>::EMAX ? 63.0f : 127.0f;
+                if (in) {
+                    uint32_t b[8];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+                    for (int i = 0; i < 8; ++i) b[i] = ckpt_byte_any(v[i], inv, most);
+                    uint8_t* q = ep.q + row * ep.cols + c0;
+                    if (ep.vec_q) {
+                        uint2 o;
+                        o.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+                        o.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+                        *reinterpret_cast<uint2*>(q) = o;
+                    } else {
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[u][v] = fmaf(va[u], vb[v], acc[u][v]);
-        }
-        __syncthreads();
-        if ((r0 + STEP) % 256 == 0 || r0 + STEP >= red) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) { sum[u][v] += acc[u][v]; acc[u][v] = 0.0f; }
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const uint64_t i = i0 + ty * 4 + u;
-        const uint32_t j = j0 + tx * 4;
-        float z[4];
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            z[v] = sum[u][v];
-            if (i >= ep.rows || j + v >= ep.cols) continue;
-            if constexpr (MODE == PRODUCT_WEIGHT) {
-                float* dw = static_cast<float*>(ep.out) + i * ep.ldo + j + v;
-                *dw = ep.accumulate ? *dw + z[v] : z[v];
-            } else {
-                const T* res = ep.residual ? static_cast<const T*>(ep.residual) + i * ep.ldr + j + v : nullptr;
-                T* out = static_cast<T*>(ep.out) + i * ep.ldo + j + v;
-                if constexpr (MODE == PRODUCT_FORWARD) {
-                    if (ep.bias) z[v] += Elem<T>::to_float(static_cast<const T*>(ep.bias)[j + v]);
-                    float y = activation(ep.act, z[v]);
-                    if (res) y += Elem<T>::to_float(*res);
-                    *out = Elem<T>::from_float(y);
-                } else {
-                    if (res) z[v] += Elem<T>::to_float(*res);
-                    if (ep.q) {
-                        const uint32_t b = ep.q[i * ep.cols + j + v];
-                        float k[4];
-                        ckpt_values4(b, ckpt_scale(ep.scales[i * ep.groups + ((j + v) >> 5)]), k);
-                        z[v] *= activation_slope(ep.act, k[0]);
+                        for (int i = 0; i < 8; ++i) if (c0 + i < ep.cols) q[i] = (uint8_t)b[i];
                     }
-                    *out = Elem<T>::from_float(z[v]);
+                    if ((c0 & 31u) == 0u) ep.scales[row * ep.groups + (c0 >> 5)] = (uint8_t)(e + 127);
                 }
             }
-        }
-        if constexpr (MODE == PRODUCT_FORWARD) {
-            if (!ep.q) continue;
-            uint32_t m = 0;                                   // eight lanes hold a group
+            if (!in) return;
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const uint32_t k = __float_as_uint(z[v]) & 0x7FFFFFFFu;
-                if (j + v < ep.cols && k < 0x7F800000u) m = max(m, k);
+            for (int i = 0; i < 8; ++i) v[i] = activation(ep.act, v[i]) + res[i];
+        } else {
+            if (!in) return;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += res[i];
+            if (ep.q) {
+                const uint2 k = load_q8(ep.q + row * ep.cols, c0, ep.cols, ep.vec_q);
+                const float s = ckpt_scale(ep.scales[row * ep.groups + (c0 >> 5)]);
+                float z[8];
+                ckpt_values4(k.x, s, z);
+                ckpt_values4(k.y, s, z + 4);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= activation_slope(ep.act, z[i]);
             }
-#pragma unroll
-            for (int d = 1; d < 8; d <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-            const int e = ckpt_exponent<T>(m);
-            const float inv = pow2(-e), most = e == Elem<T>::EMAX ? 63.0f : 127.0f;
-            if (i >= ep.rows) continue;
-#pragma unroll
-            for (int v = 0; v < 4; ++v)
-                if (j + v < ep.cols) ep.q[i * ep.cols + j + v] = (uint8_t)ckpt_byte_any(z[v], inv, most);
-            if ((tx & 7) == 0 && j < ep.cols) ep.scales[i * ep.groups + (j >> 5)] = (uint8_t)(e + 127);
         }
+        store8(static_cast<T*>(ep.out) + row * ep.ldo, c0, ep.cols, ep.vec_out, v);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The product on the 5th-generation tensor cores
+// ---------------------------------------------------------------------------
+// CTAs (CG = 1) or pairs of CTAs that share one matrix instruction (CG = 2) walk output tiles of 128 CG x BN; each CTA of
+// a pair holds 128 rows of A, half of B's rows, and the accumulator of its own 128 output rows.  A producer warp streams
+// 64-deep slices of both operands into a ring of shared-memory stages by TMA (128-byte swizzle; edges are filled with
+// zeros), one thread issues the matrix instructions into one of two accumulators in TMEM, and eight warps empty the
+// other one: they move 32 x 32 blocks through shared memory so that what they read and write in HBM is contiguous
+// along rows.
+//
+// The tensor cores add to an fp32 accumulator by cutting, not rounding: measured, a sum of n steps of 16 products comes
+// out about n 2^-24 of its size too small (2e-7 after 256 products, 9e-6 after 8192, 4e-5 after 32768 of random sign).  A
+// 16-bit result does not see that.  The weight gradient is fp32, so its accumulators are emptied every CHUNK = 4 blocks
+// (256 products) and added up in registers, with rounding.
+constexpr int TC_ROWS = 128, TC_STEP = 64, TC_THREADS = 384, TC_EPI_WARPS = 8, TC_CHUNK = 4;
+constexpr uint32_t TC_SMEM_LIMIT = 232448;
+
+template <int BN, int CG>
+struct TcShape {
+    static constexpr int B_ROWS = BN / CG;
+    static constexpr uint32_t A_BYTES = TC_ROWS * TC_STEP * 2, B_BYTES = B_ROWS * TC_STEP * 2, STAGE = A_BYTES + B_BYTES;
+    static constexpr uint32_t STAGING = TC_EPI_WARPS * 32 * 32 * 4;
+    static constexpr int STAGES = (TC_SMEM_LIMIT - 1024 - 256 - STAGING) / STAGE > 8 ? 8 : (TC_SMEM_LIMIT - 1024 - 256 - STAGING) / STAGE;
+    static constexpr uint32_t SMEM = STAGES * STAGE + STAGING + 1024 + 256;
+    static constexpr uint32_t TMEM_COLS = 2 * BN;
+};
+
+struct TcArgs {
+    uint32_t tiles_i, tiles_j, tiles;      // output tiles
+    uint32_t splits;                       // parts of the reduction; more than one: fp32 partial sums go to `partial`
+    uint32_t blocks;                       // reduction blocks of 64
+    uint32_t idesc, a_box_rows;
+    uint64_t part_stride;                  // elements between two parts
+    uint32_t part_ld;
+    float* partial;
+    int* status;
+};
+
+// Tiles in groups of 8 rows of tiles, down the rows first, so that the tiles in flight share operands in L2.
+__device__ __forceinline__ void tile_at(const TcArgs& a, uint32_t t, uint32_t& ti, uint32_t& tj) {
+    const uint32_t per = 8 * a.tiles_j, g = t / per, first = g * 8, high = min(8u, a.tiles_i - first), in = t - g * per;
+    ti = first + in % high;
+    tj = in / high;
+}
+
+// One 32 x 32 block, thread t holding row t, to its place.  The 16-byte units of a row are permuted by its number, which
+// makes both directions free of bank conflicts.
+template <typename T, int MODE>
+__device__ __forceinline__ void block_out(const TcArgs& a, const Epilogue& ep, uint32_t stage_addr, const uint32_t (&v)[32], uint64_t row0, uint32_t col0,
+                                          uint32_t split) {
+    const uint32_t lane = threadIdx.x & 31u;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage_addr + lane * 128 + ((u ^ (lane & 7)) * 16)),
+                     "r"(v[4 * u]), "r"(v[4 * u + 1]), "r"(v[4 * u + 2]), "r"(v[4 * u + 3]) : "memory");
+    }
+    __syncwarp();
+    const uint32_t c0 = col0 + (lane & 3u) * 8;
+    constexpr int UNROLL = MODE == PRODUCT_WEIGHT ? 1 : 4;     // the weight gradient's sums leave few registers
+#pragma unroll UNROLL
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t r = (lane >> 2) + 8 * i, u = (lane & 3u) * 2;
+        float f[8];
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3])
+                     : "r"(stage_addr + r * 128 + ((u ^ (r & 7)) * 16)) : "memory");
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7])
+                     : "r"(stage_addr + r * 128 + (((u + 1) ^ (r & 7)) * 16)) : "memory");
+        if (a.splits == 1) {
+            epilogue8<T, MODE>(ep, row0 + r, c0, f);
+        } else if (row0 + r < ep.rows && c0 < ep.cols) {
+            float4* p = reinterpret_cast<float4*>(a.partial + split * a.part_stride + (row0 + r) * a.part_ld + c0);
+            p[0] = make_float4(f[0], f[1], f[2], f[3]);
+            p[1] = make_float4(f[4], f[5], f[6], f[7]);
+        }
+    }
+    __syncwarp();
+}
+
+template <typename T, int MODE, int BN, int CG>
+__global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                                TcArgs a, Epilogue ep) {
+    using S = TcShape<BN, CG>;
+    constexpr bool A_MN = MODE == PRODUCT_WEIGHT, B_MN = MODE != PRODUCT_FORWARD;
+    constexpr bool SUM = MODE == PRODUCT_WEIGHT;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
+    const uint32_t staging = base + S::STAGES * S::STAGE;
+    const uint32_t bars = staging + S::STAGING;
+    const uint32_t full = bars, empty = bars + 8 * S::STAGES, tfull = empty + 8 * S::STAGES, tempty = tfull + 16, slot = tempty + 16;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
+    const uint32_t first = blockIdx.x / CG, step = gridDim.x / CG;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::STAGES; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(tfull + 8 * s, 1); mbar_init(tempty + 8 * s, TC_EPI_WARPS * CG); }
+        mbar_init_fence();
+        tma_prefetch_map(&map_a);
+        tma_prefetch_map(&map_b);
+    }
+    if (warp == 2) tmem_alloc<CG>(slot, S::TMEM_COLS);
+    tcgen05_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync();
+    tcgen05_fence_after();
+    uint32_t tmem;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+
+    const uint32_t work = a.tiles * a.splits;
+    if (warp < 4) {
+        bool ok = true;
+        if (warp == 0 && lane == 0) {
+            // in a pair the first CTA's barriers count the bytes of both
+            const uint32_t bytes = CG * ((A_MN ? S::A_BYTES : a.a_box_rows * TC_STEP * 2) + S::B_BYTES);
+            uint32_t stage = 0, phase = 0, issued = 0;
+            for (uint32_t w = first; w < work && ok; w += step) {
+                const uint32_t split = w / a.tiles;
+                uint32_t ti, tj;
+                tile_at(a, w - split * a.tiles, ti, tj);
+                const uint32_t k0 = (uint64_t)a.blocks * split / a.splits, k1 = (uint64_t)a.blocks * (split + 1) / a.splits;
+                const int32_t i0 = (int32_t)((ti * CG + rank) * TC_ROWS), j0 = (int32_t)(tj * BN + rank * S::B_ROWS);
+                for (uint32_t k = k0; k < k1; ++k) {
+                    if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1u))) break;
+                    const uint32_t sa = base + stage * S::STAGE, sb = sa + S::A_BYTES;
+                    if (rank == 0) mbar_expect_tx(full + 8 * stage, bytes);
+                    const uint32_t bar = CG == 2 ? map_to_rank(full + 8 * stage, 0) : full + 8 * stage;
+                    const int32_t r = (int32_t)(k * TC_STEP);
+                    if constexpr (A_MN) {
+#pragma unroll
+                        for (int c = 0; c < TC_ROWS; c += 64) tma_load_2d<CG>(sa + c * TC_STEP * 2, &map_a, bar, i0 + c, r);
+                    } else {
+                        tma_load_2d<CG>(sa, &map_a, bar, r, i0);
+                    }
+                    if constexpr (B_MN) {
+#pragma unroll
+                        for (int c = 0; c < S::B_ROWS; c += 64) tma_load_2d<CG>(sb + c * TC_STEP * 2, &map_b, bar, j0 + c, r);
+                    } else {
+                        tma_load_2d<CG>(sb, &map_b, bar, r, j0);
+                    }
+                    ++issued;
+                    if (++stage == S::STAGES) { stage = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok) {                     // the copies in flight land before the CTA ends (two seconds have passed since the last)
+                atomicCAS(a.status, 0, ST_TIMEOUT);
+                if (rank == 0)
+                    for (uint32_t n = issued > (uint32_t)S::STAGES ? issued - S::STAGES : 0; n < issued; ++n)
+                        mbar_wait(full + 8 * (n % S::STAGES), (n / S::STAGES) & 1u);
+            }
+        } else if (warp == 1 && lane == 0 && rank == 0) {
+            uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+            for (uint32_t w = first; w < work && ok; w += step) {
+                const uint32_t split = w / a.tiles;
+                const uint32_t k0 = (uint64_t)a.blocks * split / a.splits, k1 = (uint64_t)a.blocks * (split + 1) / a.splits;
+                for (uint32_t c0 = k0; c0 < k1 && ok;) {
+                    const uint32_t c1 = SUM ? min(c0 + TC_CHUNK, k1) : k1;
+                    if (!(ok = mbar_wait(tempty + 8 * acc, acc_phase ^ 1u))) break;
+                    tcgen05_fence_after();
+                    for (uint32_t k = c0; k < c1; ++k) {
+                        if (!(ok = mbar_wait(full + 8 * stage, phase))) break;
+                        tcgen05_fence_after();
+                        const uint32_t sa = base + stage * S::STAGE, sb = sa + S::A_BYTES;
+#pragma unroll
+                        for (int s = 0; s < TC_STEP / 16; ++s) {
+                            const uint64_t da = A_MN ? smem_desc(sa + s * 2048, TC_STEP * 128, 1024) : smem_desc(sa + s * 32, 16, 1024);
+                            const uint64_t db = B_MN ? smem_desc(sb + s * 2048, TC_STEP * 128, 1024) : smem_desc(sb + s * 32, 16, 1024);
+                            mma_f16<CG>(tmem + acc * BN, da, db, a.idesc, k > c0 || s > 0);
+                        }
+                        mma_commit<CG>(empty + 8 * stage);
+                        if (++stage == S::STAGES) { stage = 0; phase ^= 1u; }
+                    }
+                    mma_commit<CG>(tfull + 8 * acc);
+                    if ((acc ^= 1u) == 0) acc_phase ^= 1u;
+                    c0 = c1;
+                }
+            }
+            if (!ok) atomicCAS(a.status, 0, ST_TIMEOUT);
+        }
+        __syncwarp();
+    } else {
+        const uint32_t e = warp - 4, quarter = warp & 3u, half = e >> 2;
+        const uint32_t stage_addr = staging + e * 4096;
+        const uint32_t from = tmem + ((quarter * 32) << 16) + half * (BN / 2);
+        uint32_t acc = 0, acc_phase = 0;
+        bool ok = true;
+        for (uint32_t w = first; w < work && ok; w += step) {
+            const uint32_t split = w / a.tiles;
+            uint32_t ti, tj;
+            tile_at(a, w - split * a.tiles, ti, tj);
+            const uint64_t row0 = (uint64_t)(ti * CG + rank) * TC_ROWS + quarter * 32;
+            const uint32_t col0 = tj * BN + half * (BN / 2);
+            if constexpr (SUM) {
+                const uint32_t k0 = (uint64_t)a.blocks * split / a.splits, k1 = (uint64_t)a.blocks * (split + 1) / a.splits;
+                uint32_t sum[BN / 64][32];               // fp32, by their bits
+#pragma unroll
+                for (int c = 0; c < BN / 64; ++c)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) sum[c][i] = 0u;
+                for (uint32_t c0 = k0; c0 < k1; c0 += TC_CHUNK) {
+                    if (!(ok = mbar_wait(tfull + 8 * acc, acc_phase))) break;
+                    __syncwarp();
+                    tcgen05_fence_after();
+#pragma unroll
+                    for (int c = 0; c < BN / 32; ++c) {
+                        uint32_t v[16];
+                        tmem_load16(from + acc * BN + c * 16, v);
+                        tmem_load_wait(v);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            uint32_t& s = sum[c / 2][(c & 1) * 16 + i];
+                            s = __float_as_uint(__uint_as_float(s) + __uint_as_float(v[i]));
+                        }
+                    }
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_rank(tempty + 8 * acc, 0) : tempty + 8 * acc);
+                    if ((acc ^= 1u) == 0) acc_phase ^= 1u;
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int c = 0; c < BN / 64; ++c) block_out<T, MODE>(a, ep, stage_addr, sum[c], row0, col0 + c * 32, split);
+            } else {
+                if (!(ok = mbar_wait(tfull + 8 * acc, acc_phase))) break;
+                __syncwarp();
+                tcgen05_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < BN / 2; c += 32) {
+                    uint32_t v[32];
+                    tmem_load32(from + acc * BN + c, v);
+                    tmem_load_wait(v);
+                    if (c + 32 >= BN / 2) {             // this warp has taken all it needs from the accumulator
+                        tcgen05_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_rank(tempty + 8 * acc, 0) : tempty + 8 * acc);
+                    }
+                    block_out<T, MODE>(a, ep, stage_addr, v, row0, col0 + c, split);
+                }
+                if ((acc ^= 1u) == 0) acc_phase ^= 1u;
+            }
+        }
+        if (!ok && lane == 0) atomicCAS(a.status, 0, ST_TIMEOUT);
+        __syncwarp();
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync();
+    tcgen05_fence_after();
+    if (warp == 2) tmem_free<CG>(tmem, S::TMEM_COLS);
+}
+
+// Joins the parts of a split product in order and applies the epilogue; no parts at all is an empty sum.
+template <typename T, int MODE>
+__global__ void __launch_bounds__(256) product_join_kernel(const float* __restrict__ partial, uint32_t splits, uint64_t part_stride, uint32_t part_ld,
+                                                           Epilogue ep) {
+    const uint32_t chunks = 4 * ((ep.cols + 31) / 32);
+    const uint64_t total = ep.rows * chunks, stride = (uint64_t)gridDim.x * 256;
+    const uint32_t lane = threadIdx.x & 31u;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i - lane < total; i += stride) {
+        const uint64_t row = i < total ? i / chunks : ep.rows;
+        const uint32_t c0 = (uint32_t)(i - row * chunks) * 8;
+        float f[8] = {};
+        if (i < total && c0 < ep.cols) {
+            const float4* p = reinterpret_cast<const float4*>(partial + row * part_ld + c0);
+            for (uint32_t s = 0; s < splits; ++s, p += part_stride / 4) {
+                const float4 x = __ldcg(p), y = __ldcg(p + 1);
+                f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
+                f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
+            }
+        }
+        epilogue8<T, MODE>(ep, row, c0, f);
+    }
+}
+
+// Rows copied to a 16-byte aligned place with rows a multiple of 8 elements apart, where the tensor cores' loads can reach them.
+__global__ void __launch_bounds__(256) layout_kernel(const uint16_t* __restrict__ src, uint64_t ld, uint64_t rows, uint32_t cols,
+                                                     uint16_t* __restrict__ dst, uint32_t ldd) {
+    const uint32_t chunks = ldd / 8;
+    const uint64_t total = rows * chunks, stride = (uint64_t)gridDim.x * 256;
+    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += stride) {
+        const uint64_t row = i / chunks;
+        const uint32_t c0 = (uint32_t)(i - row * chunks) * 8;
+        uint16_t v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = c0 + k < cols ? src[row * ld + c0 + k] : (uint16_t)0;
+        *reinterpret_cast<uint4*>(dst + row * ldd + c0) =
+            make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16, v[6] | (uint32_t)v[7] << 16);
     }
 }
 
