@@ -100,38 +100,16 @@ __global__ void __launch_bounds__(CKPT_THREADS) checkpoint_pack_kernel(const T* 
             uint32_t m = abs_max8(raw[u]);
             m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
             m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-            int e = ckpt_exponent<T>(m);
             float f[8];
             to_floats(raw[u], f);
             uint32_t b[8];
-            if (m >= 0x7F800000u || e == Elem<T>::EMAX) {              // four lanes together
-                const uint32_t mask = 0xFu << (lane & ~3u);
-                m = 0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t a = __float_as_uint(f[i]) & 0x7FFFFFFFu;
-                    if (a < 0x7F800000u) m = max(m, a);
-                }
-                m = max(m, __shfl_xor_sync(mask, m, 1));
-                m = max(m, __shfl_xor_sync(mask, m, 2));
-                e = ckpt_exponent<T>(m);
-                const float inv = pow2(-e), most = e == Elem<T>::EMAX ? 63.0f : 127.0f;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) b[i] = ckpt_byte_any(f[i], inv, most);
-            } else {
-                const float inv = pow2(-e);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) b[i] = ckpt_byte(f[i], inv);
-            }
+            const int e = ckpt_encode8<T>(f, m, b);
             if (base + u * stride >= w.total) continue;
             const uint32_t c0 = it[u].chunk * 8;
             uint8_t* dst = q + it[u].row * w.cols + c0;
             if (w.vec) {
                 if (c0 < w.cols) {
-                    uint2 o;
-                    o.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-                    o.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
-                    __stcs(reinterpret_cast<uint2*>(dst), o);
+                    __stcs(reinterpret_cast<uint2*>(dst), ckpt_join8(b));
                 }
             } else {
 #pragma unroll
@@ -211,10 +189,9 @@ constexpr int GRAD_COLS = 256, GRAD_LANES = 8;
 struct GradArgs {
     uint64_t rows, lddy, lddz;
     uint32_t cols, groups, runs, run_rows, vec, accumulate;
-    int act;
 };
 
-template <typename T, bool KEPT>
+template <typename T, int ACT>
 __global__ void __launch_bounds__(CKPT_THREADS) activation_grad_kernel(const T* dy, const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales,
                                                                        GradArgs a, T* dz, float* __restrict__ partial,
                                                                        uint32_t* __restrict__ tickets, float* __restrict__ db) {
@@ -229,14 +206,14 @@ __global__ void __launch_bounds__(CKPT_THREADS) activation_grad_kernel(const T* 
             const Raw8<T> g = load8(dy + r * a.lddy, c0, a.cols, a.vec);
             float f[8];
             to_floats(g, f);
-            if constexpr (KEPT) {
+            if constexpr (ACT != SC_ACT_NONE) {
                 const uint2 k = load_q8(q + r * a.cols, c0, a.cols, a.vec);
                 const float s = ckpt_scale(scales[r * a.groups + (c0 >> 5)]);
                 float z[8];
                 ckpt_values4(k.x, s, z);
                 ckpt_values4(k.y, s, z + 4);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] *= activation_slope(a.act, z[i]);
+                for (int i = 0; i < 8; ++i) f[i] *= activation_slope<ACT>(z[i]);
             }
             if (dz) store8(dz + r * a.lddz, c0, a.cols, a.vec, f);
 #pragma unroll

@@ -154,7 +154,13 @@ template <typename T, int MODE, int BN, int CG>
 int launch_tiles(sc_ctx* c, const CUtensorMap& ma, const CUtensorMap& mb, const TcArgs& a, const Epilogue& ep, cudaStream_t st) {
     static std::once_flag once;
     static cudaError_t rc;
-    std::call_once(once, [] { rc = cudaFuncSetAttribute(product_kernel<T, MODE, BN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<BN, CG>::SMEM); });
+    std::call_once(once, [] {
+        cudaFuncAttributes f{};
+        rc = cudaFuncSetAttribute(product_kernel<T, MODE, BN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<BN, CG>::SMEM);
+        if (rc == cudaSuccess) rc = cudaFuncGetAttributes(&f, product_kernel<T, MODE, BN, CG>);
+        // a register split beyond the launch's total would wait for ever
+        if (rc == cudaSuccess && MODE == PRODUCT_WEIGHT && BN == 256 && f.numRegs < TC_LEAST_REGS) rc = cudaErrorInvalidDeviceFunction;
+    });
     if (rc != cudaSuccess) return SC_ERR_CUDA;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(CG * (uint32_t)std::min<uint64_t>((uint64_t)a.tiles * a.splits, c->sm_count / CG));
@@ -297,7 +303,7 @@ int sc_activation_grad(sc_ctx* ctx, int type, int act, const void* dy, size_t ld
     if (db) if (const int rc = layer_scratch(ctx, p.bytes, st)) return rc;
     GradArgs a{};
     a.rows = rows; a.lddy = lddy; a.lddz = lddz; a.cols = (uint32_t)cols; a.groups = (uint32_t)ckpt_groups(cols);
-    a.runs = p.runs; a.run_rows = p.run_rows; a.accumulate = accumulate ? 1u : 0u; a.act = act;
+    a.runs = p.runs; a.run_rows = p.run_rows; a.accumulate = accumulate ? 1u : 0u;
     a.vec = cols % 8 == 0 && aligned(dy, 16) && lddy % 8 == 0 && (!dz || (aligned(dz, 16) && lddz % 8 == 0)) && (!kept || aligned(q, 8)) ? 1u : 0u;
     float* partial = reinterpret_cast<float*>(ctx->d_layer ? ctx->d_layer + TICKET_BYTES : nullptr);
     uint32_t* tickets = reinterpret_cast<uint32_t*>(ctx->d_layer);
@@ -305,10 +311,14 @@ int sc_activation_grad(sc_ctx* ctx, int type, int act, const void* dy, size_t ld
     const uint8_t* qb = reinterpret_cast<const uint8_t*>(q);
     {
         Launch l(ctx, KIND_ACT_GRAD, st);
-#define SC_GRAD(T, KEPT) activation_grad_kernel<T, KEPT><<<grid, CKPT_THREADS, 0, st>>>( \
-            static_cast<const T*>(dy), qb, scales, a, static_cast<T*>(dz), partial, tickets, db)
-        if (type == SC_BF16) { if (kept) SC_GRAD(__nv_bfloat16, true); else SC_GRAD(__nv_bfloat16, false); }
-        else { if (kept) SC_GRAD(__half, true); else SC_GRAD(__half, false); }
+#define SC_GRAD(ACT)                                                                                                                   \
+        case ACT:                                                                                                                      \
+            if (type == SC_BF16) activation_grad_kernel<__nv_bfloat16, ACT><<<grid, CKPT_THREADS, 0, st>>>(                            \
+                static_cast<const __nv_bfloat16*>(dy), qb, scales, a, static_cast<__nv_bfloat16*>(dz), partial, tickets, db);          \
+            else activation_grad_kernel<__half, ACT><<<grid, CKPT_THREADS, 0, st>>>(                                                   \
+                static_cast<const __half*>(dy), qb, scales, a, static_cast<__half*>(dz), partial, tickets, db);                        \
+            break;
+        switch (act) { SC_GRAD(SC_ACT_NONE) SC_GRAD(SC_ACT_RELU) SC_GRAD(SC_ACT_GELU) SC_GRAD(SC_ACT_GELU_TANH) SC_GRAD(SC_ACT_SILU) }
 #undef SC_GRAD
     }
     SC_CUDA(cudaGetLastError());
@@ -331,7 +341,7 @@ int sc_linear(sc_ctx* ctx, int type, int act, const void* x, size_t ldx, const v
     ep.bias = bias; ep.residual = residual; ep.ldr = ldr; ep.out = y; ep.ldo = ldy; ep.rows = M; ep.cols = (uint32_t)N;
     ep.q = reinterpret_cast<uint8_t*>(q); ep.scales = scales; ep.groups = (uint32_t)ckpt_groups(N); ep.act = act;
     ep.vec_out = N % 8 == 0 && aligned(y, 16) && ldy % 8 == 0; ep.vec_res = N % 8 == 0 && aligned(residual, 16) && ldr % 8 == 0;
-    ep.vec_q = N % 8 == 0 && aligned(q, 8);
+    ep.vec_q = N % 8 == 0 && aligned(q, 8); ep.vec_bias = N % 8 == 0 && aligned(bias, 16);
     if (const int rc = run_product<PRODUCT_FORWARD>(ctx, KIND_LINEAR, type, Stored{x, M, K, ldx}, Stored{w, N, K, ldw}, K, ep, 0, st)) return rc;
     SC_CUDA(cudaGetLastError());
     return SC_OK;

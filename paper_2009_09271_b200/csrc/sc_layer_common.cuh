@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <type_traits>
 
 #include "../../include/sparsecomm.h"
 
@@ -51,35 +52,53 @@ template <> struct Elem<float> {
 constexpr float SQRT_HALF = 0.70710678118654752f, INV_SQRT_2PI = 0.39894228040143268f;
 constexpr float GELU_C = 1.5957691216057308f, GELU_A = 0.044715f;      // 2 sqrt(2 / pi), cubic coefficient
 
-__device__ __forceinline__ float logistic(float v) { return __fdividef(1.0f, 1.0f + __expf(-v)); }
+// 1 / (1 + 2^v): one exponential and one reciprocal, both within a few units of the last place.
+__device__ __forceinline__ float inv_1p_exp2(float v) {
+    float e, r;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(v));
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return r;
+}
+constexpr float LOG2E = 1.4426950408889634f;
 
-// (1 + tanh(u)) / 2 is the logistic function of 2 u, so the tanh form of gelu is z logistic(2 u).
-__device__ __forceinline__ float activation(int act, float z) {
+// Runs f(std::integral_constant<int, ACT>) for the activation `act`: the choice is made once for many elements.
+template <typename F>
+__device__ __forceinline__ void with_activation(int act, F&& f) {
     switch (act) {
-        case SC_ACT_RELU: return z < 0.0f ? 0.0f : z;                  // NaN passes
-        case SC_ACT_GELU: return 0.5f * z * (1.0f + erff(z * SQRT_HALF));
-        case SC_ACT_GELU_TANH: return z * logistic(GELU_C * (z + GELU_A * z * z * z));
-        case SC_ACT_SILU: return z * logistic(z);
-        default: return z;
+        case SC_ACT_RELU: f(std::integral_constant<int, SC_ACT_RELU>()); break;
+        case SC_ACT_GELU: f(std::integral_constant<int, SC_ACT_GELU>()); break;
+        case SC_ACT_GELU_TANH: f(std::integral_constant<int, SC_ACT_GELU_TANH>()); break;
+        case SC_ACT_SILU: f(std::integral_constant<int, SC_ACT_SILU>()); break;
+        default: f(std::integral_constant<int, SC_ACT_NONE>()); break;
     }
 }
 
+// (1 + tanh(u)) / 2 is the logistic function of 2 u, so the tanh form of gelu is z logistic(2 u).
+template <int ACT>
+__device__ __forceinline__ float activation(float z) {
+    if constexpr (ACT == SC_ACT_RELU) return z < 0.0f ? 0.0f : z;                  // NaN passes
+    else if constexpr (ACT == SC_ACT_GELU) return 0.5f * z * (1.0f + erff(z * SQRT_HALF));
+    else if constexpr (ACT == SC_ACT_GELU_TANH) return z * inv_1p_exp2(z * fmaf(-LOG2E * GELU_C * GELU_A, z * z, -LOG2E * GELU_C));
+    else if constexpr (ACT == SC_ACT_SILU) return z * inv_1p_exp2(-LOG2E * z);
+    else return z;
+}
+
 // Products with a logistic that has reached 0 or 1 take a bounded z: the limit is 0, never 0 * inf.
-__device__ __forceinline__ float activation_slope(int act, float z) {
-    switch (act) {
-        case SC_ACT_RELU: return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
-        case SC_ACT_GELU: return 0.5f * (1.0f + erff(z * SQRT_HALF)) + z * __expf(-0.5f * z * z) * INV_SQRT_2PI;
-        case SC_ACT_GELU_TANH: {
-            z = z > 64.0f ? 64.0f : (z < -64.0f ? -64.0f : z);         // NaN passes
-            const float s = logistic(GELU_C * (z + GELU_A * z * z * z));
-            return s + z * s * (1.0f - s) * (GELU_C + 3.0f * GELU_C * GELU_A * z * z);
-        }
-        case SC_ACT_SILU: {
-            const float s = logistic(z), b = z > 128.0f ? 128.0f : z;
-            return s + b * s * (1.0f - s);
-        }
-        default: return 1.0f;
-    }
+template <int ACT>
+__device__ __forceinline__ float activation_slope(float z) {
+    if constexpr (ACT == SC_ACT_RELU) return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
+    else if constexpr (ACT == SC_ACT_GELU) {
+        float e;
+        asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(-0.5f * LOG2E * z * z));
+        return fmaf(z * INV_SQRT_2PI, e, 0.5f * (1.0f + erff(z * SQRT_HALF)));
+    } else if constexpr (ACT == SC_ACT_GELU_TANH) {
+        z = z > 64.0f ? 64.0f : (z < -64.0f ? -64.0f : z);                         // NaN passes
+        const float zz = z * z, s = inv_1p_exp2(z * fmaf(-LOG2E * GELU_C * GELU_A, zz, -LOG2E * GELU_C));
+        return fmaf(s * z, (1.0f - s) * fmaf(3.0f * GELU_C * GELU_A, zz, GELU_C), s);
+    } else if constexpr (ACT == SC_ACT_SILU) {
+        const float s = inv_1p_exp2(-LOG2E * z), b = z > 128.0f ? 128.0f : z;
+        return fmaf(s * b, 1.0f - s, s);
+    } else return 1.0f;
 }
 
 // ---------------------------------------------------------------------------
@@ -99,6 +118,12 @@ __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)
 // |v| 2^-e <= 127 except where e has reached the type's largest, whose caller clamps.
 __device__ __forceinline__ uint32_t ckpt_byte(float v, float inv) { return __float_as_uint(fmaf(v, inv, 12582912.0f)) & 0xFFu; }
 
+// Bytes b[0..7] side by side.
+__device__ __forceinline__ uint2 ckpt_join8(const uint32_t b[8]) {
+    return make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
+                      __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
+}
+
 // The same for any v: not finite -> -128, which stands for NaN; |q| <= most.
 __device__ __forceinline__ uint32_t ckpt_byte_any(float v, float inv, float most) {
     if ((__float_as_uint(v) & 0x7FFFFFFFu) >= 0x7F800000u) return 0x80u;
@@ -116,6 +141,33 @@ __device__ __forceinline__ void ckpt_values4(uint32_t q4, float scale, float v[4
         for (int i = 0; i < 4; ++i)
             if (((u >> (8 * i)) & 0xFFu) == 0u) v[i] = __uint_as_float(0x7FFFFFFFu);
     }
+}
+
+// Eight elements of a group that four neighbouring lanes hold, `m` the largest magnitude of them all by its bits (values that
+// are not finite order above the others): their bytes and the group's exponent.  The four lanes call it together.
+template <typename T>
+__device__ __forceinline__ int ckpt_encode8(const float f[8], uint32_t m, uint32_t b[8]) {
+    int e = ckpt_exponent<T>(m);
+    if (m < 0x7F800000u && e != Elem<T>::EMAX) {
+        const float inv = pow2(-e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = ckpt_byte(f[i], inv);
+    } else {
+        const uint32_t mask = 0xFu << (threadIdx.x & 28u);
+        m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t a = __float_as_uint(f[i]) & 0x7FFFFFFFu;
+            if (a < 0x7F800000u) m = max(m, a);
+        }
+        m = max(m, __shfl_xor_sync(mask, m, 1));
+        m = max(m, __shfl_xor_sync(mask, m, 2));
+        e = ckpt_exponent<T>(m);
+        const float inv = pow2(-e), most = e == Elem<T>::EMAX ? 63.0f : 127.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) b[i] = ckpt_byte_any(f[i], inv, most);
+    }
+    return e;
 }
 
 __device__ __forceinline__ float ckpt_scale(uint32_t byte) { return __uint_as_float(byte << 23); }

@@ -21,13 +21,13 @@ struct Epilogue {
     uint32_t cols, groups;
     int act;
     uint32_t accumulate;
-    uint32_t vec_out, vec_res, vec_q;      // 16-byte (q: 8-byte) accesses are aligned and 8 columns never straddle a row's end
+    uint32_t vec_out, vec_res, vec_q, vec_bias;      // 16-byte (q: 8-byte) accesses are aligned and 8 columns never straddle a row's end
 };
 
 // What follows the product for 8 columns from c0 of one row.  All 32 lanes of a warp call it; four neighbouring lanes hold
-// 32 consecutive columns of one row, from a multiple of 32, so they share a checkpoint group.
-template <typename T, int MODE>
-__device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint32_t c0, float v[8]) {
+// 32 consecutive columns of one row, from a multiple of 32, so they share a checkpoint group.  `bias`: of these columns.
+template <typename T, int MODE, int ACT>
+__device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint32_t c0, const float bias[8], float v[8]) {
     const bool in = row < ep.rows && c0 < ep.cols;
     if constexpr (MODE == PRODUCT_WEIGHT) {
         if (!in) return;
@@ -50,33 +50,20 @@ __device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint
         float res[8] = {};
         if (in && ep.residual) to_floats(load8(static_cast<const T*>(ep.residual) + row * ep.ldr, c0, ep.cols, ep.vec_res), res);
         if constexpr (MODE == PRODUCT_FORWARD) {
-            if (in && ep.bias) {
-                float b[8];
-                to_floats(load8(static_cast<const T*>(ep.bias), c0, ep.cols, 0u), b);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] += b[i];
-            }
+            for (int i = 0; i < 8; ++i) v[i] += bias[i];
             if (ep.q) {
-                uint32_t m = 0;
+                uint32_t m = 0;                         // columns past the end hold zeros: no product, no bias
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint32_t a = __float_as_uint(v[i]) & 0x7FFFFFFFu;
-                    if (c0 + i < ep.cols && a < 0x7F800000u) m = max(m, a);
-                }
+                for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
                 m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
                 m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-                const int e = ckpt_exponent<T>(m);
-                const float inv = pow2(-e), most = e == Elem<T>::EMAX ? 63.0f : 127.0f;
+                uint32_t b[8];
+                const int e = ckpt_encode8<T>(v, m, b);
                 if (in) {
-                    uint32_t b[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) b[i] = ckpt_byte_any(v[i], inv, most);
                     uint8_t* q = ep.q + row * ep.cols + c0;
                     if (ep.vec_q) {
-                        uint2 o;
-                        o.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-                        o.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
-                        *reinterpret_cast<uint2*>(q) = o;
+                        *reinterpret_cast<uint2*>(q) = ckpt_join8(b);
                     } else {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) if (c0 + i < ep.cols) q[i] = (uint8_t)b[i];
@@ -86,23 +73,32 @@ __device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint
             }
             if (!in) return;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activation(ep.act, v[i]) + res[i];
+            for (int i = 0; i < 8; ++i) v[i] = activation<ACT>(v[i]) + res[i];
         } else {
             if (!in) return;
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += res[i];
-            if (ep.q) {
+            if constexpr (ACT != SC_ACT_NONE) {
                 const uint2 k = load_q8(ep.q + row * ep.cols, c0, ep.cols, ep.vec_q);
                 const float s = ckpt_scale(ep.scales[row * ep.groups + (c0 >> 5)]);
                 float z[8];
                 ckpt_values4(k.x, s, z);
                 ckpt_values4(k.y, s, z + 4);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] *= activation_slope(ep.act, z[i]);
+                for (int i = 0; i < 8; ++i) v[i] *= activation_slope<ACT>(z[i]);
             }
         }
         store8(static_cast<T*>(ep.out) + row * ep.ldo, c0, ep.cols, ep.vec_out, v);
     }
+}
+
+// The bias of 8 columns; zero past the end.
+template <typename T, int MODE>
+__device__ __forceinline__ void load_bias(const Epilogue& ep, uint32_t c0, float b[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) b[i] = 0.0f;
+    if constexpr (MODE == PRODUCT_FORWARD)
+        if (ep.bias && c0 < ep.cols) to_floats(load8(static_cast<const T*>(ep.bias), c0, ep.cols, ep.vec_bias), b);
 }
 
 // ---------------------------------------------------------------------------
@@ -119,7 +115,8 @@ __device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint
 // out about n 2^-24 of its size too small (2e-7 after 256 products, 9e-6 after 8192, 4e-5 after 32768 of random sign).  A
 // 16-bit result does not see that.  The weight gradient is fp32, so its accumulators are emptied every CHUNK = 4 blocks
 // (256 products) and added up in registers, with rounding.
-constexpr int TC_ROWS = 128, TC_STEP = 64, TC_THREADS = 384, TC_EPI_WARPS = 8, TC_CHUNK = 4;
+constexpr int TC_ROWS = 128, TC_STEP = 64, TC_THREADS = 384, TC_EPI_WARPS = 8, TC_CHUNK = 6;
+constexpr int TC_LEAST_REGS = 160;             // 160 x 384 >= 56 x 128 + 208 x 256, for builds that shift registers
 constexpr uint32_t TC_SMEM_LIMIT = 232448;
 
 template <int BN, int CG>
@@ -163,22 +160,53 @@ __device__ __forceinline__ void block_out(const TcArgs& a, const Epilogue& ep, u
     }
     __syncwarp();
     const uint32_t c0 = col0 + (lane & 3u) * 8;
-    constexpr int UNROLL = MODE == PRODUCT_WEIGHT ? 1 : 4;     // the weight gradient's sums leave few registers
-#pragma unroll UNROLL
-    for (int i = 0; i < 4; ++i) {
+    const auto fetch = [&](int i, float f[8]) {
         const uint32_t r = (lane >> 2) + 8 * i, u = (lane & 3u) * 2;
-        float f[8];
         asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3])
                      : "r"(stage_addr + r * 128 + ((u ^ (r & 7)) * 16)) : "memory");
         asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f[4]), "=f"(f[5]), "=f"(f[6]), "=f"(f[7])
                      : "r"(stage_addr + r * 128 + (((u + 1) ^ (r & 7)) * 16)) : "memory");
-        if (a.splits == 1) {
-            epilogue8<T, MODE>(ep, row0 + r, c0, f);
-        } else if (row0 + r < ep.rows && c0 < ep.cols) {
-            float4* p = reinterpret_cast<float4*>(a.partial + split * a.part_stride + (row0 + r) * a.part_ld + c0);
-            p[0] = make_float4(f[0], f[1], f[2], f[3]);
-            p[1] = make_float4(f[4], f[5], f[6], f[7]);
+        return row0 + r;
+    };
+    if (MODE == PRODUCT_WEIGHT || a.splits > 1) {
+        // fp32 goes out in whole 128-byte rows: eight lanes a row, four rows at a time
+        const bool part = a.splits > 1;
+        const uint32_t c = col0 + (lane & 7u) * 4;
+        const uint64_t ld = part ? a.part_ld : ep.ldo;
+        float* out = (part ? a.partial + split * a.part_stride : static_cast<float*>(ep.out)) + (row0 + (lane >> 3)) * ld + c;
+        const bool vec = part || ep.vec_out, add = !part && ep.accumulate;
+#pragma unroll 4
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t r = (lane >> 3) + 4 * i;
+            float4 f;
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
+                         : "r"(stage_addr + r * 128 + (((lane & 7u) ^ (r & 7u)) * 16)) : "memory");
+            float* o = out + (uint64_t)(4 * i) * ld;
+            if (row0 + r >= ep.rows || c >= ep.cols) continue;
+            if (vec) {
+                if (add) {
+                    const float4 x = *reinterpret_cast<const float4*>(o);
+                    f.x += x.x; f.y += x.y; f.z += x.z; f.w += x.w;
+                }
+                *reinterpret_cast<float4*>(o) = f;
+            } else {
+                const float v4[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (c + k < ep.cols) o[k] = add ? o[k] + v4[k] : v4[k];
+            }
         }
+    } else {
+        float bias[8];
+        load_bias<T, MODE>(ep, c0, bias);
+        with_activation(ep.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float f[8];
+                const uint64_t row = fetch(i, f);
+                epilogue8<T, MODE, decltype(act)::value>(ep, row, c0, bias, f);
+            }
+        });
     }
     __syncwarp();
 }
@@ -214,7 +242,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
 
     const uint32_t work = a.tiles * a.splits;
+    // The register sums of a 256-wide tile need more than an even share: of the registers that the CTA is
+    // launched with, four warps keep 56 a thread and eight get 208 (the host checks that the sum fits).
+    constexpr bool REGS = SUM && BN == 256;
     if (warp < 4) {
+        if constexpr (REGS) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         bool ok = true;
         if (warp == 0 && lane == 0) {
             // in a pair the first CTA's barriers count the bytes of both
@@ -255,26 +287,34 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                         mbar_wait(full + 8 * (n % S::STAGES), (n / S::STAGES) & 1u);
             }
         } else if (warp == 1 && lane == 0 && rank == 0) {
+            // The tensor pipe's queue holds about two instructions.  What the next block waits for is therefore looked at
+            // between the instructions of this one, never between its last and the next one's first.
             uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+            bool ready = false, vacant = false;            // seen: the next block's operands; the next accumulator empty
+            const uint64_t da0 = A_MN ? smem_desc(base, TC_STEP * 128, 1024) : smem_desc(base, 16, 1024);
+            const uint64_t db0 = B_MN ? smem_desc(base + S::A_BYTES, TC_STEP * 128, 1024) : smem_desc(base + S::A_BYTES, 16, 1024);
             for (uint32_t w = first; w < work && ok; w += step) {
                 const uint32_t split = w / a.tiles;
                 const uint32_t k0 = (uint64_t)a.blocks * split / a.splits, k1 = (uint64_t)a.blocks * (split + 1) / a.splits;
                 for (uint32_t c0 = k0; c0 < k1 && ok;) {
                     const uint32_t c1 = SUM ? min(c0 + TC_CHUNK, k1) : k1;
-                    if (!(ok = mbar_wait(tempty + 8 * acc, acc_phase ^ 1u))) break;
+                    if (!vacant && !(ok = mbar_wait(tempty + 8 * acc, acc_phase ^ 1u))) break;
+                    vacant = false;
                     tcgen05_fence_after();
                     for (uint32_t k = c0; k < c1; ++k) {
-                        if (!(ok = mbar_wait(full + 8 * stage, phase))) break;
+                        if (!ready && !(ok = mbar_wait(full + 8 * stage, phase))) break;
                         tcgen05_fence_after();
-                        const uint32_t sa = base + stage * S::STAGE, sb = sa + S::A_BYTES;
-#pragma unroll
-                        for (int s = 0; s < TC_STEP / 16; ++s) {
-                            const uint64_t da = A_MN ? smem_desc(sa + s * 2048, TC_STEP * 128, 1024) : smem_desc(sa + s * 32, 16, 1024);
-                            const uint64_t db = B_MN ? smem_desc(sb + s * 2048, TC_STEP * 128, 1024) : smem_desc(sb + s * 32, 16, 1024);
-                            mma_f16<CG>(tmem + acc * BN, da, db, a.idesc, k > c0 || s > 0);
-                        }
+                        const uint32_t next = stage + 1 == S::STAGES ? 0 : stage + 1, next_phase = next ? phase : phase ^ 1u;
+                        const uint64_t da = da0 + stage * (S::STAGE >> 4), db = db0 + stage * (S::STAGE >> 4);
+                        const uint32_t d = tmem + acc * BN;
+                        mma_f16<CG>(d, da, db, a.idesc, k > c0);
+                        mma_f16<CG>(d, da + (A_MN ? 128 : 2), db + (B_MN ? 128 : 2), a.idesc, true);
+                        if (k + 1 == c1) vacant = mbar_test(tempty + 8 * (acc ^ 1u), (acc ? acc_phase ^ 1u : acc_phase) ^ 1u);
+                        mma_f16<CG>(d, da + (A_MN ? 256 : 4), db + (B_MN ? 256 : 4), a.idesc, true);
+                        ready = mbar_test(full + 8 * next, next_phase);
+                        mma_f16<CG>(d, da + (A_MN ? 384 : 6), db + (B_MN ? 384 : 6), a.idesc, true);
                         mma_commit<CG>(empty + 8 * stage);
-                        if (++stage == S::STAGES) { stage = 0; phase ^= 1u; }
+                        stage = next; phase = next_phase;
                     }
                     mma_commit<CG>(tfull + 8 * acc);
                     if ((acc ^= 1u) == 0) acc_phase ^= 1u;
@@ -285,6 +325,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
         }
         __syncwarp();
     } else {
+        if constexpr (REGS) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         const uint32_t e = warp - 4, quarter = warp & 3u, half = e >> 2;
         const uint32_t stage_addr = staging + e * 4096;
         const uint32_t from = tmem + ((quarter * 32) << 16) + half * (BN / 2);
@@ -308,15 +349,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                     __syncwarp();
                     tcgen05_fence_after();
 #pragma unroll
-                    for (int c = 0; c < BN / 32; ++c) {
-                        uint32_t v[16];
-                        tmem_load16(from + acc * BN + c * 16, v);
+                    for (int c = 0; c < BN / 64; ++c) {
+                        uint32_t v[32];
+                        tmem_load32(from + acc * BN + c * 32, v);
                         tmem_load_wait(v);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            uint32_t& s = sum[c / 2][(c & 1) * 16 + i];
-                            s = __float_as_uint(__uint_as_float(s) + __uint_as_float(v[i]));
-                        }
+                        for (int i = 0; i < 32; ++i) sum[c][i] = __float_as_uint(__uint_as_float(sum[c][i]) + __uint_as_float(v[i]));
                     }
                     tcgen05_fence_before();
                     __syncwarp();
@@ -374,7 +412,13 @@ __global__ void __launch_bounds__(256) product_join_kernel(const float* __restri
                 f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
             }
         }
-        epilogue8<T, MODE>(ep, row, c0, f);
+        if constexpr (MODE == PRODUCT_WEIGHT) {
+            epilogue8<T, MODE, SC_ACT_NONE>(ep, row, c0, nullptr, f);
+        } else {
+            float bias[8];
+            load_bias<T, MODE>(ep, c0, bias);
+            with_activation(ep.act, [&](auto act) { epilogue8<T, MODE, decltype(act)::value>(ep, row, c0, bias, f); });
+        }
     }
 }
 
