@@ -226,6 +226,27 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
     return SC_OK;
 }
 
+template <typename T, int TOKENS>
+void run_tokens(const Stored& x, const Stored& w, const Epilogue& ep, cudaStream_t st) {
+    const bool vec = tma_ready(x) && tma_ready(w) && x.cols % 8 == 0;
+    const T *xp = static_cast<const T*>(x.p), *wp = static_cast<const T*>(w.p);
+    const uint32_t K = (uint32_t)x.cols;
+#define SC_TOKENS(WN, WK, VEC) product_tokens_kernel<T, TOKENS, WN, WK, VEC><<<(uint32_t)ceil_div(ep.cols, 4 * WN), WN * WK * 32, 0, st>>>(xp, x.ld, wp, w.ld, K, ep)
+    if (ep.q) { if (vec) SC_TOKENS(8, 4, true); else SC_TOKENS(8, 4, false); }
+    else if (vec) SC_TOKENS(2, 4, true);
+    else SC_TOKENS(2, 4, false);
+#undef SC_TOKENS
+}
+
+template <typename T>
+void run_tokens(const Stored& x, const Stored& w, const Epilogue& ep, cudaStream_t st) {
+    if (ep.rows == 1) run_tokens<T, 1>(x, w, ep, st);
+    else if (ep.rows == 2) run_tokens<T, 2>(x, w, ep, st);
+    else run_tokens<T, 4>(x, w, ep, st);
+}
+
+constexpr uint64_t FEW_TOKENS = 4;
+
 template <int MODE>
 int run_product(sc_ctx* c, int kind, int type, const Stored& A, const Stored& B, uint64_t red, const Epilogue& ep, size_t used, cudaStream_t st) {
     // the weight gradient is fp32 whatever the operands are: one build serves both types
@@ -342,6 +363,14 @@ int sc_linear(sc_ctx* ctx, int type, int act, const void* x, size_t ldx, const v
     ep.q = reinterpret_cast<uint8_t*>(q); ep.scales = scales; ep.groups = (uint32_t)ckpt_groups(N); ep.act = act;
     ep.vec_out = N % 8 == 0 && aligned(y, 16) && ldy % 8 == 0; ep.vec_res = N % 8 == 0 && aligned(residual, 16) && ldr % 8 == 0;
     ep.vec_q = N % 8 == 0 && aligned(q, 8); ep.vec_bias = N % 8 == 0 && aligned(bias, 16);
+    if (M <= FEW_TOKENS && K) {
+        Launch l(ctx, KIND_LINEAR, st);
+        const Stored xs{x, M, K, ldx}, ws{w, N, K, ldw};
+        if (type == SC_BF16) run_tokens<__nv_bfloat16>(xs, ws, ep, st);
+        else run_tokens<__half>(xs, ws, ep, st);
+        SC_CUDA(cudaGetLastError());
+        return SC_OK;
+    }
     if (const int rc = run_product<PRODUCT_FORWARD>(ctx, KIND_LINEAR, type, Stored{x, M, K, ldx}, Stored{w, N, K, ldw}, K, ep, 0, st)) return rc;
     SC_CUDA(cudaGetLastError());
     return SC_OK;

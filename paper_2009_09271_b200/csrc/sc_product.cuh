@@ -393,6 +393,75 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
     if (warp == 2) tmem_free<CG>(tmem, S::TMEM_COLS);
 }
 
+// ---------------------------------------------------------------------------
+// Forward product of a few tokens
+// ---------------------------------------------------------------------------
+// With one to four tokens the weights' bytes are everything, and four multiply-adds a weight still fit beside their loads.
+// A warp owns four rows of W and walks its share of the reduction, 16 bytes a lane and row; WK warps split a row, WN warps
+// sit side by side, and the last step joins them in shared memory.  WN = 8 puts 32 outputs, a checkpoint group, in one CTA.
+template <typename T, int TOKENS, int WN, int WK, bool VEC>
+__global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* __restrict__ x, uint64_t ldx, const T* __restrict__ w, uint64_t ldw,
+                                                                      uint32_t K, Epilogue ep) {
+    constexpr int ROWS = 4, COLS = ROWS * WN;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, wn = warp / WK, wk = warp % WK;
+    const uint32_t n0 = blockIdx.x * COLS + wn * ROWS, tokens = (uint32_t)ep.rows;
+    float acc[ROWS][TOKENS] = {};
+    constexpr uint32_t STEP = 8 * 32 * WK;
+#pragma unroll 2
+    for (uint32_t k = (wk * 32 + lane) * 8; k < K; k += STEP) {
+        Raw8<T> rw[ROWS], rx[TOKENS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            rw[r] = Raw8<T>{};
+            if (n0 + r < ep.cols) rw[r] = load8(w + (uint64_t)(n0 + r) * ldw, k, K, VEC);
+        }
+#pragma unroll
+        for (int m = 0; m < TOKENS; ++m) {
+            rx[m] = Raw8<T>{};
+            if (m < tokens) {
+                if constexpr (VEC) rx[m].v = *reinterpret_cast<const uint4*>(x + m * ldx + k);
+                else rx[m] = load8(x + m * ldx, k, K, 0u);
+            }
+        }
+        float fx[TOKENS][8];
+#pragma unroll
+        for (int m = 0; m < TOKENS; ++m) to_floats(rx[m], fx[m]);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            float fw[8];
+            to_floats(rw[r], fw);
+#pragma unroll
+            for (int m = 0; m < TOKENS; ++m)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[r][m] = fmaf(fw[i], fx[m][i], acc[r][m]);
+        }
+    }
+    __shared__ float part[WK][TOKENS][COLS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int m = 0; m < TOKENS; ++m) {
+            float v = acc[r][m];
+#pragma unroll
+            for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+            if (lane == 0) part[wk][m][wn * ROWS + r] = v;
+        }
+    __syncthreads();
+    if (warp) return;
+    // lane 4 m + j: token m, eight of the CTA's outputs
+    const uint32_t m = lane >> 2, j = (lane & 3u) * 8;
+    const bool own = m < TOKENS && j < COLS;
+    const uint32_t c0 = own ? blockIdx.x * COLS + j : ep.cols;
+    float f[8] = {}, bias[8];
+    if (own)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int s = 0; s < WK; ++s) f[i] += part[s][m][j + i];
+    load_bias<T, PRODUCT_FORWARD>(ep, c0, bias);
+    with_activation(ep.act, [&](auto act) { epilogue8<T, PRODUCT_FORWARD, decltype(act)::value>(ep, m, c0, bias, f); });
+}
+
 // Joins the parts of a split product in order and applies the epilogue; no parts at all is an empty sum.
 template <typename T, int MODE>
 __global__ void __launch_bounds__(256) product_join_kernel(const float* __restrict__ partial, uint32_t splits, uint64_t part_stride, uint32_t part_ld,
