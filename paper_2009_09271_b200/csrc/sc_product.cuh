@@ -175,7 +175,7 @@ __device__ __forceinline__ void block_out(const TcArgs& a, const Epilogue& ep, u
         const uint64_t ld = part ? a.part_ld : ep.ldo;
         float* out = (part ? a.partial + split * a.part_stride : static_cast<float*>(ep.out)) + (row0 + (lane >> 3)) * ld + c;
         const bool vec = part || ep.vec_out, add = !part && ep.accumulate;
-#pragma unroll 4
+#pragma unroll 2
         for (int i = 0; i < 8; ++i) {
             const uint32_t r = (lane >> 3) + 4 * i;
             float4 f;
@@ -200,7 +200,7 @@ __device__ __forceinline__ void block_out(const TcArgs& a, const Epilogue& ep, u
         float bias[8];
         load_bias<T, MODE>(ep, c0, bias);
         with_activation(ep.act, [&](auto act) {
-#pragma unroll
+#pragma unroll 1                                              // little code: it is fetched cold in a small call
             for (int i = 0; i < 4; ++i) {
                 float f[8];
                 const uint64_t row = fetch(i, f);
