@@ -10,23 +10,27 @@
 namespace sc {
 
 constexpr int CKPT_THREADS = 256;
-constexpr int CKPT_UNROLL = 4;                // items (8 elements) a thread has in flight
+constexpr int CKPT_UNROLL = 4;                // items a thread has in flight
 
-// Items are chunks of 8 elements, four to a group, numbered along the rows; a thread walks them with a fixed stride.
+// Items are halves of a group, 16 elements, numbered along the rows.  A thread's items are a fixed stride apart, which is
+// kept as rows and items within a row: one division at the start, an addition and a comparison from then on.
 struct ItemWalk {
-    uint64_t rows, total;                     // total = rows * chunks
-    uint32_t cols, chunks;                    // chunks per row (a multiple of 4)
-    uint32_t vec;                             // 16-byte accesses are aligned and no chunk straddles a row's end
+    uint64_t total, stride_rows;              // total = rows * items
+    uint32_t cols, items, stride_items;       // items per row (even)
+    uint32_t vec;                             // 16-byte accesses are aligned and 8 elements never straddle a row's end;
+                                              // 2: nor do 16, and q takes 16-byte accesses too; 3: rows take 32-byte ones
 };
 
-struct Item { uint64_t row; uint32_t chunk; };
-
-__device__ __forceinline__ Item item_at(const ItemWalk& w, uint64_t i) {
-    Item it;
-    if (w.total <= 0xFFFFFFFFull) { const uint32_t r = (uint32_t)i / w.chunks; it.row = r; it.chunk = (uint32_t)i - r * w.chunks; }
-    else { it.row = i / w.chunks; it.chunk = (uint32_t)(i - it.row * w.chunks); }
-    return it;
-}
+struct ItemAt {
+    uint64_t row;
+    uint32_t item;
+    __device__ ItemAt(const ItemWalk& w, uint64_t i) : row(i / w.items) { item = (uint32_t)(i - row * w.items); }
+    __device__ void next(const ItemWalk& w) {
+        row += w.stride_rows;
+        item += w.stride_items;
+        if (item >= w.items) { item -= w.items; ++row; }
+    }
+};
 
 template <typename T> struct Raw8 { uint4 v; };
 template <> struct Raw8<float> { uint4 v, w; };
@@ -45,6 +49,16 @@ __device__ __forceinline__ Raw8<T> load8(const T* row, uint32_t c0, uint32_t col
         for (int i = 0; i < 8; ++i) if (c0 + i < cols) e[i] = row[c0 + i];
     }
     return r;
+}
+
+// 32 bytes in one access: whole sectors per thread.
+__device__ __forceinline__ void load32(const void* p, uint4& a, uint4& b) {
+    asm volatile("ld.global.cs.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(p));
+}
+__device__ __forceinline__ void store32(void* p, uint4 a, uint4 b) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
 }
 
 template <typename T>
@@ -77,45 +91,74 @@ __device__ __forceinline__ uint32_t abs_max8(const Raw8<T>& r) {
     }
 }
 
-// One pass: 2 (4) bytes read and 1 + 1/32 written per element; four lanes hold a group and share its maximum.
+// One pass: 2 (4) bytes read and 1 + 1/32 written per element; two lanes hold a group and share its maximum.
 template <typename T>
 __global__ void __launch_bounds__(CKPT_THREADS) checkpoint_pack_kernel(const T* __restrict__ x, uint64_t ldx, ItemWalk w,
                                                                        uint8_t* __restrict__ q, uint8_t* __restrict__ scales) {
-    const uint64_t stride = (uint64_t)gridDim.x * CKPT_THREADS;
+    constexpr int UNROLL = sizeof(T) == 2 ? CKPT_UNROLL : 2;
+    const uint64_t stride = (uint64_t)gridDim.x * CKPT_THREADS, groups = w.items >> 1;
+    uint64_t base = (uint64_t)blockIdx.x * CKPT_THREADS + threadIdx.x;
     const uint32_t lane = threadIdx.x & 31u;
-    const uint64_t groups = w.chunks >> 2;
-    // total is a multiple of 4 and a warp's items are consecutive, so a group's four lanes stay together
-    for (uint64_t base = (uint64_t)blockIdx.x * CKPT_THREADS + threadIdx.x; base - lane < w.total; base += stride * CKPT_UNROLL) {
-        Raw8<T> raw[CKPT_UNROLL];
-        Item it[CKPT_UNROLL];
+    ItemAt at(w, base);
+    // total is even and a warp's items are consecutive, so a group's two lanes stay together
+    for (; base - lane < w.total; base += stride * UNROLL) {
+        Raw8<T> raw[UNROLL][2];
+        ItemAt from = at;
 #pragma unroll
-        for (int u = 0; u < CKPT_UNROLL; ++u) {
-            const uint64_t i = base + u * stride;
-            it[u] = item_at(w, i < w.total ? i : 0);
-            raw[u] = Raw8<T>{};
-            if (i < w.total) raw[u] = load8(x + it[u].row * ldx, it[u].chunk * 8, w.cols, w.vec);
+        for (int u = 0; u < UNROLL; ++u) {
+            raw[u][0] = raw[u][1] = Raw8<T>{};
+            if (base + u * stride < w.total) {
+                const T* row = x + at.row * ldx;
+                const uint32_t c0 = at.item * 16;
+                if (sizeof(T) == 2 && w.vec == 3) {
+                    if (c0 < w.cols) load32(row + c0, raw[u][0].v, raw[u][1].v);
+                } else {
+                    raw[u][0] = load8(row, c0, w.cols, w.vec);
+                    raw[u][1] = load8(row, c0 + 8, w.cols, w.vec);
+                }
+            }
+            at.next(w);
         }
 #pragma unroll
-        for (int u = 0; u < CKPT_UNROLL; ++u) {
-            uint32_t m = abs_max8(raw[u]);
+        for (int u = 0; u < UNROLL; ++u) {
+            uint32_t m = max(abs_max8(raw[u][0]), abs_max8(raw[u][1]));
             m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-            float f[8];
-            to_floats(raw[u], f);
-            uint32_t b[8];
-            const int e = ckpt_encode8<T>(f, m, b);
-            if (base + u * stride >= w.total) continue;
-            const uint32_t c0 = it[u].chunk * 8;
-            uint8_t* dst = q + it[u].row * w.cols + c0;
-            if (w.vec) {
-                if (c0 < w.cols) {
-                    __stcs(reinterpret_cast<uint2*>(dst), ckpt_join8(b));
-                }
-            } else {
+            int e = ckpt_exponent<T>(m);
+            const bool odd = m >= 0x7F800000u || e == Elem<T>::EMAX;   // the two lanes agree
+            if (odd) {
+                m = 0;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) if (c0 + i < w.cols) dst[i] = (uint8_t)b[i];
+                for (int h = 0; h < 2; ++h) {
+                    float f[8];
+                    to_floats(raw[u][h], f);
+                    m = max(m, finite_max8(f));
+                }
+                m = max(m, __shfl_xor_sync(3u << (lane & 30u), m, 1));
+                e = ckpt_exponent<T>(m);
             }
-            if ((it[u].chunk & 3u) == 0u) scales[it[u].row * groups + (it[u].chunk >> 2)] = (uint8_t)(e + 127);
+            uint2 b[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float f[8];
+                to_floats(raw[u][h], f);
+                b[h] = odd ? ckpt_bytes8_any<T>(f, e) : ckpt_bytes8(f, e);
+            }
+            if (base + u * stride < w.total) {
+                const uint32_t c0 = from.item * 16;
+                uint8_t* dst = q + from.row * w.cols + c0;
+                if (w.vec >= 2) {
+                    if (c0 < w.cols) __stcs(reinterpret_cast<uint4*>(dst), make_uint4(b[0].x, b[0].y, b[1].x, b[1].y));
+                } else if (w.vec) {
+                    if (c0 < w.cols) __stcs(reinterpret_cast<uint2*>(dst), b[0]);
+                    if (c0 + 8 < w.cols) __stcs(reinterpret_cast<uint2*>(dst + 8), b[1]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (c0 + i < w.cols) dst[i] = (uint8_t)((i & 4 ? b[i >> 3].y : b[i >> 3].x) >> (8 * (i & 3)));
+                }
+                if ((from.item & 1u) == 0u) scales[from.row * groups + (from.item >> 1)] = (uint8_t)(e + 127);
+            }
+            from.next(w);
         }
     }
 }
@@ -137,6 +180,23 @@ __device__ __forceinline__ void store8(T* row, uint32_t c0, uint32_t cols, uint3
     }
 }
 
+template <typename T>
+__device__ __forceinline__ uint4 packed8(const Pair v[4]) {
+    uint32_t o[4] = {};
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const float2 f = both(v[i]); o[i] = Elem<T>::pack(f.x, f.y); }
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* row, uint32_t c0, uint32_t cols, uint32_t vec, const Pair v[4]) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { const float2 p = both(v[i]); f[2 * i] = p.x; f[2 * i + 1] = p.y; }
+    store8(row, c0, cols, vec, f);
+}
+
 __device__ __forceinline__ uint2 load_q8(const uint8_t* row, uint32_t c0, uint32_t cols, uint32_t vec) {
     uint2 r = make_uint2(0u, 0u);
     if (vec) {
@@ -152,27 +212,50 @@ __device__ __forceinline__ uint2 load_q8(const uint8_t* row, uint32_t c0, uint32
 template <typename T>
 __global__ void __launch_bounds__(CKPT_THREADS) checkpoint_unpack_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, ItemWalk w,
                                                                          T* __restrict__ out, uint64_t ldo) {
-    const uint64_t stride = (uint64_t)gridDim.x * CKPT_THREADS;
-    const uint64_t groups = w.chunks >> 2;
-    for (uint64_t base = (uint64_t)blockIdx.x * CKPT_THREADS + threadIdx.x; base < w.total; base += stride * CKPT_UNROLL) {
-        uint2 raw[CKPT_UNROLL];
+    const uint64_t stride = (uint64_t)gridDim.x * CKPT_THREADS, groups = w.items >> 1;
+    uint64_t base = (uint64_t)blockIdx.x * CKPT_THREADS + threadIdx.x;
+    ItemAt at(w, base);
+    for (; base < w.total; base += stride * CKPT_UNROLL) {
+        uint2 raw[CKPT_UNROLL][2];
         uint32_t sb[CKPT_UNROLL];
-        Item it[CKPT_UNROLL];
+        ItemAt from = at;
 #pragma unroll
         for (int u = 0; u < CKPT_UNROLL; ++u) {
-            const uint64_t i = base + u * stride;
-            it[u] = item_at(w, i < w.total ? i : 0);
-            if (i >= w.total) continue;
-            raw[u] = load_q8(q + it[u].row * w.cols, it[u].chunk * 8, w.cols, w.vec);
-            sb[u] = scales[it[u].row * groups + (it[u].chunk >> 2)];
+            if (base + u * stride < w.total) {
+                const uint8_t* row = q + at.row * w.cols;
+                const uint32_t c0 = at.item * 16;
+                if (w.vec >= 2) {
+                    const uint4 v = c0 < w.cols ? __ldcs(reinterpret_cast<const uint4*>(row + c0)) : make_uint4(0u, 0u, 0u, 0u);
+                    raw[u][0] = make_uint2(v.x, v.y);
+                    raw[u][1] = make_uint2(v.z, v.w);
+                } else {
+                    raw[u][0] = load_q8(row, c0, w.cols, w.vec);
+                    raw[u][1] = load_q8(row, c0 + 8, w.cols, w.vec);
+                }
+                sb[u] = scales[at.row * groups + (at.item >> 1)];
+            }
+            at.next(w);
         }
 #pragma unroll
         for (int u = 0; u < CKPT_UNROLL; ++u) {
-            if (base + u * stride >= w.total) continue;
-            float f[8];
-            ckpt_values4(raw[u].x, ckpt_scale(sb[u]), f);
-            ckpt_values4(raw[u].y, ckpt_scale(sb[u]), f + 4);
-            store8(out + it[u].row * ldo, it[u].chunk * 8, w.cols, w.vec, f);
+            if (base + u * stride < w.total) {
+                const Scale k = ckpt_scale(sb[u]);
+                const uint32_t c0 = from.item * 16;
+                T* row = out + from.row * ldo;
+                Pair f[2][4];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (sb[u] <= LARGE_SCALE) ckpt_values8<false>(raw[u][h], k, f[h]);
+                    else ckpt_values8<true>(raw[u][h], k, f[h]);
+                }
+                if (sizeof(T) == 2 && w.vec == 3) {
+                    if (c0 < w.cols) store32(row + c0, packed8<T>(f[0]), packed8<T>(f[1]));
+                } else {
+                    store8(row, c0, w.cols, w.vec, f[0]);
+                    store8(row, c0 + 8, w.cols, w.vec, f[1]);
+                }
+            }
+            from.next(w);
         }
     }
 }
@@ -188,43 +271,65 @@ constexpr int GRAD_COLS = 256, GRAD_LANES = 8;
 
 struct GradArgs {
     uint64_t rows, lddy, lddz;
-    uint32_t cols, groups, runs, run_rows, vec, accumulate;
+    uint32_t cols, groups, runs, run_rows, accumulate;
 };
 
-template <typename T, int ACT>
-__global__ void __launch_bounds__(CKPT_THREADS) activation_grad_kernel(const T* dy, const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales,
-                                                                       GradArgs a, T* dz, float* __restrict__ partial,
-                                                                       uint32_t* __restrict__ tickets, float* __restrict__ db) {
+template <typename T, int ACT, bool VEC>
+__global__ void __launch_bounds__(CKPT_THREADS, 4) activation_grad_kernel(const T* dy, const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales,
+                                                                          GradArgs a, T* dz, float* __restrict__ partial,
+                                                                          uint32_t* __restrict__ tickets, float* __restrict__ db) {
+    constexpr int AHEAD = 2;                  // rows of a thread in flight
     const uint32_t tx = threadIdx.x & 31u, ty = threadIdx.x >> 5;
     const uint32_t c0 = blockIdx.x * GRAD_COLS + tx * 8;
-    const uint64_t r0 = (uint64_t)blockIdx.y * a.run_rows;
-    const uint64_t r1 = min(r0 + a.run_rows, a.rows);
-    float sum[8] = {};
+    const uint64_t r0 = (uint64_t)blockIdx.y * a.run_rows + ty;
+    Pair sum[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = pair(0.0f);
     if (c0 < a.cols) {
-#pragma unroll 2
-        for (uint64_t r = r0 + ty; r < r1; r += GRAD_LANES) {
-            const Raw8<T> g = load8(dy + r * a.lddy, c0, a.cols, a.vec);
-            float f[8];
-            to_floats(g, f);
-            if constexpr (ACT != SC_ACT_NONE) {
-                const uint2 k = load_q8(q + r * a.cols, c0, a.cols, a.vec);
-                const float s = ckpt_scale(scales[r * a.groups + (c0 >> 5)]);
-                float z[8];
-                ckpt_values4(k.x, s, z);
-                ckpt_values4(k.y, s, z + 4);
+        const uint32_t left = (uint32_t)(min((uint64_t)(blockIdx.y + 1) * a.run_rows, a.rows) - (uint64_t)blockIdx.y * a.run_rows);
+        const T* from = dy + r0 * a.lddy;
+        T* to = dz ? dz + r0 * a.lddz : nullptr;
+        const uint8_t *qr = q + r0 * a.cols, *sr = scales + r0 * a.groups + (c0 >> 5);
+        const uint64_t step_y = GRAD_LANES * a.lddy, step_z = GRAD_LANES * a.lddz, step_q = (uint64_t)GRAD_LANES * a.cols, step_s = (uint64_t)GRAD_LANES * a.groups;
+        for (uint32_t r = ty; r < left; r += GRAD_LANES * AHEAD) {
+            Raw8<T> g[AHEAD];
+            uint2 k[AHEAD];
+            uint32_t sb[AHEAD];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] *= activation_slope<ACT>(z[i]);
+            for (int u = 0; u < AHEAD; ++u) {
+                if (r + u * GRAD_LANES < left) {
+                    g[u] = load8(from, c0, a.cols, VEC);
+                    if constexpr (ACT != SC_ACT_NONE) {
+                        k[u] = load_q8(qr, c0, a.cols, VEC);
+                        sb[u] = *sr;
+                    }
+                }
+                from += step_y; qr += step_q; sr += step_s;
             }
-            if (dz) store8(dz + r * a.lddz, c0, a.cols, a.vec, f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += f[i];
+            for (int u = 0; u < AHEAD; ++u) {
+                if (r + u * GRAD_LANES < left) {
+                    float f[8];
+                    to_floats(g[u], f);
+                    Pair v[4], z[4];
+                    if constexpr (ACT != SC_ACT_NONE) ckpt_values8<false>(k[u], slope_scale(sb[u]), z);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        v[i] = pair(f[2 * i], f[2 * i + 1]);
+                        if constexpr (ACT != SC_ACT_NONE) v[i] = v[i] * activation_slope<ACT>(z[i]);
+                        sum[i] = sum[i] + v[i];
+                    }
+                    if (to) store8(to, c0, a.cols, VEC, v);
+                }
+                to = to ? to + step_z : nullptr;
+            }
         }
     }
     if (!db) return;
     __shared__ float join[GRAD_LANES][GRAD_COLS];
     __shared__ uint32_t last;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) join[ty][tx * 8 + i] = sum[i];
+    for (int i = 0; i < 4; ++i) { const float2 f = both(sum[i]); join[ty][tx * 8 + 2 * i] = f.x; join[ty][tx * 8 + 2 * i + 1] = f.y; }
     __syncthreads();
     const uint32_t c = blockIdx.x * GRAD_COLS + threadIdx.x;
     float total = 0.0f;

@@ -50,31 +50,35 @@ int layer_scratch(sc_ctx* c, size_t bytes, cudaStream_t st) {
     return SC_OK;
 }
 
-ItemWalk item_walk(size_t rows, size_t cols, bool vec) {
-    ItemWalk w{};
-    w.rows = rows; w.cols = (uint32_t)cols;
-    w.chunks = (uint32_t)(4 * ckpt_groups(cols));
-    w.total = (uint64_t)rows * w.chunks;
-    w.vec = vec ? 1u : 0u;
-    return w;
-}
-
 uint32_t item_grid(const sc_ctx* c, uint64_t total) {
     return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(total, CKPT_THREADS * CKPT_UNROLL), (uint64_t)c->sm_count * 8));
 }
 
+ItemWalk item_walk(const sc_ctx* c, size_t rows, size_t cols, const uint8_t* q, const void* x, size_t row_bytes) {
+    ItemWalk w{};
+    w.cols = (uint32_t)cols;
+    w.items = (uint32_t)(2 * ckpt_groups(cols));
+    w.total = (uint64_t)rows * w.items;
+    const uint64_t stride = (uint64_t)item_grid(c, w.total) * CKPT_THREADS;
+    w.stride_rows = stride / w.items;
+    w.stride_items = (uint32_t)(stride % w.items);
+    if (cols % 8 == 0 && aligned(q, 8) && aligned(x, 16) && row_bytes % 16 == 0) {
+        w.vec = 1;
+        if (cols % 16 == 0 && aligned(q, 16)) w.vec = aligned(x, 32) && row_bytes % 32 == 0 ? 3 : 2;
+    }
+    return w;
+}
+
 template <typename T>
 void launch_pack(sc_ctx* c, const void* x, size_t ldx, size_t rows, size_t cols, uint8_t* q, uint8_t* scales, cudaStream_t st) {
-    const bool vec = aligned(x, 16) && (ldx * sizeof(T)) % 16 == 0 && cols % 8 == 0 && aligned(q, 8);
-    const ItemWalk w = item_walk(rows, cols, vec);
+    const ItemWalk w = item_walk(c, rows, cols, q, x, ldx * sizeof(T));
     Launch l(c, KIND_CKPT_PACK, st);
     checkpoint_pack_kernel<T><<<item_grid(c, w.total), CKPT_THREADS, 0, st>>>(static_cast<const T*>(x), ldx, w, q, scales);
 }
 
 template <typename T>
 void launch_unpack(sc_ctx* c, const uint8_t* q, const uint8_t* scales, size_t rows, size_t cols, void* out, size_t ldo, cudaStream_t st) {
-    const bool vec = aligned(out, 16) && (ldo * sizeof(T)) % 16 == 0 && cols % 8 == 0 && aligned(q, 8);
-    const ItemWalk w = item_walk(rows, cols, vec);
+    const ItemWalk w = item_walk(c, rows, cols, q, out, ldo * sizeof(T));
     Launch l(c, KIND_CKPT_UNPACK, st);
     checkpoint_unpack_kernel<T><<<item_grid(c, w.total), CKPT_THREADS, 0, st>>>(q, scales, w, static_cast<T*>(out), ldo);
 }
@@ -325,21 +329,22 @@ int sc_activation_grad(sc_ctx* ctx, int type, int act, const void* dy, size_t ld
     GradArgs a{};
     a.rows = rows; a.lddy = lddy; a.lddz = lddz; a.cols = (uint32_t)cols; a.groups = (uint32_t)ckpt_groups(cols);
     a.runs = p.runs; a.run_rows = p.run_rows; a.accumulate = accumulate ? 1u : 0u;
-    a.vec = cols % 8 == 0 && aligned(dy, 16) && lddy % 8 == 0 && (!dz || (aligned(dz, 16) && lddz % 8 == 0)) && (!kept || aligned(q, 8)) ? 1u : 0u;
+    const bool vec = cols % 8 == 0 && aligned(dy, 16) && lddy % 8 == 0 && (!dz || (aligned(dz, 16) && lddz % 8 == 0)) && (!kept || aligned(q, 8));
     float* partial = reinterpret_cast<float*>(ctx->d_layer ? ctx->d_layer + TICKET_BYTES : nullptr);
     uint32_t* tickets = reinterpret_cast<uint32_t*>(ctx->d_layer);
     const dim3 grid(p.strips, p.runs);
     const uint8_t* qb = reinterpret_cast<const uint8_t*>(q);
     {
         Launch l(ctx, KIND_ACT_GRAD, st);
-#define SC_GRAD(ACT)                                                                                                                   \
-        case ACT:                                                                                                                      \
-            if (type == SC_BF16) activation_grad_kernel<__nv_bfloat16, ACT><<<grid, CKPT_THREADS, 0, st>>>(                            \
-                static_cast<const __nv_bfloat16*>(dy), qb, scales, a, static_cast<__nv_bfloat16*>(dz), partial, tickets, db);          \
-            else activation_grad_kernel<__half, ACT><<<grid, CKPT_THREADS, 0, st>>>(                                                   \
-                static_cast<const __half*>(dy), qb, scales, a, static_cast<__half*>(dz), partial, tickets, db);                        \
+#define SC_GRAD(T, ACT, VEC) activation_grad_kernel<T, ACT, VEC><<<grid, CKPT_THREADS, 0, st>>>( \
+            static_cast<const T*>(dy), qb, scales, a, static_cast<T*>(dz), partial, tickets, db)
+#define SC_GRAD_ACT(ACT)                                                                                     \
+        case ACT:                                                                                            \
+            if (type == SC_BF16) { if (vec) SC_GRAD(__nv_bfloat16, ACT, true); else SC_GRAD(__nv_bfloat16, ACT, false); } \
+            else { if (vec) SC_GRAD(__half, ACT, true); else SC_GRAD(__half, ACT, false); }                  \
             break;
-        switch (act) { SC_GRAD(SC_ACT_NONE) SC_GRAD(SC_ACT_RELU) SC_GRAD(SC_ACT_GELU) SC_GRAD(SC_ACT_GELU_TANH) SC_GRAD(SC_ACT_SILU) }
+        switch (act) { SC_GRAD_ACT(SC_ACT_NONE) SC_GRAD_ACT(SC_ACT_RELU) SC_GRAD_ACT(SC_ACT_GELU) SC_GRAD_ACT(SC_ACT_GELU_TANH) SC_GRAD_ACT(SC_ACT_SILU) }
+#undef SC_GRAD_ACT
 #undef SC_GRAD
     }
     SC_CUDA(cudaGetLastError());

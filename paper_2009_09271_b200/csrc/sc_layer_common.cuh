@@ -49,17 +49,71 @@ template <> struct Elem<float> {
 // ---------------------------------------------------------------------------
 // activations, in 32 bits
 // ---------------------------------------------------------------------------
-constexpr float SQRT_HALF = 0.70710678118654752f, INV_SQRT_2PI = 0.39894228040143268f;
+constexpr float INV_SQRT_2PI = 0.39894228040143268f;
 constexpr float GELU_C = 1.5957691216057308f, GELU_A = 0.044715f;      // 2 sqrt(2 / pi), cubic coefficient
 
-// 1 / (1 + 2^v): one exponential and one reciprocal, both within a few units of the last place.
-__device__ __forceinline__ float inv_1p_exp2(float v) {
-    float e, r;
-    asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(v));
-    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+// Two fp32 numbers in one register pair, and the instructions that work on both at once.
+struct Pair { unsigned long long v; };
+__device__ __forceinline__ Pair pair(float lo, float hi) {
+    Pair r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
     return r;
 }
+__device__ __forceinline__ Pair pair(float v) { return pair(v, v); }
+__device__ __forceinline__ float2 both(Pair a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+    return r;
+}
+__device__ __forceinline__ Pair operator*(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair operator+(Pair a, Pair b) {
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+// The exponential and the reciprocal flush what is below 2^-126 to zero: that far out the activations are 0 or z.
+__device__ __forceinline__ float exp2_approx(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float rcp_approx(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ Pair exp2_approx(Pair a) { const float2 f = both(a); return pair(exp2_approx(f.x), exp2_approx(f.y)); }
+__device__ __forceinline__ Pair rcp_approx(Pair a) { const float2 f = both(a); return pair(rcp_approx(f.x), rcp_approx(f.y)); }
+
 constexpr float LOG2E = 1.4426950408889634f;
+// 1 / (1 + 2^v)
+__device__ __forceinline__ Pair inv_1p_exp2(Pair v) { return rcp_approx(exp2_approx(v) + pair(1.0f)); }
+
+// Phi(-|z|), the normal distribution's tail, with e = exp(-z^2 / 2) given: e t P(t), t = 1 / (1 + 0.3 |z|).  That form of an
+// approximation to erfc is Hastings'; P is a least-squares fit, reweighted towards equal errors, to Phi(-z) / (e t) on
+// [0, 14] (1.5e-7 of the value).  The exponential is shared with the density, which the slope needs as well.
+__device__ __forceinline__ Pair normal_tail(Pair z, Pair e) {
+    const float2 f = both(z);
+    const Pair t = rcp_approx(fma2(pair(fabsf(f.x), fabsf(f.y)), pair(0.3f), pair(1.0f)));
+    Pair p = fma2(t, pair(0.0356747428f), pair(-0.1572029058f));
+    p = fma2(t, p, pair(0.2063531245f));
+    p = fma2(t, p, pair(-0.05368322389f));
+    p = fma2(t, p, pair(0.1285613688f));
+    p = fma2(t, p, pair(0.09991358065f));
+    p = fma2(t, p, pair(0.1207539403f));
+    p = fma2(t, p, pair(0.1196293f));
+    return e * (t * p);
+}
+__device__ __forceinline__ Pair exp_half_square(Pair z) { return exp2_approx(z * z * pair(-0.5f * LOG2E)); }
 
 // Runs f(std::integral_constant<int, ACT>) for the activation `act`: the choice is made once for many elements.
 template <typename F>
@@ -75,30 +129,37 @@ __device__ __forceinline__ void with_activation(int act, F&& f) {
 
 // (1 + tanh(u)) / 2 is the logistic function of 2 u, so the tanh form of gelu is z logistic(2 u).
 template <int ACT>
-__device__ __forceinline__ float activation(float z) {
-    if constexpr (ACT == SC_ACT_RELU) return z < 0.0f ? 0.0f : z;                  // NaN passes
-    else if constexpr (ACT == SC_ACT_GELU) return 0.5f * z * (1.0f + erff(z * SQRT_HALF));
-    else if constexpr (ACT == SC_ACT_GELU_TANH) return z * inv_1p_exp2(z * fmaf(-LOG2E * GELU_C * GELU_A, z * z, -LOG2E * GELU_C));
-    else if constexpr (ACT == SC_ACT_SILU) return z * inv_1p_exp2(-LOG2E * z);
+__device__ __forceinline__ Pair activation(Pair z) {
+    if constexpr (ACT == SC_ACT_RELU) {
+        const float2 f = both(z);
+        return pair(f.x < 0.0f ? 0.0f : f.x, f.y < 0.0f ? 0.0f : f.y);              // NaN passes
+    } else if constexpr (ACT == SC_ACT_GELU) {                                       // max(z, 0) - |z| Phi(-|z|)
+        const float2 f = both(z);
+        const Pair h = normal_tail(z, exp_half_square(z));                          // NaN passes through here
+        return fma2(pair(-fminf(fabsf(f.x), 64.0f), -fminf(fabsf(f.y), 64.0f)), h, pair(fmaxf(f.x, 0.0f), fmaxf(f.y, 0.0f)));
+    } else if constexpr (ACT == SC_ACT_GELU_TANH)
+        return z * inv_1p_exp2(z * fma2(z * z, pair(-LOG2E * GELU_C * GELU_A), pair(-LOG2E * GELU_C)));
+    else if constexpr (ACT == SC_ACT_SILU) return z * inv_1p_exp2(z * pair(-LOG2E));
     else return z;
 }
 
-// Products with a logistic that has reached 0 or 1 take a bounded z: the limit is 0, never 0 * inf.
+// z is a checkpoint's value, read through slope_scale(): |z| < 2^48, so that no product below overflows.  NaN passes.
 template <int ACT>
-__device__ __forceinline__ float activation_slope(float z) {
-    if constexpr (ACT == SC_ACT_RELU) return z > 0.0f ? 1.0f : (z <= 0.0f ? 0.0f : z);
-    else if constexpr (ACT == SC_ACT_GELU) {
-        float e;
-        asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(-0.5f * LOG2E * z * z));
-        return fmaf(z * INV_SQRT_2PI, e, 0.5f * (1.0f + erff(z * SQRT_HALF)));
+__device__ __forceinline__ Pair activation_slope(Pair z) {
+    if constexpr (ACT == SC_ACT_RELU) {
+        const float2 f = both(z);
+        return pair(f.x > 0.0f ? 1.0f : (f.x <= 0.0f ? 0.0f : f.x), f.y > 0.0f ? 1.0f : (f.y <= 0.0f ? 0.0f : f.y));
+    } else if constexpr (ACT == SC_ACT_GELU) {                                       // Phi(z) + z phi(z)
+        const Pair e = exp_half_square(z);
+        const float2 f = both(z), c = both(fma2(normal_tail(z, e), pair(-1.0f), pair(0.5f)));
+        return fma2(z * pair(INV_SQRT_2PI), e, pair(copysignf(c.x, f.x), copysignf(c.y, f.y)) + pair(0.5f));
     } else if constexpr (ACT == SC_ACT_GELU_TANH) {
-        z = z > 64.0f ? 64.0f : (z < -64.0f ? -64.0f : z);                         // NaN passes
-        const float zz = z * z, s = inv_1p_exp2(z * fmaf(-LOG2E * GELU_C * GELU_A, zz, -LOG2E * GELU_C));
-        return fmaf(s * z, (1.0f - s) * fmaf(3.0f * GELU_C * GELU_A, zz, GELU_C), s);
+        const Pair zz = z * z, s = inv_1p_exp2(z * fma2(zz, pair(-LOG2E * GELU_C * GELU_A), pair(-LOG2E * GELU_C)));
+        return fma2(s * z, fma2(s, pair(-1.0f), pair(1.0f)) * fma2(zz, pair(3.0f * GELU_C * GELU_A), pair(GELU_C)), s);
     } else if constexpr (ACT == SC_ACT_SILU) {
-        const float s = inv_1p_exp2(-LOG2E * z), b = z > 128.0f ? 128.0f : z;
-        return fmaf(s * b, 1.0f - s, s);
-    } else return 1.0f;
+        const Pair s = inv_1p_exp2(z * pair(-LOG2E));
+        return fma2(s * z, fma2(s, pair(-1.0f), pair(1.0f)), s);
+    } else return pair(1.0f);
 }
 
 // ---------------------------------------------------------------------------
@@ -118,58 +179,89 @@ __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)
 // |v| 2^-e <= 127 except where e has reached the type's largest, whose caller clamps.
 __device__ __forceinline__ uint32_t ckpt_byte(float v, float inv) { return __float_as_uint(fmaf(v, inv, 12582912.0f)) & 0xFFu; }
 
-// Bytes b[0..7] side by side.
-__device__ __forceinline__ uint2 ckpt_join8(const uint32_t b[8]) {
-    return make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
-                      __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
-}
-
 // The same for any v: not finite -> -128, which stands for NaN; |q| <= most.
 __device__ __forceinline__ uint32_t ckpt_byte_any(float v, float inv, float most) {
     if ((__float_as_uint(v) & 0x7FFFFFFFu) >= 0x7F800000u) return 0x80u;
     return ckpt_byte(fminf(fmaxf(rintf(v * inv), -most), most), 1.0f);
 }
 
-// Four stored bytes to their values: byte u = q + 128 as the low mantissa byte of 2^23; the difference and the product
-// are exact (one multiply-add would overflow for the largest scales).
-__device__ __forceinline__ void ckpt_values4(uint32_t q4, float scale, float v[4]) {
-    const uint32_t u = q4 ^ 0x80808080u;
+// The bytes of 8 elements side by side.
+__device__ __forceinline__ uint2 ckpt_join8(const uint32_t b[8]) {
+    return make_uint2(__byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410),
+                      __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410));
+}
+__device__ __forceinline__ uint2 ckpt_bytes8(const float f[8], int e) {
+    const float inv = pow2(-e);
+    uint32_t b[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = (__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7440 + i)) - 8388736.0f) * scale;
-    if (__vcmpeq4(u, 0u)) {
+    for (int i = 0; i < 8; ++i) b[i] = ckpt_byte(f[i], inv);
+    return ckpt_join8(b);
+}
+template <typename T>
+__device__ __forceinline__ uint2 ckpt_bytes8_any(const float f[8], int e) {
+    const float inv = pow2(-e), most = e == Elem<T>::EMAX ? 63.0f : 127.0f;
+    uint32_t b[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (((u >> (8 * i)) & 0xFFu) == 0u) v[i] = __uint_as_float(0x7FFFFFFFu);
+    for (int i = 0; i < 8; ++i) b[i] = ckpt_byte_any(f[i], inv, most);
+    return ckpt_join8(b);
+}
+// Bits of the largest finite magnitude.
+__device__ __forceinline__ uint32_t finite_max8(const float f[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t a = __float_as_uint(f[i]) & 0x7FFFFFFFu;
+        if (a < 0x7F800000u) m = max(m, a);
+    }
+    return m;
+}
+
+// Stored bytes to their values: byte u = q + 128 as the low mantissa byte of 2^23, then one exact multiply-add.  Scales above
+// 2^100, where its constant would overflow, take the difference first.
+struct Scale { float s, off; };
+__device__ __forceinline__ Scale ckpt_scale(uint32_t byte) {
+    Scale k;
+    k.s = __uint_as_float(byte << 23);
+    k.off = -8388736.0f * k.s;
+    return k;
+}
+// For the activations' slopes: every one of them has reached its limit long before 2^40, so a larger scale reads as 2^40.
+__device__ __forceinline__ Scale slope_scale(uint32_t byte) { return ckpt_scale(min(byte, 127u + 40u)); }
+
+template <bool LARGE>
+__device__ __forceinline__ void ckpt_values8(uint2 q8, Scale k, Pair v[4]) {
+    const uint32_t u[2] = {q8.x ^ 0x80808080u, q8.y ^ 0x80808080u};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const Pair f = pair(__uint_as_float(__byte_perm(u[i >> 1], 0x4B000000u, 0x7440 + 2 * (i & 1))),
+                            __uint_as_float(__byte_perm(u[i >> 1], 0x4B000000u, 0x7441 + 2 * (i & 1))));
+        v[i] = LARGE ? (f + pair(-8388736.0f)) * pair(k.s) : fma2(f, pair(k.s), pair(k.off));
+    }
+    // some byte of u is zero: q = -128, not finite
+    if ((((u[0] - 0x01010101u) & ~u[0]) | ((u[1] - 0x01010101u) & ~u[1])) & 0x80808080u) {
+        const float nan = __uint_as_float(0x7FFFFFFFu);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t two = u[i >> 1] >> (16 * (i & 1));
+            const float2 f = both(v[i]);
+            v[i] = pair((two & 0xFFu) ? f.x : nan, (two & 0xFF00u) ? f.y : nan);
+        }
     }
 }
+constexpr uint32_t LARGE_SCALE = 127 + 100;
 
 // Eight elements of a group that four neighbouring lanes hold, `m` the largest magnitude of them all by its bits (values that
-// are not finite order above the others): their bytes and the group's exponent.  The four lanes call it together.
+// are not finite order above the others): their bytes, and the group's exponent.  The four lanes call it together.
 template <typename T>
-__device__ __forceinline__ int ckpt_encode8(const float f[8], uint32_t m, uint32_t b[8]) {
-    int e = ckpt_exponent<T>(m);
-    if (m < 0x7F800000u && e != Elem<T>::EMAX) {
-        const float inv = pow2(-e);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) b[i] = ckpt_byte(f[i], inv);
-    } else {
-        const uint32_t mask = 0xFu << (threadIdx.x & 28u);
-        m = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t a = __float_as_uint(f[i]) & 0x7FFFFFFFu;
-            if (a < 0x7F800000u) m = max(m, a);
-        }
-        m = max(m, __shfl_xor_sync(mask, m, 1));
-        m = max(m, __shfl_xor_sync(mask, m, 2));
-        e = ckpt_exponent<T>(m);
-        const float inv = pow2(-e), most = e == Elem<T>::EMAX ? 63.0f : 127.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) b[i] = ckpt_byte_any(f[i], inv, most);
-    }
-    return e;
+__device__ __forceinline__ uint2 ckpt_encode8(const float f[8], uint32_t m, int& e) {
+    e = ckpt_exponent<T>(m);
+    if (m < 0x7F800000u && e != Elem<T>::EMAX) return ckpt_bytes8(f, e);
+    const uint32_t mask = 0xFu << (threadIdx.x & 28u);
+    m = finite_max8(f);
+    m = max(m, __shfl_xor_sync(mask, m, 1));
+    m = max(m, __shfl_xor_sync(mask, m, 2));
+    e = ckpt_exponent<T>(m);
+    return ckpt_bytes8_any<T>(f, e);
 }
-
-__device__ __forceinline__ float ckpt_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 }  // namespace sc

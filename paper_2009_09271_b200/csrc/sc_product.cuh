@@ -58,34 +58,39 @@ __device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint
                 for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
                 m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
                 m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-                uint32_t b[8];
-                const int e = ckpt_encode8<T>(v, m, b);
+                int e;
+                const uint2 b = ckpt_encode8<T>(v, m, e);
                 if (in) {
                     uint8_t* q = ep.q + row * ep.cols + c0;
                     if (ep.vec_q) {
-                        *reinterpret_cast<uint2*>(q) = ckpt_join8(b);
+                        *reinterpret_cast<uint2*>(q) = b;
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) if (c0 + i < ep.cols) q[i] = (uint8_t)b[i];
+                        for (int i = 0; i < 8; ++i) if (c0 + i < ep.cols) q[i] = (uint8_t)((i & 4 ? b.y : b.x) >> (8 * (i & 3)));
                     }
                     if ((c0 & 31u) == 0u) ep.scales[row * ep.groups + (c0 >> 5)] = (uint8_t)(e + 127);
                 }
             }
             if (!in) return;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activation<ACT>(v[i]) + res[i];
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = both(activation<ACT>(pair(v[2 * i], v[2 * i + 1])) + pair(res[2 * i], res[2 * i + 1]));
+                v[2 * i] = f.x; v[2 * i + 1] = f.y;
+            }
         } else {
             if (!in) return;
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += res[i];
             if constexpr (ACT != SC_ACT_NONE) {
                 const uint2 k = load_q8(ep.q + row * ep.cols, c0, ep.cols, ep.vec_q);
-                const float s = ckpt_scale(ep.scales[row * ep.groups + (c0 >> 5)]);
-                float z[8];
-                ckpt_values4(k.x, s, z);
-                ckpt_values4(k.y, s, z + 4);
+                const Scale s = slope_scale(ep.scales[row * ep.groups + (c0 >> 5)]);
+                Pair z[4];
+                ckpt_values8<false>(k, s, z);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] *= activation_slope<ACT>(z[i]);
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = both(pair(v[2 * i], v[2 * i + 1]) * activation_slope<ACT>(z[i]));
+                    v[2 * i] = f.x; v[2 * i + 1] = f.y;
+                }
             }
         }
         store8(static_cast<T*>(ep.out) + row * ep.ldo, c0, ep.cols, ep.vec_out, v);
