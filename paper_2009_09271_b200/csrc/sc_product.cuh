@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
     if (warp < 4) {
         if constexpr (REGS) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         bool ok = true;
-        if (warp == 0 && lane == 0) {
+        if (warp == 0) {
             // in a pair the first CTA's barriers count the bytes of both
             const uint32_t bytes = CG * ((A_MN ? S::A_BYTES : a.a_box_rows * TC_STEP * 2) + S::B_BYTES);
             uint32_t stage = 0, phase = 0, issued = 0;
@@ -264,38 +264,38 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                 const uint32_t k0 = (uint64_t)a.blocks * split / a.splits, k1 = (uint64_t)a.blocks * (split + 1) / a.splits;
                 const int32_t i0 = (int32_t)((ti * CG + rank) * TC_ROWS), j0 = (int32_t)(tj * BN + rank * S::B_ROWS);
                 for (uint32_t k = k0; k < k1; ++k) {
-                    if (!(ok = mbar_wait(empty + 8 * stage, phase ^ 1u))) break;
+                    if (!(ok = warp_wait(empty + 8 * stage, phase ^ 1u))) break;
                     const uint32_t sa = base + stage * S::STAGE, sb = sa + S::A_BYTES;
-                    if (rank == 0) mbar_expect_tx(full + 8 * stage, bytes);
-                    const uint32_t bar = CG == 2 ? map_to_rank(full + 8 * stage, 0) : full + 8 * stage;
-                    const int32_t r = (int32_t)(k * TC_STEP);
-                    if constexpr (A_MN) {
+                    if (elect_one()) {
+                        if (rank == 0) mbar_expect_tx(full + 8 * stage, bytes);
+                        const uint32_t bar = CG == 2 ? map_to_rank(full + 8 * stage, 0) : full + 8 * stage;
+                        const int32_t r = (int32_t)(k * TC_STEP);
+                        if constexpr (A_MN) {
 #pragma unroll
-                        for (int c = 0; c < TC_ROWS; c += 64) tma_load_2d<CG>(sa + c * TC_STEP * 2, &map_a, bar, i0 + c, r);
-                    } else {
-                        tma_load_2d<CG>(sa, &map_a, bar, r, i0);
-                    }
-                    if constexpr (B_MN) {
+                            for (int c = 0; c < TC_ROWS; c += 64) tma_load_2d<CG>(sa + c * TC_STEP * 2, &map_a, bar, i0 + c, r);
+                        } else {
+                            tma_load_2d<CG>(sa, &map_a, bar, r, i0);
+                        }
+                        if constexpr (B_MN) {
 #pragma unroll
-                        for (int c = 0; c < S::B_ROWS; c += 64) tma_load_2d<CG>(sb + c * TC_STEP * 2, &map_b, bar, j0 + c, r);
-                    } else {
-                        tma_load_2d<CG>(sb, &map_b, bar, r, j0);
+                            for (int c = 0; c < S::B_ROWS; c += 64) tma_load_2d<CG>(sb + c * TC_STEP * 2, &map_b, bar, j0 + c, r);
+                        } else {
+                            tma_load_2d<CG>(sb, &map_b, bar, r, j0);
+                        }
                     }
+                    __syncwarp();
                     ++issued;
                     if (++stage == S::STAGES) { stage = 0; phase ^= 1u; }
                 }
             }
             if (!ok) {                     // the copies in flight land before the CTA ends (two seconds have passed since the last)
-                atomicCAS(a.status, 0, ST_TIMEOUT);
+                if (lane == 0) atomicCAS(a.status, 0, ST_TIMEOUT);
                 if (rank == 0)
                     for (uint32_t n = issued > (uint32_t)S::STAGES ? issued - S::STAGES : 0; n < issued; ++n)
                         mbar_wait(full + 8 * (n % S::STAGES), (n / S::STAGES) & 1u);
             }
-        } else if (warp == 1 && lane == 0 && rank == 0) {
-            // The tensor pipe's queue holds about two instructions.  What the next block waits for is therefore looked at
-            // between the instructions of this one, never between its last and the next one's first.
+        } else if (warp == 1 && rank == 0) {
             uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
-            bool ready = false, vacant = false;            // seen: the next block's operands; the next accumulator empty
             const uint64_t da0 = A_MN ? smem_desc(base, TC_STEP * 128, 1024) : smem_desc(base, 16, 1024);
             const uint64_t db0 = B_MN ? smem_desc(base + S::A_BYTES, TC_STEP * 128, 1024) : smem_desc(base + S::A_BYTES, 16, 1024);
             for (uint32_t w = first; w < work && ok; w += step) {
@@ -303,30 +303,29 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                 const uint32_t k0 = (uint64_t)a.blocks * split / a.splits, k1 = (uint64_t)a.blocks * (split + 1) / a.splits;
                 for (uint32_t c0 = k0; c0 < k1 && ok;) {
                     const uint32_t c1 = SUM ? min(c0 + TC_CHUNK, k1) : k1;
-                    if (!vacant && !(ok = mbar_wait(tempty + 8 * acc, acc_phase ^ 1u))) break;
-                    vacant = false;
+                    if (!(ok = warp_wait(tempty + 8 * acc, acc_phase ^ 1u))) break;
                     tcgen05_fence_after();
                     for (uint32_t k = c0; k < c1; ++k) {
-                        if (!ready && !(ok = mbar_wait(full + 8 * stage, phase))) break;
+                        if (!(ok = warp_wait(full + 8 * stage, phase))) break;
                         tcgen05_fence_after();
                         const uint32_t next = stage + 1 == S::STAGES ? 0 : stage + 1, next_phase = next ? phase : phase ^ 1u;
                         const uint64_t da = da0 + stage * (S::STAGE >> 4), db = db0 + stage * (S::STAGE >> 4);
                         const uint32_t d = tmem + acc * BN;
-                        mma_f16<CG>(d, da, db, a.idesc, k > c0);
-                        mma_f16<CG>(d, da + (A_MN ? 128 : 2), db + (B_MN ? 128 : 2), a.idesc, true);
-                        if (k + 1 == c1) vacant = mbar_test(tempty + 8 * (acc ^ 1u), (acc ? acc_phase ^ 1u : acc_phase) ^ 1u);
-                        mma_f16<CG>(d, da + (A_MN ? 256 : 4), db + (B_MN ? 256 : 4), a.idesc, true);
-                        ready = mbar_test(full + 8 * next, next_phase);
-                        mma_f16<CG>(d, da + (A_MN ? 384 : 6), db + (B_MN ? 384 : 6), a.idesc, true);
-                        mma_commit<CG>(empty + 8 * stage);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                mma_f16<CG>(d, da + (A_MN ? 128 : 2) * i, db + (B_MN ? 128 : 2) * i, a.idesc, k > c0 || i > 0);
+                            mma_commit<CG>(empty + 8 * stage);
+                            if (k + 1 == c1) mma_commit<CG>(tfull + 8 * acc);
+                        }
+                        __syncwarp();
                         stage = next; phase = next_phase;
                     }
-                    mma_commit<CG>(tfull + 8 * acc);
                     if ((acc ^= 1u) == 0) acc_phase ^= 1u;
                     c0 = c1;
                 }
             }
-            if (!ok) atomicCAS(a.status, 0, ST_TIMEOUT);
+            if (!ok && lane == 0) atomicCAS(a.status, 0, ST_TIMEOUT);
         }
         __syncwarp();
     } else {
@@ -350,7 +349,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
 #pragma unroll
                     for (int i = 0; i < 32; ++i) sum[c][i] = 0u;
                 for (uint32_t c0 = k0; c0 < k1; c0 += TC_CHUNK) {
-                    if (!(ok = mbar_wait(tfull + 8 * acc, acc_phase))) break;
+                    if (!(ok = warp_wait(tfull + 8 * acc, acc_phase))) break;
                     __syncwarp();
                     tcgen05_fence_after();
 #pragma unroll
@@ -370,7 +369,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
 #pragma unroll
                 for (int c = 0; c < BN / 64; ++c) block_out<T, MODE>(a, ep, stage_addr, sum[c], row0, col0 + c * 32, split);
             } else {
-                if (!(ok = mbar_wait(tfull + 8 * acc, acc_phase))) break;
+                if (!(ok = warp_wait(tfull + 8 * acc, acc_phase))) break;
                 __syncwarp();
                 tcgen05_fence_after();
 #pragma unroll 1
