@@ -96,6 +96,8 @@ template <typename T>
 __global__ void __launch_bounds__(CKPT_THREADS) checkpoint_pack_kernel(const T* __restrict__ x, uint64_t ldx, ItemWalk w,
                                                                        uint8_t* __restrict__ q, uint8_t* __restrict__ scales) {
     constexpr int UNROLL = sizeof(T) == 2 ? CKPT_UNROLL : 2;
+    wait_for_predecessor();
+    release_successor();
     const uint64_t stride = (uint64_t)gridDim.x * CKPT_THREADS, groups = w.items >> 1;
     uint64_t base = (uint64_t)blockIdx.x * CKPT_THREADS + threadIdx.x;
     const uint32_t lane = threadIdx.x & 31u;
@@ -212,6 +214,8 @@ __device__ __forceinline__ uint2 load_q8(const uint8_t* row, uint32_t c0, uint32
 template <typename T>
 __global__ void __launch_bounds__(CKPT_THREADS) checkpoint_unpack_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, ItemWalk w,
                                                                          T* __restrict__ out, uint64_t ldo) {
+    wait_for_predecessor();
+    release_successor();
     const uint64_t stride = (uint64_t)gridDim.x * CKPT_THREADS, groups = w.items >> 1;
     uint64_t base = (uint64_t)blockIdx.x * CKPT_THREADS + threadIdx.x;
     ItemAt at(w, base);
@@ -279,6 +283,8 @@ __global__ void __launch_bounds__(CKPT_THREADS, 4) activation_grad_kernel(const 
                                                                           GradArgs a, T* dz, float* __restrict__ partial,
                                                                           uint32_t* __restrict__ tickets, float* __restrict__ db) {
     constexpr int AHEAD = 2;                  // rows of a thread in flight
+    wait_for_predecessor();
+    release_successor();
     const uint32_t tx = threadIdx.x & 31u, ty = threadIdx.x >> 5;
     const uint32_t c0 = blockIdx.x * GRAD_COLS + tx * 8;
     const uint64_t r0 = (uint64_t)blockIdx.y * a.run_rows + ty;

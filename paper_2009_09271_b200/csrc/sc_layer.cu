@@ -54,6 +54,24 @@ uint32_t item_grid(const sc_ctx* c, uint64_t total) {
     return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(total, CKPT_THREADS * CKPT_UNROLL), (uint64_t)c->sm_count * 8));
 }
 
+// Launches a layer kernel (optionally in clusters) that may begin while its predecessor on the stream ends.
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st, A... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2]{};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim = {(unsigned)cluster, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 ItemWalk item_walk(const sc_ctx* c, size_t rows, size_t cols, const uint8_t* q, const void* x, size_t row_bytes) {
     ItemWalk w{};
     w.cols = (uint32_t)cols;
@@ -73,14 +91,14 @@ template <typename T>
 void launch_pack(sc_ctx* c, const void* x, size_t ldx, size_t rows, size_t cols, uint8_t* q, uint8_t* scales, cudaStream_t st) {
     const ItemWalk w = item_walk(c, rows, cols, q, x, ldx * sizeof(T));
     Launch l(c, KIND_CKPT_PACK, st);
-    checkpoint_pack_kernel<T><<<item_grid(c, w.total), CKPT_THREADS, 0, st>>>(static_cast<const T*>(x), ldx, w, q, scales);
+    launch(checkpoint_pack_kernel<T>, item_grid(c, w.total), CKPT_THREADS, 0, 1, st, static_cast<const T*>(x), ldx, w, q, scales);
 }
 
 template <typename T>
 void launch_unpack(sc_ctx* c, const uint8_t* q, const uint8_t* scales, size_t rows, size_t cols, void* out, size_t ldo, cudaStream_t st) {
     const ItemWalk w = item_walk(c, rows, cols, q, out, ldo * sizeof(T));
     Launch l(c, KIND_CKPT_UNPACK, st);
-    checkpoint_unpack_kernel<T><<<item_grid(c, w.total), CKPT_THREADS, 0, st>>>(q, scales, w, static_cast<T*>(out), ldo);
+    launch(checkpoint_unpack_kernel<T>, item_grid(c, w.total), CKPT_THREADS, 0, 1, st, q, scales, w, static_cast<T*>(out), ldo);
 }
 
 struct GradPlan { uint32_t strips, runs, run_rows; size_t bytes; };
@@ -166,17 +184,8 @@ int launch_tiles(sc_ctx* c, const CUtensorMap& ma, const CUtensorMap& mb, const 
         if (rc == cudaSuccess && MODE == PRODUCT_WEIGHT && BN == 256 && f.numRegs < TC_LEAST_REGS) rc = cudaErrorInvalidDeviceFunction;
     });
     if (rc != cudaSuccess) return SC_ERR_CUDA;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(CG * (uint32_t)std::min<uint64_t>((uint64_t)a.tiles * a.splits, c->sm_count / CG));
-    cfg.blockDim = dim3(TC_THREADS);
-    cfg.dynamicSmemBytes = TcShape<BN, CG>::SMEM;
-    cfg.stream = st;
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim = {CG, 1, 1};
-    cfg.attrs = &attr;
-    cfg.numAttrs = CG == 2 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, product_kernel<T, MODE, BN, CG>, ma, mb, a, ep) == cudaSuccess ? SC_OK : SC_ERR_CUDA;
+    const uint32_t grid = CG * (uint32_t)std::min<uint64_t>((uint64_t)a.tiles * a.splits, c->sm_count / CG);
+    return launch(product_kernel<T, MODE, BN, CG>, grid, TC_THREADS, TcShape<BN, CG>::SMEM, CG, st, ma, mb, a, ep) == cudaSuccess ? SC_OK : SC_ERR_CUDA;
 }
 
 template <typename T, int MODE>
@@ -186,7 +195,7 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
     const uint32_t join_grid = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(ep.rows * chunks, 256), (uint64_t)c->sm_count * 8));
     if (red == 0) {
         Launch l(c, KIND_LAYER_JOIN, st);
-        product_join_kernel<T, MODE><<<join_grid, 256, 0, st>>>(nullptr, 0, 0, 0, ep);
+        launch(product_join_kernel<T, MODE>, join_grid, 256, 0, 1, st, nullptr, 0, 0, 0, ep);
         return SC_OK;
     }
     const ProductPlan p = product_plan(c, ep.rows, ep.cols, red);
@@ -201,8 +210,8 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
         if (tma_ready(*m)) continue;
         const uint32_t ldd = (uint32_t)round8(m->cols);
         Launch l(c, KIND_LAYER_LAYOUT, st);
-        layout_kernel<<<(uint32_t)std::min<uint64_t>(ceil_div(m->rows * (ldd / 8), 256), (uint64_t)c->sm_count * 8), 256, 0, st>>>(
-            static_cast<const uint16_t*>(m->p), m->ld, m->rows, (uint32_t)m->cols, reinterpret_cast<uint16_t*>(at), ldd);
+        launch(layout_kernel, (uint32_t)std::min<uint64_t>(ceil_div(m->rows * (ldd / 8), 256), (uint64_t)c->sm_count * 8), 256, 0, 1, st,
+               static_cast<const uint16_t*>(m->p), m->ld, m->rows, (uint32_t)m->cols, reinterpret_cast<uint16_t*>(at), ldd);
         m->p = at; m->ld = ldd;
         at += layout_bytes(m->rows, m->cols);
     }
@@ -225,7 +234,7 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
     }
     if (p.splits > 1) {
         Launch l(c, KIND_LAYER_JOIN, st);
-        product_join_kernel<T, MODE><<<join_grid, 256, 0, st>>>(partial, p.splits, a.part_stride, a.part_ld, ep);
+        launch(product_join_kernel<T, MODE>, join_grid, 256, 0, 1, st, partial, p.splits, a.part_stride, a.part_ld, ep);
     }
     return SC_OK;
 }
@@ -235,7 +244,7 @@ void run_tokens(const Stored& x, const Stored& w, const Epilogue& ep, cudaStream
     const bool vec = tma_ready(x) && tma_ready(w) && x.cols % 8 == 0;
     const T *xp = static_cast<const T*>(x.p), *wp = static_cast<const T*>(w.p);
     const uint32_t K = (uint32_t)x.cols;
-#define SC_TOKENS(WN, WK, VEC) product_tokens_kernel<T, TOKENS, WN, WK, VEC><<<(uint32_t)ceil_div(ep.cols, 4 * WN), WN * WK * 32, 0, st>>>(xp, x.ld, wp, w.ld, K, ep)
+#define SC_TOKENS(WN, WK, VEC) launch(product_tokens_kernel<T, TOKENS, WN, WK, VEC>, (uint32_t)ceil_div(ep.cols, 4 * WN), WN * WK * 32, 0, 1, st, xp, x.ld, wp, w.ld, K, ep)
     if (ep.q) { if (vec) SC_TOKENS(8, 4, true); else SC_TOKENS(8, 4, false); }
     else if (vec) SC_TOKENS(2, 4, true);
     else SC_TOKENS(2, 4, false);
@@ -336,7 +345,7 @@ int sc_activation_grad(sc_ctx* ctx, int type, int act, const void* dy, size_t ld
     const uint8_t* qb = reinterpret_cast<const uint8_t*>(q);
     {
         Launch l(ctx, KIND_ACT_GRAD, st);
-#define SC_GRAD(T, ACT, VEC) activation_grad_kernel<T, ACT, VEC><<<grid, CKPT_THREADS, 0, st>>>( \
+#define SC_GRAD(T, ACT, VEC) launch(activation_grad_kernel<T, ACT, VEC>, grid, CKPT_THREADS, 0, 1, st, \
             static_cast<const T*>(dy), qb, scales, a, static_cast<T*>(dz), partial, tickets, db)
 #define SC_GRAD_ACT(ACT)                                                                                     \
         case ACT:                                                                                            \

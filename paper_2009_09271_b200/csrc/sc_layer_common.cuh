@@ -14,6 +14,12 @@ constexpr uint32_t CKPT_GROUP = 32;           // features that share one scale
 
 __host__ __device__ inline uint64_t ckpt_groups(uint64_t cols) { return (cols + CKPT_GROUP - 1) / CKPT_GROUP; }
 
+// Layer kernels are launched so that they may begin while their predecessor on the stream ends: what precedes
+// wait_for_predecessor() touches nothing in HBM, and release_successor() lets the next such kernel begin likewise.  Every
+// kernel that is launched that way waits, so a kernel's end implies the end of all before it.
+__device__ __forceinline__ void wait_for_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void release_successor() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ---------------------------------------------------------------------------
 // types
 // ---------------------------------------------------------------------------

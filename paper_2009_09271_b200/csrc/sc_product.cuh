@@ -245,6 +245,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
     tcgen05_fence_after();
     uint32_t tmem;
     asm volatile("ld.shared.b32 %0, [%1];" : "=r"(tmem) : "r"(slot));
+    wait_for_predecessor();
+    release_successor();
 
     const uint32_t work = a.tiles * a.splits;
     // The register sums of a 256-wide tile need more than an even share: of the registers that the CTA is
@@ -407,6 +409,8 @@ template <typename T, int TOKENS, int WN, int WK, bool VEC>
 __global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* __restrict__ x, uint64_t ldx, const T* __restrict__ w, uint64_t ldw,
                                                                       uint32_t K, Epilogue ep) {
     constexpr int ROWS = 4, COLS = ROWS * WN;
+    wait_for_predecessor();
+    release_successor();
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, wn = warp / WK, wk = warp % WK;
     const uint32_t n0 = blockIdx.x * COLS + wn * ROWS, tokens = (uint32_t)ep.rows;
     float acc[ROWS][TOKENS] = {};
@@ -470,6 +474,8 @@ __global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* _
 template <typename T, int MODE>
 __global__ void __launch_bounds__(256) product_join_kernel(const float* __restrict__ partial, uint32_t splits, uint64_t part_stride, uint32_t part_ld,
                                                            Epilogue ep) {
+    wait_for_predecessor();
+    release_successor();
     const uint32_t chunks = 4 * ((ep.cols + 31) / 32);
     const uint64_t total = ep.rows * chunks, stride = (uint64_t)gridDim.x * 256;
     const uint32_t lane = threadIdx.x & 31u;
@@ -498,6 +504,8 @@ __global__ void __launch_bounds__(256) product_join_kernel(const float* __restri
 // Rows copied to a 16-byte aligned place with rows a multiple of 8 elements apart, where the tensor cores' loads can reach them.
 __global__ void __launch_bounds__(256) layout_kernel(const uint16_t* __restrict__ src, uint64_t ld, uint64_t rows, uint32_t cols,
                                                      uint16_t* __restrict__ dst, uint32_t ldd) {
+    wait_for_predecessor();
+    release_successor();
     const uint32_t chunks = ldd / 8;
     const uint64_t total = rows * chunks, stride = (uint64_t)gridDim.x * 256;
     for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += stride) {
