@@ -159,14 +159,16 @@ def _want(t: torch.Tensor, dtype, name: str, cuda: bool = True) -> None:
 
 def _matrix(t: torch.Tensor, rows: int, cols: int, dtype, name: str) -> int:
     """Checks a CUDA matrix [rows, cols] whose rows are contiguous; returns the distance between rows in elements."""
+    if t.dtype is dtype and t.is_cuda and t.shape == (rows, cols):
+        ld, step = t.stride()
+        if ld >= cols and step == 1:
+            return ld
+        if (step == 1 or cols <= 1) and (ld >= cols or rows <= 1):
+            return max(ld, cols)
+        raise TypeError(f"{name}: the last dimension must be contiguous and rows must not overlap")
     if t.dtype != dtype or not t.is_cuda or t.dim() != 2:
         raise TypeError(f"{name}: expected a 2-D CUDA {dtype} tensor")
-    if t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{name}: expected shape {(rows, cols)}, got {tuple(t.shape)}")
-    ld, step = t.stride()
-    if (step != 1 and cols > 1) or (ld < cols and rows > 1):
-        raise TypeError(f"{name}: the last dimension must be contiguous and rows must not overlap")
-    return max(ld, cols)
+    raise ValueError(f"{name}: expected shape {(rows, cols)}, got {tuple(t.shape)}")
 
 
 def _vector(t: torch.Tensor, n: int, dtype, name: str) -> None:
@@ -184,11 +186,12 @@ def _kept(q, scales, rows: int, cols: int) -> None:
 
 
 def _layer_type(t: torch.Tensor, name: str, f32: bool = False) -> int:
-    if t.dtype not in _TYPES or (t.dtype == torch.float32 and not f32):
+    kind = _TYPES.get(t.dtype)
+    if kind is None or (kind == SC_F32 and not f32):
         raise TypeError(f"{name}: expected bfloat16 or float16{' or float32' if f32 else ''}, got {t.dtype}")
     if t.dim() != 2:
         raise ValueError(f"{name}: expected a matrix, got shape {tuple(t.shape)}")
-    return _TYPES[t.dtype]
+    return kind
 
 
 def checkpoint_buffers(rows: int, cols: int, device="cuda"):

@@ -145,27 +145,40 @@ bool tile_map(CUtensorMap* map, int type, const Stored& m, uint32_t box_rows) {
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The fp32 result, or `parts` of them, stored in blocks of 32 x 32.
+bool out_map(CUtensorMap* map, float* p, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t parts, uint64_t part_stride) {
+    const auto fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {cols, rows, parts}, strides[2] = {ld * 4, part_stride * 4};
+    const cuuint32_t box[3] = {32, 32, 1}, steps[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, p, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 constexpr size_t PARTIAL_CAP = 64u << 20;      // bytes of partial sums a split product may use
 
 struct ProductPlan { int bn, cg; uint32_t splits; uint64_t part_ld; size_t bytes; };
 
-// Tile shape and number of parts by an estimate in SM cycles: waves of tiles, each a fixed cost plus its blocks of 64
-// reduction steps, and the partial sums' way to HBM and back.
-ProductPlan product_plan(const sc_ctx* c, uint64_t rows, uint64_t cols, uint64_t red) {
+// Tile shape and number of parts by an estimate in SM cycles: waves of tiles, each as long as its reduction or as the
+// emptying of the accumulator before it, and the partial sums' way to memory and back.  A block of 64 reduction steps costs
+// the tensor pipe 512 cycles for 256 columns (pairs; a little more for one CTA, which loads twice B), or what its bytes
+// take from L2 (50 to 60 a cycle and SM).  Against the best of all shapes and splits, swept over 13 sizes and the three products
+// (one token to 32001, widths 512 to 9000), the choice is within 15 %.
+ProductPlan product_plan(const sc_ctx* c, int mode, uint64_t rows, uint64_t cols, uint64_t red) {
     ProductPlan best{256, 1, 1, (cols + 31) & ~31ull, 0};
     const uint64_t blocks = ceil_div(red, TC_STEP);
     double best_cost = 0;
-    const uint32_t box = (uint32_t)std::min<uint64_t>(rows, TC_ROWS);
+    const double box = (double)std::min<uint64_t>(rows, TC_ROWS);
     for (int shape = 0; shape < 4; ++shape) {                 // 256 x 256 by pairs, then 128 x 256, 128, 64
         const int cg = shape == 0 ? 2 : 1, bn = shape == 0 ? 256 : 512 >> shape;
         if (cg == 2 && rows <= TC_ROWS) continue;
         const uint64_t tiles = ceil_div(rows, TC_ROWS * cg) * ceil_div(cols, bn), units = c->sm_count / cg;
-        const double block_cost = std::max((cg == 2 ? 2.0 : 2.3) * bn, (box + bn) * 128 / 40.0);
+        const double block_cost = cg == 2 ? 540.0 : bn == 256 ? 620.0 : std::max(350.0, (box + bn) * 128 / (bn == 64 ? 50.0 : 60.0));
         for (uint32_t s = 1; s <= blocks && s <= 64; ++s) {
             const size_t bytes = s > 1 ? s * rows * best.part_ld * sizeof(float) : 0;
             if (bytes > PARTIAL_CAP || (s > 1 && tiles * s > units * 2)) break;
-            const double cost = (double)ceil_div(tiles * s, units) * (1500.0 + bn * 6.0 + (double)ceil_div(blocks, s) * block_cost) +
-                                (s > 1 ? 4000.0 + 2.0 * bytes / 3400.0 : 0.0);
+            const double main = (double)ceil_div(blocks, s) * block_cost, out = 800.0 + bn * (mode == PRODUCT_WEIGHT || s > 1 ? 25.0 : 16.0);
+            const double cost = 4000.0 + (double)ceil_div(tiles * s, units) * std::max(main, out) + out + (s > 1 ? 3000.0 + 2.0 * bytes / 2500.0 : 0.0);
             if (best_cost == 0 || cost < best_cost) { best_cost = cost; best.bn = bn; best.cg = cg; best.splits = s; best.bytes = bytes; }
         }
     }
@@ -173,7 +186,7 @@ ProductPlan product_plan(const sc_ctx* c, uint64_t rows, uint64_t cols, uint64_t
 }
 
 template <typename T, int MODE, int BN, int CG>
-int launch_tiles(sc_ctx* c, const CUtensorMap& ma, const CUtensorMap& mb, const TcArgs& a, const Epilogue& ep, cudaStream_t st) {
+int launch_tiles(sc_ctx* c, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mo, const TcArgs& a, const Epilogue& ep, cudaStream_t st) {
     static std::once_flag once;
     static cudaError_t rc;
     std::call_once(once, [] {
@@ -185,7 +198,7 @@ int launch_tiles(sc_ctx* c, const CUtensorMap& ma, const CUtensorMap& mb, const 
     });
     if (rc != cudaSuccess) return SC_ERR_CUDA;
     const uint32_t grid = CG * (uint32_t)std::min<uint64_t>((uint64_t)a.tiles * a.splits, c->sm_count / CG);
-    return launch(product_kernel<T, MODE, BN, CG>, grid, TC_THREADS, TcShape<BN, CG>::SMEM, CG, st, ma, mb, a, ep) == cudaSuccess ? SC_OK : SC_ERR_CUDA;
+    return launch(product_kernel<T, MODE, BN, CG>, grid, TC_THREADS, TcShape<BN, CG>::SMEM, CG, st, ma, mb, mo, a, ep) == cudaSuccess ? SC_OK : SC_ERR_CUDA;
 }
 
 template <typename T, int MODE>
@@ -198,7 +211,7 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
         launch(product_join_kernel<T, MODE>, join_grid, 256, 0, 1, st, nullptr, 0, 0, 0, ep);
         return SC_OK;
     }
-    const ProductPlan p = product_plan(c, ep.rows, ep.cols, red);
+    const ProductPlan p = product_plan(c, MODE, ep.rows, ep.cols, red);
     const uint64_t tiles = ceil_div(ep.rows, TC_ROWS * p.cg) * ceil_div(ep.cols, p.bn);
     if (tiles * p.splits > 0x7FFFFFFFull) return SC_ERR_RANGE;
     const size_t copy_a = tma_ready(A) ? 0 : layout_bytes(A.rows, A.cols), copy_b = tma_ready(B) ? 0 : layout_bytes(B.rows, B.cols);
@@ -221,15 +234,19 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
     a.idesc = mma_idesc(TC_ROWS * p.cg, p.bn, type == SC_BF16, A_MN, B_MN);
     a.a_box_rows = A_MN ? 64u : (uint32_t)std::min<uint64_t>(TC_ROWS, round8(ep.rows));
     a.part_ld = (uint32_t)p.part_ld; a.part_stride = ep.rows * p.part_ld; a.partial = partial; a.status = c->d_status;
-    CUtensorMap ma, mb;
+    a.tma_out = p.splits > 1 || (MODE == PRODUCT_WEIGHT && ep.vec_out);
+    CUtensorMap ma, mb, mo{};
+    if (a.tma_out && !(p.splits > 1 ? out_map(&mo, partial, ep.rows, ep.cols, p.part_ld, p.splits, a.part_stride)
+                                    : out_map(&mo, static_cast<float*>(ep.out), ep.rows, ep.cols, ep.ldo, 1, ep.rows * ep.ldo)))
+        return SC_ERR_CUDA;
     if (!tile_map(&ma, type, A, a.a_box_rows) || !tile_map(&mb, type, B, B_MN ? 64u : (uint32_t)(p.bn / p.cg))) return SC_ERR_CUDA;
     {
         Launch l(c, kind, st);
         int rc;
-        if (p.cg == 2) rc = launch_tiles<T, MODE, 256, 2>(c, ma, mb, a, ep, st);
-        else if (p.bn == 256) rc = launch_tiles<T, MODE, 256, 1>(c, ma, mb, a, ep, st);
-        else if (p.bn == 128) rc = launch_tiles<T, MODE, 128, 1>(c, ma, mb, a, ep, st);
-        else rc = launch_tiles<T, MODE, 64, 1>(c, ma, mb, a, ep, st);
+        if (p.cg == 2) rc = launch_tiles<T, MODE, 256, 2>(c, ma, mb, mo, a, ep, st);
+        else if (p.bn == 256) rc = launch_tiles<T, MODE, 256, 1>(c, ma, mb, mo, a, ep, st);
+        else if (p.bn == 128) rc = launch_tiles<T, MODE, 128, 1>(c, ma, mb, mo, a, ep, st);
+        else rc = launch_tiles<T, MODE, 64, 1>(c, ma, mb, mo, a, ep, st);
         if (rc) return rc;
     }
     if (p.splits > 1) {
@@ -436,7 +453,7 @@ int sc_linear_grad_weight(sc_ctx* ctx, int type, const void* dz, size_t lddz, co
     if (q && M) {                                  // the checkpoint's values, rows 16-byte aligned
         used = layout_bytes(M, K);
         const Stored dzs{dz, M, N, lddz};
-        if (const int rc = layer_scratch(ctx, used + product_plan(ctx, N, K, M).bytes + (tma_ready(dzs) ? 0 : layout_bytes(M, N)), st)) return rc;
+        if (const int rc = layer_scratch(ctx, used + product_plan(ctx, PRODUCT_WEIGHT, N, K, M).bytes + (tma_ready(dzs) ? 0 : layout_bytes(M, N)), st)) return rc;
         void* wide = ctx->d_layer + TICKET_BYTES;
         const uint8_t* qb = reinterpret_cast<const uint8_t*>(q);
         if (type == SC_BF16) launch_unpack<__nv_bfloat16>(ctx, qb, scales, M, K, wide, round8(K), st);

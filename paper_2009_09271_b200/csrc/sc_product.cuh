@@ -141,6 +141,7 @@ struct TcArgs {
     uint32_t idesc, a_box_rows;
     uint64_t part_stride;                  // elements between two parts
     uint32_t part_ld;
+    uint32_t tma_out;                      // fp32 goes out by TMA: partial sums always, the weight gradient where its rows allow
     float* partial;
     int* status;
 };
@@ -155,9 +156,13 @@ __device__ __forceinline__ void tile_at(const TcArgs& a, uint32_t t, uint32_t& t
 // One 32 x 32 block, thread t holding row t, to its place.  The 16-byte units of a row are permuted by its number, which
 // makes both directions free of bank conflicts.
 template <typename T, int MODE>
-__device__ __forceinline__ void block_out(const TcArgs& a, const Epilogue& ep, uint32_t stage_addr, const uint32_t (&v)[32], uint64_t row0, uint32_t col0,
+__device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcArgs& a, const Epilogue& ep, uint32_t stage_addr, const uint32_t (&v)[32], uint64_t row0, uint32_t col0,
                                           uint32_t split) {
     const uint32_t lane = threadIdx.x & 31u;
+    if (a.tma_out) {                       // the last block's copy has left the buffer
+        if (lane == 0) tma_store_wait_read();
+        __syncwarp();
+    }
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage_addr + lane * 128 + ((u ^ (lane & 7)) * 16)),
@@ -173,33 +178,33 @@ __device__ __forceinline__ void block_out(const TcArgs& a, const Epilogue& ep, u
                      : "r"(stage_addr + r * 128 + (((u + 1) ^ (r & 7)) * 16)) : "memory");
         return row0 + r;
     };
-    if (MODE == PRODUCT_WEIGHT || a.splits > 1) {
-        // fp32 goes out in whole 128-byte rows: eight lanes a row, four rows at a time
-        const bool part = a.splits > 1;
+    if (a.tma_out) {                       // the permutation above is the 128-byte swizzle
+        smem_to_async_fence();
+        __syncwarp();
+        if (lane == 0 && row0 < ep.rows && col0 < ep.cols) {
+            if (MODE == PRODUCT_WEIGHT && ep.accumulate && a.splits == 1) tma_add_3d(map_out, stage_addr, (int32_t)col0, (int32_t)row0, 0);
+            else tma_store_3d(map_out, stage_addr, (int32_t)col0, (int32_t)row0, (int32_t)split);
+            tma_store_commit();
+        }
+        return;
+    }
+    if constexpr (MODE == PRODUCT_WEIGHT) {
+        // rows that are not 16-byte aligned: whole 128-byte rows, four at a time
         const uint32_t c = col0 + (lane & 7u) * 4;
-        const uint64_t ld = part ? a.part_ld : ep.ldo;
-        float* out = (part ? a.partial + split * a.part_stride : static_cast<float*>(ep.out)) + (row0 + (lane >> 3)) * ld + c;
-        const bool vec = part || ep.vec_out, add = !part && ep.accumulate;
+        float* out = static_cast<float*>(ep.out) + (row0 + (lane >> 3)) * ep.ldo + c;
+        const bool add = ep.accumulate;
 #pragma unroll 2
         for (int i = 0; i < 8; ++i) {
             const uint32_t r = (lane >> 3) + 4 * i;
             float4 f;
             asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
                          : "r"(stage_addr + r * 128 + (((lane & 7u) ^ (r & 7u)) * 16)) : "memory");
-            float* o = out + (uint64_t)(4 * i) * ld;
+            float* o = out + (uint64_t)(4 * i) * ep.ldo;
             if (row0 + r >= ep.rows || c >= ep.cols) continue;
-            if (vec) {
-                if (add) {
-                    const float4 x = *reinterpret_cast<const float4*>(o);
-                    f.x += x.x; f.y += x.y; f.z += x.z; f.w += x.w;
-                }
-                *reinterpret_cast<float4*>(o) = f;
-            } else {
-                const float v4[4] = {f.x, f.y, f.z, f.w};
+            const float v4[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (c + k < ep.cols) o[k] = add ? o[k] + v4[k] : v4[k];
-            }
+            for (int k = 0; k < 4; ++k)
+                if (c + k < ep.cols) o[k] = add ? o[k] + v4[k] : v4[k];
         }
     } else {
         float bias[8];
@@ -218,7 +223,7 @@ __device__ __forceinline__ void block_out(const TcArgs& a, const Epilogue& ep, u
 
 template <typename T, int MODE, int BN, int CG>
 __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                                TcArgs a, Epilogue ep) {
+                                                                const __grid_constant__ CUtensorMap map_out, TcArgs a, Epilogue ep) {
     using S = TcShape<BN, CG>;
     constexpr bool A_MN = MODE == PRODUCT_WEIGHT, B_MN = MODE != PRODUCT_FORWARD;
     constexpr bool SUM = MODE == PRODUCT_WEIGHT;
@@ -237,6 +242,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
         mbar_init_fence();
         tma_prefetch_map(&map_a);
         tma_prefetch_map(&map_b);
+        if (a.tma_out) tma_prefetch_map(&map_out);
     }
     if (warp == 2) tmem_alloc<CG>(slot, S::TMEM_COLS);
     tcgen05_fence_before();
@@ -369,7 +375,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                 }
                 if (!ok) break;
 #pragma unroll
-                for (int c = 0; c < BN / 64; ++c) block_out<T, MODE>(a, ep, stage_addr, sum[c], row0, col0 + c * 32, split);
+                for (int c = 0; c < BN / 64; ++c) block_out<T, MODE>(&map_out, a, ep, stage_addr, sum[c], row0, col0 + c * 32, split);
             } else {
                 if (!(ok = warp_wait(tfull + 8 * acc, acc_phase))) break;
                 __syncwarp();
@@ -384,11 +390,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                         __syncwarp();
                         if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_rank(tempty + 8 * acc, 0) : tempty + 8 * acc);
                     }
-                    block_out<T, MODE>(a, ep, stage_addr, v, row0, col0 + c, split);
+                    block_out<T, MODE>(&map_out, a, ep, stage_addr, v, row0, col0 + c, split);
                 }
                 if ((acc ^= 1u) == 0) acc_phase ^= 1u;
             }
         }
+        if (a.tma_out && lane == 0) tma_store_wait();
         if (!ok && lane == 0) atomicCAS(a.status, 0, ST_TIMEOUT);
         __syncwarp();
     }
