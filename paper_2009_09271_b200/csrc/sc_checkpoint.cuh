@@ -282,7 +282,6 @@ template <typename T, int ACT, bool VEC>
 __global__ void __launch_bounds__(CKPT_THREADS, 4) activation_grad_kernel(const T* dy, const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales,
                                                                           GradArgs a, T* dz, float* __restrict__ partial,
                                                                           uint32_t* __restrict__ tickets, float* __restrict__ db) {
-    constexpr int AHEAD = 2;                  // rows of a thread in flight
     wait_for_predecessor();
     release_successor();
     const uint32_t tx = threadIdx.x & 31u, ty = threadIdx.x >> 5;
@@ -294,41 +293,44 @@ __global__ void __launch_bounds__(CKPT_THREADS, 4) activation_grad_kernel(const 
     if (c0 < a.cols) {
         const uint32_t left = (uint32_t)(min((uint64_t)(blockIdx.y + 1) * a.run_rows, a.rows) - (uint64_t)blockIdx.y * a.run_rows);
         const T* from = dy + r0 * a.lddy;
-        T* to = dz ? dz + r0 * a.lddz : nullptr;
+        T* to = dz + r0 * a.lddz;
         const uint8_t *qr = q + r0 * a.cols, *sr = scales + r0 * a.groups + (c0 >> 5);
         const uint64_t step_y = GRAD_LANES * a.lddy, step_z = GRAD_LANES * a.lddz, step_q = (uint64_t)GRAD_LANES * a.cols, step_s = (uint64_t)GRAD_LANES * a.groups;
-        for (uint32_t r = ty; r < left; r += GRAD_LANES * AHEAD) {
-            Raw8<T> g[AHEAD];
-            uint2 k[AHEAD];
-            uint32_t sb[AHEAD];
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                if (r + u * GRAD_LANES < left) {
-                    g[u] = load8(from, c0, a.cols, VEC);
-                    if constexpr (ACT != SC_ACT_NONE) {
-                        k[u] = load_q8(qr, c0, a.cols, VEC);
-                        sb[u] = *sr;
-                    }
+        // a thread works on one row while its next one is on the way
+        struct Row { Raw8<T> g; uint2 k; uint32_t sb; };
+        const auto fetch = [&](Row& row, uint32_t r) {
+            if (r < left) {
+                row.g = load8(from, c0, a.cols, VEC);
+                if constexpr (ACT != SC_ACT_NONE) {
+                    row.k = load_q8(qr, c0, a.cols, VEC);
+                    row.sb = *sr;
                 }
-                from += step_y; qr += step_q; sr += step_s;
             }
+            from += step_y; qr += step_q; sr += step_s;
+        };
+        const auto work = [&](const Row& row, uint32_t r) {
+            if (r < left) {
+                float f[8];
+                to_floats(row.g, f);
+                Pair v[4], z[4];
+                if constexpr (ACT != SC_ACT_NONE) ckpt_values8<false>(row.k, slope_scale(row.sb), z);
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                if (r + u * GRAD_LANES < left) {
-                    float f[8];
-                    to_floats(g[u], f);
-                    Pair v[4], z[4];
-                    if constexpr (ACT != SC_ACT_NONE) ckpt_values8<false>(k[u], slope_scale(sb[u]), z);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        v[i] = pair(f[2 * i], f[2 * i + 1]);
-                        if constexpr (ACT != SC_ACT_NONE) v[i] = v[i] * activation_slope<ACT>(z[i]);
-                        sum[i] = sum[i] + v[i];
-                    }
-                    if (to) store8(to, c0, a.cols, VEC, v);
+                for (int i = 0; i < 4; ++i) {
+                    v[i] = pair(f[2 * i], f[2 * i + 1]);
+                    if constexpr (ACT != SC_ACT_NONE) v[i] = v[i] * activation_slope<ACT>(z[i]);
+                    sum[i] = sum[i] + v[i];
                 }
-                to = to ? to + step_z : nullptr;
+                if (dz) store8(to, c0, a.cols, VEC, v);
             }
+            to += step_z;
+        };
+        Row x, y;
+        fetch(x, ty);
+        for (uint32_t r = ty; r < left; r += 2 * GRAD_LANES) {
+            fetch(y, r + GRAD_LANES);
+            work(x, r);
+            fetch(x, r + 2 * GRAD_LANES);
+            work(y, r + GRAD_LANES);
         }
     }
     if (!db) return;

@@ -51,7 +51,7 @@ int layer_scratch(sc_ctx* c, size_t bytes, cudaStream_t st) {
 }
 
 uint32_t item_grid(const sc_ctx* c, uint64_t total) {
-    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(total, CKPT_THREADS * CKPT_UNROLL), (uint64_t)c->sm_count * 8));
+    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(total, CKPT_THREADS), (uint64_t)c->sm_count * 8));
 }
 
 // Launches a layer kernel (optionally in clusters) that may begin while its predecessor on the stream ends.

@@ -152,9 +152,9 @@ __device__ __forceinline__ Pair activation(Pair z) {
 // z is a checkpoint's value, read through slope_scale(): |z| < 2^48, so that no product below overflows.  NaN passes.
 template <int ACT>
 __device__ __forceinline__ Pair activation_slope(Pair z) {
-    if constexpr (ACT == SC_ACT_RELU) {
-        const float2 f = both(z);
-        return pair(f.x > 0.0f ? 1.0f : (f.x <= 0.0f ? 0.0f : f.x), f.y > 0.0f ? 1.0f : (f.y <= 0.0f ? 0.0f : f.y));
+    if constexpr (ACT == SC_ACT_RELU) {                                              // 0 z keeps NaN
+        const float2 f = both(z), n = both(z * pair(0.0f));
+        return pair(f.x > 0.0f ? 1.0f : n.x, f.y > 0.0f ? 1.0f : n.y);
     } else if constexpr (ACT == SC_ACT_GELU) {                                       // Phi(z) + z phi(z)
         const Pair e = exp_half_square(z);
         const float2 f = both(z), c = both(fma2(normal_tail(z, e), pair(-1.0f), pair(0.5f)));
