@@ -119,7 +119,8 @@ int sc_topk_path_detail(sc_ctx* ctx, void* stream, uint32_t* h_counts);
  * SC_ERR_TIMEOUT in the status word and let the kernel return.  sc_debug_set_poll_limits changes the
  * two limits for later calls of this context (0 restores the default).  sc_debug_wait_probe launches a
  * small kernel that runs one of the waits where what it waits for never arrives: which = 0, a barrier
- * that expects one CTA more than the launch has; which = 1, a look-back at a count nobody publishes.
+ * that expects one CTA more than the launch has; which = 1, a look-back at a count nobody publishes;
+ * which = 2, a wait of the layer products (about two seconds by default, here 100 cycles per barrier poll if that is less).
  * The kernel returns when the limit is reached (set a small one first); sc_sync_status then reports
  * SC_ERR_TIMEOUT. */
 int sc_debug_set_poll_limits(sc_ctx* ctx, uint32_t lookback_polls, uint32_t barrier_polls);
@@ -228,7 +229,8 @@ int sc_step_host(sc_ctx* ctx, int scheme, int W, const float* h_grads, float* re
  * Each run of 32 elements of a row has one scale 2^e, stored as e + 127: e is the least exponent with
  * m <= 127 * 2^e for the largest finite magnitude m of the run, within [-126, 122] (SC_F16: [-24, 10]);
  * q = x 2^-e rounded to the nearest integer, ties to even, and within +-127 (+-63 where e is the largest of its range).
- * An element that is not finite is kept as q = -128, which reads as NaN.  The value q * 2^e is exactly a value of
+ * An element that is not finite is kept as q = -128, which reads as NaN.  Elements within half a step of 0 read as 0, where
+ * relu's slope is 0.  The value q * 2^e is exactly a value of
  * the type, so what reads a checkpoint adds no rounding of its own.
  * --------------------------------------------------------------------------------------------------------- */
 enum { SC_BF16 = 0, SC_F16 = 1, SC_F32 = 2 /* checkpoints only */ };
@@ -247,7 +249,7 @@ int sc_checkpoint_unpack(sc_ctx* ctx, int type, const int8_t* q, const uint8_t* 
                          void* out, size_t ldo, void* stream);
 
 /* dz = dy * act'(z^) with z^ the checkpoint (q, scales) of the pre-activation, and db[cols] = column sums of dz
- * before its rounding (accumulate: added to db).  dz or db may be NULL; dz may be dy.  With SC_ACT_NONE the
+ * before its rounding (accumulate: added to db).  dz or db may be NULL; dz may be dy (same ld).  With SC_ACT_NONE the
  * checkpoint is not read: the call gives the bias gradient of dy. */
 int sc_activation_grad(sc_ctx* ctx, int type, int act, const void* dy, size_t lddy, const int8_t* q, const uint8_t* scales,
                        size_t rows, size_t cols, void* dz, size_t lddz, float* db, int accumulate, void* stream);

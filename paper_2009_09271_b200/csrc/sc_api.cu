@@ -776,9 +776,13 @@ int sc_debug_set_poll_limits(sc_ctx* c, uint32_t lookback_polls, uint32_t barrie
 }
 
 int sc_debug_wait_probe(sc_ctx* c, int which, void* stream) {
-    if (!c || (which != 0 && which != 1)) return SC_ERR_INVALID;
+    if (!c || which < 0 || which > 2) return SC_ERR_INVALID;
     DeviceGuard guard(c->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (which == 2) {
+        ++c->launches;
+        return layer_wait_probe(c, 100ll * c->barrier_poll_limit, st);
+    }
     PackParams k{};
     if (++c->epoch >= (1u << 28)) {
         SC_CUDA(cudaMemsetAsync(c->d_desc, 0, (size_t)c->max_W * c->max_tiles_per_worker * 2 * sizeof(unsigned long long), st));

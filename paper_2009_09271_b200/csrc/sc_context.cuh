@@ -162,3 +162,6 @@ class Launch {
 };
 
 }  // namespace
+
+// sc_layer.cu: a kernel that waits as the layer products do, for something that never arrives.
+int layer_wait_probe(sc_ctx* c, long long limit_cycles, cudaStream_t st);

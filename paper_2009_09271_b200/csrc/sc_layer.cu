@@ -118,7 +118,11 @@ GradPlan grad_plan(const sc_ctx* c, size_t rows, size_t cols) {
 // matrix products
 // ---------------------------------------------------------------------------
 // A stored 16-bit matrix: `rows` rows of `cols` elements, `ld` apart.
-struct Stored { const void* p; uint64_t rows, cols, ld; };
+struct Stored {
+    const void* p;
+    uint64_t rows, cols, ld;
+    Stored(const void* p_, uint64_t rows_, uint64_t cols_, uint64_t ld_) : p(p_), rows(rows_), cols(cols_), ld(rows_ > 1 ? ld_ : (cols_ + 7) & ~7ull) {}
+};
 
 inline uint64_t round8(uint64_t n) { return (n + 7) & ~7ull; }
 inline bool tma_ready(const Stored& m) { return aligned(m.p, 16) && m.ld % 8 == 0; }
@@ -234,9 +238,10 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
     a.idesc = mma_idesc(TC_ROWS * p.cg, p.bn, type == SC_BF16, A_MN, B_MN);
     a.a_box_rows = A_MN ? 64u : (uint32_t)std::min<uint64_t>(TC_ROWS, round8(ep.rows));
     a.part_ld = (uint32_t)p.part_ld; a.part_stride = ep.rows * p.part_ld; a.partial = partial; a.status = c->d_status;
+    // partial sums are whole to the next multiple of 32 columns: a checkpoint group's maximum is taken over all of its columns
     a.tma_out = p.splits > 1 || (MODE == PRODUCT_WEIGHT && ep.vec_out);
     CUtensorMap ma, mb, mo{};
-    if (a.tma_out && !(p.splits > 1 ? out_map(&mo, partial, ep.rows, ep.cols, p.part_ld, p.splits, a.part_stride)
+    if (a.tma_out && !(p.splits > 1 ? out_map(&mo, partial, ep.rows, p.part_ld, p.part_ld, p.splits, a.part_stride)
                                     : out_map(&mo, static_cast<float*>(ep.out), ep.rows, ep.cols, ep.ldo, 1, ep.rows * ep.ldo)))
         return SC_ERR_CUDA;
     if (!tile_map(&ma, type, A, a.a_box_rows) || !tile_map(&mb, type, B, B_MN ? 64u : (uint32_t)(p.bn / p.cg))) return SC_ERR_CUDA;
@@ -285,7 +290,21 @@ int run_product(sc_ctx* c, int kind, int type, const Stored& A, const Stored& B,
     return run_product<__nv_bfloat16, MODE>(c, kind, type, A, B, red, ep, used, st);
 }
 
+// A wait of the layer products where nothing arrives.
+__global__ void layer_wait_probe_kernel(long long limit, int* status) {
+    __shared__ __align__(8) unsigned long long word;
+    const uint32_t bar = smem_addr(&word);
+    if (threadIdx.x == 0) { mbar_init(bar, 1); mbar_init_fence(); }
+    __syncwarp();
+    if (!warp_wait(bar, 0, limit) && threadIdx.x == 0) atomicCAS(status, 0, ST_TIMEOUT);
+}
+
 }  // namespace
+
+int layer_wait_probe(sc_ctx* c, long long limit_cycles, cudaStream_t st) {
+    layer_wait_probe_kernel<<<1, 32, 0, st>>>(std::min(limit_cycles, MBAR_LIMIT_CYCLES), c->d_status);
+    return cudaGetLastError() == cudaSuccess ? SC_OK : SC_ERR_CUDA;
+}
 
 extern "C" {
 
@@ -343,7 +362,7 @@ int sc_activation_grad(sc_ctx* ctx, int type, int act, const void* dy, size_t ld
     if (cols == 0) return SC_OK;
     const bool kept = act != SC_ACT_NONE;
     if (kept && rows && (!q || !scales)) return SC_ERR_INVALID;
-    if (ceil_div(cols, GRAD_COLS) > MAX_TICKETS) return SC_ERR_RANGE;
+    if (db && ceil_div(cols, GRAD_COLS) > MAX_TICKETS) return SC_ERR_RANGE;
     DeviceGuard guard(ctx->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (rows == 0) {

@@ -53,16 +53,18 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
 }
 // Waits for the phase of the given parity to complete; gives up after about two seconds.
 constexpr long long MBAR_LIMIT_CYCLES = 4000000000ll;
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, long long limit = MBAR_LIMIT_CYCLES) {
     if (mbar_try(bar, parity)) return true;
     const long long t0 = clock64();
     while (!mbar_try(bar, parity))
-        if (clock64() - t0 > MBAR_LIMIT_CYCLES) return false;
+        if (clock64() - t0 > limit) return false;
     return true;
 }
 
 // The same for a whole warp, whose lanes agree on the outcome and stay together.
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity)); }
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, long long limit = MBAR_LIMIT_CYCLES) {
+    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, limit));
+}
 
 // -- TMA ------------------------------------------------------------------------
 __device__ __forceinline__ void tma_prefetch_map(const CUtensorMap* m) {

@@ -420,6 +420,65 @@ def test_capture_in_a_graph(ctx):
     own.close()
 
 
+def test_rows_past_32_bits(ctx):
+    """Rows so far apart that element offsets pass 2^32, in every product, and the same through the copies of unaligned rows."""
+    for step in ((1 << 31) - 1024, (1 << 31) - 1023):
+        store = torch.zeros(2 * step + 4096, dtype=torch.bfloat16, device="cuda")           # 8.6 GB
+        g = rng(4)
+        far = store.as_strided((3, 200), (step, 1))
+        far.copy_(normal(g, 3, 200).to(torch.bfloat16))
+        w = (normal(g, 72, 200) / 14).to(torch.bfloat16)
+        xs = far.clone()
+        for rows in (3,):
+            y, want = torch.empty(rows, 72, dtype=torch.bfloat16, device="cuda"), torch.empty(rows, 72, dtype=torch.bfloat16, device="cuda")
+            ctx.sc_linear(sc.SC_ACT_NONE, far, w, y)
+            ctx.sc_linear(sc.SC_ACT_NONE, xs, w, want)
+            assert torch.equal(y, want)
+            v = (normal(g, 200, 72) / 14).to(torch.bfloat16)
+            ctx.sc_linear_grad_input(far, v, y)
+            ctx.sc_linear_grad_input(xs, v, want)
+            assert torch.equal(y, want)
+            dw, dww = torch.empty(200, 72, device="cuda"), torch.empty(200, 72, device="cuda")
+            ctx.sc_linear_grad_weight(far, dw, x=want)
+            ctx.sc_linear_grad_weight(xs, dww, x=want)
+            assert torch.equal(dw, dww)
+        out = store.as_strided((3, 72), (step, 1))
+        ctx.sc_linear(sc.SC_ACT_NONE, xs, w, out)
+        ctx.sc_linear(sc.SC_ACT_NONE, xs, w, want)
+        assert torch.equal(out, want)
+        del store, far, out
+
+
+def test_tokens_and_tiles_agree_at_the_border(ctx):
+    """One to four tokens take the kernel without tiles, five the tensor tiles: the same sums within their bounds."""
+    for M in (1, 2, 3, 4, 5):
+        for N, K in ((1000, 8), (33, 5000), (4096, 264)):
+            check_linear(ctx, torch.bfloat16, "gelu_tanh", M, N, K, True, True, True)
+            check_linear(ctx, torch.float16, "relu", M, N, K, False, False, False, 1, 1)
+
+
+def test_product_wait_runs_out_and_the_context_stays_usable():
+    own = sc.Context(max_n=1)
+    own.sc_debug_set_poll_limits(2000, 2000)
+    own.sc_debug_wait_probe(2)
+    assert own.sc_sync_status() == -5
+    assert own.sc_sync_status() == 0
+    check_linear(own, torch.bfloat16, "silu", 130, 264, 136, True, False, True)
+    assert own.sc_sync_status() == 0
+    own.close()
+
+
+def test_broadcast_and_transposed_inputs_are_refused(ctx):
+    row = torch.zeros(1, 64, dtype=torch.bfloat16, device="cuda")
+    y, w = torch.zeros(8, 32, dtype=torch.bfloat16, device="cuda"), torch.zeros(32, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(TypeError):
+        ctx.sc_linear(0, row.expand(8, 64), w, y)
+    with pytest.raises(TypeError):
+        ctx.sc_activation_grad(0, row.expand(8, 64), None, None, torch.zeros(8, 64, dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(TypeError):
+        ctx.sc_linear_grad_input(y, w.t().contiguous().t(), torch.zeros(8, 64, dtype=torch.bfloat16, device="cuda"))
+
+
 # -- gradients against differences -----------------------------------------------------------------------------------
 @pytest.mark.parametrize("act", ACTS[1:])
 def test_gradients_against_differences(ctx, act):
