@@ -239,7 +239,7 @@ enum { SC_ACT_NONE = 0, SC_ACT_RELU = 1, SC_ACT_GELU = 2 /* z Phi(z) */,
 
 /* The layer operators keep their workspace in the context.  A call that needs more than it has allocates
  * (synchronous), or returns SC_ERR_WORKSPACE while its stream is being captured.  sc_layer_reserve allocates
- * ahead what any layer call of at most these sizes needs. */
+ * ahead what any layer call of at most these sizes needs.  A block that captured calls used is kept until sc_destroy. */
 int sc_layer_reserve(sc_ctx* ctx, size_t M, size_t N, size_t K);
 
 /* Checkpoint of x, and the values of a checkpoint (rounded to `type` where the checkpoint was made from another). */
@@ -267,7 +267,7 @@ int sc_linear_grad_input(sc_ctx* ctx, int type, int act, const void* dz, size_t 
                          const void* residual, size_t ldr, const int8_t* q, const uint8_t* scales,
                          size_t M, size_t N, size_t K, void* dx, size_t lddx, void* stream);
 
-/* dW = dz^T x in fp32, rows of lddw (accumulate: added to dW).  The layer's input is given once: as x, or as its
+/* dW = dz^T x in fp32, rows of lddw (accumulate: added to dW, where values below 2^-126 may count as 0).  The layer's input is given once: as x, or as its
  * checkpoint (q, scales) with x NULL. */
 int sc_linear_grad_weight(sc_ctx* ctx, int type, const void* dz, size_t lddz, const void* x, size_t ldx,
                           const int8_t* q, const uint8_t* scales, size_t M, size_t N, size_t K,

@@ -672,6 +672,7 @@ void sc_destroy(sc_ctx* c) {
     cudaFree(c->d_flagged); cudaFree(c->d_seeds); cudaFree(c->d_status);
     cudaFree(c->d_stage_grads); cudaFree(c->d_stage_vals); cudaFree(c->d_stage_idx); cudaFree(c->d_stage_out);
     cudaFree(c->d_layer);
+    for (int i = 0; i < c->layer_retired_count; ++i) cudaFree(c->layer_retired[i]);
     for (cudaEvent_t e : c->ev_worker) cudaEventDestroy(e);
     for (auto& r : c->prof_recs) { cudaEventDestroy(r.a); cudaEventDestroy(r.b); }
     for (cudaEvent_t e : c->prof_free) cudaEventDestroy(e);

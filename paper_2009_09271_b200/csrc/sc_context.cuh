@@ -94,6 +94,10 @@ struct sc_ctx {
     // layer operators (sc_layer.cu): one block, grown on demand, and tickets that are zero between calls
     unsigned char* d_layer = nullptr;
     size_t layer_bytes = 0;
+    bool layer_captured = false;                 // a captured call used the block: growing must not free it
+    static constexpr int MAX_RETIRED = 64;
+    unsigned char* layer_retired[MAX_RETIRED] = {};
+    int layer_retired_count = 0;
 };
 
 namespace {

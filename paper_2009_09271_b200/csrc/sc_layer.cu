@@ -30,18 +30,27 @@ constexpr size_t TICKET_BYTES = 65536;
 constexpr uint32_t MAX_TICKETS = TICKET_BYTES / sizeof(uint32_t);
 
 int layer_scratch(sc_ctx* c, size_t bytes, cudaStream_t st) {
-    if (c->d_layer && c->layer_bytes >= bytes) return SC_OK;
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
     SC_CUDA(cudaStreamIsCapturing(st, &cap));
-    if (cap != cudaStreamCaptureStatusNone) return SC_ERR_WORKSPACE;      // reserve before the capture
-    if (c->d_layer) {
-        SC_CUDA(cudaStreamSynchronize(st));
-        cudaFree(c->d_layer);
-        c->scratch_bytes -= TICKET_BYTES + c->layer_bytes;
-        c->d_layer = nullptr; c->layer_bytes = 0;
+    const bool capturing = cap != cudaStreamCaptureStatusNone;
+    if (c->d_layer && c->layer_bytes >= bytes) {
+        c->layer_captured |= capturing;
+        return SC_OK;
     }
+    if (capturing) return SC_ERR_WORKSPACE;                               // reserve before the capture
     bytes = (bytes + 255) & ~(size_t)255;
     void* p = nullptr;
+    if (c->d_layer) {
+        SC_CUDA(cudaStreamSynchronize(st));
+        if (c->layer_captured) {                                          // a graph may still use it: kept until sc_destroy
+            if (c->layer_retired_count == sc_ctx::MAX_RETIRED) return SC_ERR_WORKSPACE;
+            c->layer_retired[c->layer_retired_count++] = c->d_layer;
+        } else {
+            cudaFree(c->d_layer);
+            c->scratch_bytes -= TICKET_BYTES + c->layer_bytes;
+        }
+        c->d_layer = nullptr; c->layer_bytes = 0; c->layer_captured = false;
+    }
     if (cudaMalloc(&p, TICKET_BYTES + bytes) != cudaSuccess) { cudaGetLastError(); return SC_ERR_WORKSPACE; }
     if (cudaMemsetAsync(p, 0, TICKET_BYTES, st) != cudaSuccess) { cudaFree(p); return SC_ERR_CUDA; }
     c->d_layer = static_cast<unsigned char*>(p);
@@ -312,9 +321,9 @@ int sc_layer_reserve(sc_ctx* ctx, size_t M, size_t N, size_t K) {
     if (!ctx) return SC_ERR_INVALID;
     if (M >= MAX_DIM || N >= MAX_DIM || K >= MAX_DIM) return SC_ERR_RANGE;
     DeviceGuard guard(ctx->device);
-    const size_t grad = M && N && K ? std::max(grad_plan(ctx, M, N).bytes, grad_plan(ctx, M, K).bytes) : 0;
-    const size_t x = layout_bytes(M, K), w = K % 8 ? layout_bytes(N, K) : 0, z = N % 8 ? layout_bytes(M, N) : 0;
-    const size_t bytes = std::max(grad, PARTIAL_CAP + x + w + z);
+    // the operands' copies (x^ always, the others where rows are not 16-byte aligned) and partial sums; the bias gradient's
+    // partial rows are far below the latter
+    const size_t bytes = PARTIAL_CAP + layout_bytes(M, K) + layout_bytes(N, K) + layout_bytes(M, N);
     return layer_scratch(ctx, bytes, nullptr);
 }
 

@@ -182,6 +182,7 @@ __device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcAr
         smem_to_async_fence();
         __syncwarp();
         if (lane == 0 && row0 < ep.rows && col0 < ep.cols) {
+            // the addition happens in L2, without waiting for what is there: one per element, so in no order that could change
             if (MODE == PRODUCT_WEIGHT && ep.accumulate && a.splits == 1) tma_add_3d(map_out, stage_addr, (int32_t)col0, (int32_t)row0, 0);
             else tma_store_3d(map_out, stage_addr, (int32_t)col0, (int32_t)row0, (int32_t)split);
             tma_store_commit();
@@ -189,22 +190,23 @@ __device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcAr
         return;
     }
     if constexpr (MODE == PRODUCT_WEIGHT) {
-        // rows that are not 16-byte aligned: whole 128-byte rows, four at a time
-        const uint32_t c = col0 + (lane & 7u) * 4;
-        float* out = static_cast<float*>(ep.out) + (row0 + (lane >> 3)) * ep.ldo + c;
-        const bool add = ep.accumulate;
-#pragma unroll 2
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t r = (lane >> 3) + 4 * i;
-            float4 f;
-            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w)
-                         : "r"(stage_addr + r * 128 + (((lane & 7u) ^ (r & 7u)) * 16)) : "memory");
-            float* o = out + (uint64_t)(4 * i) * ep.ldo;
-            if (row0 + r >= ep.rows || c >= ep.cols) continue;
-            const float v4[4] = {f.x, f.y, f.z, f.w};
+        // Rows at any 4-byte offset: one row of 32 a store, eight rows at a time.
+        const uint32_t c = col0 + lane;
+        float* out = static_cast<float*>(ep.out) + row0 * ep.ldo + c;
+        const uint32_t rows = c < ep.cols && row0 < ep.rows ? (uint32_t)min((uint64_t)32, ep.rows - row0) : 0u;
+#pragma unroll 1
+        for (uint32_t r0 = 0; r0 < 32; r0 += 8) {
+            float f[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (c + k < ep.cols) o[k] = add ? o[k] + v4[k] : v4[k];
+            for (uint32_t i = 0; i < 8; ++i)
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f[i]) : "r"(stage_addr + (r0 + i) * 128 + (((lane >> 2) ^ i) * 16) + (lane & 3u) * 4) : "memory");
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) {
+                if (r0 + i >= rows) continue;
+                float* o = out + (uint64_t)(r0 + i) * ep.ldo;
+                if (ep.accumulate) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(o), "f"(f[i]) : "memory");
+                else *o = f[i];
+            }
         }
     } else {
         float bias[8];

@@ -417,6 +417,15 @@ def test_capture_in_a_graph(ctx):
     torch.cuda.synchronize()
     for got, ref in zip((dw, dx, db), want):
         assert torch.equal(got, ref)
+    own.sc_layer_reserve(4 * M, N, K)                       # a larger workspace leaves the graph's own in place
+    for t in (dw, dx, db):
+        t.fill_(0)
+    torch.empty(1 << 28, device="cuda", dtype=torch.uint8).fill_(255)
+    graph.replay()
+    torch.cuda.synchronize()
+    for got, ref in zip((dw, dx, db), want):
+        assert torch.equal(got, ref)
+    del graph
     own.close()
 
 
