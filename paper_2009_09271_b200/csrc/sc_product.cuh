@@ -200,12 +200,14 @@ __device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcAr
 #pragma unroll
             for (uint32_t i = 0; i < 8; ++i)
                 asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f[i]) : "r"(stage_addr + (r0 + i) * 128 + (((lane >> 2) ^ i) * 16) + (lane & 3u) * 4) : "memory");
+            if (ep.accumulate) {
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) {
-                if (r0 + i >= rows) continue;
-                float* o = out + (uint64_t)(r0 + i) * ep.ldo;
-                if (ep.accumulate) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(o), "f"(f[i]) : "memory");
-                else *o = f[i];
+                for (uint32_t i = 0; i < 8; ++i, out += ep.ldo)
+                    if (r0 + i < rows) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(out), "f"(f[i]) : "memory");
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i, out += ep.ldo)
+                    if (r0 + i < rows) *out = f[i];
             }
         }
     } else {
