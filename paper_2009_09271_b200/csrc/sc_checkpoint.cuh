@@ -17,8 +17,7 @@ constexpr int CKPT_UNROLL = 4;                // items a thread has in flight
 struct ItemWalk {
     uint64_t total, stride_rows;              // total = rows * items
     uint32_t cols, items, stride_items;       // items per row (even)
-    uint32_t vec;                             // 16-byte accesses are aligned and 8 elements never straddle a row's end;
-                                              // 2: nor do 16, and q takes 16-byte accesses too; 3: rows take 32-byte ones
+    uint32_t grain_x, grain_q;                // elements that one access of a row, or of q, may take
 };
 
 struct ItemAt {
@@ -35,18 +34,82 @@ struct ItemAt {
 template <typename T> struct Raw8 { uint4 v; };
 template <> struct Raw8<float> { uint4 v, w; };
 
-template <typename T>
-__device__ __forceinline__ Raw8<T> load8(const T* row, uint32_t c0, uint32_t cols, uint32_t vec) {
-    Raw8<T> r{};
-    if (vec) {
-        if (c0 < cols) {
-            r.v = __ldcs(reinterpret_cast<const uint4*>(row + c0));
-            if constexpr (sizeof(T) == 4) r.w = __ldcs(reinterpret_cast<const uint4*>(row + c0) + 1);
-        }
+// A grain is the widest run of elements, a power of two, at whose multiples every row of a matrix is aligned to the run's size:
+// 16-bit rows of grain 8 take 16-byte accesses, and so on down to single elements.  What is narrower than 16 bytes, and a
+// row's ragged end, goes through these functions, which are kept out of line.
+static __device__ __noinline__ uint4 load_narrow(const uint16_t* p, uint32_t n, uint32_t grain) {
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (n >= 8 && grain >= 4) {
+        const uint2 a = *reinterpret_cast<const uint2*>(p), b = *(reinterpret_cast<const uint2*>(p) + 1);
+        v = make_uint4(a.x, a.y, b.x, b.y);
+    } else if (n >= 8 && grain == 2) {
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(p);
+        v = make_uint4(w[0], w[1], w[2], w[3]);
     } else {
-        T* e = reinterpret_cast<T*>(&r);
+        uint16_t e[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (c0 + i < cols) e[i] = row[c0 + i];
+        for (int i = 0; i < 8; ++i) e[i] = i < (int)n ? p[i] : (uint16_t)0;
+        v = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+    }
+    return v;
+}
+static __device__ __noinline__ void store_narrow(uint16_t* p, uint4 v, uint32_t n, uint32_t grain) {
+    if (n >= 8 && grain >= 4) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(v.x, v.y);
+        *(reinterpret_cast<uint2*>(p) + 1) = make_uint2(v.z, v.w);
+    } else if (n >= 8 && grain == 2) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(p);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    } else {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i < (int)n) p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+    }
+}
+static __device__ __noinline__ uint2 load_q_narrow(const uint8_t* p, uint32_t n, uint32_t grain) {
+    if (n >= 8 && grain >= 4) return make_uint2(*reinterpret_cast<const uint32_t*>(p), *(reinterpret_cast<const uint32_t*>(p) + 1));
+    uint32_t v[2] = {0u, 0u};
+    if (n >= 8 && grain == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i < (int)n) v[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+    }
+    return make_uint2(v[0], v[1]);
+}
+static __device__ __noinline__ void store_q_narrow(uint8_t* p, uint2 v, uint32_t n, uint32_t grain) {
+    const uint32_t w[2] = {v.x, v.y};
+    if (n >= 8 && grain >= 4) {
+        reinterpret_cast<uint32_t*>(p)[0] = v.x;
+        reinterpret_cast<uint32_t*>(p)[1] = v.y;
+    } else if (n >= 8 && grain == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (i < (int)n) p[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+    }
+}
+
+// Eight elements from column c0; zero past the row's end.
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const T* row, uint32_t c0, uint32_t cols, uint32_t grain) {
+    Raw8<T> r{};
+    if constexpr (sizeof(T) == 2) {
+        if (grain >= 8 && c0 + 8 <= cols) r.v = __ldcs(reinterpret_cast<const uint4*>(row + c0));
+        else if (c0 < cols) r.v = load_narrow(reinterpret_cast<const uint16_t*>(row + c0), cols - c0, grain);
+    } else {
+        if (grain >= 4 && c0 + 8 <= cols) {
+            r.v = __ldcs(reinterpret_cast<const uint4*>(row + c0));
+            r.w = __ldcs(reinterpret_cast<const uint4*>(row + c0) + 1);
+        } else {
+            uint32_t e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = c0 + i < cols ? __float_as_uint(row[c0 + i]) : 0u;
+            r.v = make_uint4(e[0], e[1], e[2], e[3]);
+            r.w = make_uint4(e[4], e[5], e[6], e[7]);
+        }
     }
     return r;
 }
@@ -91,9 +154,15 @@ __device__ __forceinline__ uint32_t abs_max8(const Raw8<T>& r) {
     }
 }
 
+// `dst`: where column c0 is kept.
+__device__ __forceinline__ void store_q8(uint8_t* dst, uint32_t c0, uint32_t cols, uint32_t grain, uint2 v) {
+    if (grain >= 8 && c0 + 8 <= cols) __stcs(reinterpret_cast<uint2*>(dst), v);
+    else if (c0 < cols) store_q_narrow(dst, v, cols - c0, grain);
+}
+
 // One pass: 2 (4) bytes read and 1 + 1/32 written per element; two lanes hold a group and share its maximum.
 template <typename T>
-__global__ void __launch_bounds__(CKPT_THREADS) checkpoint_pack_kernel(const T* __restrict__ x, uint64_t ldx, ItemWalk w,
+__global__ void __launch_bounds__(CKPT_THREADS, sizeof(T) == 2 ? 4 : 3) checkpoint_pack_kernel(const T* __restrict__ x, uint64_t ldx, ItemWalk w,
                                                                        uint8_t* __restrict__ q, uint8_t* __restrict__ scales) {
     constexpr int UNROLL = sizeof(T) == 2 ? CKPT_UNROLL : 2;
     wait_for_predecessor();
@@ -112,11 +181,11 @@ __global__ void __launch_bounds__(CKPT_THREADS) checkpoint_pack_kernel(const T* 
             if (base + u * stride < w.total) {
                 const T* row = x + at.row * ldx;
                 const uint32_t c0 = at.item * 16;
-                if (sizeof(T) == 2 && w.vec == 3) {
-                    if (c0 < w.cols) load32(row + c0, raw[u][0].v, raw[u][1].v);
+                if (sizeof(T) == 2 && w.grain_x >= 16 && c0 + 16 <= w.cols) {
+                    load32(row + c0, raw[u][0].v, raw[u][1].v);
                 } else {
-                    raw[u][0] = load8(row, c0, w.cols, w.vec);
-                    raw[u][1] = load8(row, c0 + 8, w.cols, w.vec);
+                    raw[u][0] = load8(row, c0, w.cols, w.grain_x);
+                    raw[u][1] = load8(row, c0 + 8, w.cols, w.grain_x);
                 }
             }
             at.next(w);
@@ -148,15 +217,11 @@ __global__ void __launch_bounds__(CKPT_THREADS) checkpoint_pack_kernel(const T* 
             if (base + u * stride < w.total) {
                 const uint32_t c0 = from.item * 16;
                 uint8_t* dst = q + from.row * w.cols + c0;
-                if (w.vec >= 2) {
-                    if (c0 < w.cols) __stcs(reinterpret_cast<uint4*>(dst), make_uint4(b[0].x, b[0].y, b[1].x, b[1].y));
-                } else if (w.vec) {
-                    if (c0 < w.cols) __stcs(reinterpret_cast<uint2*>(dst), b[0]);
-                    if (c0 + 8 < w.cols) __stcs(reinterpret_cast<uint2*>(dst + 8), b[1]);
+                if (w.grain_q >= 16 && c0 + 16 <= w.cols) {
+                    __stcs(reinterpret_cast<uint4*>(dst), make_uint4(b[0].x, b[0].y, b[1].x, b[1].y));
                 } else {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (c0 + i < w.cols) dst[i] = (uint8_t)((i & 4 ? b[i >> 3].y : b[i >> 3].x) >> (8 * (i & 3)));
+                    store_q8(dst, c0, w.cols, w.grain_q, b[0]);
+                    store_q8(dst + 8, c0 + 8, w.cols, w.grain_q, b[1]);
                 }
                 if ((from.item & 1u) == 0u) scales[from.row * groups + (from.item >> 1)] = (uint8_t)(e + 127);
             }
@@ -166,19 +231,17 @@ __global__ void __launch_bounds__(CKPT_THREADS) checkpoint_pack_kernel(const T* 
 }
 
 template <typename T>
-__device__ __forceinline__ void store8(T* row, uint32_t c0, uint32_t cols, uint32_t vec, const float f[8]) {
-    if (vec) {
-        if (c0 >= cols) return;
-        if constexpr (sizeof(T) == 2) {
-            const uint4 o = make_uint4(Elem<T>::pack(f[0], f[1]), Elem<T>::pack(f[2], f[3]), Elem<T>::pack(f[4], f[5]), Elem<T>::pack(f[6], f[7]));
-            *reinterpret_cast<uint4*>(row + c0) = o;
-        } else {
-            *reinterpret_cast<float4*>(row + c0) = make_float4(f[0], f[1], f[2], f[3]);
-            *(reinterpret_cast<float4*>(row + c0) + 1) = make_float4(f[4], f[5], f[6], f[7]);
-        }
+__device__ __forceinline__ void store8(T* row, uint32_t c0, uint32_t cols, uint32_t grain, const float f[8]) {
+    if constexpr (sizeof(T) == 2) {
+        const uint4 o = make_uint4(Elem<T>::pack(f[0], f[1]), Elem<T>::pack(f[2], f[3]), Elem<T>::pack(f[4], f[5]), Elem<T>::pack(f[6], f[7]));
+        if (grain >= 8 && c0 + 8 <= cols) *reinterpret_cast<uint4*>(row + c0) = o;
+        else if (c0 < cols) store_narrow(reinterpret_cast<uint16_t*>(row + c0), o, cols - c0, grain);
+    } else if (grain >= 4 && c0 + 8 <= cols) {
+        *reinterpret_cast<float4*>(row + c0) = make_float4(f[0], f[1], f[2], f[3]);
+        *(reinterpret_cast<float4*>(row + c0) + 1) = make_float4(f[4], f[5], f[6], f[7]);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (c0 + i < cols) row[c0 + i] = Elem<T>::from_float(f[i]);
+        for (int i = 0; i < 8; ++i) if (c0 + i < cols) row[c0 + i] = f[i];
     }
 }
 
@@ -192,27 +255,20 @@ __device__ __forceinline__ uint4 packed8(const Pair v[4]) {
     return make_uint4(o[0], o[1], o[2], o[3]);
 }
 template <typename T>
-__device__ __forceinline__ void store8(T* row, uint32_t c0, uint32_t cols, uint32_t vec, const Pair v[4]) {
+__device__ __forceinline__ void store8(T* row, uint32_t c0, uint32_t cols, uint32_t grain, const Pair v[4]) {
     float f[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) { const float2 p = both(v[i]); f[2 * i] = p.x; f[2 * i + 1] = p.y; }
-    store8(row, c0, cols, vec, f);
+    store8(row, c0, cols, grain, f);
 }
 
-__device__ __forceinline__ uint2 load_q8(const uint8_t* row, uint32_t c0, uint32_t cols, uint32_t vec) {
-    uint2 r = make_uint2(0u, 0u);
-    if (vec) {
-        if (c0 < cols) r = __ldcs(reinterpret_cast<const uint2*>(row + c0));
-    } else {
-        uint8_t* b = reinterpret_cast<uint8_t*>(&r);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) if (c0 + i < cols) b[i] = row[c0 + i];
-    }
-    return r;
+__device__ __forceinline__ uint2 load_q8(const uint8_t* row, uint32_t c0, uint32_t cols, uint32_t grain) {
+    if (grain >= 8 && c0 + 8 <= cols) return __ldcs(reinterpret_cast<const uint2*>(row + c0));
+    return c0 < cols ? load_q_narrow(row + c0, cols - c0, grain) : make_uint2(0u, 0u);
 }
 
 template <typename T>
-__global__ void __launch_bounds__(CKPT_THREADS) checkpoint_unpack_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, ItemWalk w,
+__global__ void __launch_bounds__(CKPT_THREADS, sizeof(T) == 2 ? 4 : 3) checkpoint_unpack_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, ItemWalk w,
                                                                          T* __restrict__ out, uint64_t ldo) {
     wait_for_predecessor();
     release_successor();
@@ -228,13 +284,13 @@ __global__ void __launch_bounds__(CKPT_THREADS) checkpoint_unpack_kernel(const u
             if (base + u * stride < w.total) {
                 const uint8_t* row = q + at.row * w.cols;
                 const uint32_t c0 = at.item * 16;
-                if (w.vec >= 2) {
-                    const uint4 v = c0 < w.cols ? __ldcs(reinterpret_cast<const uint4*>(row + c0)) : make_uint4(0u, 0u, 0u, 0u);
+                if (w.grain_q >= 16 && c0 + 16 <= w.cols) {
+                    const uint4 v = __ldcs(reinterpret_cast<const uint4*>(row + c0));
                     raw[u][0] = make_uint2(v.x, v.y);
                     raw[u][1] = make_uint2(v.z, v.w);
                 } else {
-                    raw[u][0] = load_q8(row, c0, w.cols, w.vec);
-                    raw[u][1] = load_q8(row, c0 + 8, w.cols, w.vec);
+                    raw[u][0] = load_q8(row, c0, w.cols, w.grain_q);
+                    raw[u][1] = load_q8(row, c0 + 8, w.cols, w.grain_q);
                 }
                 sb[u] = scales[at.row * groups + (at.item >> 1)];
             }
@@ -252,11 +308,11 @@ __global__ void __launch_bounds__(CKPT_THREADS) checkpoint_unpack_kernel(const u
                     if (sb[u] <= LARGE_SCALE) ckpt_values8<false>(raw[u][h], k, f[h]);
                     else ckpt_values8<true>(raw[u][h], k, f[h]);
                 }
-                if (sizeof(T) == 2 && w.vec == 3) {
-                    if (c0 < w.cols) store32(row + c0, packed8<T>(f[0]), packed8<T>(f[1]));
+                if (sizeof(T) == 2 && w.grain_x >= 16 && c0 + 16 <= w.cols) {
+                    store32(row + c0, packed8<T>(f[0]), packed8<T>(f[1]));
                 } else {
-                    store8(row, c0, w.cols, w.vec, f[0]);
-                    store8(row, c0 + 8, w.cols, w.vec, f[1]);
+                    store8(row, c0, w.cols, w.grain_x, f[0]);
+                    store8(row, c0 + 8, w.cols, w.grain_x, f[1]);
                 }
             }
             from.next(w);
@@ -275,10 +331,10 @@ constexpr int GRAD_COLS = 256, GRAD_LANES = 8;
 
 struct GradArgs {
     uint64_t rows, lddy, lddz;
-    uint32_t cols, groups, runs, run_rows, accumulate;
+    uint32_t cols, groups, runs, run_rows, accumulate, grain_y, grain_z, grain_q;
 };
 
-template <typename T, int ACT, bool VEC>
+template <typename T, int ACT, bool WIDE>
 __global__ void __launch_bounds__(CKPT_THREADS, 4) activation_grad_kernel(const T* dy, const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales,
                                                                           GradArgs a, T* dz, float* __restrict__ partial,
                                                                           uint32_t* __restrict__ tickets, float* __restrict__ db) {
@@ -300,9 +356,9 @@ __global__ void __launch_bounds__(CKPT_THREADS, 4) activation_grad_kernel(const 
         struct Row { Raw8<T> g; uint2 k; uint32_t sb; };
         const auto fetch = [&](Row& row, uint32_t r) {
             if (r < left) {
-                row.g = load8(from, c0, a.cols, VEC);
+                row.g = load8(from, c0, a.cols, WIDE ? 8u : a.grain_y);
                 if constexpr (ACT != SC_ACT_NONE) {
-                    row.k = load_q8(qr, c0, a.cols, VEC);
+                    row.k = load_q8(qr, c0, a.cols, WIDE ? 8u : a.grain_q);
                     row.sb = *sr;
                 }
             }
@@ -320,7 +376,7 @@ __global__ void __launch_bounds__(CKPT_THREADS, 4) activation_grad_kernel(const 
                     if constexpr (ACT != SC_ACT_NONE) v[i] = v[i] * activation_slope<ACT>(z[i]);
                     sum[i] = sum[i] + v[i];
                 }
-                if (dz) store8(to, c0, a.cols, VEC, v);
+                if (dz) store8(to, c0, a.cols, WIDE ? 8u : a.grain_z, v);
             }
             to += step_z;
         };

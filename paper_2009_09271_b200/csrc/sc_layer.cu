@@ -17,6 +17,12 @@ inline bool known_type(int type) { return type == SC_BF16 || type == SC_F16; }
 inline bool known_act(int act) { return act >= SC_ACT_NONE && act <= SC_ACT_SILU; }
 inline size_t type_bytes(int type) { return type == SC_F32 ? 4 : 2; }
 
+// The widest run of elements, up to `most`, at whose multiples rows `ld` apart are aligned to the run's size.
+uint32_t grain_of(const void* p, size_t ld, size_t elem, uint32_t most) {
+    while (most > 1 && (!aligned(p, most * elem) || ld % most)) most /= 2;
+    return most;
+}
+
 // A matrix argument: rows of `cols` elements, `ld` apart.
 int check_matrix(const void* p, size_t ld, size_t rows, size_t cols, size_t elem) {
     if (rows >= MAX_DIM || cols >= MAX_DIM) return SC_ERR_RANGE;
@@ -81,7 +87,7 @@ cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, in
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 
-ItemWalk item_walk(const sc_ctx* c, size_t rows, size_t cols, const uint8_t* q, const void* x, size_t row_bytes) {
+ItemWalk item_walk(const sc_ctx* c, size_t rows, size_t cols, const uint8_t* q, const void* x, size_t ldx, size_t elem) {
     ItemWalk w{};
     w.cols = (uint32_t)cols;
     w.items = (uint32_t)(2 * ckpt_groups(cols));
@@ -89,23 +95,21 @@ ItemWalk item_walk(const sc_ctx* c, size_t rows, size_t cols, const uint8_t* q, 
     const uint64_t stride = (uint64_t)item_grid(c, w.total) * CKPT_THREADS;
     w.stride_rows = stride / w.items;
     w.stride_items = (uint32_t)(stride % w.items);
-    if (cols % 8 == 0 && aligned(q, 8) && aligned(x, 16) && row_bytes % 16 == 0) {
-        w.vec = 1;
-        if (cols % 16 == 0 && aligned(q, 16)) w.vec = aligned(x, 32) && row_bytes % 32 == 0 ? 3 : 2;
-    }
+    w.grain_x = grain_of(x, rows > 1 ? ldx : 0, elem, 16);
+    w.grain_q = grain_of(q, rows > 1 ? cols : 0, 1, 16);
     return w;
 }
 
 template <typename T>
 void launch_pack(sc_ctx* c, const void* x, size_t ldx, size_t rows, size_t cols, uint8_t* q, uint8_t* scales, cudaStream_t st) {
-    const ItemWalk w = item_walk(c, rows, cols, q, x, ldx * sizeof(T));
+    const ItemWalk w = item_walk(c, rows, cols, q, x, ldx, sizeof(T));
     Launch l(c, KIND_CKPT_PACK, st);
     launch(checkpoint_pack_kernel<T>, item_grid(c, w.total), CKPT_THREADS, 0, 1, st, static_cast<const T*>(x), ldx, w, q, scales);
 }
 
 template <typename T>
 void launch_unpack(sc_ctx* c, const uint8_t* q, const uint8_t* scales, size_t rows, size_t cols, void* out, size_t ldo, cudaStream_t st) {
-    const ItemWalk w = item_walk(c, rows, cols, q, out, ldo * sizeof(T));
+    const ItemWalk w = item_walk(c, rows, cols, q, out, ldo, sizeof(T));
     Launch l(c, KIND_CKPT_UNPACK, st);
     launch(checkpoint_unpack_kernel<T>, item_grid(c, w.total), CKPT_THREADS, 0, 1, st, q, scales, w, static_cast<T*>(out), ldo);
 }
@@ -232,14 +236,22 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
     unsigned char* at = c->d_layer ? c->d_layer + TICKET_BYTES + used : nullptr;
     float* partial = reinterpret_cast<float*>(at);
     at += p.bytes;
+    LayoutArgs copies[2];
+    int ncopies = 0;
+    uint64_t work = 0;
     for (Stored* m : {&A, &B}) {
         if (tma_ready(*m)) continue;
         const uint32_t ldd = (uint32_t)round8(m->cols);
-        Launch l(c, KIND_LAYER_LAYOUT, st);
-        launch(layout_kernel, (uint32_t)std::min<uint64_t>(ceil_div(m->rows * (ldd / 8), 256), (uint64_t)c->sm_count * 8), 256, 0, 1, st,
-               static_cast<const uint16_t*>(m->p), m->ld, m->rows, (uint32_t)m->cols, reinterpret_cast<uint16_t*>(at), ldd);
+        copies[ncopies++] = LayoutArgs{static_cast<const uint16_t*>(m->p), reinterpret_cast<uint16_t*>(at), m->ld, m->rows, (uint32_t)m->cols, ldd,
+                                       std::min(4u, grain_of(m->p, m->rows > 1 ? m->ld : 0, 2, 8))};
+        work = std::max(work, m->rows * (ldd / 8));
         m->p = at; m->ld = ldd;
         at += layout_bytes(m->rows, m->cols);
+    }
+    if (ncopies) {
+        Launch l(c, KIND_LAYER_LAYOUT, st);
+        launch(layout_kernel, dim3((uint32_t)std::min<uint64_t>(ceil_div(work, 256), (uint64_t)c->sm_count * 8), ncopies), 256, 0, 1, st, copies[0],
+               copies[ncopies - 1]);
     }
     TcArgs a{};
     a.tiles_i = (uint32_t)ceil_div(ep.rows, TC_ROWS * p.cg); a.tiles_j = (uint32_t)ceil_div(ep.cols, p.bn); a.tiles = (uint32_t)tiles;
@@ -248,7 +260,7 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
     a.a_box_rows = A_MN ? 64u : (uint32_t)std::min<uint64_t>(TC_ROWS, round8(ep.rows));
     a.part_ld = (uint32_t)p.part_ld; a.part_stride = ep.rows * p.part_ld; a.partial = partial; a.status = c->d_status;
     // partial sums are whole to the next multiple of 32 columns: a checkpoint group's maximum is taken over all of its columns
-    a.tma_out = p.splits > 1 || (MODE == PRODUCT_WEIGHT && ep.vec_out);
+    a.tma_out = p.splits > 1 || (MODE == PRODUCT_WEIGHT && ep.grain_out >= 4);
     CUtensorMap ma, mb, mo{};
     if (a.tma_out && !(p.splits > 1 ? out_map(&mo, partial, ep.rows, p.part_ld, p.part_ld, p.splits, a.part_stride)
                                     : out_map(&mo, static_cast<float*>(ep.out), ep.rows, ep.cols, ep.ldo, 1, ep.rows * ep.ldo)))
@@ -272,12 +284,13 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
 
 template <typename T, int TOKENS>
 void run_tokens(const Stored& x, const Stored& w, const Epilogue& ep, cudaStream_t st) {
-    const bool vec = tma_ready(x) && tma_ready(w) && x.cols % 8 == 0;
+    const uint32_t gx = grain_of(x.p, x.rows > 1 ? x.ld : 0, 2, 8), gw = grain_of(w.p, w.rows > 1 ? w.ld : 0, 2, 8);
+    const bool wide = gx == 8 && gw == 8;
     const T *xp = static_cast<const T*>(x.p), *wp = static_cast<const T*>(w.p);
     const uint32_t K = (uint32_t)x.cols;
-#define SC_TOKENS(WN, WK, VEC) launch(product_tokens_kernel<T, TOKENS, WN, WK, VEC>, (uint32_t)ceil_div(ep.cols, 4 * WN), WN * WK * 32, 0, 1, st, xp, x.ld, wp, w.ld, K, ep)
-    if (ep.q) { if (vec) SC_TOKENS(8, 4, true); else SC_TOKENS(8, 4, false); }
-    else if (vec) SC_TOKENS(2, 4, true);
+#define SC_TOKENS(WN, WK, WIDE) launch(product_tokens_kernel<T, TOKENS, WN, WK, WIDE>, (uint32_t)ceil_div(ep.cols, 4 * WN), WN * WK * 32, 0, 1, st, xp, x.ld, wp, w.ld, K, gx, gw, ep)
+    if (ep.q) { if (wide) SC_TOKENS(8, 4, true); else SC_TOKENS(8, 4, false); }
+    else if (wide) SC_TOKENS(2, 4, true);
     else SC_TOKENS(2, 4, false);
 #undef SC_TOKENS
 }
@@ -297,6 +310,29 @@ int run_product(sc_ctx* c, int kind, int type, const Stored& A, const Stored& B,
     if constexpr (MODE != PRODUCT_WEIGHT)
         if (type == SC_F16) return run_product<__half, MODE>(c, kind, type, A, B, red, ep, used, st);
     return run_product<__nv_bfloat16, MODE>(c, kind, type, A, B, red, ep, used, st);
+}
+
+constexpr uint64_t FEW_WEIGHT_TOKENS = 16;
+
+template <typename T, int TOKENS, bool KEPT>
+void launch_weight_tokens(sc_ctx* c, const void* dz, size_t lddz, const void* x, size_t ldx, const uint8_t* q, const uint8_t* scales, size_t M,
+                          const Epilogue& ep, cudaStream_t st) {
+    // rows per CTA: 256, or as few as fill the GPU a few times over
+    const uint64_t columns = ceil_div(ep.cols, 128);
+    uint32_t run = 256;
+    while (run > 16 && columns * ceil_div(ep.rows, run) < (uint64_t)c->sm_count * 3) run /= 2;
+    run = (uint32_t)std::max<uint64_t>(run, ceil_div(ep.rows, 65535));
+    launch(weight_tokens_kernel<T, TOKENS, KEPT>, dim3((uint32_t)columns, (uint32_t)ceil_div(ep.rows, run)), 256, run * TOKENS * sizeof(float), 1, st,
+           static_cast<const T*>(dz), lddz, static_cast<const T*>(x), ldx, q, scales, (uint32_t)M, run, ep);
+}
+
+template <typename T>
+void run_weight_tokens(sc_ctx* c, const void* dz, size_t lddz, const void* x, size_t ldx, const uint8_t* q, const uint8_t* scales, size_t M, const Epilogue& ep,
+                       cudaStream_t st) {
+    if (q) { if (M <= 4) launch_weight_tokens<T, 4, true>(c, dz, lddz, x, ldx, q, scales, M, ep, st);
+             else launch_weight_tokens<T, 16, true>(c, dz, lddz, x, ldx, q, scales, M, ep, st); }
+    else if (M <= 4) launch_weight_tokens<T, 4, false>(c, dz, lddz, x, ldx, q, scales, M, ep, st);
+    else launch_weight_tokens<T, 16, false>(c, dz, lddz, x, ldx, q, scales, M, ep, st);
 }
 
 // A wait of the layer products where nothing arrives.
@@ -383,19 +419,22 @@ int sc_activation_grad(sc_ctx* ctx, int type, int act, const void* dy, size_t ld
     GradArgs a{};
     a.rows = rows; a.lddy = lddy; a.lddz = lddz; a.cols = (uint32_t)cols; a.groups = (uint32_t)ckpt_groups(cols);
     a.runs = p.runs; a.run_rows = p.run_rows; a.accumulate = accumulate ? 1u : 0u;
-    const bool vec = cols % 8 == 0 && aligned(dy, 16) && lddy % 8 == 0 && (!dz || (aligned(dz, 16) && lddz % 8 == 0)) && (!kept || aligned(q, 8));
+    a.grain_y = grain_of(dy, rows > 1 ? lddy : 0, 2, 8);
+    a.grain_z = grain_of(dz, rows > 1 ? lddz : 0, 2, 8);
+    a.grain_q = grain_of(q, rows > 1 ? cols : 0, 1, 8);
+    const bool wide = a.grain_y == 8 && a.grain_z == 8 && (!kept || a.grain_q == 8);
     float* partial = reinterpret_cast<float*>(ctx->d_layer ? ctx->d_layer + TICKET_BYTES : nullptr);
     uint32_t* tickets = reinterpret_cast<uint32_t*>(ctx->d_layer);
     const dim3 grid(p.strips, p.runs);
     const uint8_t* qb = reinterpret_cast<const uint8_t*>(q);
     {
         Launch l(ctx, KIND_ACT_GRAD, st);
-#define SC_GRAD(T, ACT, VEC) launch(activation_grad_kernel<T, ACT, VEC>, grid, CKPT_THREADS, 0, 1, st, \
+#define SC_GRAD(T, ACT, WIDE) launch(activation_grad_kernel<T, ACT, WIDE>, grid, CKPT_THREADS, 0, 1, st, \
             static_cast<const T*>(dy), qb, scales, a, static_cast<T*>(dz), partial, tickets, db)
 #define SC_GRAD_ACT(ACT)                                                                                     \
         case ACT:                                                                                            \
-            if (type == SC_BF16) { if (vec) SC_GRAD(__nv_bfloat16, ACT, true); else SC_GRAD(__nv_bfloat16, ACT, false); } \
-            else { if (vec) SC_GRAD(__half, ACT, true); else SC_GRAD(__half, ACT, false); }                  \
+            if (type == SC_BF16) { if (wide) SC_GRAD(__nv_bfloat16, ACT, true); else SC_GRAD(__nv_bfloat16, ACT, false); } \
+            else { if (wide) SC_GRAD(__half, ACT, true); else SC_GRAD(__half, ACT, false); }                  \
             break;
         switch (act) { SC_GRAD_ACT(SC_ACT_NONE) SC_GRAD_ACT(SC_ACT_RELU) SC_GRAD_ACT(SC_ACT_GELU) SC_GRAD_ACT(SC_ACT_GELU_TANH) SC_GRAD_ACT(SC_ACT_SILU) }
 #undef SC_GRAD_ACT
@@ -420,8 +459,8 @@ int sc_linear(sc_ctx* ctx, int type, int act, const void* x, size_t ldx, const v
     Epilogue ep{};
     ep.bias = bias; ep.residual = residual; ep.ldr = ldr; ep.out = y; ep.ldo = ldy; ep.rows = M; ep.cols = (uint32_t)N;
     ep.q = reinterpret_cast<uint8_t*>(q); ep.scales = scales; ep.groups = (uint32_t)ckpt_groups(N); ep.act = act;
-    ep.vec_out = N % 8 == 0 && aligned(y, 16) && ldy % 8 == 0; ep.vec_res = N % 8 == 0 && aligned(residual, 16) && ldr % 8 == 0;
-    ep.vec_q = N % 8 == 0 && aligned(q, 8); ep.vec_bias = N % 8 == 0 && aligned(bias, 16);
+    ep.grain_out = grain_of(y, M > 1 ? ldy : 0, 2, 8); ep.grain_res = grain_of(residual, M > 1 ? ldr : 0, 2, 8);
+    ep.grain_q = grain_of(q, M > 1 ? N : 0, 1, 8); ep.grain_bias = grain_of(bias, 0, 2, 8);
     if (M <= FEW_TOKENS && K) {
         Launch l(ctx, KIND_LINEAR, st);
         const Stored xs{x, M, K, ldx}, ws{w, N, K, ldw};
@@ -455,8 +494,8 @@ int sc_linear_grad_input(sc_ctx* ctx, int type, int act, const void* dz, size_t 
         ep.scales = const_cast<uint8_t*>(scales);
         ep.groups = (uint32_t)ckpt_groups(K);
     }
-    ep.vec_out = K % 8 == 0 && aligned(dx, 16) && lddx % 8 == 0; ep.vec_res = K % 8 == 0 && aligned(residual, 16) && ldr % 8 == 0;
-    ep.vec_q = K % 8 == 0 && aligned(q, 8);
+    ep.grain_out = grain_of(dx, M > 1 ? lddx : 0, 2, 8); ep.grain_res = grain_of(residual, M > 1 ? ldr : 0, 2, 8);
+    ep.grain_q = grain_of(q, M > 1 ? K : 0, 1, 8);
     if (const int rc = run_product<PRODUCT_INPUT>(ctx, KIND_LINEAR_DX, type, Stored{dz, M, N, lddz}, Stored{w, N, K, ldw}, N, ep, 0, st)) return rc;
     SC_CUDA(cudaGetLastError());
     return SC_OK;
@@ -476,7 +515,17 @@ int sc_linear_grad_weight(sc_ctx* ctx, int type, const void* dz, size_t lddz, co
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     Epilogue ep{};
     ep.out = dw; ep.ldo = lddw; ep.rows = N; ep.cols = (uint32_t)K; ep.accumulate = accumulate ? 1u : 0u;
-    ep.vec_out = K % 8 == 0 && aligned(dw, 16) && lddw % 4 == 0;
+    if (N == 1) ep.ldo = lddw = (K + 3) & ~(size_t)3;                // the distance between rows says nothing
+    ep.grain_out = grain_of(dw, lddw, 4, 4);
+    ep.groups = (uint32_t)ckpt_groups(K);
+    if (M && M <= FEW_WEIGHT_TOKENS && N <= 65535ull * 256) {
+        const uint8_t* qb = reinterpret_cast<const uint8_t*>(q);
+        Launch l(ctx, KIND_LINEAR_DW, st);
+        if (type == SC_BF16) run_weight_tokens<__nv_bfloat16>(ctx, dz, lddz, x, ldx, qb, scales, M, ep, st);
+        else run_weight_tokens<__half>(ctx, dz, lddz, x, ldx, qb, scales, M, ep, st);
+        SC_CUDA(cudaGetLastError());
+        return SC_OK;
+    }
     size_t used = 0;
     if (q && M) {                                  // the checkpoint's values, rows 16-byte aligned
         used = layout_bytes(M, K);

@@ -21,7 +21,7 @@ struct Epilogue {
     uint32_t cols, groups;
     int act;
     uint32_t accumulate;
-    uint32_t vec_out, vec_res, vec_q, vec_bias;      // 16-byte (q: 8-byte) accesses are aligned and 8 columns never straddle a row's end
+    uint32_t grain_out, grain_res, grain_q, grain_bias;      // elements that one access of a row may take
 };
 
 // What follows the product for 8 columns from c0 of one row.  All 32 lanes of a warp call it; four neighbouring lanes hold
@@ -32,23 +32,15 @@ __device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint
     if constexpr (MODE == PRODUCT_WEIGHT) {
         if (!in) return;
         float* out = static_cast<float*>(ep.out) + row * ep.ldo + c0;
-        if (ep.vec_out) {
-            float4* o = reinterpret_cast<float4*>(out);
-            float4 a = make_float4(v[0], v[1], v[2], v[3]), b = make_float4(v[4], v[5], v[6], v[7]);
-            if (ep.accumulate) {
-                const float4 x = o[0], y = o[1];
-                a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
-                b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
-            }
-            o[0] = a; o[1] = b;
-        } else {
+        if (ep.accumulate) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c0 + i < ep.cols) out[i] = ep.accumulate ? out[i] + v[i] : v[i];
+            for (int i = 0; i < 8; ++i) if (c0 + i < ep.cols) out[i] += v[i];
+        } else {
+            store8(out - c0, c0, ep.cols, ep.grain_out, v);
         }
     } else {
         float res[8] = {};
-        if (in && ep.residual) to_floats(load8(static_cast<const T*>(ep.residual) + row * ep.ldr, c0, ep.cols, ep.vec_res), res);
+        if (in && ep.residual) to_floats(load8(static_cast<const T*>(ep.residual) + row * ep.ldr, c0, ep.cols, ep.grain_res), res);
         if constexpr (MODE == PRODUCT_FORWARD) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += bias[i];
@@ -61,13 +53,7 @@ __device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint
                 int e;
                 const uint2 b = ckpt_encode8<T>(v, m, e);
                 if (in) {
-                    uint8_t* q = ep.q + row * ep.cols + c0;
-                    if (ep.vec_q) {
-                        *reinterpret_cast<uint2*>(q) = b;
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) if (c0 + i < ep.cols) q[i] = (uint8_t)((i & 4 ? b.y : b.x) >> (8 * (i & 3)));
-                    }
+                    store_q8(ep.q + row * ep.cols + c0, c0, ep.cols, ep.grain_q, b);
                     if ((c0 & 31u) == 0u) ep.scales[row * ep.groups + (c0 >> 5)] = (uint8_t)(e + 127);
                 }
             }
@@ -82,7 +68,7 @@ __device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += res[i];
             if constexpr (ACT != SC_ACT_NONE) {
-                const uint2 k = load_q8(ep.q + row * ep.cols, c0, ep.cols, ep.vec_q);
+                const uint2 k = load_q8(ep.q + row * ep.cols, c0, ep.cols, ep.grain_q);
                 const Scale s = slope_scale(ep.scales[row * ep.groups + (c0 >> 5)]);
                 Pair z[4];
                 ckpt_values8<false>(k, s, z);
@@ -93,7 +79,7 @@ __device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint
                 }
             }
         }
-        store8(static_cast<T*>(ep.out) + row * ep.ldo, c0, ep.cols, ep.vec_out, v);
+        store8(static_cast<T*>(ep.out) + row * ep.ldo, c0, ep.cols, ep.grain_out, v);
     }
 }
 
@@ -103,7 +89,7 @@ __device__ __forceinline__ void load_bias(const Epilogue& ep, uint32_t c0, float
 #pragma unroll
     for (int i = 0; i < 8; ++i) b[i] = 0.0f;
     if constexpr (MODE == PRODUCT_FORWARD)
-        if (ep.bias && c0 < ep.cols) to_floats(load8(static_cast<const T*>(ep.bias), c0, ep.cols, ep.vec_bias), b);
+        if (ep.bias && c0 < ep.cols) to_floats(load8(static_cast<const T*>(ep.bias), c0, ep.cols, ep.grain_bias), b);
 }
 
 // ---------------------------------------------------------------------------
@@ -416,9 +402,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
 // With one to four tokens the weights' bytes are everything, and four multiply-adds a weight still fit beside their loads.
 // A warp owns four rows of W and walks its share of the reduction, 16 bytes a lane and row; WK warps split a row, WN warps
 // sit side by side, and the last step joins them in shared memory.  WN = 8 puts 32 outputs, a checkpoint group, in one CTA.
-template <typename T, int TOKENS, int WN, int WK, bool VEC>
+template <typename T, int TOKENS, int WN, int WK, bool WIDE>
 __global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* __restrict__ x, uint64_t ldx, const T* __restrict__ w, uint64_t ldw,
-                                                                      uint32_t K, Epilogue ep) {
+                                                                      uint32_t K, uint32_t grain_x, uint32_t grain_w, Epilogue ep) {
     constexpr int ROWS = 4, COLS = ROWS * WN;
     wait_for_predecessor();
     release_successor();
@@ -432,14 +418,14 @@ __global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* _
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             rw[r] = Raw8<T>{};
-            if (n0 + r < ep.cols) rw[r] = load8(w + (uint64_t)(n0 + r) * ldw, k, K, VEC);
+            if (n0 + r < ep.cols) rw[r] = load8(w + (uint64_t)(n0 + r) * ldw, k, K, WIDE ? 8u : grain_w);
         }
 #pragma unroll
         for (int m = 0; m < TOKENS; ++m) {
             rx[m] = Raw8<T>{};
             if (m < tokens) {
-                if constexpr (VEC) rx[m].v = *reinterpret_cast<const uint4*>(x + m * ldx + k);
-                else rx[m] = load8(x + m * ldx, k, K, 0u);
+                if (WIDE && k + 8 <= K) rx[m].v = *reinterpret_cast<const uint4*>(x + m * ldx + k);
+                else rx[m] = load8(x + m * ldx, k, K, WIDE ? 8u : grain_x);
             }
         }
         float fx[TOKENS][8];
@@ -481,6 +467,65 @@ __global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* _
     with_activation(ep.act, [&](auto act) { epilogue8<T, PRODUCT_FORWARD, decltype(act)::value>(ep, m, c0, bias, f); });
 }
 
+// ---------------------------------------------------------------------------
+// Weight gradient of a few tokens
+// ---------------------------------------------------------------------------
+// Up to 16 tokens: the fp32 result's own bytes are everything (16 multiply-adds a value still fit beside them), so each
+// value is made where it is stored.  A CTA owns 128 columns and `run` rows; every warp holds the columns' inputs in
+// registers, read from the checkpoint or from x, and walks its rows with the rows' dz in shared memory, one 128-byte
+// store at a time, whatever the alignment.
+template <typename T, int TOKENS, bool KEPT>
+__global__ void __launch_bounds__(256) weight_tokens_kernel(const T* __restrict__ dz, uint64_t lddz, const T* __restrict__ x, uint64_t ldx,
+                                                            const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, uint32_t tokens, uint32_t run,
+                                                            Epilogue ep) {
+    extern __shared__ float rows_dz[];              // [run][TOKENS]
+    wait_for_predecessor();
+    release_successor();
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint32_t c0 = blockIdx.x * 128 + lane, K = ep.cols;
+    const uint64_t n0 = (uint64_t)blockIdx.y * run;
+    const uint32_t rows = (uint32_t)min((uint64_t)run, ep.rows - n0);
+    for (uint32_t i = threadIdx.x; i < rows * TOKENS; i += 256) {
+        const uint32_t m = i / rows, r = i - m * rows;
+        rows_dz[r * TOKENS + m] = m < tokens ? Elem<T>::to_float(dz[m * lddz + n0 + r]) : 0.0f;
+    }
+    float v[TOKENS][4];
+#pragma unroll
+    for (int m = 0; m < TOKENS; ++m)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t c = c0 + 32 * j;
+            v[m][j] = 0.0f;
+            if (m < (int)tokens && c < K) {
+                if constexpr (KEPT) {
+                    const int k = (int8_t)q[(uint64_t)m * K + c];
+                    v[m][j] = k == -128 ? __uint_as_float(0x7FFFFFFFu) : (float)k * __uint_as_float((uint32_t)scales[(uint64_t)m * ep.groups + (c >> 5)] << 23);
+                } else {
+                    v[m][j] = Elem<T>::to_float(x[m * ldx + c]);
+                }
+            }
+        }
+    __syncthreads();
+    float* out = static_cast<float*>(ep.out) + n0 * ep.ldo + c0;
+#pragma unroll 1
+    for (uint32_t r = warp; r < rows; r += 8) {
+        float acc[4] = {};
+#pragma unroll
+        for (int m = 0; m < TOKENS; m += 4) {
+            const float4 d = *reinterpret_cast<const float4*>(&rows_dz[r * TOKENS + m]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = fmaf(d.w, v[m + 3][j], fmaf(d.z, v[m + 2][j], fmaf(d.y, v[m + 1][j], fmaf(d.x, v[m][j], acc[j]))));
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float* o = out + r * ep.ldo + 32 * j;
+            if (c0 + 32 * j >= K) continue;
+            if (ep.accumulate) asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(o), "f"(acc[j]) : "memory");
+            else *o = acc[j];
+        }
+    }
+}
+
 // Joins the parts of a split product in order and applies the epilogue; no parts at all is an empty sum.
 template <typename T, int MODE>
 __global__ void __launch_bounds__(256) product_join_kernel(const float* __restrict__ partial, uint32_t splits, uint64_t part_stride, uint32_t part_ld,
@@ -513,21 +558,40 @@ __global__ void __launch_bounds__(256) product_join_kernel(const float* __restri
 }
 
 // Rows copied to a 16-byte aligned place with rows a multiple of 8 elements apart, where the tensor cores' loads can reach them.
-__global__ void __launch_bounds__(256) layout_kernel(const uint16_t* __restrict__ src, uint64_t ld, uint64_t rows, uint32_t cols,
-                                                     uint16_t* __restrict__ dst, uint32_t ldd) {
+// Rows of single-element alignment are read 32 elements a warp and access, the others a chunk of 8 a thread.
+struct LayoutArgs {
+    const uint16_t* src;
+    uint16_t* dst;
+    uint64_t ld, rows;
+    uint32_t cols, ldd, grain;
+};
+__device__ __forceinline__ void layout_rows(const LayoutArgs& a, uint32_t block, uint32_t blocks) {
+    const uint64_t first = (uint64_t)block * 256 + threadIdx.x, stride = (uint64_t)blocks * 256;
+    if (a.grain == 1) {
+        const uint32_t lane = threadIdx.x & 31u, runs = (a.ldd + 255) / 256;
+        for (uint64_t i = first >> 5; i < a.rows * runs; i += stride >> 5) {
+            const uint64_t row = i / runs;
+            const uint32_t c0 = (uint32_t)(i - row * runs) * 256 + lane;
+            uint16_t v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = c0 + 32 * k < a.cols ? a.src[row * a.ld + c0 + 32 * k] : (uint16_t)0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) if (c0 + 32 * k < a.ldd) a.dst[row * a.ldd + c0 + 32 * k] = v[k];
+        }
+    } else {
+        const uint32_t chunks = a.ldd / 8;
+        for (uint64_t i = first; i < a.rows * chunks; i += stride) {
+            const uint64_t row = i / chunks;
+            const uint32_t c0 = (uint32_t)(i - row * chunks) * 8;
+            *reinterpret_cast<uint4*>(a.dst + row * a.ldd + c0) = load_narrow(a.src + row * a.ld + c0, a.cols - c0, a.grain);
+        }
+    }
+}
+// One or both operands of a product: blockIdx.y chooses.
+static __global__ void __launch_bounds__(256) layout_kernel(LayoutArgs a, LayoutArgs b) {
     wait_for_predecessor();
     release_successor();
-    const uint32_t chunks = ldd / 8;
-    const uint64_t total = rows * chunks, stride = (uint64_t)gridDim.x * 256;
-    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += stride) {
-        const uint64_t row = i / chunks;
-        const uint32_t c0 = (uint32_t)(i - row * chunks) * 8;
-        uint16_t v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = c0 + k < cols ? src[row * ld + c0 + k] : (uint16_t)0;
-        *reinterpret_cast<uint4*>(dst + row * ldd + c0) =
-            make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16, v[6] | (uint32_t)v[7] << 16);
-    }
+    layout_rows(blockIdx.y ? b : a, blockIdx.x, gridDim.x);
 }
 
 }  // namespace sc

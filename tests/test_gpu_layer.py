@@ -466,6 +466,51 @@ def test_tokens_and_tiles_agree_at_the_border(ctx):
             check_linear(ctx, torch.float16, "relu", M, N, K, False, False, False, 1, 1)
 
 
+@pytest.mark.parametrize("M", [1, 4, 5, 16, 17])
+@pytest.mark.parametrize("N,K", [(1000, 33), (70, 260), (2049, 129)])
+def test_weight_gradient_of_few_tokens(ctx, M, N, K):
+    """Up to sixteen tokens take the kernel without tiles, seventeen the tensor tiles."""
+    for how, extra, offset in (("kept", 0, 0), ("dense", 0, 0), ("kept", 3, 1), ("dense", 8, 3)):
+        check_weight_grad(ctx, torch.bfloat16, M, N, K, how, extra, offset)
+        check_weight_grad(ctx, torch.float16, M, N, K, how, extra, offset)
+
+
+def test_weight_gradient_passes_nan_of_a_checkpoint(ctx):
+    for M in (3, 40):
+        x = torch.ones(M, 70, device="cuda")
+        x[1, 5], x[2, 69] = float("inf"), float("nan")
+        q, scales = sc.checkpoint_buffers(M, 70)
+        ctx.sc_checkpoint_pack(x, q, scales)
+        dw = torch.empty(36, 70, device="cuda")
+        ctx.sc_linear_grad_weight(torch.ones(M, 36, dtype=torch.bfloat16, device="cuda"), dw, q=q, scales=scales)
+        bad = torch.zeros(70, dtype=torch.bool, device="cuda")
+        bad[5] = bad[69] = True
+        assert bool(torch.isnan(dw[:, bad]).all()) and bool((dw[:, ~bad] == M).all())
+
+
+@pytest.mark.parametrize("cols", [1, 2, 4, 6, 12, 1002, 1004, 999])
+@pytest.mark.parametrize("extra,offset", [(0, 0), (2, 2), (4, 4), (1, 0), (7, 8), (8, 4)])
+def test_every_alignment_of_rows(ctx, cols, extra, offset):
+    """Rows aligned to 2, 4, 8 and 16 bytes, dense or apart, in every elementwise operator and both products' epilogues."""
+    rows = 37
+    g = rng(cols + extra)
+    for dtype in TYPES:
+        x = normal(g, rows, cols).to(dtype)
+        q, scales = sc.checkpoint_buffers(rows, cols)
+        ctx.sc_checkpoint_pack(strided(x, extra, offset), q, scales)
+        wq, ws, wv = checkpoint64(x, dtype)
+        assert torch.equal(q.cpu(), wq) and torch.equal(scales.cpu(), ws)
+        out = strided(torch.zeros_like(x), extra, offset)
+        ctx.sc_checkpoint_unpack(q, scales, out)
+        assert torch.equal(out.double().cpu(), wv)
+        dz, ref = strided(torch.zeros_like(x), extra, offset), torch.empty(rows, cols, dtype=dtype, device="cuda")
+        ctx.sc_activation_grad(sc.SC_ACT_SILU, strided(x, extra, offset), q, scales, dz)
+        ctx.sc_activation_grad(sc.SC_ACT_SILU, x, q, scales, ref)
+        assert torch.equal(dz, ref)
+    check_linear(ctx, torch.bfloat16, "relu", rows, cols, 72, True, True, True, extra, offset)
+    check_input_grad(ctx, torch.float16, "silu", rows, 40, cols, True, extra, offset)
+
+
 def test_product_wait_runs_out_and_the_context_stays_usable():
     own = sc.Context(max_n=1)
     own.sc_debug_set_poll_limits(2000, 2000)
