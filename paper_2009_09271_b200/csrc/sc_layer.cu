@@ -312,17 +312,15 @@ int run_product(sc_ctx* c, int kind, int type, const Stored& A, const Stored& B,
     return run_product<__nv_bfloat16, MODE>(c, kind, type, A, B, red, ep, used, st);
 }
 
-constexpr uint64_t FEW_WEIGHT_TOKENS = 16;
+constexpr uint64_t FEW_WEIGHT_TOKENS = 8;
 
 template <typename T, int TOKENS, bool KEPT>
 void launch_weight_tokens(sc_ctx* c, const void* dz, size_t lddz, const void* x, size_t ldx, const uint8_t* q, const uint8_t* scales, size_t M,
                           const Epilogue& ep, cudaStream_t st) {
-    // rows per CTA: 256, or as few as fill the GPU a few times over
-    const uint64_t columns = ceil_div(ep.cols, 128);
-    uint32_t run = 256;
-    while (run > 16 && columns * ceil_div(ep.rows, run) < (uint64_t)c->sm_count * 3) run /= 2;
-    run = (uint32_t)std::max<uint64_t>(run, ceil_div(ep.rows, 65535));
-    launch(weight_tokens_kernel<T, TOKENS, KEPT>, dim3((uint32_t)columns, (uint32_t)ceil_div(ep.rows, run)), 256, run * TOKENS * sizeof(float), 1, st,
+    // rows per CTA: one round of the CTAs that fit on the SMs, where that leaves 8 to 512 rows each
+    const uint64_t columns = ceil_div(ep.cols, 128), strips = std::max<uint64_t>(1, (uint64_t)c->sm_count * (TOKENS == 4 ? 5 : 3) / columns);
+    const uint32_t run = (uint32_t)std::min<uint64_t>(512, std::max<uint64_t>(8, ceil_div(ep.rows, strips)));
+    launch(weight_tokens_kernel<T, TOKENS, KEPT>, dim3((uint32_t)columns, (uint32_t)ceil_div(ep.rows, run)), 256, run * TOKENS * sizeof(float2), 1, st,
            static_cast<const T*>(dz), lddz, static_cast<const T*>(x), ldx, q, scales, (uint32_t)M, run, ep);
 }
 
@@ -330,9 +328,9 @@ template <typename T>
 void run_weight_tokens(sc_ctx* c, const void* dz, size_t lddz, const void* x, size_t ldx, const uint8_t* q, const uint8_t* scales, size_t M, const Epilogue& ep,
                        cudaStream_t st) {
     if (q) { if (M <= 4) launch_weight_tokens<T, 4, true>(c, dz, lddz, x, ldx, q, scales, M, ep, st);
-             else launch_weight_tokens<T, 16, true>(c, dz, lddz, x, ldx, q, scales, M, ep, st); }
+             else launch_weight_tokens<T, 8, true>(c, dz, lddz, x, ldx, q, scales, M, ep, st); }
     else if (M <= 4) launch_weight_tokens<T, 4, false>(c, dz, lddz, x, ldx, q, scales, M, ep, st);
-    else launch_weight_tokens<T, 16, false>(c, dz, lddz, x, ldx, q, scales, M, ep, st);
+    else launch_weight_tokens<T, 8, false>(c, dz, lddz, x, ldx, q, scales, M, ep, st);
 }
 
 // A wait of the layer products where nothing arrives.
@@ -518,7 +516,7 @@ int sc_linear_grad_weight(sc_ctx* ctx, int type, const void* dz, size_t lddz, co
     if (N == 1) ep.ldo = lddw = (K + 3) & ~(size_t)3;                // the distance between rows says nothing
     ep.grain_out = grain_of(dw, lddw, 4, 4);
     ep.groups = (uint32_t)ckpt_groups(K);
-    if (M && M <= FEW_WEIGHT_TOKENS && N <= 65535ull * 256) {
+    if (M && M <= FEW_WEIGHT_TOKENS && N <= 65535ull * 8) {
         const uint8_t* qb = reinterpret_cast<const uint8_t*>(q);
         Launch l(ctx, KIND_LINEAR_DW, st);
         if (type == SC_BF16) run_weight_tokens<__nv_bfloat16>(ctx, dz, lddz, x, ldx, qb, scales, M, ep, st);

@@ -470,15 +470,15 @@ __global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* _
 // ---------------------------------------------------------------------------
 // Weight gradient of a few tokens
 // ---------------------------------------------------------------------------
-// Up to 16 tokens: the fp32 result's own bytes are everything (16 multiply-adds a value still fit beside them), so each
+// Up to 8 tokens: the fp32 result's own bytes are everything (8 multiply-adds a value, two at a time, fit beside them), so each
 // value is made where it is stored.  A CTA owns 128 columns and `run` rows; every warp holds the columns' inputs in
-// registers, read from the checkpoint or from x, and walks its rows with the rows' dz in shared memory, one 128-byte
-// store at a time, whatever the alignment.
+// registers, read from the checkpoint or from x, and walks its rows with the rows' dz in shared memory (each twice, as the
+// paired arithmetic wants it), one 128-byte store at a time, whatever the alignment.
 template <typename T, int TOKENS, bool KEPT>
 __global__ void __launch_bounds__(256) weight_tokens_kernel(const T* __restrict__ dz, uint64_t lddz, const T* __restrict__ x, uint64_t ldx,
                                                             const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, uint32_t tokens, uint32_t run,
                                                             Epilogue ep) {
-    extern __shared__ float rows_dz[];              // [run][TOKENS]
+    extern __shared__ __align__(16) float2 rows_dz[];              // [run][TOKENS]
     wait_for_predecessor();
     release_successor();
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
@@ -487,35 +487,55 @@ __global__ void __launch_bounds__(256) weight_tokens_kernel(const T* __restrict_
     const uint32_t rows = (uint32_t)min((uint64_t)run, ep.rows - n0);
     for (uint32_t i = threadIdx.x; i < rows * TOKENS; i += 256) {
         const uint32_t m = i / rows, r = i - m * rows;
-        rows_dz[r * TOKENS + m] = m < tokens ? Elem<T>::to_float(dz[m * lddz + n0 + r]) : 0.0f;
+        const float d = m < tokens ? Elem<T>::to_float(dz[m * lddz + n0 + r]) : 0.0f;
+        rows_dz[r * TOKENS + m] = make_float2(d, d);
     }
+    // all loads first, from clamped places; columns past the end are not stored
     float v[TOKENS][4];
+    if constexpr (KEPT) {
+        uint32_t k[TOKENS][4];
 #pragma unroll
-    for (int m = 0; m < TOKENS; ++m)
+        for (int m = 0; m < TOKENS; ++m)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t c = c0 + 32 * j;
-            v[m][j] = 0.0f;
-            if (m < (int)tokens && c < K) {
-                if constexpr (KEPT) {
-                    const int k = (int8_t)q[(uint64_t)m * K + c];
-                    v[m][j] = k == -128 ? __uint_as_float(0x7FFFFFFFu) : (float)k * __uint_as_float((uint32_t)scales[(uint64_t)m * ep.groups + (c >> 5)] << 23);
-                } else {
-                    v[m][j] = Elem<T>::to_float(x[m * ldx + c]);
-                }
+            for (int j = 0; j < 4; ++j) {
+                const uint64_t row = min((uint32_t)m, tokens - 1);
+                const uint32_t c = min(c0 + 32 * j, K - 1);
+                k[m][j] = q[row * K + c];
+                v[m][j] = __uint_as_float((uint32_t)scales[row * ep.groups + (c >> 5)] << 23);
             }
-        }
+#pragma unroll
+        for (int m = 0; m < TOKENS; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[m][j] *= (float)(int8_t)k[m][j];
+                if (k[m][j] == 0x80u) v[m][j] = __uint_as_float(0x7FFFFFFFu);
+                if (m >= (int)tokens) v[m][j] = 0.0f;
+            }
+    } else {
+#pragma unroll
+        for (int m = 0; m < TOKENS; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[m][j] = Elem<T>::to_float(x[min((uint32_t)m, tokens - 1) * ldx + min(c0 + 32 * j, K - 1)]);
+#pragma unroll
+        for (int m = 0; m < TOKENS; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (m >= (int)tokens) v[m][j] = 0.0f;
+    }
     __syncthreads();
     float* out = static_cast<float*>(ep.out) + n0 * ep.ldo + c0;
-#pragma unroll 1
+#pragma unroll 2
     for (uint32_t r = warp; r < rows; r += 8) {
-        float acc[4] = {};
+        Pair lo[2] = {pair(0.0f), pair(0.0f)}, hi[2] = {pair(0.0f), pair(0.0f)};     // two chains each
 #pragma unroll
-        for (int m = 0; m < TOKENS; m += 4) {
+        for (int m = 0; m < TOKENS; m += 2) {
             const float4 d = *reinterpret_cast<const float4*>(&rows_dz[r * TOKENS + m]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] = fmaf(d.w, v[m + 3][j], fmaf(d.z, v[m + 2][j], fmaf(d.y, v[m + 1][j], fmaf(d.x, v[m][j], acc[j]))));
+            lo[0] = fma2(pair(d.x, d.y), pair(v[m][0], v[m][1]), lo[0]);
+            hi[0] = fma2(pair(d.x, d.y), pair(v[m][2], v[m][3]), hi[0]);
+            lo[1] = fma2(pair(d.z, d.w), pair(v[m + 1][0], v[m + 1][1]), lo[1]);
+            hi[1] = fma2(pair(d.z, d.w), pair(v[m + 1][2], v[m + 1][3]), hi[1]);
         }
+        const float2 a01 = both(lo[0] + lo[1]), a23 = both(hi[0] + hi[1]);
+        const float acc[4] = {a01.x, a01.y, a23.x, a23.y};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float* o = out + r * ep.ldo + 32 * j;
