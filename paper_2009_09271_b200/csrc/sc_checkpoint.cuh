@@ -320,6 +320,119 @@ __global__ void __launch_bounds__(CKPT_THREADS, sizeof(T) == 2 ? 4 : 3) checkpoi
     }
 }
 
+// The same for rows, or a q, that take narrow accesses only: a lane works on two neighbouring elements, so that a warp's
+// accesses stay contiguous; sixteen lanes hold a group.  Three times the instructions of the wide form, a quarter of its
+// transactions on such rows.
+constexpr int NARROW_UNROLL = 4;              // runs of 64 elements a warp has in flight
+
+struct NarrowWalk {
+    uint64_t total, stride_rows;              // total = rows * runs; a warp's runs are a fixed stride apart, in rows and runs
+    uint32_t cols, runs, stride_runs;         // runs of 64 elements a row
+    uint32_t two_x, two_q;                    // whether two elements of a row, or of q, go in one access
+};
+struct RunAt {
+    uint64_t row;
+    uint32_t run;
+    __device__ RunAt(const NarrowWalk& w, uint64_t i) : row(i / w.runs) { run = (uint32_t)(i - row * w.runs); }
+    __device__ void next(const NarrowWalk& w) {
+        row += w.stride_rows;
+        run += w.stride_runs;
+        if (run >= w.runs) { run -= w.runs; ++row; }
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(CKPT_THREADS) checkpoint_pack_narrow_kernel(const T* __restrict__ x, uint64_t ldx, NarrowWalk w,
+                                                                              uint8_t* __restrict__ q, uint8_t* __restrict__ scales) {
+    wait_for_predecessor();
+    release_successor();
+    const uint32_t lane = threadIdx.x & 31u, groups = (w.cols + CKPT_GROUP - 1) / CKPT_GROUP;
+    const uint64_t first = ((uint64_t)blockIdx.x * CKPT_THREADS + threadIdx.x) >> 5, stride = (uint64_t)gridDim.x * (CKPT_THREADS / 32);
+    RunAt at(w, first);
+    for (uint64_t base = first; base < w.total; base += stride * NARROW_UNROLL) {
+        float f[NARROW_UNROLL][2];
+        uint64_t row[NARROW_UNROLL];
+        uint32_t c[NARROW_UNROLL];
+#pragma unroll
+        for (int u = 0; u < NARROW_UNROLL; ++u) {
+            row[u] = at.row;
+            c[u] = base + u * stride < w.total ? at.run * 64 + lane * 2 : w.cols;
+            at.next(w);
+            const T* p = x + row[u] * ldx + c[u];
+            f[u][0] = f[u][1] = 0.0f;
+            if (sizeof(T) == 2 && w.two_x && c[u] + 1 < w.cols) {
+                uint32_t v = *reinterpret_cast<const uint32_t*>(p);
+                const T* e = reinterpret_cast<const T*>(&v);
+                f[u][0] = Elem<T>::to_float(e[0]);
+                f[u][1] = Elem<T>::to_float(e[1]);
+            } else {
+                if (c[u] < w.cols) f[u][0] = Elem<T>::to_float(p[0]);
+                if (c[u] + 1 < w.cols) f[u][1] = Elem<T>::to_float(p[1]);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < NARROW_UNROLL; ++u) {
+            const uint32_t a = __float_as_uint(f[u][0]) & 0x7FFFFFFFu, b = __float_as_uint(f[u][1]) & 0x7FFFFFFFu;
+            uint32_t m = max(a < 0x7F800000u ? a : 0u, b < 0x7F800000u ? b : 0u);
+#pragma unroll
+            for (int d = 1; d < 16; d <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+            const int e = ckpt_exponent<T>(m);
+            const float inv = pow2(-e), most = e == Elem<T>::EMAX ? 63.0f : 127.0f;
+            const uint32_t b0 = ckpt_byte_any(f[u][0], inv, most), b1 = ckpt_byte_any(f[u][1], inv, most);
+            uint8_t* dst = q + row[u] * w.cols + c[u];
+            if (w.two_q && c[u] + 1 < w.cols) {
+                *reinterpret_cast<uint16_t*>(dst) = (uint16_t)(b0 | b1 << 8);
+            } else {
+                if (c[u] < w.cols) dst[0] = (uint8_t)b0;
+                if (c[u] + 1 < w.cols) dst[1] = (uint8_t)b1;
+            }
+            if ((lane & 15u) == 0u && c[u] < w.cols) scales[row[u] * groups + (c[u] >> 5)] = (uint8_t)(e + 127);
+        }
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(CKPT_THREADS) checkpoint_unpack_narrow_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, NarrowWalk w,
+                                                                                T* __restrict__ out, uint64_t ldo) {
+    wait_for_predecessor();
+    release_successor();
+    const uint32_t lane = threadIdx.x & 31u, groups = (w.cols + CKPT_GROUP - 1) / CKPT_GROUP;
+    const uint64_t first = ((uint64_t)blockIdx.x * CKPT_THREADS + threadIdx.x) >> 5, stride = (uint64_t)gridDim.x * (CKPT_THREADS / 32);
+    RunAt at(w, first);
+    for (uint64_t base = first; base < w.total; base += stride * NARROW_UNROLL) {
+        uint32_t b[NARROW_UNROLL], sb[NARROW_UNROLL], c[NARROW_UNROLL];
+        uint64_t row[NARROW_UNROLL];
+#pragma unroll
+        for (int u = 0; u < NARROW_UNROLL; ++u) {
+            row[u] = at.row;
+            c[u] = base + u * stride < w.total ? at.run * 64 + lane * 2 : w.cols;
+            at.next(w);
+            const uint8_t* p = q + row[u] * w.cols + c[u];
+            b[u] = sb[u] = 0u;
+            if (w.two_q && c[u] + 1 < w.cols) {
+                b[u] = *reinterpret_cast<const uint16_t*>(p);
+            } else {
+                if (c[u] < w.cols) b[u] = p[0];
+                if (c[u] + 1 < w.cols) b[u] |= (uint32_t)p[1] << 8;
+            }
+            if (c[u] < w.cols) sb[u] = scales[row[u] * groups + (c[u] >> 5)];
+        }
+#pragma unroll
+        for (int u = 0; u < NARROW_UNROLL; ++u) {
+            const float s = __uint_as_float(sb[u] << 23), nan = __uint_as_float(0x7FFFFFFFu);
+            const uint32_t lo = b[u] & 0xFFu, hi = b[u] >> 8;
+            const T v[2] = {Elem<T>::from_float(lo == 0x80u ? nan : (float)(int8_t)lo * s), Elem<T>::from_float(hi == 0x80u ? nan : (float)(int8_t)hi * s)};
+            T* dst = out + row[u] * ldo + c[u];
+            if (sizeof(T) == 2 && w.two_x && c[u] + 1 < w.cols) {
+                *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint16_t*>(&v[0]) | (uint32_t)*reinterpret_cast<const uint16_t*>(&v[1]) << 16;
+            } else {
+                if (c[u] < w.cols) dst[0] = v[0];
+                if (c[u] + 1 < w.cols) dst[1] = v[1];
+            }
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------
 // dz = dy * act'(z^) and db = column sums of dz
 // ---------------------------------------------------------------------------

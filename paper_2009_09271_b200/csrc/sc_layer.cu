@@ -100,18 +100,42 @@ ItemWalk item_walk(const sc_ctx* c, size_t rows, size_t cols, const uint8_t* q, 
     return w;
 }
 
+// Rows that are aligned to single elements only, or such a q, take the narrow form (NARROW_NOTE).
+bool narrow_walk(const sc_ctx* c, const ItemWalk& wide, size_t rows, size_t cols, NarrowWalk& w, uint32_t& grid) {
+    if (wide.grain_q > 1 && wide.grain_x > 1) return false;
+    w.cols = (uint32_t)cols;
+    w.runs = (uint32_t)ceil_div(cols, 64);
+    w.total = (uint64_t)rows * w.runs;
+    grid = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(w.total, CKPT_THREADS / 32), (uint64_t)c->sm_count * 8));
+    const uint64_t stride = (uint64_t)grid * (CKPT_THREADS / 32);
+    w.stride_rows = stride / w.runs;
+    w.stride_runs = (uint32_t)(stride % w.runs);
+    w.two_x = wide.grain_x >= 2; w.two_q = wide.grain_q >= 2;
+    return true;
+}
+
 template <typename T>
 void launch_pack(sc_ctx* c, const void* x, size_t ldx, size_t rows, size_t cols, uint8_t* q, uint8_t* scales, cudaStream_t st) {
     const ItemWalk w = item_walk(c, rows, cols, q, x, ldx, sizeof(T));
+    NarrowWalk n{};
+    uint32_t grid = 0;
     Launch l(c, KIND_CKPT_PACK, st);
-    launch(checkpoint_pack_kernel<T>, item_grid(c, w.total), CKPT_THREADS, 0, 1, st, static_cast<const T*>(x), ldx, w, q, scales);
+    if (narrow_walk(c, w, rows, cols, n, grid))
+        launch(checkpoint_pack_narrow_kernel<T>, grid, CKPT_THREADS, 0, 1, st, static_cast<const T*>(x), ldx, n, q, scales);
+    else
+        launch(checkpoint_pack_kernel<T>, item_grid(c, w.total), CKPT_THREADS, 0, 1, st, static_cast<const T*>(x), ldx, w, q, scales);
 }
 
 template <typename T>
 void launch_unpack(sc_ctx* c, const uint8_t* q, const uint8_t* scales, size_t rows, size_t cols, void* out, size_t ldo, cudaStream_t st) {
     const ItemWalk w = item_walk(c, rows, cols, q, out, ldo, sizeof(T));
+    NarrowWalk n{};
+    uint32_t grid = 0;
     Launch l(c, KIND_CKPT_UNPACK, st);
-    launch(checkpoint_unpack_kernel<T>, item_grid(c, w.total), CKPT_THREADS, 0, 1, st, q, scales, w, static_cast<T*>(out), ldo);
+    if (narrow_walk(c, w, rows, cols, n, grid))
+        launch(checkpoint_unpack_narrow_kernel<T>, grid, CKPT_THREADS, 0, 1, st, q, scales, n, static_cast<T*>(out), ldo);
+    else
+        launch(checkpoint_unpack_kernel<T>, item_grid(c, w.total), CKPT_THREADS, 0, 1, st, q, scales, w, static_cast<T*>(out), ldo);
 }
 
 struct GradPlan { uint32_t strips, runs, run_rows; size_t bytes; };
@@ -170,6 +194,16 @@ bool out_map(CUtensorMap* map, float* p, uint64_t rows, uint64_t cols, uint64_t 
     const cuuint32_t box[3] = {32, 32, 1}, steps[3] = {1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, p, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The 16-bit result, stored in blocks of 32 x 32.
+bool rows_map(CUtensorMap* map, int type, void* p, uint64_t rows, uint64_t cols, uint64_t ld) {
+    const auto fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {ld * 2};
+    const cuuint32_t box[2] = {32, 32}, steps[2] = {1, 1};
+    return fn(map, type == SC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, p, dims, strides, box, steps,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 constexpr size_t PARTIAL_CAP = 64u << 20;      // bytes of partial sums a split product may use
@@ -261,7 +295,10 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
     a.part_ld = (uint32_t)p.part_ld; a.part_stride = ep.rows * p.part_ld; a.partial = partial; a.status = c->d_status;
     // partial sums are whole to the next multiple of 32 columns: a checkpoint group's maximum is taken over all of its columns
     a.tma_out = p.splits > 1 || (MODE == PRODUCT_WEIGHT && ep.grain_out >= 4);
+    if constexpr (MODE != PRODUCT_WEIGHT)
+        a.rows_form = p.splits == 1 && ep.grain_out >= 8 && (!ep.residual || ep.grain_res >= 8) && (!ep.q || ep.grain_q >= 8);
     CUtensorMap ma, mb, mo{};
+    if (a.rows_form && !rows_map(&mo, type, ep.out, ep.rows, ep.cols, ep.rows > 1 ? ep.ldo : round8(ep.cols))) return SC_ERR_CUDA;
     if (a.tma_out && !(p.splits > 1 ? out_map(&mo, partial, ep.rows, p.part_ld, p.part_ld, p.splits, a.part_stride)
                                     : out_map(&mo, static_cast<float*>(ep.out), ep.rows, ep.cols, ep.ldo, 1, ep.rows * ep.ldo)))
         return SC_ERR_CUDA;
@@ -458,7 +495,7 @@ int sc_linear(sc_ctx* ctx, int type, int act, const void* x, size_t ldx, const v
     ep.bias = bias; ep.residual = residual; ep.ldr = ldr; ep.out = y; ep.ldo = ldy; ep.rows = M; ep.cols = (uint32_t)N;
     ep.q = reinterpret_cast<uint8_t*>(q); ep.scales = scales; ep.groups = (uint32_t)ckpt_groups(N); ep.act = act;
     ep.grain_out = grain_of(y, M > 1 ? ldy : 0, 2, 8); ep.grain_res = grain_of(residual, M > 1 ? ldr : 0, 2, 8);
-    ep.grain_q = grain_of(q, M > 1 ? N : 0, 1, 8); ep.grain_bias = grain_of(bias, 0, 2, 8);
+    ep.grain_q = grain_of(q, M > 1 ? N : 0, 1, 16); ep.grain_bias = grain_of(bias, 0, 2, 8);
     if (M <= FEW_TOKENS && K) {
         Launch l(ctx, KIND_LINEAR, st);
         const Stored xs{x, M, K, ldx}, ws{w, N, K, ldw};
@@ -493,7 +530,7 @@ int sc_linear_grad_input(sc_ctx* ctx, int type, int act, const void* dz, size_t 
         ep.groups = (uint32_t)ckpt_groups(K);
     }
     ep.grain_out = grain_of(dx, M > 1 ? lddx : 0, 2, 8); ep.grain_res = grain_of(residual, M > 1 ? ldr : 0, 2, 8);
-    ep.grain_q = grain_of(q, M > 1 ? K : 0, 1, 8);
+    ep.grain_q = grain_of(q, M > 1 ? K : 0, 1, 16);
     if (const int rc = run_product<PRODUCT_INPUT>(ctx, KIND_LINEAR_DX, type, Stored{dz, M, N, lddz}, Stored{w, N, K, ldw}, N, ep, 0, st)) return rc;
     SC_CUDA(cudaGetLastError());
     return SC_OK;

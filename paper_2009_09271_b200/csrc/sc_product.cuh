@@ -26,8 +26,10 @@ struct Epilogue {
 
 // What follows the product for 8 columns from c0 of one row.  All 32 lanes of a warp call it; four neighbouring lanes hold
 // 32 consecutive columns of one row, from a multiple of 32, so they share a checkpoint group.  `bias`: of these columns.
+// `slot`: 0, or the row's 128 bytes of shared memory, where the 16-bit result and the checkpoint's bytes (from byte 64) are
+// left for rows_out instead of being written to rows that take narrow accesses only.
 template <typename T, int MODE, int ACT>
-__device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint32_t c0, const float bias[8], float v[8]) {
+__device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint32_t c0, const float bias[8], float v[8], uint32_t slot = 0) {
     const bool in = row < ep.rows && c0 < ep.cols;
     if constexpr (MODE == PRODUCT_WEIGHT) {
         if (!in) return;
@@ -52,8 +54,9 @@ __device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint
                 m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
                 int e;
                 const uint2 b = ckpt_encode8<T>(v, m, e);
+                if (slot) asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(slot + 64 + (c0 & 31u)), "r"(b.x), "r"(b.y) : "memory");
                 if (in) {
-                    store_q8(ep.q + row * ep.cols + c0, c0, ep.cols, ep.grain_q, b);
+                    if (!slot) store_q8(ep.q + row * ep.cols + c0, c0, ep.cols, ep.grain_q, b);
                     if ((c0 & 31u) == 0u) ep.scales[row * ep.groups + (c0 >> 5)] = (uint8_t)(e + 127);
                 }
             }
@@ -79,7 +82,56 @@ __device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint
                 }
             }
         }
-        store8(static_cast<T*>(ep.out) + row * ep.ldo, c0, ep.cols, ep.grain_out, v);
+        if (slot) {
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(slot + (c0 & 31u) * 2), "r"(Elem<T>::pack(v[0], v[1])), "r"(Elem<T>::pack(v[2], v[3])),
+                         "r"(Elem<T>::pack(v[4], v[5])), "r"(Elem<T>::pack(v[6], v[7])) : "memory");
+        } else {
+            store8(static_cast<T*>(ep.out) + row * ep.ldo, c0, ep.cols, ep.grain_out, v);
+        }
+    }
+}
+
+// The 32 x 32 block that epilogue8 left in shared memory, to rows of any alignment: neighbouring lanes write neighbouring
+// elements, two at a time where the rows allow.
+static __device__ __noinline__ void rows_out(const Epilogue& ep, uint32_t stage_addr, uint64_t row0, uint32_t col0, bool kept) {
+    const uint32_t lane = threadIdx.x & 31u;
+    const uint32_t rows = row0 < ep.rows ? (uint32_t)min((uint64_t)32, ep.rows - row0) : 0u, cols = col0 < ep.cols ? min(32u, ep.cols - col0) : 0u;
+    uint16_t* y = static_cast<uint16_t*>(ep.out) + row0 * ep.ldo + col0;
+    if (ep.grain_out >= 2) {
+        const uint32_t c = (lane & 15u) * 2;
+#pragma unroll 4
+        for (uint32_t r = lane >> 4; r < rows; r += 2) {
+            uint32_t v;
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(stage_addr + r * 128 + c * 2) : "memory");
+            if (c + 1 < cols) *reinterpret_cast<uint32_t*>(y + r * ep.ldo + c) = v;
+            else if (c < cols) y[r * ep.ldo + c] = (uint16_t)v;
+        }
+    } else {
+#pragma unroll 4
+        for (uint32_t r = 0; r < rows; ++r) {
+            uint16_t v;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(stage_addr + r * 128 + lane * 2) : "memory");
+            if (lane < cols) y[r * ep.ldo + lane] = v;
+        }
+    }
+    if (!kept) return;
+    uint8_t* q = ep.q + row0 * ep.cols + col0;
+    if (ep.grain_q >= 2) {
+        const uint32_t c = (lane & 15u) * 2;
+#pragma unroll 4
+        for (uint32_t r = lane >> 4; r < rows; r += 2) {
+            uint16_t v;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(stage_addr + r * 128 + 64 + c) : "memory");
+            if (c + 1 < cols) *reinterpret_cast<uint16_t*>(q + (uint64_t)r * ep.cols + c) = v;
+            else if (c < cols) q[(uint64_t)r * ep.cols + c] = (uint8_t)v;
+        }
+    } else {
+#pragma unroll 4
+        for (uint32_t r = 0; r < rows; ++r) {
+            uint32_t v;
+            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(stage_addr + r * 128 + 64 + lane) : "memory");
+            if (lane < cols) q[(uint64_t)r * ep.cols + lane] = (uint8_t)v;
+        }
     }
 }
 
@@ -128,6 +180,7 @@ struct TcArgs {
     uint64_t part_stride;                  // elements between two parts
     uint32_t part_ld;
     uint32_t tma_out;                      // fp32 goes out by TMA: partial sums always, the weight gradient where its rows allow
+    uint32_t rows_form;                    // 16-bit result and all that goes with it: rows take 16-byte accesses (q: 8-byte)
     float* partial;
     int* status;
 };
@@ -199,16 +252,141 @@ __device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcAr
     } else {
         float bias[8];
         load_bias<T, MODE>(ep, c0, bias);
+        const bool narrow = ep.grain_out == 1 || (MODE == PRODUCT_FORWARD && ep.q && ep.grain_q == 1);
         with_activation(ep.act, [&](auto act) {
 #pragma unroll 1                                              // little code: it is fetched cold in a small call
             for (int i = 0; i < 4; ++i) {
                 float f[8];
                 const uint64_t row = fetch(i, f);
-                epilogue8<T, MODE, decltype(act)::value>(ep, row, c0, bias, f);
+                if (narrow) __syncwarp();                     // the row's four lanes have read it
+                epilogue8<T, MODE, decltype(act)::value>(ep, row, c0, bias, f, narrow ? stage_addr + (uint32_t)(row - row0) * 128 : 0u);
             }
         });
+        if (narrow) {
+            __syncwarp();
+            rows_out(ep, stage_addr, row0, col0, MODE == PRODUCT_FORWARD && ep.q);
+        }
     }
     __syncwarp();
+}
+
+// One 32 x 32 block of a 16-bit result, thread t holding row t from TMEM to the end: a checkpoint group is one thread's own, its
+// bytes go out as one sector, and the result leaves by TMA from a 2 KB buffer of 64-byte rows (64-byte swizzle), two of
+// which take turns.  About a third of the instructions of block_out, which serves rows of other alignments.
+template <typename T, int MODE, int ACT>
+__device__ __forceinline__ void block_rows(const CUtensorMap* map_out, const Epilogue& ep, uint32_t buffer, const uint32_t (&v)[32], uint64_t row0,
+                                           uint32_t col0) {
+    const uint32_t lane = threadIdx.x & 31u;
+    const uint64_t row = row0 + lane;
+    const bool in = row < ep.rows && col0 < ep.cols, whole = col0 + 32 <= ep.cols;
+    Pair z[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+    if constexpr (MODE == PRODUCT_FORWARD) {
+        if (ep.bias) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float b[8];
+                load_bias<T, MODE>(ep, col0 + 8 * j, b);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[4 * j + i] = z[4 * j + i] + pair(b[2 * i], b[2 * i + 1]);
+            }
+        }
+        if (ep.q) {
+            uint32_t m = 0;                                 // columns past the end hold no product and no bias
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float2 f = both(z[i]);
+                m = max(max(m, __float_as_uint(f.x) & 0x7FFFFFFFu), __float_as_uint(f.y) & 0x7FFFFFFFu);
+            }
+            int e = ckpt_exponent<T>(m);
+            const bool odd = m >= 0x7F800000u || e == Elem<T>::EMAX;
+            if (odd) {
+                m = 0;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float2 f = both(z[i]);
+                    const uint32_t a = __float_as_uint(f.x) & 0x7FFFFFFFu, b = __float_as_uint(f.y) & 0x7FFFFFFFu;
+                    m = max(max(m, a < 0x7F800000u ? a : 0u), b < 0x7F800000u ? b : 0u);
+                }
+                e = ckpt_exponent<T>(m);
+            }
+            uint2 b[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float f[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { const float2 p = both(z[4 * j + i]); f[2 * i] = p.x; f[2 * i + 1] = p.y; }
+                b[j] = ckpt_bytes8(f, e);
+            }
+            if (odd) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float f[8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { const float2 p = both(z[4 * j + i]); f[2 * i] = p.x; f[2 * i + 1] = p.y; }
+                    b[j] = ckpt_bytes8_any<T>(f, e);
+                }
+            }
+            if (in) {
+                uint8_t* q = ep.q + row * ep.cols + col0;
+                if (whole && ep.grain_q >= 16) {
+                    reinterpret_cast<uint4*>(q)[0] = make_uint4(b[0].x, b[0].y, b[1].x, b[1].y);
+                    reinterpret_cast<uint4*>(q)[1] = make_uint4(b[2].x, b[2].y, b[3].x, b[3].y);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) store_q8(q + 8 * j, col0 + 8 * j, ep.cols, ep.grain_q, b[j]);
+                }
+                ep.scales[row * ep.groups + (col0 >> 5)] = (uint8_t)(e + 127);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[i] = activation<ACT>(z[i]);
+    }
+    if (ep.residual && in) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float r[8];
+            to_floats(load8(static_cast<const T*>(ep.residual) + row * ep.ldr, col0 + 8 * j, ep.cols, 8u), r);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[4 * j + i] = z[4 * j + i] + pair(r[2 * i], r[2 * i + 1]);
+        }
+    }
+    if constexpr (MODE == PRODUCT_INPUT && ACT != SC_ACT_NONE) {
+        if (in) {
+            const uint8_t* q = ep.q + row * ep.cols;
+            const Scale s = slope_scale(ep.scales[row * ep.groups + (col0 >> 5)]);
+            uint2 k[4];
+            if (whole && ep.grain_q >= 16) {
+                const uint4 a = __ldcs(reinterpret_cast<const uint4*>(q + col0)), b = __ldcs(reinterpret_cast<const uint4*>(q + col0) + 1);
+                k[0] = make_uint2(a.x, a.y); k[1] = make_uint2(a.z, a.w); k[2] = make_uint2(b.x, b.y); k[3] = make_uint2(b.z, b.w);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) k[j] = load_q8(q, col0 + 8 * j, ep.cols, ep.grain_q);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                Pair h[4];
+                ckpt_values8<false>(k[j], s, h);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[4 * j + i] = z[4 * j + i] * activation_slope<ACT>(h[i]);
+            }
+        }
+    }
+    if (lane == 0) tma_store_wait_read_but_one();           // the copy before last has left this buffer
+    __syncwarp();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const uint4 o = packed8<T>(z + 4 * u);
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buffer + lane * 64 + ((u ^ ((lane >> 1) & 3)) * 16)), "r"(o.x), "r"(o.y), "r"(o.z),
+                     "r"(o.w) : "memory");
+    }
+    smem_to_async_fence();
+    __syncwarp();
+    if (lane == 0) {
+        if (row0 < ep.rows && col0 < ep.cols) tma_store_2d(map_out, buffer, (int32_t)col0, (int32_t)row0);
+        tma_store_commit();
+    }
 }
 
 template <typename T, int MODE, int BN, int CG>
@@ -232,7 +410,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
         mbar_init_fence();
         tma_prefetch_map(&map_a);
         tma_prefetch_map(&map_b);
-        if (a.tma_out) tma_prefetch_map(&map_out);
+        if (a.tma_out || a.rows_form) tma_prefetch_map(&map_out);
     }
     if (warp == 2) tmem_alloc<CG>(slot, S::TMEM_COLS);
     tcgen05_fence_before();
@@ -380,12 +558,17 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                         __syncwarp();
                         if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_rank(tempty + 8 * acc, 0) : tempty + 8 * acc);
                     }
-                    block_out<T, MODE>(&map_out, a, ep, stage_addr, v, row0, col0 + c, split);
+                    if (a.rows_form)
+                        with_activation(ep.act, [&](auto act) {
+                            block_rows<T, MODE, decltype(act)::value>(&map_out, ep, stage_addr + (c & 32) * 64, v, row0, col0 + c);
+                        });
+                    else
+                        block_out<T, MODE>(&map_out, a, ep, stage_addr, v, row0, col0 + c, split);
                 }
                 if ((acc ^= 1u) == 0) acc_phase ^= 1u;
             }
         }
-        if (a.tma_out && lane == 0) tma_store_wait();
+        if ((a.tma_out || a.rows_form) && lane == 0) tma_store_wait();
         if (!ok && lane == 0) atomicCAS(a.status, 0, ST_TIMEOUT);
         __syncwarp();
     }
