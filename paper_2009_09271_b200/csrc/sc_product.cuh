@@ -22,6 +22,7 @@ struct Epilogue {
     int act;
     uint32_t accumulate;
     uint32_t grain_out, grain_res, grain_q, grain_bias;      // elements that one access of a row may take
+    uint32_t scales_by4;       // block_rows: four neighbouring scales of a row go out in one access
 };
 
 // What follows the product for 8 columns from c0 of one row.  All 32 lanes of a warp call it; four neighbouring lanes hold
@@ -275,7 +276,7 @@ __device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcAr
 // which take turns.  About a third of the instructions of block_out, which serves rows of other alignments.
 template <typename T, int MODE, int ACT>
 __device__ __forceinline__ void block_rows(const CUtensorMap* map_out, const Epilogue& ep, uint32_t buffer, const uint32_t (&v)[32], uint64_t row0,
-                                           uint32_t col0) {
+                                           uint32_t col0, uint32_t& scale4) {
     const uint32_t lane = threadIdx.x & 31u;
     const uint64_t row = row0 + lane;
     const bool in = row < ep.rows && col0 < ep.cols, whole = col0 + 32 <= ep.cols;
@@ -330,14 +331,21 @@ __device__ __forceinline__ void block_rows(const CUtensorMap* map_out, const Epi
             }
             if (in) {
                 uint8_t* q = ep.q + row * ep.cols + col0;
-                if (whole && ep.grain_q >= 16) {
-                    reinterpret_cast<uint4*>(q)[0] = make_uint4(b[0].x, b[0].y, b[1].x, b[1].y);
-                    reinterpret_cast<uint4*>(q)[1] = make_uint4(b[2].x, b[2].y, b[3].x, b[3].y);
+                const uint4 b01 = make_uint4(b[0].x, b[0].y, b[1].x, b[1].y), b23 = make_uint4(b[2].x, b[2].y, b[3].x, b[3].y);
+                if (whole && ep.grain_q >= 32) {
+                    store32(q, b01, b23);
+                } else if (whole && ep.grain_q >= 16) {
+                    reinterpret_cast<uint4*>(q)[0] = b01;
+                    reinterpret_cast<uint4*>(q)[1] = b23;
                 } else {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) store_q8(q + 8 * j, col0 + 8 * j, ep.cols, ep.grain_q, b[j]);
                 }
-                ep.scales[row * ep.groups + (col0 >> 5)] = (uint8_t)(e + 127);
+                // the scales of four blocks in a row go out together where they are aligned; a warp's first block is one of four
+                scale4 = scale4 >> 8 | (uint32_t)(e + 127) << 24;
+                uint8_t* s = ep.scales + row * ep.groups + (col0 >> 5);
+                if (!ep.scales_by4) *s = (uint8_t)(e + 127);
+                else if ((col0 & 96u) == 96u) *reinterpret_cast<uint32_t*>(s - 3) = scale4;
             }
         }
 #pragma unroll
@@ -548,6 +556,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                 if (!(ok = warp_wait(tfull + 8 * acc, acc_phase))) break;
                 __syncwarp();
                 tcgen05_fence_after();
+                uint32_t scale4 = 0;
 #pragma unroll 1
                 for (int c = 0; c < BN / 2; c += 32) {
                     uint32_t v[32];
@@ -560,7 +569,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                     }
                     if (a.rows_form)
                         with_activation(ep.act, [&](auto act) {
-                            block_rows<T, MODE, decltype(act)::value>(&map_out, ep, stage_addr + (c & 32) * 64, v, row0, col0 + c);
+                            block_rows<T, MODE, decltype(act)::value>(&map_out, ep, stage_addr + (c & 32) * 64, v, row0, col0 + c, scale4);
                         });
                     else
                         block_out<T, MODE>(&map_out, a, ep, stage_addr, v, row0, col0 + c, split);
