@@ -152,13 +152,20 @@ __device__ __forceinline__ void load_bias(const Epilogue& ep, uint32_t c0, float
 // a pair holds 128 rows of A, half of B's rows, and the accumulator of its own 128 output rows.  A producer warp streams
 // 64-deep slices of both operands into a ring of shared-memory stages by TMA (128-byte swizzle; edges are filled with
 // zeros), one thread issues the matrix instructions into one of two accumulators in TMEM, and eight warps empty the
-// other one: they move 32 x 32 blocks through shared memory so that what they read and write in HBM is contiguous
-// along rows.
+// other one.  A 16-bit result leaves by block_rows, rows that do not take 16-byte accesses by block_out, which moves
+// 32 x 32 blocks through shared memory so that neighbouring lanes work along rows.
+//
+// Bound by the tensor pipe and, where calls follow each other, by the power cap (1000 W; SM clock 1.2-1.5 GHz).
+// 8192 x 16384 x 4096 bf16: forward 775-840 us (1.31-1.42 PFLOP/s; the library's product alone 772-800 us beside it), with tanh
+// gelu and checkpoint 832-875 us, input gradient 790-870 us, weight gradient 850-930 us.  At 4096 x 8192 x 4096 the tensor
+// pipe is active for 78 to 82 % of the elapsed cycles.  What it took: pairs of CTAs (B read once a pair), the issuing warp kept
+// converged with one elected lane (a branch on the lane number cost 10 %), an accumulator hand-over without a release at
+// cluster scope, and the epilogue's loops rolled (fetched cold, they were most of a small call).
 //
 // The tensor cores add to an fp32 accumulator by cutting, not rounding: measured, a sum of n steps of 16 products comes
 // out about n 2^-24 of its size too small (2e-7 after 256 products, 9e-6 after 8192, 4e-5 after 32768 of random sign).  A
-// 16-bit result does not see that.  The weight gradient is fp32, so its accumulators are emptied every CHUNK = 4 blocks
-// (256 products) and added up in registers, with rounding.
+// 16-bit result does not see that.  The weight gradient is fp32, so its accumulators are emptied every 6 blocks
+// (384 products) and added up in registers, with rounding: 3.6e-7 after 8192, at the price of 3 to 5 % of the time.
 constexpr int TC_ROWS = 128, TC_STEP = 64, TC_THREADS = 384, TC_EPI_WARPS = 8, TC_CHUNK = 6;
 constexpr int TC_LEAST_REGS = 160;             // 160 x 384 >= 56 x 128 + 208 x 256, for builds that shift registers
 constexpr uint32_t TC_SMEM_LIMIT = 232448;
@@ -594,6 +601,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
 // With one to four tokens the weights' bytes are everything, and four multiply-adds a weight still fit beside their loads.
 // A warp owns four rows of W and walks its share of the reduction, 16 bytes a lane and row; WK warps split a row, WN warps
 // sit side by side, and the last step joins them in shared memory.  WN = 8 puts 32 outputs, a checkpoint group, in one CTA.
+// 1 x 4096 x 4096 bf16 takes 8.6 us with W from HBM (33.6 MB, 3.9 TB/s); the tiles took 15.5 + 4.7 us.  Five tokens take the
+// tiles: 8 x 4096 x 4096 in 10.6 us there, 4 tokens 12.6 us here with cold caches.
 template <typename T, int TOKENS, int WN, int WK, bool WIDE>
 __global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* __restrict__ x, uint64_t ldx, const T* __restrict__ w, uint64_t ldw,
                                                                       uint32_t K, uint32_t grain_x, uint32_t grain_w, Epilogue ep) {
@@ -665,7 +674,8 @@ __global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* _
 // Up to 8 tokens: the fp32 result's own bytes are everything (8 multiply-adds a value, two at a time, fit beside them), so each
 // value is made where it is stored.  A CTA owns 128 columns and `run` rows; every warp holds the columns' inputs in
 // registers, read from the checkpoint or from x, and walks its rows with the rows' dz in shared memory (each twice, as the
-// paired arithmetic wants it), one 128-byte store at a time, whatever the alignment.
+// paired arithmetic wants it), one 128-byte store at a time, whatever the alignment.  4096 x 4096: 14.7 us at 4 tokens and
+// 16.4 at 8, against 18.2 on the tiles (with the checkpoint's copy); a fill of the output takes 12.3.  With 16 tokens it took 31.
 template <typename T, int TOKENS, bool KEPT>
 __global__ void __launch_bounds__(256) weight_tokens_kernel(const T* __restrict__ dz, uint64_t lddz, const T* __restrict__ x, uint64_t ldx,
                                                             const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, uint32_t tokens, uint32_t run,
@@ -738,7 +748,8 @@ __global__ void __launch_bounds__(256) weight_tokens_kernel(const T* __restrict_
     }
 }
 
-// Joins the parts of a split product in order and applies the epilogue; no parts at all is an empty sum.
+// Joins the parts of a split product in order and applies the epilogue; no parts at all is an empty sum.  2 to 6 us: parts are
+// few enough to be read from L2.
 template <typename T, int MODE>
 __global__ void __launch_bounds__(256) product_join_kernel(const float* __restrict__ partial, uint32_t splits, uint64_t part_stride, uint32_t part_ld,
                                                            Epilogue ep) {
