@@ -129,9 +129,15 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+# the current stream's handle, without the Stream object that torch.cuda.current_stream() makes around it (3 us)
+_raw_stream, _current_device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream(stream) -> Optional[int]:
-    if stream is None:                          # the current stream's handle, without the Stream object around it (3 us)
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
+    if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(_current_device()) or None
+        stream = torch.cuda.current_stream()
     return stream.cuda_stream or None
 
 

@@ -94,6 +94,10 @@ struct sc_ctx {
     // layer operators (sc_layer.cu): one block, grown on demand, and tickets that are zero between calls
     unsigned char* d_layer = nullptr;
     size_t layer_bytes = 0;
+    struct LayerPlan { uint64_t rows, cols, red; int mode, bn, cg; uint32_t splits; uint64_t part_ld; size_t bytes; };
+    static constexpr int LAYER_PLANS = 16;
+    LayerPlan layer_plans[LAYER_PLANS] = {};     // tile shapes of the sizes seen last
+    int layer_plan_next = 0;
     bool layer_captured = false;                 // a captured call used the block: growing must not free it
     static constexpr int MAX_RETIRED = 64;
     unsigned char* layer_retired[MAX_RETIRED] = {};

@@ -1,6 +1,6 @@
 // Host side of the layer operators declared in include/sparsecomm.h: argument checks, scratch, launches.
 #include <algorithm>
-#include <mutex>
+#include <atomic>
 
 #include "sc_checkpoint.cuh"
 #include "sc_context.cuh"
@@ -58,7 +58,8 @@ int layer_scratch(sc_ctx* c, size_t bytes, cudaStream_t st) {
         c->d_layer = nullptr; c->layer_bytes = 0; c->layer_captured = false;
     }
     if (cudaMalloc(&p, TICKET_BYTES + bytes) != cudaSuccess) { cudaGetLastError(); return SC_ERR_WORKSPACE; }
-    if (cudaMemsetAsync(p, 0, TICKET_BYTES, st) != cudaSuccess) { cudaFree(p); return SC_ERR_CUDA; }
+    // finished before any stream can use it
+    if (cudaMemsetAsync(p, 0, TICKET_BYTES, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) { cudaFree(p); return SC_ERR_CUDA; }
     c->d_layer = static_cast<unsigned char*>(p);
     c->layer_bytes = bytes;
     c->scratch_bytes += TICKET_BYTES + bytes;
@@ -209,15 +210,17 @@ bool rows_map(CUtensorMap* map, int type, void* p, uint64_t rows, uint64_t cols,
 
 constexpr size_t PARTIAL_CAP = 64u << 20;      // bytes of partial sums a split product may use
 
-struct ProductPlan { int bn, cg; uint32_t splits; uint64_t part_ld; size_t bytes; };
+using ProductPlan = sc_ctx::LayerPlan;
 
 // Tile shape and number of parts by an estimate in SM cycles: waves of tiles, each as long as its reduction or as the
 // emptying of the accumulator before it, and the partial sums' way to memory and back.  A block of 64 reduction steps costs
 // the tensor pipe 512 cycles for 256 columns (pairs; a little more for one CTA, which loads twice B), or what its bytes
 // take from L2 (50 to 60 a cycle and SM).  Against the best of all shapes and splits, swept over 13 sizes and the three products
 // (one token to 32001, widths 512 to 9000), the choice is within 15 %.
-ProductPlan product_plan(const sc_ctx* c, int mode, uint64_t rows, uint64_t cols, uint64_t red) {
-    ProductPlan best{256, 1, 1, (cols + 31) & ~31ull, 0};
+ProductPlan product_plan(sc_ctx* c, int mode, uint64_t rows, uint64_t cols, uint64_t red) {
+    for (const ProductPlan& p : c->layer_plans)                // a step's few sizes come again and again
+        if (p.rows == rows && p.cols == cols && p.red == red && p.mode == mode) return p;
+    ProductPlan best{rows, cols, red, mode, 256, 1, 1, (cols + 31) & ~31ull, 0};
     const uint64_t blocks = ceil_div(red, TC_STEP);
     double best_cost = 0;
     const double box = (double)std::min<uint64_t>(rows, TC_ROWS);
@@ -234,21 +237,23 @@ ProductPlan product_plan(const sc_ctx* c, int mode, uint64_t rows, uint64_t cols
             if (best_cost == 0 || cost < best_cost) { best_cost = cost; best.bn = bn; best.cg = cg; best.splits = s; best.bytes = bytes; }
         }
     }
+    c->layer_plans[c->layer_plan_next] = best;
+    c->layer_plan_next = (c->layer_plan_next + 1) % sc_ctx::LAYER_PLANS;
     return best;
 }
 
 template <typename T, int MODE, int BN, int CG>
 int launch_tiles(sc_ctx* c, const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mo, const TcArgs& a, const Epilogue& ep, cudaStream_t st) {
-    static std::once_flag once;
-    static cudaError_t rc;
-    std::call_once(once, [] {
+    static std::atomic<uint64_t> ready{0};         // devices on which this build may use its shared memory
+    const uint64_t bit = c->device < 64 ? 1ull << c->device : 0;
+    if (!(ready.load(std::memory_order_relaxed) & bit)) {
         cudaFuncAttributes f{};
-        rc = cudaFuncSetAttribute(product_kernel<T, MODE, BN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<BN, CG>::SMEM);
-        if (rc == cudaSuccess) rc = cudaFuncGetAttributes(&f, product_kernel<T, MODE, BN, CG>);
+        SC_CUDA(cudaFuncSetAttribute(product_kernel<T, MODE, BN, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, TcShape<BN, CG>::SMEM));
+        SC_CUDA(cudaFuncGetAttributes(&f, product_kernel<T, MODE, BN, CG>));
         // a register split beyond the launch's total would wait for ever
-        if (rc == cudaSuccess && MODE == PRODUCT_WEIGHT && BN == 256 && f.numRegs < TC_LEAST_REGS) rc = cudaErrorInvalidDeviceFunction;
-    });
-    if (rc != cudaSuccess) return SC_ERR_CUDA;
+        if (MODE == PRODUCT_WEIGHT && BN == 256 && f.numRegs < TC_LEAST_REGS) return SC_ERR_UNSUPPORTED;
+        ready.fetch_or(bit, std::memory_order_relaxed);
+    }
     const uint32_t grid = CG * (uint32_t)std::min<uint64_t>((uint64_t)a.tiles * a.splits, c->sm_count / CG);
     return launch(product_kernel<T, MODE, BN, CG>, grid, TC_THREADS, TcShape<BN, CG>::SMEM, CG, st, ma, mb, mo, a, ep) == cudaSuccess ? SC_OK : SC_ERR_CUDA;
 }
