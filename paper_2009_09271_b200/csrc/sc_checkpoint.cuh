@@ -456,6 +456,7 @@ struct GradArgs {
     uint32_t cols, groups, runs, run_rows, accumulate, grain_y, grain_z, grain_q;
 };
 
+// WIDE: a multiple of 8 columns, rows that take 16-byte accesses and a q that takes 8-byte ones.
 template <typename T, int ACT, bool WIDE>
 __global__ void __launch_bounds__(CKPT_THREADS, 4) activation_grad_kernel(const T* dy, const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales,
                                                                           GradArgs a, T* dz, float* __restrict__ partial,
@@ -478,9 +479,11 @@ __global__ void __launch_bounds__(CKPT_THREADS, 4) activation_grad_kernel(const 
         struct Row { Raw8<T> g; uint2 k; uint32_t sb; };
         const auto fetch = [&](Row& row, uint32_t r) {
             if (r < left) {
-                row.g = load8(from, c0, a.cols, WIDE ? 8u : a.grain_y);
+                if constexpr (WIDE) row.g.v = __ldcs(reinterpret_cast<const uint4*>(from + c0));
+                else row.g = load8(from, c0, a.cols, a.grain_y);
                 if constexpr (ACT != SC_ACT_NONE) {
-                    row.k = load_q8(qr, c0, a.cols, WIDE ? 8u : a.grain_q);
+                    if constexpr (WIDE) row.k = __ldcs(reinterpret_cast<const uint2*>(qr + c0));
+                    else row.k = load_q8(qr, c0, a.cols, a.grain_q);
                     row.sb = *sr;
                 }
             }
@@ -498,7 +501,10 @@ __global__ void __launch_bounds__(CKPT_THREADS, 4) activation_grad_kernel(const 
                     if constexpr (ACT != SC_ACT_NONE) v[i] = v[i] * activation_slope<ACT>(z[i]);
                     sum[i] = sum[i] + v[i];
                 }
-                if (dz) store8(to, c0, a.cols, WIDE ? 8u : a.grain_z, v);
+                if (dz) {
+                    if constexpr (WIDE) *reinterpret_cast<uint4*>(to + c0) = packed8<T>(v);
+                    else store8(to, c0, a.cols, a.grain_z, v);
+                }
             }
             to += step_z;
         };

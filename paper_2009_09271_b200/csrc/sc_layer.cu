@@ -466,7 +466,7 @@ int sc_activation_grad(sc_ctx* ctx, int type, int act, const void* dy, size_t ld
     a.grain_y = grain_of(dy, rows > 1 ? lddy : 0, 2, 8);
     a.grain_z = grain_of(dz, rows > 1 ? lddz : 0, 2, 8);
     a.grain_q = grain_of(q, rows > 1 ? cols : 0, 1, 8);
-    const bool wide = a.grain_y == 8 && a.grain_z == 8 && (!kept || a.grain_q == 8);
+    const bool wide = cols % 8 == 0 && a.grain_y == 8 && a.grain_z == 8 && (!kept || a.grain_q == 8);
     float* partial = reinterpret_cast<float*>(ctx->d_layer ? ctx->d_layer + TICKET_BYTES : nullptr);
     uint32_t* tickets = reinterpret_cast<uint32_t*>(ctx->d_layer);
     const dim3 grid(p.strips, p.runs);

@@ -524,7 +524,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
         const uint32_t e = warp - 4, quarter = warp & 3u, half = e >> 2;
         const uint32_t stage_addr = staging + e * 4096;
         const uint32_t from = tmem + ((quarter * 32) << 16) + half * (BN / 2);
-        uint32_t acc = 0, acc_phase = 0;
+        uint32_t acc = 0, acc_phase = 0, turn = 0;
         bool ok = true;
         for (uint32_t w = first; w < work && ok; w += step) {
             const uint32_t split = w / a.tiles;
@@ -574,11 +574,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                         __syncwarp();
                         if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_rank(tempty + 8 * acc, 0) : tempty + 8 * acc);
                     }
-                    if (a.rows_form)
+                    if (a.rows_form) {
                         with_activation(ep.act, [&](auto act) {
-                            block_rows<T, MODE, decltype(act)::value>(&map_out, ep, stage_addr + (c & 32) * 64, v, row0, col0 + c, scale4);
+                            block_rows<T, MODE, decltype(act)::value>(&map_out, ep, stage_addr + turn, v, row0, col0 + c, scale4);
                         });
-                    else
+                        turn ^= 2048u;                      // the two buffers take turns from block to block, whatever the tile
+                    } else
                         block_out<T, MODE>(&map_out, a, ep, stage_addr, v, row0, col0 + c, split);
                 }
                 if ((acc ^= 1u) == 0) acc_phase ^= 1u;

@@ -458,6 +458,14 @@ def test_rows_past_32_bits(ctx):
         del store, far, out
 
 
+@pytest.mark.parametrize("M,N,K", [(5181, 264, 88), (2500, 640, 72), (20000, 64, 64)])
+def test_many_narrow_tiles_a_cta(ctx, M, N, K):
+    """Short sums over more tiles than CTAs: the accumulators, the output buffers and the copies from them all take turns."""
+    for _ in range(3):
+        check_linear(ctx, torch.bfloat16, "relu", M, N, K, True, False, True)
+        check_input_grad(ctx, torch.float16, "silu", M, K, N, True)
+
+
 def test_tokens_and_tiles_agree_at_the_border(ctx):
     """One to four tokens take the kernel without tiles, five the tensor tiles: the same sums within their bounds."""
     for M in (1, 2, 3, 4, 5):
