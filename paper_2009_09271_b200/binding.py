@@ -178,6 +178,8 @@ def _matrix(t: torch.Tensor, rows: int, cols: int, dtype, name: str) -> int:
 
 
 def _vector(t: torch.Tensor, n: int, dtype, name: str) -> None:
+    if t.dtype is dtype and t.is_cuda and t.numel() == n and t.is_contiguous():
+        return
     _want(t, dtype, name)
     if t.numel() != n:
         raise ValueError(f"{name}: expected {n} elements, got {t.numel()}")

@@ -602,8 +602,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
 // With one to four tokens the weights' bytes are everything, and four multiply-adds a weight still fit beside their loads.
 // A warp owns four rows of W and walks its share of the reduction, 16 bytes a lane and row; WK warps split a row, WN warps
 // sit side by side, and the last step joins them in shared memory.  WN = 8 puts 32 outputs, a checkpoint group, in one CTA.
-// 1 x 4096 x 4096 bf16 takes 8.6 us with W from HBM (33.6 MB, 3.9 TB/s); the tiles took 15.5 + 4.7 us.  Five tokens take the
-// tiles: 8 x 4096 x 4096 in 10.6 us there, 4 tokens 12.6 us here with cold caches.
+// 1 x 4096 x 4096 bf16 takes 7.8 us with W from HBM (33.6 MB, 4.3 TB/s), 1 x 16384 x 4096 24.7 us (5.4 TB/s), 1 x 1024 x 1024 2.0 us:
+// bound by the weights' bytes, from three tokens on by the registers that limit the loads in flight.
 template <typename T, int TOKENS, int WN, int WK, bool WIDE>
 __global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* __restrict__ x, uint64_t ldx, const T* __restrict__ w, uint64_t ldw,
                                                                       uint32_t K, uint32_t grain_x, uint32_t grain_w, Epilogue ep) {

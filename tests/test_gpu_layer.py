@@ -467,9 +467,10 @@ def test_many_narrow_tiles_a_cta(ctx, M, N, K):
 
 
 def test_tokens_and_tiles_agree_at_the_border(ctx):
-    """One to four tokens take the kernel without tiles, five the tensor tiles: the same sums within their bounds."""
+    """One or two tokens, and four of short calls, take the kernel without tiles, five the tensor tiles: the same sums within their
+    bounds."""
     for M in (1, 2, 3, 4, 5):
-        for N, K in ((1000, 8), (33, 5000), (4096, 264)):
+        for N, K in ((1000, 8), (33, 5000), (4096, 264), (4096, 2056)):
             check_linear(ctx, torch.bfloat16, "gelu_tanh", M, N, K, True, True, True)
             check_linear(ctx, torch.float16, "relu", M, N, K, False, False, False, 1, 1)
 
