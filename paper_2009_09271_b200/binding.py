@@ -228,6 +228,23 @@ def sc_aggregate_static(W: int, vals, idx, k: int, n: int, out, stream=None) -> 
         raise SparseCommError(code, f"sc_aggregate_static (limits: W <= {STATIC_MAX_W}, n <= {STATIC_MAX_N})")
 
 
+_LAYER_CALLS = ("sc_checkpoint_pack", "sc_checkpoint_unpack", "sc_activation_grad", "sc_linear", "sc_linear_grad_input", "sc_linear_grad_weight")
+_calls = None
+
+
+def _layer_calls(lib):
+    """The layer operators' entry points: from the compiled caller where it was built, else through ctypes (same arguments)."""
+    global _calls
+    if _calls is None:
+        try:
+            from . import _sc_calls
+            _sc_calls.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _LAYER_CALLS))
+            _calls = _sc_calls
+        except ImportError:
+            _calls = lib
+    return _calls
+
+
 class Context:
     """Owns an sc_ctx (scratch memory on the current CUDA device)."""
 
@@ -240,11 +257,12 @@ class Context:
         self._lib = lib
         self._h = ctypes.c_void_p()
         _check(lib.sc_create(ctypes.byref(self._h), max_n, max_W, max_segments), "sc_create")
+        self._layer, self._handle = _layer_calls(lib), self._h.value
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h:
             self._lib.sc_destroy(self._h)
-            self._h = None
+            self._h = self._handle = None
 
     def __del__(self):
         try:
@@ -389,7 +407,7 @@ class Context:
         rows, cols = x.shape
         ldx = _matrix(x, rows, cols, x.dtype, "x")
         _kept(q, scales, rows, cols)
-        _check(self._lib.sc_checkpoint_pack(self._h, kind, _ptr(x), ldx, rows, cols, _ptr(q), _ptr(scales), _stream(stream)),
+        _check(self._layer.sc_checkpoint_pack(self._handle, kind, _ptr(x), ldx, rows, cols, _ptr(q), _ptr(scales), _stream(stream)),
                "sc_checkpoint_pack")
 
     def sc_checkpoint_unpack(self, q, scales, out, stream=None) -> None:
@@ -398,7 +416,7 @@ class Context:
         rows, cols = out.shape
         ldo = _matrix(out, rows, cols, out.dtype, "out")
         _kept(q, scales, rows, cols)
-        _check(self._lib.sc_checkpoint_unpack(self._h, kind, _ptr(q), _ptr(scales), rows, cols, _ptr(out), ldo, _stream(stream)),
+        _check(self._layer.sc_checkpoint_unpack(self._handle, kind, _ptr(q), _ptr(scales), rows, cols, _ptr(out), ldo, _stream(stream)),
                "sc_checkpoint_unpack")
 
     def sc_activation_grad(self, act: int, dy, q, scales, dz, db=None, accumulate: bool = False, stream=None) -> None:
@@ -412,7 +430,7 @@ class Context:
         lddz = cols if dz is None else _matrix(dz, rows, cols, dy.dtype, "dz")
         if db is not None:
             _vector(db, cols, torch.float32, "db")
-        _check(self._lib.sc_activation_grad(self._h, kind, act, _ptr(dy), lddy, _ptr(q), _ptr(scales), rows, cols, _ptr(dz), lddz,
+        _check(self._layer.sc_activation_grad(self._handle, kind, act, _ptr(dy), lddy, _ptr(q), _ptr(scales), rows, cols, _ptr(dz), lddz,
                                             _ptr(db), 1 if accumulate else 0, _stream(stream)), "sc_activation_grad")
 
     def sc_linear(self, act: int, x, w, y, bias=None, residual=None, q=None, scales=None, stream=None) -> None:
@@ -430,7 +448,7 @@ class Context:
         ldr = N if residual is None else _matrix(residual, M, N, x.dtype, "residual")
         if q is not None or scales is not None:
             _kept(q, scales, M, N)
-        _check(self._lib.sc_linear(self._h, kind, act, _ptr(x), ldx, _ptr(w), ldw, _ptr(bias), _ptr(residual), ldr, M, N, K,
+        _check(self._layer.sc_linear(self._handle, kind, act, _ptr(x), ldx, _ptr(w), ldw, _ptr(bias), _ptr(residual), ldr, M, N, K,
                                    _ptr(y), ldy, _ptr(q), _ptr(scales), _stream(stream)), "sc_linear")
 
     def sc_linear_grad_input(self, dz, w, dx, residual=None, act: int = SC_ACT_NONE, q=None, scales=None, stream=None) -> None:
@@ -446,7 +464,7 @@ class Context:
         ldr = K if residual is None else _matrix(residual, M, K, dz.dtype, "residual")
         if act != SC_ACT_NONE:
             _kept(q, scales, M, K)
-        _check(self._lib.sc_linear_grad_input(self._h, kind, act, _ptr(dz), lddz, _ptr(w), ldw, _ptr(residual), ldr, _ptr(q), _ptr(scales),
+        _check(self._layer.sc_linear_grad_input(self._handle, kind, act, _ptr(dz), lddz, _ptr(w), ldw, _ptr(residual), ldr, _ptr(q), _ptr(scales),
                                               M, N, K, _ptr(dx), lddx, _stream(stream)), "sc_linear_grad_input")
 
     def sc_linear_grad_weight(self, dz, dw, x=None, q=None, scales=None, accumulate: bool = False, stream=None) -> None:
@@ -465,5 +483,5 @@ class Context:
             ldx = _matrix(x, M, K, dz.dtype, "x")
         else:
             _kept(q, scales, M, K)
-        _check(self._lib.sc_linear_grad_weight(self._h, kind, _ptr(dz), lddz, _ptr(x), ldx, _ptr(q), _ptr(scales), M, N, K,
+        _check(self._layer.sc_linear_grad_weight(self._handle, kind, _ptr(dz), lddz, _ptr(x), ldx, _ptr(q), _ptr(scales), M, N, K,
                                                _ptr(dw), lddw, 1 if accumulate else 0, _stream(stream)), "sc_linear_grad_weight")

@@ -5,17 +5,21 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparsecomm.so")
 SOURCES = ["sc_api.cu", "sc_layer.cu"]
+# the layer operators' calls without ctypes; the binding does without where Python's headers are not installed
+CALLS_SOURCE = os.path.join(CSRC, "sc_calls.c")
+CALLS = os.path.join(HERE, "_sc_calls" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
 
 def _dependencies():
     """Every file under csrc/ plus the public header."""
-    deps = [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith((".cu", ".cuh", ".h"))]
+    deps = [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith((".cu", ".cuh", ".h", ".c"))]
     deps.append(os.path.join(HERE, "..", "include", "sparsecomm.h"))
     deps.append(os.path.abspath(__file__))
     return deps
@@ -37,8 +41,16 @@ def _nvcc() -> str:
     raise RuntimeError("nvcc not found: the CUDA library cannot be built")
 
 
+def _python_headers() -> str:
+    return sysconfig.get_paths()["include"]
+
+
+def _calls_wanted() -> bool:
+    return os.path.exists(os.path.join(_python_headers(), "Python.h")) and (shutil.which("gcc") or shutil.which("cc")) is not None
+
+
 def needs_build() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or (_calls_wanted() and not os.path.exists(CALLS)):
         return True
     t = os.path.getmtime(LIB)
     return any(os.path.getmtime(d) > t for d in _dependencies())
@@ -60,6 +72,11 @@ def build(force: bool = False, verbose: bool = False) -> str:
             link = subprocess.run(flags + ["-shared", "-o", LIB] + objects, capture_output=True, text=True)
             said.append(link.stdout + link.stderr)
             failed = link.returncode != 0
+        if not failed and _calls_wanted():
+            made = subprocess.run([shutil.which("gcc") or shutil.which("cc"), "-O2", "-shared", "-fPIC", "-I", _python_headers(), "-o", CALLS, CALLS_SOURCE],
+                                  capture_output=True, text=True)
+            said.append(made.stdout + made.stderr)
+            failed = made.returncode != 0
     if failed or verbose:
         sys.stderr.write("".join(said))
     if failed:

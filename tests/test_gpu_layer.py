@@ -531,6 +531,15 @@ def test_product_wait_runs_out_and_the_context_stays_usable():
     own.close()
 
 
+def test_a_closed_context_is_refused():
+    own = sc.Context(max_n=1)
+    own.close()
+    x = torch.zeros(8, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(sc.SparseCommError) as e:
+        own.sc_linear(0, x, x, torch.zeros(8, 8, dtype=torch.bfloat16, device="cuda"))
+    assert e.value.code == -1
+
+
 def test_broadcast_and_transposed_inputs_are_refused(ctx):
     row = torch.zeros(1, 64, dtype=torch.bfloat16, device="cuda")
     y, w = torch.zeros(8, 32, dtype=torch.bfloat16, device="cuda"), torch.zeros(32, 64, dtype=torch.bfloat16, device="cuda")

@@ -47,3 +47,21 @@ def test_null_context_is_an_error_code():
     assert lib.sc_layer_reserve(None, 1, 1, 1) == -1
     assert lib.sc_checkpoint_pack(None, 0, None, 0, 0, 0, None, None, None) == -1
     assert lib.sc_linear_grad_weight(None, 0, None, 0, None, 0, None, None, 0, 0, 0, None, 0, 0, None) == -1
+
+
+def test_compiled_calls_agree_with_ctypes():
+    """The compiled caller and ctypes reach the same functions with the same arguments: argument errors come back alike."""
+    lib = sc.load_library()
+    calls = binding._layer_calls(lib)
+    for name, args in (("sc_checkpoint_pack", (None, 0, None, 0, 0, 0, None, None, None)),
+                       ("sc_checkpoint_unpack", (None, 0, None, None, 0, 0, None, 0, None)),
+                       ("sc_activation_grad", (None, 0, 0, None, 0, None, None, 0, 0, None, 0, None, 0, None)),
+                       ("sc_linear", (None, 0, 0, None, 0, None, 0, None, None, 0, 0, 0, 0, None, 0, None, None, None)),
+                       ("sc_linear_grad_input", (None, 0, 0, None, 0, None, 0, None, 0, None, None, 0, 0, 0, None, 0, None)),
+                       ("sc_linear_grad_weight", (None, 0, None, 0, None, 0, None, None, 0, 0, 0, None, 0, 0, None))):
+        assert getattr(calls, name)(*args) == getattr(lib, name)(*args) == -1
+        if calls is not lib:
+            with pytest.raises(TypeError):
+                getattr(calls, name)(*args[:-1])
+            with pytest.raises((TypeError, OverflowError)):
+                getattr(calls, name)(*args[:1], "0", *args[2:])
