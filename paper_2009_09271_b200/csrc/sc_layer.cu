@@ -300,12 +300,14 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
     a.a_box_rows = A_MN ? 64u : (uint32_t)std::min<uint64_t>(TC_ROWS, round8(ep.rows));
     a.part_ld = (uint32_t)p.part_ld; a.part_stride = ep.rows * p.part_ld; a.partial = partial; a.status = c->d_status;
     // partial sums are whole to the next multiple of 32 columns: a checkpoint group's maximum is taken over all of its columns
-    a.tma_out = p.splits > 1 || (MODE == PRODUCT_WEIGHT && ep.grain_out >= 4);
+    // A tile store ends on a 16-byte boundary: measured, it writes a row's last, partly covered 16 bytes whole.  Results whose
+    // rows are not a multiple of 16 bytes long leave by the kernels' own stores.
+    a.tma_out = p.splits > 1 || (MODE == PRODUCT_WEIGHT && ep.grain_out >= 4 && ep.cols % 4 == 0);
     if constexpr (MODE != PRODUCT_WEIGHT)
         // a warp's 128 columns of a 256-wide tile are four whole groups of the row
         ep.scales_by4 = MODE == PRODUCT_FORWARD && p.bn == 256 && ep.cols % 128 == 0 && aligned(ep.scales, 4);
     if constexpr (MODE != PRODUCT_WEIGHT)
-        a.rows_form = p.splits == 1 && ep.grain_out >= 8 && (!ep.residual || ep.grain_res >= 8) && (!ep.q || ep.grain_q >= 8);
+        a.rows_form = p.splits == 1 && ep.cols % 8 == 0 && ep.grain_out >= 8 && (!ep.residual || ep.grain_res >= 8) && (!ep.q || ep.grain_q >= 8);
     CUtensorMap ma, mb, mo{};
     if (a.rows_form && !rows_map(&mo, type, ep.out, ep.rows, ep.cols, ep.rows > 1 ? ep.ldo : round8(ep.cols))) return SC_ERR_CUDA;
     if (a.tma_out && !(p.splits > 1 ? out_map(&mo, partial, ep.rows, p.part_ld, p.part_ld, p.splits, a.part_stride)

@@ -499,6 +499,41 @@ def test_weight_gradient_passes_nan_of_a_checkpoint(ctx):
 
 @pytest.mark.parametrize("cols", [1, 2, 4, 6, 12, 1002, 1004, 999])
 @pytest.mark.parametrize("extra,offset", [(0, 0), (2, 2), (4, 4), (1, 0), (7, 8), (8, 4)])
+def test_nothing_is_written_between_or_behind_rows(ctx, cols, extra, offset):
+    """Outputs inside a larger buffer: what lies between their rows, and behind the last, stays as it was."""
+    for rows in (1, 5, 150):
+        for dtype in TYPES:
+            g = rng(rows + cols)
+            x, w = normal(g, rows, 72).to(dtype), normal(g, cols, 72).to(dtype)
+            dz, v = normal(g, rows, 40).to(dtype), normal(g, 40, cols).to(dtype)
+            q, scales, _ = kept_of(g, rows, cols)
+
+            def guarded(call, t=dtype):
+                ld = cols + extra
+                store = torch.full((offset + rows * ld + 64,), 3.0, device="cuda").to(t)
+                call(store[offset:offset + rows * ld].view(rows, ld)[:, :cols])
+                store[offset:offset + rows * ld].view(rows, ld)[:, :cols] = 3
+                assert bool((store == 3).all())
+
+            guarded(lambda out: ctx.sc_linear(sc.SC_ACT_GELU, x, w, out, residual=out))
+            guarded(lambda out: ctx.sc_linear_grad_input(dz, v, out))
+            guarded(lambda out: ctx.sc_checkpoint_unpack(q, scales, out))
+            guarded(lambda out: ctx.sc_activation_grad(sc.SC_ACT_SILU, normal(g, rows, cols).to(dtype), q, scales, out))
+            for tokens in (6, 40, 700):
+                a, b = normal(g, tokens, rows).to(dtype), normal(g, tokens, cols).to(dtype)
+                guarded(lambda out: ctx.sc_linear_grad_weight(a, out, x=b), torch.float32)
+                guarded(lambda out: ctx.sc_linear_grad_weight(a, out, x=b, accumulate=True), torch.float32)
+            kept = torch.full((rows * cols + 64,), 9, dtype=torch.int8, device="cuda")
+            marks = torch.full((rows * -(-cols // GROUP) + 64,), 9, dtype=torch.uint8, device="cuda")
+            kq, ks = kept[:rows * cols].view(rows, cols), marks[:rows * -(-cols // GROUP)].view(rows, -1)
+            y = torch.empty(rows, cols, dtype=dtype, device="cuda")
+            for call in (lambda: ctx.sc_linear(sc.SC_ACT_RELU, x, w, y, q=kq, scales=ks), lambda: ctx.sc_checkpoint_pack(y, kq, ks)):
+                call()
+                assert bool((kept[rows * cols:] == 9).all()) and bool((marks[rows * -(-cols // GROUP):] == 9).all())
+
+
+@pytest.mark.parametrize("cols", [1, 2, 4, 6, 12, 1002, 1004, 999])
+@pytest.mark.parametrize("extra,offset", [(0, 0), (2, 2), (4, 4), (1, 0), (7, 8), (8, 4)])
 def test_every_alignment_of_rows(ctx, cols, extra, offset):
     """Rows aligned to 2, 4, 8 and 16 bytes, dense or apart, in every elementwise operator and both products' epilogues."""
     rows = 37
