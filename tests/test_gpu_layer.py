@@ -497,6 +497,44 @@ def test_weight_gradient_passes_nan_of_a_checkpoint(ctx):
         assert bool(torch.isnan(dw[:, bad]).all()) and bool((dw[:, ~bad] == M).all())
 
 
+@pytest.mark.parametrize("length,ld", [(35, 40), (999, 1000), (1002, 1008), (65, 128), (130, 136), (37, 37)])
+def test_nothing_between_input_rows_is_read(ctx, length, ld):
+    """NaN between the rows of every input leaves the outputs alone."""
+    for dtype in TYPES:
+        def spaced(t):
+            store = torch.full((t.shape[0], ld), float("nan"), dtype=dtype, device="cuda")
+            store[:, :length] = t
+            return store[:, :length]
+
+        g = rng(length)
+        for rows in (3, 150):
+            a, b = normal(g, rows, length).to(dtype), normal(g, 72, length).to(dtype)
+            y, want = torch.empty(rows, 72, dtype=dtype, device="cuda"), torch.empty(rows, 72, dtype=dtype, device="cuda")
+            ctx.sc_linear(sc.SC_ACT_NONE, spaced(a), spaced(b), y)
+            ctx.sc_linear(sc.SC_ACT_NONE, a, b, want)
+            assert bool(torch.isfinite(y).all())
+            assert_close(y, want.double(), product_slack(a, b.t(), length), dtype, "y")
+            dx, wide = torch.empty(rows, length, dtype=dtype, device="cuda"), torch.empty(rows, length, dtype=dtype, device="cuda")
+            ctx.sc_linear_grad_input(want, spaced(b), dx, residual=spaced(a))
+            ctx.sc_linear_grad_input(want, b, wide, residual=a)
+            assert bool(torch.isfinite(dx).all())
+            assert_close(dx, wide.double(), product_slack(want, b, 72), dtype, "dx")
+            dw, dense = torch.empty(length, length, device="cuda"), torch.empty(length, length, device="cuda")
+            ctx.sc_linear_grad_weight(spaced(a), dw, x=spaced(a))
+            ctx.sc_linear_grad_weight(a, dense, x=a)
+            assert bool(torch.isfinite(dw).all())
+            assert_close(dw, dense.double(), product_slack(a.t(), a, rows), torch.float32, "dw")
+            q, scales = sc.checkpoint_buffers(rows, length)
+            q2, scales2 = sc.checkpoint_buffers(rows, length)
+            ctx.sc_checkpoint_pack(spaced(a), q, scales)
+            ctx.sc_checkpoint_pack(a, q2, scales2)
+            assert torch.equal(q, q2) and torch.equal(scales, scales2)
+            dz, db, db2 = torch.empty_like(a), torch.empty(length, device="cuda"), torch.empty(length, device="cuda")
+            ctx.sc_activation_grad(sc.SC_ACT_GELU, spaced(a), q, scales, dz, db)
+            ctx.sc_activation_grad(sc.SC_ACT_GELU, a, q, scales, None, db2)
+            assert bool(torch.isfinite(dz).all()) and torch.equal(db, db2)
+
+
 @pytest.mark.parametrize("cols", [1, 2, 4, 6, 12, 1002, 1004, 999])
 @pytest.mark.parametrize("extra,offset", [(0, 0), (2, 2), (4, 4), (1, 0), (7, 8), (8, 4)])
 def test_nothing_is_written_between_or_behind_rows(ctx, cols, extra, offset):
