@@ -33,7 +33,6 @@ int check_matrix(const void* p, size_t ld, size_t rows, size_t cols, size_t elem
 
 // The layer operators' scratch: 64 KB of tickets, zero between calls, then `bytes` of workspace.
 constexpr size_t TICKET_BYTES = 65536;
-constexpr uint32_t MAX_TICKETS = TICKET_BYTES / sizeof(uint32_t);
 
 int layer_scratch(sc_ctx* c, size_t bytes, cudaStream_t st) {
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
@@ -142,7 +141,8 @@ void launch_unpack(sc_ctx* c, const uint8_t* q, const uint8_t* scales, size_t ro
 
 struct GradPlan { uint32_t strips, runs, run_rows; size_t bytes; };
 
-// Runs of rows: enough CTAs to fill the GPU (about eight per SM), none of fewer than 32 rows.
+// Runs of rows: enough CTAs to fill the GPU (about eight per SM), none of fewer than 32 rows.  A strip has a ticket where it has more
+// than one run, which takes at most four strips per SM: far fewer than there are tickets.
 GradPlan grad_plan(const sc_ctx* c, size_t rows, size_t cols) {
     GradPlan p{};
     p.strips = (uint32_t)ceil_div(cols, GRAD_COLS);
@@ -455,7 +455,6 @@ int sc_activation_grad(sc_ctx* ctx, int type, int act, const void* dy, size_t ld
     if (cols == 0) return SC_OK;
     const bool kept = act != SC_ACT_NONE;
     if (kept && rows && (!q || !scales)) return SC_ERR_INVALID;
-    if (db && ceil_div(cols, GRAD_COLS) > MAX_TICKETS) return SC_ERR_RANGE;
     DeviceGuard guard(ctx->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (rows == 0) {
