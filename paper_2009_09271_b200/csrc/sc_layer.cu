@@ -31,7 +31,7 @@ int check_matrix(const void* p, size_t ld, size_t rows, size_t cols, size_t elem
     return p && aligned(p, elem) ? SC_OK : SC_ERR_INVALID;
 }
 
-// The layer operators' scratch: 64 KB of tickets, zero between calls, then `bytes` of workspace.
+// The layer operators' scratch: 64 KB of tickets, zero between calls, then `bytes` of workspace.  Only calls that use it ask for it.
 constexpr size_t TICKET_BYTES = 65536;
 
 int layer_scratch(sc_ctx* c, size_t bytes, cudaStream_t st) {
@@ -272,8 +272,9 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
     const uint64_t tiles = ceil_div(ep.rows, TC_ROWS * p.cg) * ceil_div(ep.cols, p.bn);
     if (tiles * p.splits > 0x7FFFFFFFull) return SC_ERR_RANGE;
     const size_t copy_a = tma_ready(A) ? 0 : layout_bytes(A.rows, A.cols), copy_b = tma_ready(B) ? 0 : layout_bytes(B.rows, B.cols);
-    if (const int rc = layer_scratch(c, used + p.bytes + copy_a + copy_b, st)) return rc;
-    unsigned char* at = c->d_layer ? c->d_layer + TICKET_BYTES + used : nullptr;
+    const size_t need = used + p.bytes + copy_a + copy_b;
+    if (need) if (const int rc = layer_scratch(c, need, st)) return rc;
+    unsigned char* at = need ? c->d_layer + TICKET_BYTES + used : nullptr;
     float* partial = reinterpret_cast<float*>(at);
     at += p.bytes;
     LayoutArgs copies[2];
@@ -462,7 +463,7 @@ int sc_activation_grad(sc_ctx* ctx, int type, int act, const void* dy, size_t ld
         return SC_OK;
     }
     const GradPlan p = grad_plan(ctx, rows, cols);
-    if (db) if (const int rc = layer_scratch(ctx, p.bytes, st)) return rc;
+    if (db && p.runs > 1) if (const int rc = layer_scratch(ctx, p.bytes, st)) return rc;
     GradArgs a{};
     a.rows = rows; a.lddy = lddy; a.lddz = lddz; a.cols = (uint32_t)cols; a.groups = (uint32_t)ckpt_groups(cols);
     a.runs = p.runs; a.run_rows = p.run_rows; a.accumulate = accumulate ? 1u : 0u;

@@ -25,3 +25,46 @@ def test_column_sums_of_very_wide_rows(rows):
     assert bool(((db.double() - want).abs() <= (rows + 2) * 2.0 ** -23 * dy.double().abs().sum(0)).all())
     assert own.sc_sync_status() == 0
     own.close()
+
+
+def test_calls_without_workspace_are_captured_on_a_new_context():
+    """Aligned rows, one part, one run of rows: nothing to allocate, so nothing to refuse while a stream is captured."""
+    M, N, K = 200, 256, 64
+    x, w, dz, v = normal(2, M, K), normal(3, N, K), normal(4, M, K), normal(5, K, N)
+    few = normal(6, 64, N), normal(7, 64, K)
+    outs = [torch.empty(M, N, dtype=BF16, device="cuda"), torch.empty(M, N, dtype=BF16, device="cuda"), torch.empty(N, K, device="cuda"),
+            torch.empty(N, device="cuda")]
+
+    def step(c):
+        c.sc_linear(sc.SC_ACT_SILU, x, w, outs[0])
+        c.sc_linear_grad_input(dz, v, outs[1])
+        c.sc_linear_grad_weight(few[0], outs[2], x=few[1])
+        c.sc_activation_grad(sc.SC_ACT_NONE, few[0][:32], None, None, None, outs[3])
+
+    other = sc.Context(max_n=1)
+    other.sc_layer_reserve(M, N, K)
+    step(other)
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+    for t in outs:
+        t.zero_()
+    own = sc.Context(max_n=1)
+    held = own.scratch_bytes
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    refused = None
+    with torch.cuda.graph(graph):
+        try:
+            step(own)
+        except sc.SparseCommError as e:
+            refused = e.code
+    assert refused is None
+    assert own.scratch_bytes == held
+    graph.replay()
+    torch.cuda.synchronize()
+    for got, ref in zip(outs, want):
+        assert torch.equal(got, ref)
+    assert own.sc_sync_status() == 0
+    del graph
+    own.close()
+    other.close()
