@@ -408,7 +408,12 @@ int sc_layer_reserve(sc_ctx* ctx, size_t M, size_t N, size_t K) {
     DeviceGuard guard(ctx->device);
     // the operands' copies (x^ always, the others where rows are not 16-byte aligned) and partial sums; the bias gradient's
     // partial rows are far below the latter
-    const size_t bytes = PARTIAL_CAP + layout_bytes(M, K) + layout_bytes(N, K) + layout_bytes(M, N);
+    const size_t copies[3] = {layout_bytes(M, K), layout_bytes(N, K), layout_bytes(M, N)};
+    size_t bytes = PARTIAL_CAP;
+    for (const size_t n : copies) {
+        if (n > SIZE_MAX / 4) return SC_ERR_WORKSPACE;                    // a sum of three would wrap
+        bytes += n;
+    }
     return layer_scratch(ctx, bytes, nullptr);
 }
 

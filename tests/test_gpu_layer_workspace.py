@@ -68,3 +68,15 @@ def test_calls_without_workspace_are_captured_on_a_new_context():
     del graph
     own.close()
     other.close()
+
+
+def test_a_reservation_beyond_64_bits_is_refused():
+    """Three copies of matrices of this size add up to 2^64 bytes and a little more."""
+    M, N, K = 1753412483, 1753409644, 1753417036
+    total = (64 << 20) + sum(-(-rows * -(-cols // 8) * 16 // 256) * 256 for rows, cols in ((M, K), (N, K), (M, N)))
+    assert 2 ** 64 <= total < 2 ** 64 + 2 ** 32
+    own = sc.Context(max_n=1)
+    held = own.scratch_bytes
+    code = sc.load_library().sc_layer_reserve(own._h, M, N, K)
+    assert code == -3 and own.scratch_bytes == held
+    own.close()
