@@ -97,12 +97,12 @@ template <typename T>
 __device__ __forceinline__ Raw8<T> load8(const T* row, uint32_t c0, uint32_t cols, uint32_t grain) {
     Raw8<T> r{};
     if constexpr (sizeof(T) == 2) {
-        if (grain >= 8 && c0 + 8 <= cols) r.v = __ldcs(reinterpret_cast<const uint4*>(row + c0));
+        if (grain >= 8 && c0 + 8 <= cols) r.v = load_stream16(row + c0);
         else if (c0 < cols) r.v = load_narrow(reinterpret_cast<const uint16_t*>(row + c0), cols - c0, grain);
     } else {
         if (grain >= 4 && c0 + 8 <= cols) {
-            r.v = __ldcs(reinterpret_cast<const uint4*>(row + c0));
-            r.w = __ldcs(reinterpret_cast<const uint4*>(row + c0) + 1);
+            r.v = load_stream16(row + c0);
+            r.w = load_stream16(reinterpret_cast<const uint4*>(row + c0) + 1);
         } else {
             uint32_t e[8];
 #pragma unroll
@@ -164,8 +164,8 @@ __device__ __forceinline__ void store_q8(uint8_t* dst, uint32_t c0, uint32_t col
 // 16384 x 8192 bf16 in 68-71 us, 5.8-6.0 TB/s (0.89-0.94 of the measured copy rate); items of half a group and 32-byte accesses
 // brought it there from 0.65 (8 elements a thread: twice the address arithmetic, 16-byte halves of sectors).
 template <typename T>
-__global__ void __launch_bounds__(CKPT_THREADS, sizeof(T) == 2 ? 4 : 3) checkpoint_pack_kernel(const T* __restrict__ x, uint64_t ldx, ItemWalk w,
-                                                                       uint8_t* __restrict__ q, uint8_t* __restrict__ scales) {
+__global__ void __launch_bounds__(CKPT_THREADS, sizeof(T) == 2 ? 4 : 3) checkpoint_pack_kernel(const T* x, uint64_t ldx, ItemWalk w,
+                                                                       uint8_t* q, uint8_t* scales) {
     constexpr int UNROLL = sizeof(T) == 2 ? CKPT_UNROLL : 2;
     wait_for_predecessor();
     release_successor();
@@ -265,14 +265,14 @@ __device__ __forceinline__ void store8(T* row, uint32_t c0, uint32_t cols, uint3
 }
 
 __device__ __forceinline__ uint2 load_q8(const uint8_t* row, uint32_t c0, uint32_t cols, uint32_t grain) {
-    if (grain >= 8 && c0 + 8 <= cols) return __ldcs(reinterpret_cast<const uint2*>(row + c0));
+    if (grain >= 8 && c0 + 8 <= cols) return load_stream8(row + c0);
     return c0 < cols ? load_q_narrow(row + c0, cols - c0, grain) : make_uint2(0u, 0u);
 }
 
 // The reverse, bound by HBM in the same way: 16384 x 8192 bf16 in 71 us, 5.75 TB/s (0.89).
 template <typename T>
-__global__ void __launch_bounds__(CKPT_THREADS, sizeof(T) == 2 ? 4 : 3) checkpoint_unpack_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, ItemWalk w,
-                                                                         T* __restrict__ out, uint64_t ldo) {
+__global__ void __launch_bounds__(CKPT_THREADS, sizeof(T) == 2 ? 4 : 3) checkpoint_unpack_kernel(const uint8_t* q, const uint8_t* scales, ItemWalk w,
+                                                                         T* out, uint64_t ldo) {
     wait_for_predecessor();
     release_successor();
     const uint64_t stride = (uint64_t)gridDim.x * CKPT_THREADS, groups = w.items >> 1;
@@ -288,7 +288,7 @@ __global__ void __launch_bounds__(CKPT_THREADS, sizeof(T) == 2 ? 4 : 3) checkpoi
                 const uint8_t* row = q + at.row * w.cols;
                 const uint32_t c0 = at.item * 16;
                 if (w.grain_q >= 16 && c0 + 16 <= w.cols) {
-                    const uint4 v = __ldcs(reinterpret_cast<const uint4*>(row + c0));
+                    const uint4 v = load_stream16(row + c0);
                     raw[u][0] = make_uint2(v.x, v.y);
                     raw[u][1] = make_uint2(v.z, v.w);
                 } else {
@@ -345,8 +345,8 @@ struct RunAt {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(CKPT_THREADS) checkpoint_pack_narrow_kernel(const T* __restrict__ x, uint64_t ldx, NarrowWalk w,
-                                                                              uint8_t* __restrict__ q, uint8_t* __restrict__ scales) {
+__global__ void __launch_bounds__(CKPT_THREADS) checkpoint_pack_narrow_kernel(const T* x, uint64_t ldx, NarrowWalk w,
+                                                                              uint8_t* q, uint8_t* scales) {
     wait_for_predecessor();
     release_successor();
     const uint32_t lane = threadIdx.x & 31u, groups = (w.cols + CKPT_GROUP - 1) / CKPT_GROUP;
@@ -395,8 +395,8 @@ __global__ void __launch_bounds__(CKPT_THREADS) checkpoint_pack_narrow_kernel(co
 }
 
 template <typename T>
-__global__ void __launch_bounds__(CKPT_THREADS) checkpoint_unpack_narrow_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, NarrowWalk w,
-                                                                                T* __restrict__ out, uint64_t ldo) {
+__global__ void __launch_bounds__(CKPT_THREADS) checkpoint_unpack_narrow_kernel(const uint8_t* q, const uint8_t* scales, NarrowWalk w,
+                                                                                T* out, uint64_t ldo) {
     wait_for_predecessor();
     release_successor();
     const uint32_t lane = threadIdx.x & 31u, groups = (w.cols + CKPT_GROUP - 1) / CKPT_GROUP;
@@ -458,9 +458,9 @@ struct GradArgs {
 
 // WIDE: a multiple of 8 columns, rows that take 16-byte accesses and a q that takes 8-byte ones.
 template <typename T, int ACT, bool WIDE>
-__global__ void __launch_bounds__(CKPT_THREADS, 4) activation_grad_kernel(const T* dy, const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales,
-                                                                          GradArgs a, T* dz, float* __restrict__ partial,
-                                                                          uint32_t* __restrict__ tickets, float* __restrict__ db) {
+__global__ void __launch_bounds__(CKPT_THREADS, 4) activation_grad_kernel(const T* dy, const uint8_t* q, const uint8_t* scales,
+                                                                          GradArgs a, T* dz, float* partial,
+                                                                          uint32_t* tickets, float* db) {
     wait_for_predecessor();
     release_successor();
     const uint32_t tx = threadIdx.x & 31u, ty = threadIdx.x >> 5;
@@ -479,10 +479,10 @@ __global__ void __launch_bounds__(CKPT_THREADS, 4) activation_grad_kernel(const 
         struct Row { Raw8<T> g; uint2 k; uint32_t sb; };
         const auto fetch = [&](Row& row, uint32_t r) {
             if (r < left) {
-                if constexpr (WIDE) row.g.v = __ldcs(reinterpret_cast<const uint4*>(from + c0));
+                if constexpr (WIDE) row.g.v = load_stream16(from + c0);
                 else row.g = load8(from, c0, a.cols, a.grain_y);
                 if constexpr (ACT != SC_ACT_NONE) {
-                    if constexpr (WIDE) row.k = __ldcs(reinterpret_cast<const uint2*>(qr + c0));
+                    if constexpr (WIDE) row.k = load_stream8(qr + c0);
                     else row.k = load_q8(qr, c0, a.cols, a.grain_q);
                     row.sb = *sr;
                 }
@@ -537,7 +537,7 @@ __global__ void __launch_bounds__(CKPT_THREADS, 4) activation_grad_kernel(const 
         __threadfence();
         total = 0.0f;
         if (c < a.cols)
-            for (uint32_t j = 0; j < a.runs; ++j) total += __ldcg(&partial[(uint64_t)j * a.cols + c]);
+            for (uint32_t j = 0; j < a.runs; ++j) total += load_l2(&partial[(uint64_t)j * a.cols + c]);
         if (threadIdx.x == 0) tickets[blockIdx.x] = 0u;               // zero again for the next call
     }
     if (c < a.cols) db[c] = a.accumulate ? db[c] + total : total;

@@ -19,6 +19,30 @@ __host__ __device__ inline uint64_t ckpt_groups(uint64_t cols) { return (cols + 
 // kernel that is launched that way waits, so a kernel's end implies the end of all before it.
 __device__ __forceinline__ void wait_for_predecessor() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void release_successor() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+// What a predecessor may have written is therefore not read-only for the kernel's whole life: no pointer of these kernels is declared
+// __restrict__, which would allow loads ahead of the wait and through the path for constant data, and loads with a cache hint are
+// the ones below, whose volatile statements keep their place behind the wait and behind fences.
+__device__ __forceinline__ uint4 load_stream16(const void* p) {
+    uint4 r;
+    asm volatile("ld.global.cs.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
+}
+__device__ __forceinline__ uint2 load_stream8(const void* p) {
+    uint2 r;
+    asm volatile("ld.global.cs.v2.b32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
+    return r;
+}
+// From L2, where other CTAs of the same kernel, or the one before it, have left their sums.
+__device__ __forceinline__ float load_l2(const float* p) {
+    float r;
+    asm volatile("ld.global.cg.f32 %0, [%1];" : "=f"(r) : "l"(p) : "memory");
+    return r;
+}
+__device__ __forceinline__ float4 load_l2(const float4* p) {
+    float4 r;
+    asm volatile("ld.global.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(r.x), "=f"(r.y), "=f"(r.z), "=f"(r.w) : "l"(p));
+    return r;
+}
 
 // ---------------------------------------------------------------------------
 // types

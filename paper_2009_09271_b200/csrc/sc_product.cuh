@@ -373,7 +373,7 @@ __device__ __forceinline__ void block_rows(const CUtensorMap* map_out, const Epi
             const Scale s = slope_scale(ep.scales[row * ep.groups + (col0 >> 5)]);
             uint2 k[4];
             if (whole && ep.grain_q >= 16) {
-                const uint4 a = __ldcs(reinterpret_cast<const uint4*>(q + col0)), b = __ldcs(reinterpret_cast<const uint4*>(q + col0) + 1);
+                const uint4 a = load_stream16(q + col0), b = load_stream16(reinterpret_cast<const uint4*>(q + col0) + 1);
                 k[0] = make_uint2(a.x, a.y); k[1] = make_uint2(a.z, a.w); k[2] = make_uint2(b.x, b.y); k[3] = make_uint2(b.z, b.w);
             } else {
 #pragma unroll
@@ -605,7 +605,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
 // 1 x 4096 x 4096 bf16 takes 7.8 us with W from HBM (33.6 MB, 4.3 TB/s), 1 x 16384 x 4096 24.7 us (5.4 TB/s), 1 x 1024 x 1024 2.0 us:
 // bound by the weights' bytes, from three tokens on by the registers that limit the loads in flight.
 template <typename T, int TOKENS, int WN, int WK, bool WIDE>
-__global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* __restrict__ x, uint64_t ldx, const T* __restrict__ w, uint64_t ldw,
+__global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* x, uint64_t ldx, const T* w, uint64_t ldw,
                                                                       uint32_t K, uint32_t grain_x, uint32_t grain_w, Epilogue ep) {
     constexpr int ROWS = 4, COLS = ROWS * WN;
     wait_for_predecessor();
@@ -678,8 +678,8 @@ __global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* _
 // paired arithmetic wants it), one 128-byte store at a time, whatever the alignment.  4096 x 4096: 14.7 us at 4 tokens and
 // 16.4 at 8, against 18.2 on the tiles (with the checkpoint's copy); a fill of the output takes 12.3.  With 16 tokens it took 31.
 template <typename T, int TOKENS, bool KEPT>
-__global__ void __launch_bounds__(256) weight_tokens_kernel(const T* __restrict__ dz, uint64_t lddz, const T* __restrict__ x, uint64_t ldx,
-                                                            const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, uint32_t tokens, uint32_t run,
+__global__ void __launch_bounds__(256) weight_tokens_kernel(const T* dz, uint64_t lddz, const T* x, uint64_t ldx,
+                                                            const uint8_t* q, const uint8_t* scales, uint32_t tokens, uint32_t run,
                                                             Epilogue ep) {
     extern __shared__ __align__(16) float2 rows_dz[];              // [run][TOKENS]
     wait_for_predecessor();
@@ -752,7 +752,7 @@ __global__ void __launch_bounds__(256) weight_tokens_kernel(const T* __restrict_
 // Joins the parts of a split product in order and applies the epilogue; no parts at all is an empty sum.  2 to 6 us: parts are
 // few enough to be read from L2.
 template <typename T, int MODE>
-__global__ void __launch_bounds__(256) product_join_kernel(const float* __restrict__ partial, uint32_t splits, uint64_t part_stride, uint32_t part_ld,
+__global__ void __launch_bounds__(256) product_join_kernel(const float* partial, uint32_t splits, uint64_t part_stride, uint32_t part_ld,
                                                            Epilogue ep) {
     wait_for_predecessor();
     release_successor();
@@ -766,7 +766,7 @@ __global__ void __launch_bounds__(256) product_join_kernel(const float* __restri
         if (i < total && c0 < ep.cols) {
             const float4* p = reinterpret_cast<const float4*>(partial + row * part_ld + c0);
             for (uint32_t s = 0; s < splits; ++s, p += part_stride / 4) {
-                const float4 x = __ldcg(p), y = __ldcg(p + 1);
+                const float4 x = load_l2(p), y = load_l2(p + 1);
                 f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
                 f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
             }
