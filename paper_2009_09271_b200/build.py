@@ -45,12 +45,24 @@ def _python_headers() -> str:
     return sysconfig.get_paths()["include"]
 
 
+def _cc():
+    return shutil.which("gcc") or shutil.which("cc")
+
+
 def _calls_wanted() -> bool:
-    return os.path.exists(os.path.join(_python_headers(), "Python.h")) and (shutil.which("gcc") or shutil.which("cc")) is not None
+    return os.path.exists(os.path.join(_python_headers(), "Python.h")) and _cc() is not None
+
+
+def _caller_is_current() -> bool:
+    """The compiled caller is not older than its sources; it may be missing where it cannot be built."""
+    if not os.path.exists(CALLS):
+        return not _calls_wanted()
+    sources = (CALLS_SOURCE, os.path.join(HERE, "..", "include", "sparsecomm.h"))
+    return all(os.path.getmtime(CALLS) >= os.path.getmtime(d) for d in sources)
 
 
 def needs_build() -> bool:
-    if not os.path.exists(LIB) or (_calls_wanted() and not os.path.exists(CALLS)):
+    if not os.path.exists(LIB) or not _caller_is_current():
         return True
     t = os.path.getmtime(LIB)
     return any(os.path.getmtime(d) > t for d in _dependencies())
@@ -59,6 +71,10 @@ def needs_build() -> bool:
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not needs_build():
         return LIB
+    # a caller built from other declarations must not outlive a build that ends without one
+    if os.path.exists(CALLS):
+        os.remove(CALLS)
+    said, failed = [], ""
     # one nvcc per translation unit, side by side, then the link
     with tempfile.TemporaryDirectory(prefix="sparsecomm_build_") as tmp:
         objects = [os.path.join(tmp, os.path.splitext(src)[0] + ".o") for src in SOURCES]
@@ -67,20 +83,22 @@ def build(force: bool = False, verbose: bool = False) -> str:
                                  stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
                 for src, obj in zip(SOURCES, objects)]
         said = [job.communicate()[0] for job in jobs]
-        failed = any(job.returncode != 0 for job in jobs)
+        if any(job.returncode != 0 for job in jobs):
+            failed = "nvcc failed building libsparsecomm.so"
         if not failed:
             link = subprocess.run(flags + ["-shared", "-o", LIB] + objects, capture_output=True, text=True)
             said.append(link.stdout + link.stderr)
-            failed = link.returncode != 0
+            if link.returncode != 0:
+                failed = "nvcc failed linking libsparsecomm.so"
         if not failed and _calls_wanted():
-            made = subprocess.run([shutil.which("gcc") or shutil.which("cc"), "-O2", "-shared", "-fPIC", "-I", _python_headers(), "-o", CALLS, CALLS_SOURCE],
-                                  capture_output=True, text=True)
+            made = subprocess.run([_cc(), "-O2", "-shared", "-fPIC", "-I", _python_headers(), "-o", CALLS, CALLS_SOURCE], capture_output=True, text=True)
             said.append(made.stdout + made.stderr)
-            failed = made.returncode != 0
+            if made.returncode != 0:
+                failed = f"the C compiler failed building {os.path.basename(CALLS)}"
     if failed or verbose:
         sys.stderr.write("".join(said))
     if failed:
-        raise RuntimeError("nvcc failed building libsparsecomm.so")
+        raise RuntimeError(failed)
     return LIB
 
 
