@@ -242,6 +242,12 @@ enum { SC_ACT_NONE = 0, SC_ACT_RELU = 1, SC_ACT_GELU = 2 /* z Phi(z) */,
  * ahead what any layer call of at most these sizes needs.  A block that captured calls used is kept until sc_destroy. */
 int sc_layer_reserve(sc_ctx* ctx, size_t M, size_t N, size_t K);
 
+/* Instrumentation for tests: later products of this context run in tiles of rows x cols outputs (256 x 256, 128 x 256, 128 x 128 or
+ * 128 x 64), their sums cut into `parts` (1 to 64), instead of what the library chooses for the size; 0, 0, 0 restores its choice.  Products
+ * of up to 128 rows take no 256-row tiles, sums no more parts than blocks of 64 terms or 64 MB of partial sums allow, and the few
+ * tokens that are served without tiles still are.  Host-side state, no device work. */
+int sc_debug_layer_tiles(sc_ctx* ctx, int rows, int cols, int parts);
+
 /* Checkpoint of x, and the values of a checkpoint (rounded to `type` where the checkpoint was made from another). */
 int sc_checkpoint_pack(sc_ctx* ctx, int type, const void* x, size_t ldx, size_t rows, size_t cols,
                        int8_t* q, uint8_t* scales, void* stream);

@@ -28,7 +28,7 @@ EXPORTS = ["sc_create", "sc_destroy", "sc_strerror", "sc_sync_status", "sc_set_g
            "sc_topk_path_counts", "sc_topk_path_detail", "sc_debug_set_poll_limits", "sc_debug_wait_probe", "sc_profile", "sc_profile_kinds", "sc_profile_name", "sc_profile_read",
            "sc_compress", "sc_compress_batch", "sc_aggregate", "sc_aggregate_shared", "sc_aggregate_static", "sc_aggregate_apply",
            "sc_aggregate_apply_shared", "sc_step", "sc_step_apply", "sc_step_host",
-           "sc_layer_reserve", "sc_checkpoint_pack", "sc_checkpoint_unpack", "sc_activation_grad", "sc_linear", "sc_linear_grad_input",
+           "sc_layer_reserve", "sc_debug_layer_tiles", "sc_checkpoint_pack", "sc_checkpoint_unpack", "sc_activation_grad", "sc_linear", "sc_linear_grad_input",
            "sc_linear_grad_weight"]
 
 
@@ -108,13 +108,14 @@ def load_library() -> ctypes.CDLL:
                                  vp, vp]
     lib.sc_step_host.restype = ci
     lib.sc_layer_reserve.argtypes = [vp, sz, sz, sz]
+    lib.sc_debug_layer_tiles.argtypes = [vp, ci, ci, ci]
     lib.sc_checkpoint_pack.argtypes = [vp, ci, vp, sz, sz, sz, vp, vp, vp]
     lib.sc_checkpoint_unpack.argtypes = [vp, ci, vp, vp, sz, sz, vp, sz, vp]
     lib.sc_activation_grad.argtypes = [vp, ci, ci, vp, sz, vp, vp, sz, sz, vp, sz, vp, ci, vp]
     lib.sc_linear.argtypes = [vp, ci, ci, vp, sz, vp, sz, vp, vp, sz, sz, sz, sz, vp, sz, vp, vp, vp]
     lib.sc_linear_grad_input.argtypes = [vp, ci, ci, vp, sz, vp, sz, vp, sz, vp, vp, sz, sz, sz, vp, sz, vp]
     lib.sc_linear_grad_weight.argtypes = [vp, ci, vp, sz, vp, sz, vp, vp, sz, sz, sz, vp, sz, ci, vp]
-    for name in ("sc_layer_reserve", "sc_checkpoint_pack", "sc_checkpoint_unpack", "sc_activation_grad", "sc_linear",
+    for name in ("sc_layer_reserve", "sc_debug_layer_tiles", "sc_checkpoint_pack", "sc_checkpoint_unpack", "sc_activation_grad", "sc_linear",
                  "sc_linear_grad_input", "sc_linear_grad_weight"):
         getattr(lib, name).restype = ci
     _lib = lib
@@ -400,6 +401,9 @@ class Context:
     def sc_layer_reserve(self, M: int, N: int, K: int) -> None:
         """Allocates ahead the workspace of layer calls of at most these sizes (before a stream capture, for instance)."""
         _check(self._lib.sc_layer_reserve(self._h, M, N, K), "sc_layer_reserve")
+
+    def sc_debug_layer_tiles(self, rows: int = 0, cols: int = 0, parts: int = 0) -> None:
+        _check(self._lib.sc_debug_layer_tiles(self._h, rows, cols, parts), "sc_debug_layer_tiles")
 
     def sc_checkpoint_pack(self, x, q, scales, stream=None) -> None:
         """q, scales <- the 8-bit checkpoint of x [rows, cols] (bfloat16, float16 or float32)."""

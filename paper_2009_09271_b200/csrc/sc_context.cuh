@@ -98,6 +98,8 @@ struct sc_ctx {
     static constexpr int LAYER_PLANS = 16;
     LayerPlan layer_plans[LAYER_PLANS] = {};     // tile shapes of the sizes seen last
     int layer_plan_next = 0;
+    int layer_force_bn = 0, layer_force_cg = 1;  // sc_debug_layer_tiles: 0, or the width and the CTAs of every tile
+    uint32_t layer_force_parts = 1;
     bool layer_captured = false;                 // a captured call used the block: growing must not free it
     static constexpr int MAX_RETIRED = 64;
     unsigned char* layer_retired[MAX_RETIRED] = {};

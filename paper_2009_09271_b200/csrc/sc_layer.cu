@@ -222,6 +222,12 @@ ProductPlan product_plan(sc_ctx* c, int mode, uint64_t rows, uint64_t cols, uint
         if (p.rows == rows && p.cols == cols && p.red == red && p.mode == mode) return p;
     ProductPlan best{rows, cols, red, mode, 256, 1, 1, (cols + 31) & ~31ull, 0};
     const uint64_t blocks = ceil_div(red, TC_STEP);
+    if (c->layer_force_bn && !(c->layer_force_cg == 2 && rows <= TC_ROWS)) {
+        const uint64_t parts = std::min<uint64_t>(c->layer_force_parts, blocks), bytes = parts > 1 ? parts * rows * best.part_ld * sizeof(float) : 0;
+        best.bn = c->layer_force_bn; best.cg = c->layer_force_cg;
+        if (bytes <= PARTIAL_CAP) { best.splits = (uint32_t)parts; best.bytes = bytes; }
+        return best;
+    }
     double best_cost = 0;
     const double box = (double)std::min<uint64_t>(rows, TC_ROWS);
     for (int shape = 0; shape < 4; ++shape) {                 // 256 x 256 by pairs, then 128 x 256, 128, 64
@@ -415,6 +421,16 @@ int sc_layer_reserve(sc_ctx* ctx, size_t M, size_t N, size_t K) {
         bytes += n;
     }
     return layer_scratch(ctx, bytes, nullptr);
+}
+
+int sc_debug_layer_tiles(sc_ctx* ctx, int rows, int cols, int parts) {
+    if (!ctx) return SC_ERR_INVALID;
+    const bool none = rows == 0 && cols == 0 && parts == 0;
+    const bool pair = rows == 256 && cols == 256, single = rows == 128 && (cols == 64 || cols == 128 || cols == 256);
+    if (!none && ((!pair && !single) || parts < 1 || parts > 64)) return SC_ERR_INVALID;
+    ctx->layer_force_bn = cols; ctx->layer_force_cg = pair ? 2 : 1; ctx->layer_force_parts = (uint32_t)parts;
+    for (ProductPlan& p : ctx->layer_plans) p = ProductPlan{};
+    return SC_OK;
 }
 
 int sc_checkpoint_pack(sc_ctx* ctx, int type, const void* x, size_t ldx, size_t rows, size_t cols, int8_t* q, uint8_t* scales, void* stream) {
