@@ -222,8 +222,10 @@ int sc_step_host(sc_ctx* ctx, int scheme, int W, const float* h_grads, float* re
  *
  * Matrices are rows of the stated length, `ld` elements apart (ld >= the row's length; any value, any base
  * aligned to its element; 16-byte aligned rows are the fast case).  Everything is computed in fp32 from the 16-bit
- * inputs and rounded once, to the type of the output.  Empty sizes are allowed: no rows or columns, nothing is
- * written; an empty sum is 0.  Sizes are below 2^31.  Unless a call says otherwise outputs alias no input.
+ * inputs and rounded once, to the type of the output.  The tensor cores add 16 products at a time to their fp32 sums and cut
+ * instead of rounding, so that a sum of n products may be up to n 2^-27 of its largest running value short (16384 of one
+ * sign: at most 1.2e-4 of the result); dW, an fp32 result, is added up with rounding every 384 products.  Empty sizes are allowed: no rows or
+ * columns, nothing is written; an empty sum is 0.  Sizes are below 2^31.  Unless a call says otherwise outputs alias no input.
  *
  * Checkpoint of a matrix [rows, cols]: q, rows * cols int8, and scales, rows * ceil(cols / 32) bytes, both dense.
  * Each run of 32 elements of a row has one scale 2^e, stored as e + 127: e is the least exponent with
