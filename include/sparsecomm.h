@@ -276,7 +276,7 @@ int sc_linear_grad_input(sc_ctx* ctx, int type, int act, const void* dz, size_t 
                          size_t M, size_t N, size_t K, void* dx, size_t lddx, void* stream);
 
 /* dW = dz^T x in fp32, rows of lddw (accumulate: added to dW, where values below 2^-126 may count as 0).  The layer's input is given once: as x, or as its
- * checkpoint (q, scales) with x NULL. */
+ * checkpoint (q, scales) with x NULL, whose values are those of sc_checkpoint_unpack to `type`. */
 int sc_linear_grad_weight(sc_ctx* ctx, int type, const void* dz, size_t lddz, const void* x, size_t ldx,
                           const int8_t* q, const uint8_t* scales, size_t M, size_t N, size_t K,
                           float* dw, size_t lddw, int accumulate, void* stream);

@@ -711,6 +711,8 @@ __global__ void __launch_bounds__(256) weight_tokens_kernel(const T* dz, uint64_
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 v[m][j] *= (float)(int8_t)k[m][j];
+                // a bf16 value whatever the checkpoint was made from; an fp16 value unless that was a type of wider range: rounded then, as by unpacking
+                if constexpr (std::is_same<T, __half>::value) v[m][j] = __half2float(__float2half_rn(v[m][j]));
                 if (k[m][j] == 0x80u) v[m][j] = __uint_as_float(0x7FFFFFFFu);
                 if (m >= (int)tokens) v[m][j] = 0.0f;
             }
