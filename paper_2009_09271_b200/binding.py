@@ -187,15 +187,18 @@ def _vector(t: torch.Tensor, n: int, dtype, name: str) -> None:
 
 
 def _kept(q, scales, rows: int, cols: int) -> None:
-    """Checks a checkpoint of a [rows, cols] matrix."""
+    """Checks a checkpoint of a [rows, cols] matrix; matrices have its shape, views of other dimensions its number of elements."""
     groups = -(-cols // CHECKPOINT_GROUP)
     if (q is not None and scales is not None and q.dtype is torch.int8 and scales.dtype is torch.uint8 and q.is_cuda and scales.is_cuda
-            and q.numel() == rows * cols and scales.numel() == rows * groups and q.is_contiguous() and scales.is_contiguous()):
+            and q.shape == (rows, cols) and scales.shape == (rows, groups) and q.is_contiguous() and scales.is_contiguous()):
         return
     if q is None or scales is None:
         raise ValueError("q and scales: a checkpoint is both or neither")
     _vector(q, rows * cols, torch.int8, "q")
     _vector(scales, rows * groups, torch.uint8, "scales")
+    for t, want, name in ((q, (rows, cols), "q"), (scales, (rows, groups), "scales")):
+        if t.dim() == 2 and t.shape != want:
+            raise ValueError(f"{name}: expected shape {want}, got {tuple(t.shape)}")
 
 
 def _layer_type(t: torch.Tensor, name: str, f32: bool = False) -> int:
