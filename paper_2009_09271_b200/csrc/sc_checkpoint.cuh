@@ -161,8 +161,8 @@ __device__ __forceinline__ void store_q8(uint8_t* dst, uint32_t c0, uint32_t col
 }
 
 // One pass: 2 (4) bytes read and 1 + 1/32 written per element; two lanes hold a group and share its maximum.  Bound by HBM:
-// 16384 x 8192 bf16 in 68-71 us, 5.8-6.0 TB/s (0.89-0.94 of the measured copy rate); items of half a group and 32-byte accesses
-// brought it there from 0.65 (8 elements a thread: twice the address arithmetic, 16-byte halves of sectors).
+// 16384 x 8192 bf16 in 67-71 us, 5.8-6.1 TB/s (0.89-0.95 of the measured copy rate); items of half a group and 32-byte accesses
+// brought it there from 0.65 (8 elements a thread: twice the address arithmetic, 16-byte halves of sectors).  From fp32 108 us (0.97).
 template <typename T>
 __global__ void __launch_bounds__(CKPT_THREADS, sizeof(T) == 2 ? 4 : 3) checkpoint_pack_kernel(const T* x, uint64_t ldx, ItemWalk w,
                                                                        uint8_t* q, uint8_t* scales) {
@@ -269,7 +269,8 @@ __device__ __forceinline__ uint2 load_q8(const uint8_t* row, uint32_t c0, uint32
     return c0 < cols ? load_q_narrow(row + c0, cols - c0, grain) : make_uint2(0u, 0u);
 }
 
-// The reverse, bound by HBM in the same way: 16384 x 8192 bf16 in 71 us, 5.75 TB/s (0.89).
+// The reverse, bound by HBM in the same way: 16384 x 8192 bf16 in 71 us, 5.75 TB/s (0.89).  To fp32 165 us (0.63), in 16-byte stores
+// that lie 64 bytes apart across a warp.
 template <typename T>
 __global__ void __launch_bounds__(CKPT_THREADS, sizeof(T) == 2 ? 4 : 3) checkpoint_unpack_kernel(const uint8_t* q, const uint8_t* scales, ItemWalk w,
                                                                          T* out, uint64_t ldo) {
@@ -444,11 +445,13 @@ __global__ void __launch_bounds__(CKPT_THREADS) checkpoint_unpack_narrow_kernel(
 // partial row per run; the last CTA of a strip to finish adds the runs' partial rows in order, so the result does not
 // depend on the order in which the CTAs ran.
 //
-// 2 + 1 + 1/32 bytes read and 2 written per element.  8192 x 16384 bf16: the bias gradient alone 92 us (0.90 of the measured
-// copy rate), relu 116 us (0.90), silu 124-133 us (0.79-0.84), tanh gelu 138-145 us (0.73-0.76), gelu 156 us (0.67).  The first
-// two are bound by HBM, the others by instruction issue (21 an element for tanh gelu, of which two on the special-function
-// unit): paired fp32 arithmetic and one exponential shared by gelu's tail and density took them from 0.37 and 0.50.  Four
-// CTAs per SM with one row ahead beat three with two, or two with three.
+// 2 + 1 + 1/32 bytes read and 2 written per element.  8192 x 16384 bf16: the bias gradient alone (2 bytes read) 49 us (0.84 of the
+// measured copy rate), relu 114-116 us (0.90-0.92), silu 120-133 us (0.79-0.87), tanh gelu 130-145 us (0.72-0.80), gelu 149 us (0.70).
+// The first two are bound by HBM.  In the others no unit is full: tanh gelu and gelu use 60 and 64 % of the issue slots,
+// the multiply-add pipe 48 and 55 % of the cycles, the special-function unit 48 and 41 %; 35 and 27 % of a warp's
+// time goes by waiting for its loads (silu 48 %), of which a thread has one row of dy and q, 24 bytes, in flight.  Paired fp32 arithmetic
+// and one exponential shared by gelu's tail and density took them from 0.37 and 0.50.  Four CTAs per SM with one row ahead
+// beat three with two, or two with three.
 constexpr int GRAD_COLS = 256, GRAD_LANES = 8;
 
 struct GradArgs {

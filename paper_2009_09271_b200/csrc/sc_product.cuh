@@ -157,14 +157,14 @@ __device__ __forceinline__ void load_bias(const Epilogue& ep, uint32_t c0, float
 //
 // Bound by the tensor pipe and, where calls follow each other, by the power cap (1000 W; SM clock 1.2-1.5 GHz).
 // 8192 x 16384 x 4096 bf16: forward 775-840 us (1.31-1.42 PFLOP/s; the library's product alone 772-800 us beside it), with tanh
-// gelu and checkpoint 832-875 us, input gradient 790-870 us, weight gradient 850-930 us.  At 4096 x 8192 x 4096 the tensor
+// gelu and checkpoint 832-900 us, input gradient 790-890 us, weight gradient 850-935 us.  At 4096 x 8192 x 4096 the tensor
 // pipe is active for 78 to 82 % of the elapsed cycles.  What it took: pairs of CTAs (B read once a pair), the issuing warp kept
 // converged with one elected lane (a branch on the lane number cost 10 %), an accumulator hand-over without a release at
 // cluster scope, and the epilogue's loops rolled (fetched cold, they were most of a small call).
 //
 // The tensor cores add to an fp32 accumulator by cutting, not rounding: measured, a sum of n steps of 16 products comes
 // out about n 2^-24 of its size too small (2e-7 after 256 products, 9e-6 after 8192, 4e-5 after 32768 of random sign).  A
-// 16-bit result does not see that.  The weight gradient is fp32, so its accumulators are emptied every 6 blocks
+// bf16 result does not see that; of an fp16 one 16384 products of one sign take up to a quarter of a half step.  The weight gradient is fp32, so its accumulators are emptied every 6 blocks
 // (384 products) and added up in registers, with rounding: 3.6e-7 after 8192, at the price of 3 to 5 % of the time.
 constexpr int TC_ROWS = 128, TC_STEP = 64, TC_THREADS = 384, TC_EPI_WARPS = 8, TC_CHUNK = 6;
 constexpr int TC_LEAST_REGS = 160;             // 160 x 384 >= 56 x 128 + 208 x 256, for builds that shift registers
@@ -675,8 +675,8 @@ __global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* x
 // Up to 8 tokens: the fp32 result's own bytes are everything (8 multiply-adds a value, two at a time, fit beside them), so each
 // value is made where it is stored.  A CTA owns 128 columns and `run` rows; every warp holds the columns' inputs in
 // registers, read from the checkpoint or from x, and walks its rows with the rows' dz in shared memory (each twice, as the
-// paired arithmetic wants it), one 128-byte store at a time, whatever the alignment.  4096 x 4096: 14.7 us at 4 tokens and
-// 16.4 at 8, against 18.2 on the tiles (with the checkpoint's copy); a fill of the output takes 12.3.  With 16 tokens it took 31.
+// paired arithmetic wants it), one 128-byte store at a time, whatever the alignment.  4096 x 4096: 14.4 us at 4 tokens and
+// 16.3 at 8, against 18.2 on the tiles (with the checkpoint's copy); a fill of the output takes 12.3.  With 16 tokens it took 31.
 template <typename T, int TOKENS, bool KEPT>
 __global__ void __launch_bounds__(256) weight_tokens_kernel(const T* dz, uint64_t lddz, const T* x, uint64_t ldx,
                                                             const uint8_t* q, const uint8_t* scales, uint32_t tokens, uint32_t run,
