@@ -281,6 +281,51 @@ int sc_linear_grad_weight(sc_ctx* ctx, int type, const void* dz, size_t lddz, co
                           const int8_t* q, const uint8_t* scales, size_t M, size_t N, size_t K,
                           float* dw, size_t lddw, int accumulate, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------
+ * What stands between two such layers of a residual network, and a linear layer on 8-bit integers.  The conventions are the layer
+ * operators': types SC_BF16 and SC_F16, matrices as rows ld apart, fp32 inside and one rounding at the end, empty sizes allowed,
+ * sc_layer_reserve(rows, cols, cols) for a call's workspace.
+ *
+ * 8-bit rows of a matrix: q int8, and scales, one fp32 a row.  With m the row's largest magnitude the scale is m / 127 (at most the largest
+ * number whose 127-fold is finite) and q = rint(v * (127 * (1 / m))), each operation rounded to fp32, ties to even; the value is q * scale.  Rows with m < 2^-100 have
+ * scale 0 and q = 0.  A row with an element that is not finite has scale NaN and q = 0, so that all that reads it is NaN.
+ * --------------------------------------------------------------------------------------------------------- */
+
+/* 8-bit rows of x (SC_F32 too), a token's or an output channel's; and their values, rounded to `type`. */
+int sc_quantize(sc_ctx* ctx, int type, const void* x, size_t ldx, size_t rows, size_t cols, int8_t* q, size_t ldq, float* scales, void* stream);
+int sc_dequantize(sc_ctx* ctx, int type, const int8_t* q, size_t ldq, const float* scales, size_t rows, size_t cols, void* out, size_t ldo,
+                  void* stream);
+
+/* sc_linear on 8-bit rows of x [M, K] and W [N, K]: z[m, n] = (sum_k x[m, k] w[n, k]) * x_scales[m] * w_scales[n] + bias[n],
+ * y = act(z) + residual, the checkpoint of z on request.  The sums are exact integers, so no result depends on the order of their terms;
+ * K < 131072 (SC_ERR_RANGE).  Its gradients are the layer operators': sc_linear_grad_input with W in 16 bits, and
+ * sc_linear_grad_weight with x from sc_dequantize (the rounding to 8 bits is passed straight through). */
+int sc_linear_quantized(sc_ctx* ctx, int type, int act, const int8_t* x, size_t ldx, const float* x_scales, const int8_t* w, size_t ldw,
+                        const float* w_scales, const void* bias, const void* residual, size_t ldr, size_t M, size_t N, size_t K, void* y, size_t ldy,
+                        int8_t* q, uint8_t* scales, void* stream);
+
+/* Dropout with probability p in [0, 1]: y = residual + (kept ? x * 65536 / (65536 - t) : 0), t = rint(65536 p); residual may be NULL.
+ * The mask is not stored but drawn from (seed, row, column): with key = mix64(seed, 0x64726F70) and mix64 the generator of the seeded
+ * schemes, the four elements of a row from column 4 j share the 64 bits of mix64(key, row * ceil(cols / 4) + j), 16 bits each, the lowest first;
+ * an element is kept where its bits are at least t.  Its gradient is the same call, without a residual, on dy.  y may be x or residual
+ * (same ld). */
+int sc_dropout(sc_ctx* ctx, int type, const void* x, size_t ldx, const void* residual, size_t ldr, double p, uint64_t seed, size_t rows, size_t cols,
+               void* y, size_t ldy, void* stream);
+
+/* h = residual + dropout(x; p, seed), r = (mean of the row's h^2 + eps)^(-1/2), y = h r gamma; gamma[cols] is of the type, residual may be
+ * NULL, p = 0 drops nothing.  y is written in 16 bits, as 8-bit rows (q and scales), or both; h on request (NULL: not written).  y and q are
+ * made from the fp32 h.  Squares are summed in fp32: a row whose sum is not finite gives NaN.  h and y may be x or residual (same ld), each another. */
+int sc_rms_norm(sc_ctx* ctx, int type, const void* x, size_t ldx, const void* residual, size_t ldr, const void* gamma, float eps, double p, uint64_t seed,
+                size_t rows, size_t cols, void* h, size_t ldh, void* y, size_t ldy, int8_t* q, size_t ldq, float* scales, void* stream);
+
+/* The norm's gradient, from dy and the h that the forward call wrote (its x where it had neither residual nor dropout):
+ * dh = residual + r (g - u mean(g u)), g = gamma dy, u = h r: the gradient of h, plus that of what else read h (residual, NULL: none);
+ * dx = dropout(dh; p, seed): the gradient of x; dgamma[cols] = column sums of dy u, fp32 (accumulate: added to dgamma).  dh, dx or dgamma may be
+ * NULL.  dh and dx may be dy, h or residual (same ld), each another. */
+int sc_rms_norm_grad(sc_ctx* ctx, int type, const void* dy, size_t lddy, const void* h, size_t ldh, const void* gamma, float eps, const void* residual,
+                     size_t ldr, double p, uint64_t seed, size_t rows, size_t cols, void* dh, size_t lddh, void* dx, size_t lddx, float* dgamma,
+                     int accumulate, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,7 +29,11 @@ EXPORTS = ["sc_create", "sc_destroy", "sc_strerror", "sc_sync_status", "sc_set_g
            "sc_compress", "sc_compress_batch", "sc_aggregate", "sc_aggregate_shared", "sc_aggregate_static", "sc_aggregate_apply",
            "sc_aggregate_apply_shared", "sc_step", "sc_step_apply", "sc_step_host",
            "sc_layer_reserve", "sc_debug_layer_tiles", "sc_checkpoint_pack", "sc_checkpoint_unpack", "sc_activation_grad", "sc_linear", "sc_linear_grad_input",
-           "sc_linear_grad_weight"]
+           "sc_linear_grad_weight", "sc_quantize", "sc_dequantize", "sc_linear_quantized", "sc_dropout", "sc_rms_norm", "sc_rms_norm_grad"]
+
+
+_LAYER_CALLS = ("sc_checkpoint_pack", "sc_checkpoint_unpack", "sc_activation_grad", "sc_linear", "sc_linear_grad_input", "sc_linear_grad_weight",
+                "sc_quantize", "sc_dequantize", "sc_linear_quantized", "sc_dropout", "sc_rms_norm", "sc_rms_norm_grad")
 
 
 class ScSegment(ctypes.Structure):
@@ -115,8 +119,13 @@ def load_library() -> ctypes.CDLL:
     lib.sc_linear.argtypes = [vp, ci, ci, vp, sz, vp, sz, vp, vp, sz, sz, sz, sz, vp, sz, vp, vp, vp]
     lib.sc_linear_grad_input.argtypes = [vp, ci, ci, vp, sz, vp, sz, vp, sz, vp, vp, sz, sz, sz, vp, sz, vp]
     lib.sc_linear_grad_weight.argtypes = [vp, ci, vp, sz, vp, sz, vp, vp, sz, sz, sz, vp, sz, ci, vp]
-    for name in ("sc_layer_reserve", "sc_debug_layer_tiles", "sc_checkpoint_pack", "sc_checkpoint_unpack", "sc_activation_grad", "sc_linear",
-                 "sc_linear_grad_input", "sc_linear_grad_weight"):
+    lib.sc_quantize.argtypes = [vp, ci, vp, sz, sz, sz, vp, sz, vp, vp]
+    lib.sc_dequantize.argtypes = [vp, ci, vp, sz, vp, sz, sz, vp, sz, vp]
+    lib.sc_linear_quantized.argtypes = [vp, ci, ci, vp, sz, vp, vp, sz, vp, vp, vp, sz, sz, sz, sz, vp, sz, vp, vp, vp]
+    lib.sc_dropout.argtypes = [vp, ci, vp, sz, vp, sz, ctypes.c_double, u64, sz, sz, vp, sz, vp]
+    lib.sc_rms_norm.argtypes = [vp, ci, vp, sz, vp, sz, vp, ctypes.c_float, ctypes.c_double, u64, sz, sz, vp, sz, vp, sz, vp, sz, vp, vp]
+    lib.sc_rms_norm_grad.argtypes = [vp, ci, vp, sz, vp, sz, vp, ctypes.c_float, vp, sz, ctypes.c_double, u64, sz, sz, vp, sz, vp, sz, vp, ci, vp]
+    for name in ("sc_layer_reserve", "sc_debug_layer_tiles") + _LAYER_CALLS:
         getattr(lib, name).restype = ci
     _lib = lib
     return lib
@@ -216,6 +225,25 @@ def checkpoint_buffers(rows: int, cols: int, device="cuda"):
             torch.empty(rows, -(-cols // CHECKPOINT_GROUP), dtype=torch.uint8, device=device))
 
 
+def quantized_buffers(rows: int, cols: int, device="cuda"):
+    """(q, scales) for the 8-bit rows of a [rows, cols] matrix: int8, and one float32 a row."""
+    return torch.empty(rows, cols, dtype=torch.int8, device=device), torch.empty(rows, dtype=torch.float32, device=device)
+
+
+def _eight_bit_rows(q, scales, rows: int, cols: int, name: str = "q", scales_name: str = "scales") -> int:
+    """Checks 8-bit rows [rows, cols] and their scales; returns the distance between rows."""
+    if q is None or scales is None:
+        raise ValueError(f"{name} and {scales_name}: 8-bit rows are both or neither")
+    _vector(scales, rows, torch.float32, scales_name)
+    return _matrix(q, rows, cols, torch.int8, name)
+
+
+def _probability(p: float) -> float:
+    if not 0.0 <= p <= 1.0:
+        raise ValueError(f"p: expected a probability, got {p}")
+    return p
+
+
 STATIC_MAX_N, STATIC_MAX_W = 1 << 24, 64
 
 
@@ -232,7 +260,6 @@ def sc_aggregate_static(W: int, vals, idx, k: int, n: int, out, stream=None) -> 
         raise SparseCommError(code, f"sc_aggregate_static (limits: W <= {STATIC_MAX_W}, n <= {STATIC_MAX_N})")
 
 
-_LAYER_CALLS = ("sc_checkpoint_pack", "sc_checkpoint_unpack", "sc_activation_grad", "sc_linear", "sc_linear_grad_input", "sc_linear_grad_weight")
 _calls = None
 
 
@@ -262,6 +289,7 @@ class Context:
         self._h = ctypes.c_void_p()
         _check(lib.sc_create(ctypes.byref(self._h), max_n, max_W, max_segments), "sc_create")
         self._layer, self._handle = _layer_calls(lib), self._h.value
+        self._device = torch.cuda.current_device()
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h:
@@ -492,3 +520,106 @@ class Context:
             _kept(q, scales, M, K)
         _check(self._layer.sc_linear_grad_weight(self._handle, kind, _ptr(dz), lddz, _ptr(x), ldx, _ptr(q), _ptr(scales), M, N, K,
                                                _ptr(dw), lddw, 1 if accumulate else 0, _stream(stream)), "sc_linear_grad_weight")
+
+    # -- 8-bit rows, norm, dropout -----------------------------------------------
+    def _here(self, *tensors) -> None:
+        """The tensors (None: not given) are on the context's device."""
+        for t in tensors:
+            if t is not None and t.get_device() != self._device:
+                raise ValueError(f"tensors must be on the context's device, cuda:{self._device}; got one on {t.device}")
+
+    def _queue(self, stream) -> Optional[int]:
+        """The given stream, or the current one of the context's device, whichever device is current."""
+        if stream is None and _raw_stream is not None:
+            return _raw_stream(self._device) or None
+        return _stream(torch.cuda.current_stream(self._device) if stream is None else stream)
+
+    def sc_quantize(self, x, q, scales, stream=None) -> None:
+        """q, scales <- the 8-bit rows of x [rows, cols] (bfloat16, float16 or float32)."""
+        kind = _layer_type(x, "x", f32=True)
+        rows, cols = x.shape
+        ldx = _matrix(x, rows, cols, x.dtype, "x")
+        ldq = _eight_bit_rows(q, scales, rows, cols)
+        self._here(x, q, scales)
+        _check(self._layer.sc_quantize(self._handle, kind, _ptr(x), ldx, rows, cols, _ptr(q), ldq, _ptr(scales), self._queue(stream)), "sc_quantize")
+
+    def sc_dequantize(self, q, scales, out, stream=None) -> None:
+        """out [rows, cols] <- the values of 8-bit rows."""
+        kind = _layer_type(out, "out", f32=True)
+        rows, cols = out.shape
+        ldo = _matrix(out, rows, cols, out.dtype, "out")
+        ldq = _eight_bit_rows(q, scales, rows, cols)
+        self._here(q, scales, out)
+        _check(self._layer.sc_dequantize(self._handle, kind, _ptr(q), ldq, _ptr(scales), rows, cols, _ptr(out), ldo, self._queue(stream)), "sc_dequantize")
+
+    def sc_linear_quantized(self, act: int, x, x_scales, w, w_scales, y, bias=None, residual=None, q=None, scales=None, stream=None) -> None:
+        """y [M, N] <- act(z) + residual, z = (x W^T) x_scales w_scales + bias with 8-bit rows x [M, K] and w [N, K]; q, scales <- the
+        checkpoint of z."""
+        kind = _layer_type(y, "y")
+        M, N = y.shape
+        ldy = _matrix(y, M, N, y.dtype, "y")
+        if x is None or x.dim() != 2:
+            raise ValueError("x: expected a matrix")
+        K = x.shape[1]
+        ldx = _eight_bit_rows(x, x_scales, M, K, "x", "x_scales")
+        ldw = _eight_bit_rows(w, w_scales, N, K, "w", "w_scales")
+        if bias is not None:
+            _vector(bias, N, y.dtype, "bias")
+        ldr = N if residual is None else _matrix(residual, M, N, y.dtype, "residual")
+        if q is not None or scales is not None:
+            _kept(q, scales, M, N)
+        self._here(x, x_scales, w, w_scales, y, bias, residual, q, scales)
+        _check(self._layer.sc_linear_quantized(self._handle, kind, act, _ptr(x), ldx, _ptr(x_scales), _ptr(w), ldw, _ptr(w_scales), _ptr(bias),
+                                               _ptr(residual), ldr, M, N, K, _ptr(y), ldy, _ptr(q), _ptr(scales), self._queue(stream)),
+               "sc_linear_quantized")
+
+    def sc_dropout(self, x, y, p: float, seed: int, residual=None, stream=None) -> None:
+        """y <- residual + dropout(x): each element kept with probability 1 - p and scaled by its reciprocal, by the mask that (seed, row,
+        column) give.  The gradient is the same call on dy, without a residual.  y may be x or residual."""
+        kind = _layer_type(x, "x")
+        rows, cols = x.shape
+        ldx = _matrix(x, rows, cols, x.dtype, "x")
+        ldy = _matrix(y, rows, cols, x.dtype, "y")
+        ldr = cols if residual is None else _matrix(residual, rows, cols, x.dtype, "residual")
+        self._here(x, y, residual)
+        _check(self._layer.sc_dropout(self._handle, kind, _ptr(x), ldx, _ptr(residual), ldr, _probability(p), int(seed) & 0xFFFFFFFFFFFFFFFF, rows, cols,
+                                      _ptr(y), ldy, self._queue(stream)), "sc_dropout")
+
+    def sc_rms_norm(self, x, gamma, eps: float, y=None, q=None, scales=None, residual=None, h=None, p: float = 0.0, seed: int = 0, stream=None) -> None:
+        """h <- residual + dropout(x; p, seed); y, or its 8-bit rows q and scales, or both <- h / sqrt(mean(h^2) + eps) * gamma."""
+        kind = _layer_type(x, "x")
+        rows, cols = x.shape
+        dtype = x.dtype
+        ldx = _matrix(x, rows, cols, dtype, "x")
+        _vector(gamma, cols, dtype, "gamma")
+        if y is None and q is None:
+            raise ValueError("y, or q and scales, must be given")
+        ldy = cols if y is None else _matrix(y, rows, cols, dtype, "y")
+        ldq = cols if q is None and scales is None else _eight_bit_rows(q, scales, rows, cols)
+        ldr = cols if residual is None else _matrix(residual, rows, cols, dtype, "residual")
+        ldh = cols if h is None else _matrix(h, rows, cols, dtype, "h")
+        self._here(x, gamma, y, q, scales, residual, h)
+        _check(self._layer.sc_rms_norm(self._handle, kind, _ptr(x), ldx, _ptr(residual), ldr, _ptr(gamma), eps, _probability(p),
+                                       int(seed) & 0xFFFFFFFFFFFFFFFF, rows, cols, _ptr(h), ldh, _ptr(y), ldy, _ptr(q), ldq, _ptr(scales),
+                                       self._queue(stream)), "sc_rms_norm")
+
+    def sc_rms_norm_grad(self, dy, h, gamma, eps: float, dh=None, dgamma=None, residual=None, dx=None, p: float = 0.0, seed: int = 0,
+                         accumulate: bool = False, stream=None) -> None:
+        """dh <- residual + the norm's gradient at h; dx <- dropout(dh; p, seed); dgamma <- (dgamma +) column sums of dy h / rms(h), float32."""
+        kind = _layer_type(dy, "dy")
+        rows, cols = dy.shape
+        dtype = dy.dtype
+        lddy = _matrix(dy, rows, cols, dtype, "dy")
+        ldh = _matrix(h, rows, cols, dtype, "h")
+        _vector(gamma, cols, dtype, "gamma")
+        if dh is None and dx is None and dgamma is None:
+            raise ValueError("dh, dx or dgamma must be given")
+        lddh = cols if dh is None else _matrix(dh, rows, cols, dtype, "dh")
+        lddx = cols if dx is None else _matrix(dx, rows, cols, dtype, "dx")
+        ldr = cols if residual is None else _matrix(residual, rows, cols, dtype, "residual")
+        if dgamma is not None:
+            _vector(dgamma, cols, torch.float32, "dgamma")
+        self._here(dy, h, gamma, dh, dgamma, residual, dx)
+        _check(self._layer.sc_rms_norm_grad(self._handle, kind, _ptr(dy), lddy, _ptr(h), ldh, _ptr(gamma), eps, _ptr(residual), ldr, _probability(p),
+                                            int(seed) & 0xFFFFFFFFFFFFFFFF, rows, cols, _ptr(dh), lddh, _ptr(dx), lddx, _ptr(dgamma),
+                                            1 if accumulate else 0, self._queue(stream)), "sc_rms_norm_grad")

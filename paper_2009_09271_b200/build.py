@@ -11,7 +11,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparsecomm.so")
-SOURCES = ["sc_api.cu", "sc_layer.cu"]
+SOURCES = ["sc_api.cu", "sc_layer.cu", "sc_norm.cu", "sc_quantized.cu"]
 # the layer operators' calls without ctypes; the binding does without where Python's headers are not installed
 CALLS_SOURCE = os.path.join(CSRC, "sc_calls.c")
 CALLS = os.path.join(HERE, "_sc_calls" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))

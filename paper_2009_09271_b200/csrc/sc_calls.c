@@ -16,11 +16,22 @@ static struct {
                                 size_t, size_t, void*, size_t, void*);
     int (*sc_linear_grad_weight)(sc_ctx*, int, const void*, size_t, const void*, size_t, const int8_t*, const uint8_t*, size_t, size_t, size_t, float*, size_t,
                                  int, void*);
+    int (*sc_quantize)(sc_ctx*, int, const void*, size_t, size_t, size_t, int8_t*, size_t, float*, void*);
+    int (*sc_dequantize)(sc_ctx*, int, const int8_t*, size_t, const float*, size_t, size_t, void*, size_t, void*);
+    int (*sc_linear_quantized)(sc_ctx*, int, int, const int8_t*, size_t, const float*, const int8_t*, size_t, const float*, const void*, const void*, size_t,
+                               size_t, size_t, size_t, void*, size_t, int8_t*, uint8_t*, void*);
+    int (*sc_dropout)(sc_ctx*, int, const void*, size_t, const void*, size_t, double, uint64_t, size_t, size_t, void*, size_t, void*);
+    int (*sc_rms_norm)(sc_ctx*, int, const void*, size_t, const void*, size_t, const void*, float, double, uint64_t, size_t, size_t, void*, size_t, void*,
+                       size_t, int8_t*, size_t, float*, void*);
+    int (*sc_rms_norm_grad)(sc_ctx*, int, const void*, size_t, const void*, size_t, const void*, float, const void*, size_t, double, uint64_t, size_t, size_t,
+                            void*, size_t, void*, size_t, float*, int, void*);
 } fn;
 
 static void* P(PyObject* o) { return o == Py_None ? NULL : PyLong_AsVoidPtr(o); }
 static size_t U(PyObject* o) { return PyLong_AsSize_t(o); }
 static int I(PyObject* o) { return (int)PyLong_AsLong(o); }
+static double D(PyObject* o) { return PyFloat_AsDouble(o); }
+static uint64_t S(PyObject* o) { return PyLong_AsUnsignedLongLongMask(o); }
 
 /* Converts the arguments, then calls without the interpreter lock: a first call may allocate and wait. */
 #define WRAPPER(name, count, ...)                                                                  \
@@ -69,22 +80,53 @@ WRAPPER(sc_linear_grad_input, 17, (sc_ctx*)h, t, act, dz, lddz, w, ldw, r, ldr, 
     size_t lddz = U(a[3]), ldx = U(a[5]), M = U(a[8]), N = U(a[9]), K = U(a[10]), lddw = U(a[12]);
 WRAPPER(sc_linear_grad_weight, 15, (sc_ctx*)h, t, dz, lddz, x, ldx, (const int8_t*)q, (const uint8_t*)s, M, N, K, (float*)dw, lddw, add, st)
 
-/* bind(pack, unpack, activation_grad, linear, grad_input, grad_weight): the functions' addresses. */
+#define CONVERT_sc_quantize \
+    void *h = P(a[0]), *x = P(a[2]), *q = P(a[6]), *s = P(a[8]), *st = P(a[9]); int t = I(a[1]); size_t ldx = U(a[3]), r = U(a[4]), c = U(a[5]), ldq = U(a[7]);
+WRAPPER(sc_quantize, 10, (sc_ctx*)h, t, x, ldx, r, c, (int8_t*)q, ldq, (float*)s, st)
+
+#define CONVERT_sc_dequantize \
+    void *h = P(a[0]), *q = P(a[2]), *s = P(a[4]), *o = P(a[7]), *st = P(a[9]); int t = I(a[1]); size_t ldq = U(a[3]), r = U(a[5]), c = U(a[6]), ldo = U(a[8]);
+WRAPPER(sc_dequantize, 10, (sc_ctx*)h, t, (const int8_t*)q, ldq, (const float*)s, r, c, o, ldo, st)
+
+#define CONVERT_sc_linear_quantized                                                                                                  \
+    void *h = P(a[0]), *x = P(a[3]), *xs = P(a[5]), *w = P(a[6]), *ws = P(a[8]), *b = P(a[9]), *r = P(a[10]), *y = P(a[15]), *q = P(a[17]), \
+         *s = P(a[18]), *st = P(a[19]);                                                                                                \
+    int t = I(a[1]), act = I(a[2]);                                                                                                    \
+    size_t ldx = U(a[4]), ldw = U(a[7]), ldr = U(a[11]), M = U(a[12]), N = U(a[13]), K = U(a[14]), ldy = U(a[16]);
+WRAPPER(sc_linear_quantized, 20, (sc_ctx*)h, t, act, (const int8_t*)x, ldx, (const float*)xs, (const int8_t*)w, ldw, (const float*)ws, b, r, ldr, M, N, K, y,
+        ldy, (int8_t*)q, (uint8_t*)s, st)
+
+#define CONVERT_sc_dropout                                                                                                           \
+    void *h = P(a[0]), *x = P(a[2]), *r = P(a[4]), *y = P(a[10]), *st = P(a[12]); int t = I(a[1]); double p = D(a[6]); uint64_t seed = S(a[7]); \
+    size_t ldx = U(a[3]), ldr = U(a[5]), rows = U(a[8]), cols = U(a[9]), ldy = U(a[11]);
+WRAPPER(sc_dropout, 13, (sc_ctx*)h, t, x, ldx, r, ldr, p, seed, rows, cols, y, ldy, st)
+
+#define CONVERT_sc_rms_norm                                                                                                          \
+    void *h = P(a[0]), *x = P(a[2]), *r = P(a[4]), *g = P(a[6]), *o = P(a[12]), *y = P(a[14]), *q = P(a[16]), *s = P(a[18]), *st = P(a[19]); \
+    int t = I(a[1]); double eps = D(a[7]), p = D(a[8]); uint64_t seed = S(a[9]);                                                         \
+    size_t ldx = U(a[3]), ldr = U(a[5]), rows = U(a[10]), cols = U(a[11]), ldh = U(a[13]), ldy = U(a[15]), ldq = U(a[17]);
+WRAPPER(sc_rms_norm, 20, (sc_ctx*)h, t, x, ldx, r, ldr, g, (float)eps, p, seed, rows, cols, o, ldh, y, ldy, (int8_t*)q, ldq, (float*)s, st)
+
+#define CONVERT_sc_rms_norm_grad                                                                                                     \
+    void *h = P(a[0]), *dy = P(a[2]), *o = P(a[4]), *g = P(a[6]), *r = P(a[8]), *dh = P(a[14]), *dx = P(a[16]), *dg = P(a[18]), *st = P(a[20]); \
+    int t = I(a[1]), add = I(a[19]); double eps = D(a[7]), p = D(a[10]); uint64_t seed = S(a[11]);                                       \
+    size_t ldy = U(a[3]), ldo = U(a[5]), ldr = U(a[9]), rows = U(a[12]), cols = U(a[13]), lddh = U(a[15]), lddx = U(a[17]);
+WRAPPER(sc_rms_norm_grad, 21, (sc_ctx*)h, t, dy, ldy, o, ldo, g, (float)eps, r, ldr, p, seed, rows, cols, dh, lddh, dx, lddx, (float*)dg, add, st)
+
+/* bind(addresses): the functions' addresses, in the order of `fn`. */
 static PyObject* bind(PyObject* self, PyObject* const* a, Py_ssize_t n) {
-    void* p[6];
+    void** to[] = {(void**)&fn.sc_checkpoint_pack, (void**)&fn.sc_checkpoint_unpack, (void**)&fn.sc_activation_grad, (void**)&fn.sc_linear,
+                   (void**)&fn.sc_linear_grad_input, (void**)&fn.sc_linear_grad_weight, (void**)&fn.sc_quantize, (void**)&fn.sc_dequantize,
+                   (void**)&fn.sc_linear_quantized, (void**)&fn.sc_dropout, (void**)&fn.sc_rms_norm, (void**)&fn.sc_rms_norm_grad};
+    void* p[sizeof(to) / sizeof(to[0])];
     (void)self;
-    if (n != 6) {
-        PyErr_SetString(PyExc_TypeError, "bind: six addresses");
+    if (n != (Py_ssize_t)(sizeof(to) / sizeof(to[0]))) {
+        PyErr_SetString(PyExc_TypeError, "bind: an address for each function");
         return NULL;
     }
-    for (int i = 0; i < 6; ++i) p[i] = P(a[i]);
+    for (Py_ssize_t i = 0; i < n; ++i) p[i] = P(a[i]);
     if (PyErr_Occurred()) return NULL;
-    *(void**)&fn.sc_checkpoint_pack = p[0];
-    *(void**)&fn.sc_checkpoint_unpack = p[1];
-    *(void**)&fn.sc_activation_grad = p[2];
-    *(void**)&fn.sc_linear = p[3];
-    *(void**)&fn.sc_linear_grad_input = p[4];
-    *(void**)&fn.sc_linear_grad_weight = p[5];
+    for (Py_ssize_t i = 0; i < n; ++i) *to[i] = p[i];
     Py_RETURN_NONE;
 }
 
@@ -96,6 +138,12 @@ static PyMethodDef methods[] = {METHOD("bind", bind),
                                 METHOD("sc_linear", sc_linear_py),
                                 METHOD("sc_linear_grad_input", sc_linear_grad_input_py),
                                 METHOD("sc_linear_grad_weight", sc_linear_grad_weight_py),
+                                METHOD("sc_quantize", sc_quantize_py),
+                                METHOD("sc_dequantize", sc_dequantize_py),
+                                METHOD("sc_linear_quantized", sc_linear_quantized_py),
+                                METHOD("sc_dropout", sc_dropout_py),
+                                METHOD("sc_rms_norm", sc_rms_norm_py),
+                                METHOD("sc_rms_norm_grad", sc_rms_norm_grad_py),
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_sc_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__sc_calls(void) { return PyModule_Create(&module); }

@@ -136,12 +136,13 @@ class DeviceGuard {
 enum { KIND_SCATTER = 0, KIND_MASK_COUNT, KIND_ROW_SCAN, KIND_RANDK_PACK, KIND_RANDBLOCK, KIND_AGG_BOUNDS, KIND_AGG_TILES,
        KIND_AGG_WARP, KIND_AGG_FINE, KIND_AGG_APPLY, KIND_TINY, KIND_BRACKET, KIND_MAIN, KIND_FILTER, KIND_FINISH, KIND_RESOLVE_SMALL, KIND_EMIT,
        KIND_FALLBACK, KIND_CKPT_PACK, KIND_CKPT_UNPACK, KIND_ACT_GRAD, KIND_LINEAR, KIND_LINEAR_DX, KIND_LINEAR_DW, KIND_LAYER_JOIN,
-       KIND_LAYER_LAYOUT, KIND_COUNT };
+       KIND_LAYER_LAYOUT, KIND_QUANTIZE, KIND_DEQUANTIZE, KIND_LINEAR_QUANTIZED, KIND_RMS_NORM, KIND_RMS_NORM_GRAD, KIND_DROPOUT, KIND_COUNT };
 const char* const kKindNames[KIND_COUNT] = {"randk_scatter", "mask_count", "row_scan", "randk_pack", "randblock", "agg_bounds",
                                             "agg_tiles", "agg_warp", "agg_fine", "agg_apply", "topk_tiny", "topk_bracket",
                                             "topk_main", "topk_filter", "topk_finish", "topk_resolve_small", "topk_emit", "topk_fallback",
                                             "checkpoint_pack", "checkpoint_unpack", "activation_grad", "linear", "linear_grad_input",
-                                            "linear_grad_weight", "layer_join", "layer_layout"};
+                                            "linear_grad_weight", "layer_join", "layer_layout", "quantize", "dequantize", "linear_quantized", "rms_norm",
+                                            "rms_norm_grad", "dropout"};
 
 // Counts a kernel launch and, when profiling is on, brackets it with two events.
 class Launch {

@@ -2,6 +2,7 @@
 //   forward       y  = act(x W^T + b) + residual          A = x [M, K],   B = W [N, K],    r over K
 //   input grad    dx = (dz W + residual) * act'(z^)       A = dz [M, N],  B = W^T [K, N],  r over N
 //   weight grad   dW (+)= dz^T x^                         A = dz^T [N, M], B = x^T [K, M], r over M
+// and the forward product of 8-bit integers, whose exact sums its epilogue scales: z = (xq wq^T) sx sw + b.
 #pragma once
 #include "sc_checkpoint.cuh"
 #include "sc_layer_common.cuh"
@@ -9,7 +10,11 @@
 
 namespace sc {
 
-enum { PRODUCT_FORWARD = 0, PRODUCT_INPUT = 1, PRODUCT_WEIGHT = 2 };
+enum { PRODUCT_FORWARD = 0, PRODUCT_INPUT = 1, PRODUCT_WEIGHT = 2, PRODUCT_QUANTIZED = 3 };
+// What follows a product of 8-bit integers once its sums are scaled is the forward product's epilogue.
+__host__ __device__ constexpr int epilogue_of(int mode) { return mode == PRODUCT_QUANTIZED ? PRODUCT_FORWARD : mode; }
+// Terms of a reduction in one block: 128 bytes of an operand's row.
+__host__ __device__ constexpr int product_step(int mode) { return mode == PRODUCT_QUANTIZED ? 128 : 64; }
 
 struct Epilogue {
     const void* bias;          // forward: [cols] or null
@@ -23,7 +28,25 @@ struct Epilogue {
     uint32_t accumulate;
     uint32_t grain_out, grain_res, grain_q, grain_bias;      // elements that one access of a row may take
     uint32_t scales_by4;       // block_rows: four neighbouring scales of a row go out in one access
+    const float* row_scale;    // 8-bit product: a scale for each row and each column of the result
+    const float* col_scale;
 };
+
+// 8-bit product: the scales of 8 columns, zero past the end, and a row's sums (by their bits) times both scales.
+template <int MODE>
+__device__ __forceinline__ void load_col_scales(const Epilogue& ep, uint32_t c0, float s[8]) {
+    if constexpr (MODE == PRODUCT_QUANTIZED)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = c0 + i < ep.cols ? ep.col_scale[c0 + i] : 0.0f;
+}
+template <int MODE>
+__device__ __forceinline__ void scale8(const Epilogue& ep, uint64_t row, const float s[8], float v[8]) {
+    if constexpr (MODE == PRODUCT_QUANTIZED) {
+        const float r = row < ep.rows ? ep.row_scale[row] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)__float_as_int(v[i]) * r * s[i];
+    }
+}
 
 // What follows the product for 8 columns from c0 of one row.  All 32 lanes of a warp call it; four neighbouring lanes hold
 // 32 consecutive columns of one row, from a multiple of 32, so they share a checkpoint group.  `bias`: of these columns.
@@ -183,7 +206,7 @@ struct TcShape {
 struct TcArgs {
     uint32_t tiles_i, tiles_j, tiles;      // output tiles
     uint32_t splits;                       // parts of the reduction; more than one: fp32 partial sums go to `partial`
-    uint32_t blocks;                       // reduction blocks of 64
+    uint32_t blocks;                       // reduction blocks, 128 bytes of a row each
     uint32_t idesc, a_box_rows;
     uint64_t part_stride;                  // elements between two parts
     uint32_t part_ld;
@@ -258,21 +281,24 @@ __device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcAr
             }
         }
     } else {
-        float bias[8];
-        load_bias<T, MODE>(ep, c0, bias);
-        const bool narrow = ep.grain_out == 1 || (MODE == PRODUCT_FORWARD && ep.q && ep.grain_q == 1);
+        constexpr int NEXT = epilogue_of(MODE);
+        float bias[8], scales[8];
+        load_bias<T, NEXT>(ep, c0, bias);
+        load_col_scales<MODE>(ep, c0, scales);
+        const bool narrow = ep.grain_out == 1 || (NEXT == PRODUCT_FORWARD && ep.q && ep.grain_q == 1);
         with_activation(ep.act, [&](auto act) {
 #pragma unroll 1                                              // little code: it is fetched cold in a small call
             for (int i = 0; i < 4; ++i) {
                 float f[8];
                 const uint64_t row = fetch(i, f);
                 if (narrow) __syncwarp();                     // the row's four lanes have read it
-                epilogue8<T, MODE, decltype(act)::value>(ep, row, c0, bias, f, narrow ? stage_addr + (uint32_t)(row - row0) * 128 : 0u);
+                scale8<MODE>(ep, row, scales, f);
+                epilogue8<T, NEXT, decltype(act)::value>(ep, row, c0, bias, f, narrow ? stage_addr + (uint32_t)(row - row0) * 128 : 0u);
             }
         });
         if (narrow) {
             __syncwarp();
-            rows_out(ep, stage_addr, row0, col0, MODE == PRODUCT_FORWARD && ep.q);
+            rows_out(ep, stage_addr, row0, col0, NEXT == PRODUCT_FORWARD && ep.q);
         }
     }
     __syncwarp();
@@ -281,15 +307,28 @@ __device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcAr
 // One 32 x 32 block of a 16-bit result, thread t holding row t from TMEM to the end: a checkpoint group is one thread's own, its
 // bytes go out as one sector, and the result leaves by TMA from a 2 KB buffer of 64-byte rows (64-byte swizzle), two of
 // which take turns.  About a third of the instructions of block_out, which serves rows of other alignments.
-template <typename T, int MODE, int ACT>
+template <typename T, int PRODUCT, int ACT>
 __device__ __forceinline__ void block_rows(const CUtensorMap* map_out, const Epilogue& ep, uint32_t buffer, const uint32_t (&v)[32], uint64_t row0,
                                            uint32_t col0, uint32_t& scale4) {
     const uint32_t lane = threadIdx.x & 31u;
     const uint64_t row = row0 + lane;
     const bool in = row < ep.rows && col0 < ep.cols, whole = col0 + 32 <= ep.cols;
+    constexpr int MODE = epilogue_of(PRODUCT);
     Pair z[16];
+    if constexpr (PRODUCT == PRODUCT_QUANTIZED) {
+        const Pair r = pair(row < ep.rows ? ep.row_scale[row] : 0.0f);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) z[i] = pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+        for (int j = 0; j < 4; ++j) {
+            float s[8];
+            load_col_scales<PRODUCT>(ep, col0 + 8 * j, s);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                z[4 * j + i] = pair((float)(int32_t)v[8 * j + 2 * i], (float)(int32_t)v[8 * j + 2 * i + 1]) * r * pair(s[2 * i], s[2 * i + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[i] = pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+    }
     if constexpr (MODE == PRODUCT_FORWARD) {
         if (ep.bias) {
 #pragma unroll
@@ -408,7 +447,7 @@ template <typename T, int MODE, int BN, int CG>
 __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                                 const __grid_constant__ CUtensorMap map_out, TcArgs a, Epilogue ep) {
     using S = TcShape<BN, CG>;
-    constexpr bool A_MN = MODE == PRODUCT_WEIGHT, B_MN = MODE != PRODUCT_FORWARD;
+    constexpr bool A_MN = MODE == PRODUCT_WEIGHT, B_MN = epilogue_of(MODE) != PRODUCT_FORWARD;
     constexpr bool SUM = MODE == PRODUCT_WEIGHT;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
@@ -460,7 +499,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                     if (elect_one()) {
                         if (rank == 0) mbar_expect_tx(full + 8 * stage, bytes);
                         const uint32_t bar = CG == 2 ? map_to_rank(full + 8 * stage, 0) : full + 8 * stage;
-                        const int32_t r = (int32_t)(k * TC_STEP);
+                        const int32_t r = (int32_t)(k * product_step(MODE));
                         if constexpr (A_MN) {
 #pragma unroll
                             for (int c = 0; c < TC_ROWS; c += 64) tma_load_2d<CG>(sa + c * TC_STEP * 2, &map_a, bar, i0 + c, r);
@@ -505,7 +544,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                         if (elect_one()) {
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
-                                mma_f16<CG>(d, da + (A_MN ? 128 : 2) * i, db + (B_MN ? 128 : 2) * i, a.idesc, k > c0 || i > 0);
+                                if constexpr (MODE == PRODUCT_QUANTIZED) mma_i8<CG>(d, da + 2 * i, db + 2 * i, a.idesc, k > c0 || i > 0);
+                                else mma_f16<CG>(d, da + (A_MN ? 128 : 2) * i, db + (B_MN ? 128 : 2) * i, a.idesc, k > c0 || i > 0);
                             mma_commit<CG>(empty + 8 * stage);
                             if (k + 1 == c1) mma_commit<CG>(tfull + 8 * acc);
                         }
@@ -769,16 +809,23 @@ __global__ void __launch_bounds__(256) product_join_kernel(const float* partial,
             const float4* p = reinterpret_cast<const float4*>(partial + row * part_ld + c0);
             for (uint32_t s = 0; s < splits; ++s, p += part_stride / 4) {
                 const float4 x = load_l2(p), y = load_l2(p + 1);
-                f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
-                f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
+                const float part[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if constexpr (MODE == PRODUCT_QUANTIZED) f[j] = __int_as_float(__float_as_int(f[j]) + __float_as_int(part[j]));
+                    else f[j] += part[j];
+                }
             }
         }
         if constexpr (MODE == PRODUCT_WEIGHT) {
             epilogue8<T, MODE, SC_ACT_NONE>(ep, row, c0, nullptr, f);
         } else {
-            float bias[8];
-            load_bias<T, MODE>(ep, c0, bias);
-            with_activation(ep.act, [&](auto act) { epilogue8<T, MODE, decltype(act)::value>(ep, row, c0, bias, f); });
+            constexpr int NEXT = epilogue_of(MODE);
+            float bias[8], scales[8];
+            load_bias<T, NEXT>(ep, c0, bias);
+            load_col_scales<MODE>(ep, c0, scales);
+            scale8<MODE>(ep, row, scales, f);
+            with_activation(ep.act, [&](auto act) { epilogue8<T, NEXT, decltype(act)::value>(ep, row, c0, bias, f); });
         }
     }
 }
@@ -813,11 +860,31 @@ __device__ __forceinline__ void layout_rows(const LayoutArgs& a, uint32_t block,
         }
     }
 }
+// The same for bytes, to rows a multiple of 16 apart: 16 bytes a thread, read in runs of the rows' alignment.
+__device__ __forceinline__ void layout_byte_rows(const LayoutArgs& a, uint32_t block, uint32_t blocks) {
+    const uint8_t* src = reinterpret_cast<const uint8_t*>(a.src);
+    uint8_t* dst = reinterpret_cast<uint8_t*>(a.dst);
+    const uint32_t chunks = a.ldd / 16;
+    for (uint64_t i = (uint64_t)block * 256 + threadIdx.x; i < a.rows * chunks; i += (uint64_t)blocks * 256) {
+        const uint64_t row = i / chunks;
+        const uint32_t c0 = (uint32_t)(i - row * chunks) * 16;
+        const uint8_t* p = src + row * a.ld + c0;
+        uint2 v[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) v[h] = c0 + 8 * h < a.cols ? load_q_narrow(p + 8 * h, a.cols - c0 - 8 * h, a.grain) : make_uint2(0u, 0u);
+        *reinterpret_cast<uint4*>(dst + row * a.ldd + c0) = make_uint4(v[0].x, v[0].y, v[1].x, v[1].y);
+    }
+}
 // One or both operands of a product: blockIdx.y chooses.
 static __global__ void __launch_bounds__(256) layout_kernel(LayoutArgs a, LayoutArgs b) {
     wait_for_predecessor();
     release_successor();
     layout_rows(blockIdx.y ? b : a, blockIdx.x, gridDim.x);
+}
+static __global__ void __launch_bounds__(256) layout_bytes_kernel(LayoutArgs a, LayoutArgs b) {
+    wait_for_predecessor();
+    release_successor();
+    layout_byte_rows(blockIdx.y ? b : a, blockIdx.x, gridDim.x);
 }
 
 }  // namespace sc

@@ -7,15 +7,20 @@
 
 namespace {
 
-// A stored 16-bit matrix: `rows` rows of `cols` elements, `ld` apart.
+// A stored matrix of 16-bit (or 8-bit) elements: `rows` rows of `cols` elements, `ld` apart.
 struct Stored {
     const void* p;
     uint64_t rows, cols, ld;
-    Stored(const void* p_, uint64_t rows_, uint64_t cols_, uint64_t ld_) : p(p_), rows(rows_), cols(cols_), ld(rows_ > 1 ? ld_ : (cols_ + 7) & ~7ull) {}
+    uint32_t elem;
+    Stored(const void* p_, uint64_t rows_, uint64_t cols_, uint64_t ld_, uint32_t elem_ = 2)
+        : p(p_), rows(rows_), cols(cols_), ld(rows_ > 1 ? ld_ : (cols_ + 15) & ~15ull), elem(elem_) {}
 };
 
 inline uint64_t round8(uint64_t n) { return (n + 7) & ~7ull; }
-inline bool tma_ready(const Stored& m) { return aligned(m.p, 16) && m.ld % 8 == 0; }
+inline bool tma_ready(const Stored& m) { return aligned(m.p, 16) && m.ld * m.elem % 16 == 0; }
+// A copy's rows are 16-byte aligned: elements between them, and its bytes.
+inline uint64_t layout_ld(const Stored& m) { return m.elem == 1 ? (m.cols + 15) & ~15ull : round8(m.cols); }
+inline size_t layout_bytes(const Stored& m) { return (m.rows * layout_ld(m) * m.elem + 255) & ~(size_t)255; }
 inline size_t layout_bytes(uint64_t rows, uint64_t cols) { return (rows * round8(cols) * 2 + 255) & ~(size_t)255; }
 
 inline decltype(&cuTensorMapEncodeTiled) encode_fn() {
@@ -28,13 +33,14 @@ inline decltype(&cuTensorMapEncodeTiled) encode_fn() {
     return fn;
 }
 
-// Boxes of 64 elements (one 128-byte swizzled row) by `box_rows` rows; what lies outside the matrix reads as zero.
+// Boxes of 64 16-bit (128 8-bit) elements, one 128-byte swizzled row, by `box_rows` rows; what lies outside the matrix reads as zero.
 inline bool tile_map(CUtensorMap* map, int type, const Stored& m, uint32_t box_rows) {
     const auto fn = encode_fn();
     if (!fn) return false;
-    const cuuint64_t dims[2] = {m.cols, m.rows}, strides[1] = {m.ld * 2};
-    const cuuint32_t box[2] = {64, box_rows}, steps[2] = {1, 1};
-    return fn(map, type == SC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(m.p), dims, strides, box,
+    const cuuint64_t dims[2] = {m.cols, m.rows}, strides[1] = {m.ld * m.elem};
+    const cuuint32_t box[2] = {128 / m.elem, box_rows}, steps[2] = {1, 1};
+    const CUtensorMapDataType kind = m.elem == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : type == SC_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    return fn(map, kind, 2, const_cast<void*>(m.p), dims, strides, box,
               steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -74,7 +80,7 @@ inline ProductPlan product_plan(sc_ctx* c, int mode, uint64_t rows, uint64_t col
     for (const ProductPlan& p : c->layer_plans)                // a step's few sizes come again and again
         if (p.rows == rows && p.cols == cols && p.red == red && p.mode == mode) return p;
     ProductPlan best{rows, cols, red, mode, 256, 1, 1, (cols + 31) & ~31ull, 0};
-    const uint64_t blocks = ceil_div(red, TC_STEP);
+    const uint64_t blocks = ceil_div(red, product_step(mode));
     if (c->layer_force_bn && !(c->layer_force_cg == 2 && rows <= TC_ROWS)) {
         const uint64_t parts = std::min<uint64_t>(c->layer_force_parts, blocks), bytes = parts > 1 ? parts * rows * best.part_ld * sizeof(float) : 0;
         best.bn = c->layer_force_bn; best.cg = c->layer_force_cg;
@@ -119,7 +125,7 @@ int launch_tiles(sc_ctx* c, const CUtensorMap& ma, const CUtensorMap& mb, const 
 
 template <typename T, int MODE>
 int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red, Epilogue ep, size_t used, cudaStream_t st) {
-    constexpr bool A_MN = MODE == PRODUCT_WEIGHT, B_MN = MODE != PRODUCT_FORWARD;
+    constexpr bool A_MN = MODE == PRODUCT_WEIGHT, B_MN = epilogue_of(MODE) != PRODUCT_FORWARD;
     const uint64_t chunks = 4 * ckpt_groups(ep.cols);
     const uint32_t join_grid = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(ep.rows * chunks, 256), (uint64_t)c->sm_count * 8));
     if (red == 0) {
@@ -130,7 +136,7 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
     const ProductPlan p = product_plan(c, MODE, ep.rows, ep.cols, red);
     const uint64_t tiles = ceil_div(ep.rows, TC_ROWS * p.cg) * ceil_div(ep.cols, p.bn);
     if (tiles * p.splits > 0x7FFFFFFFull) return SC_ERR_RANGE;
-    const size_t copy_a = tma_ready(A) ? 0 : layout_bytes(A.rows, A.cols), copy_b = tma_ready(B) ? 0 : layout_bytes(B.rows, B.cols);
+    const size_t copy_a = tma_ready(A) ? 0 : layout_bytes(A), copy_b = tma_ready(B) ? 0 : layout_bytes(B);
     const size_t need = used + p.bytes + copy_a + copy_b;
     if (need) if (const int rc = layer_scratch(c, need, st)) return rc;
     unsigned char* at = need ? c->d_layer + TICKET_BYTES + used : nullptr;
@@ -141,22 +147,22 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
     uint64_t work = 0;
     for (Stored* m : {&A, &B}) {
         if (tma_ready(*m)) continue;
-        const uint32_t ldd = (uint32_t)round8(m->cols);
+        const uint32_t ldd = (uint32_t)layout_ld(*m);
         copies[ncopies++] = LayoutArgs{static_cast<const uint16_t*>(m->p), reinterpret_cast<uint16_t*>(at), m->ld, m->rows, (uint32_t)m->cols, ldd,
-                                       std::min(4u, grain_of(m->p, m->rows > 1 ? m->ld : 0, 2, 8))};
-        work = std::max(work, m->rows * (ldd / 8));
+                                       std::min(4u, grain_of(m->p, m->rows > 1 ? m->ld : 0, m->elem, 8))};
+        work = std::max(work, m->rows * (ldd * m->elem / 16));
         m->p = at; m->ld = ldd;
-        at += layout_bytes(m->rows, m->cols);
+        at += layout_bytes(*m);
     }
     if (ncopies) {
         Launch l(c, KIND_LAYER_LAYOUT, st);
-        launch(layout_kernel, dim3((uint32_t)std::min<uint64_t>(ceil_div(work, 256), (uint64_t)c->sm_count * 8), ncopies), 256, 0, 1, st, copies[0],
+        launch(MODE == PRODUCT_QUANTIZED ? layout_bytes_kernel : layout_kernel, dim3((uint32_t)std::min<uint64_t>(ceil_div(work, 256), (uint64_t)c->sm_count * 8), ncopies), 256, 0, 1, st, copies[0],
                copies[ncopies - 1]);
     }
     TcArgs a{};
     a.tiles_i = (uint32_t)ceil_div(ep.rows, TC_ROWS * p.cg); a.tiles_j = (uint32_t)ceil_div(ep.cols, p.bn); a.tiles = (uint32_t)tiles;
-    a.splits = p.splits; a.blocks = (uint32_t)ceil_div(red, TC_STEP);
-    a.idesc = mma_idesc(TC_ROWS * p.cg, p.bn, type == SC_BF16, A_MN, B_MN);
+    a.splits = p.splits; a.blocks = (uint32_t)ceil_div(red, product_step(MODE));
+    a.idesc = MODE == PRODUCT_QUANTIZED ? mma_idesc_i8(TC_ROWS * p.cg, p.bn) : mma_idesc(TC_ROWS * p.cg, p.bn, type == SC_BF16, A_MN, B_MN);
     a.a_box_rows = A_MN ? 64u : (uint32_t)std::min<uint64_t>(TC_ROWS, round8(ep.rows));
     a.part_ld = (uint32_t)p.part_ld; a.part_stride = ep.rows * p.part_ld; a.partial = partial; a.status = c->d_status;
     // partial sums are whole to the next multiple of 32 columns: a checkpoint group's maximum is taken over all of its columns
@@ -165,7 +171,7 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
     a.tma_out = p.splits > 1 || (MODE == PRODUCT_WEIGHT && ep.grain_out >= 4 && ep.cols % 4 == 0);
     if constexpr (MODE != PRODUCT_WEIGHT)
         // a warp's 128 columns of a 256-wide tile are four whole groups of the row
-        ep.scales_by4 = MODE == PRODUCT_FORWARD && p.bn == 256 && ep.cols % 128 == 0 && aligned(ep.scales, 4);
+        ep.scales_by4 = epilogue_of(MODE) == PRODUCT_FORWARD && p.bn == 256 && ep.cols % 128 == 0 && aligned(ep.scales, 4);
     if constexpr (MODE != PRODUCT_WEIGHT)
         a.rows_form = p.splits == 1 && ep.cols % 8 == 0 && ep.grain_out >= 8 && (!ep.residual || ep.grain_res >= 8) && (!ep.q || ep.grain_q >= 8);
     CUtensorMap ma, mb, mo{};

@@ -1,0 +1,47 @@
+// Host side of the linear layer on 8-bit integers, declared in include/sparsecomm.h.
+#include "sc_product_host.cuh"
+
+namespace {
+
+constexpr uint64_t MAX_TERMS = 131071;        // products of up to 2^14 that a 32-bit integer sum holds: 131071 2^14 < 2^31
+
+template <typename T>
+int run(sc_ctx* c, int type, const Stored& x, const Stored& w, const Epilogue& ep, cudaStream_t st) {
+    // an empty sum has nothing to scale: the forward product's epilogue alone
+    if (x.cols == 0) return run_product<T, PRODUCT_FORWARD>(c, KIND_LINEAR_QUANTIZED, type, x, w, 0, ep, 0, st);
+    return run_product<T, PRODUCT_QUANTIZED>(c, KIND_LINEAR_QUANTIZED, type, x, w, x.cols, ep, 0, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+int sc_linear_quantized(sc_ctx* ctx, int type, int act, const int8_t* x, size_t ldx, const float* x_scales, const int8_t* w, size_t ldw,
+                        const float* w_scales, const void* bias, const void* residual, size_t ldr, size_t M, size_t N, size_t K, void* y, size_t ldy,
+                        int8_t* q, uint8_t* scales, void* stream) {
+    if (!ctx) return SC_ERR_INVALID;
+    if (!known_type(type)) return SC_ERR_UNSUPPORTED;
+    if (!known_act(act) || (q == nullptr) != (scales == nullptr) || !aligned(bias, 2) || !aligned(x_scales, 4) || !aligned(w_scales, 4)) return SC_ERR_INVALID;
+    if (const int rc = check_matrix(x, ldx, M, K, 1)) return rc;
+    if (const int rc = check_matrix(w, ldw, N, K, 1)) return rc;
+    if (const int rc = check_matrix(y, ldy, M, N, 2)) return rc;
+    if (residual) if (const int rc = check_matrix(residual, ldr, M, N, 2)) return rc;
+    if (K > MAX_TERMS) return SC_ERR_RANGE;
+    if (M == 0 || N == 0) return SC_OK;
+    if (K && (!x_scales || !w_scales)) return SC_ERR_INVALID;
+    DeviceGuard guard(ctx->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    Epilogue ep{};
+    ep.bias = bias; ep.residual = residual; ep.ldr = ldr; ep.out = y; ep.ldo = ldy; ep.rows = M; ep.cols = (uint32_t)N;
+    ep.q = reinterpret_cast<uint8_t*>(q); ep.scales = scales; ep.groups = (uint32_t)ckpt_groups(N); ep.act = act;
+    ep.row_scale = x_scales; ep.col_scale = w_scales;
+    ep.grain_out = grain_of(y, M > 1 ? ldy : 0, 2, 8); ep.grain_res = grain_of(residual, M > 1 ? ldr : 0, 2, 8);
+    ep.grain_q = grain_of(q, M > 1 ? N : 0, 1, 32); ep.grain_bias = grain_of(bias, 0, 2, 8);
+    const Stored xs{x, M, K, ldx, 1}, ws{w, N, K, ldw, 1};
+    const int rc = type == SC_BF16 ? run<__nv_bfloat16>(ctx, type, xs, ws, ep, st) : run<__half>(ctx, type, xs, ws, ep, st);
+    if (rc) return rc;
+    SC_CUDA(cudaGetLastError());
+    return SC_OK;
+}
+
+}  // extern "C"

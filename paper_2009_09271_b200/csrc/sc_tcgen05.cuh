@@ -129,6 +129,16 @@ __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint
         asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
+// 8-bit integers, 32 terms of the reduction an instruction, exact 32-bit integer sums.
+template <int CG>
+__device__ __forceinline__ void mma_i8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+    if constexpr (CG == 1)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+}
 // Arrives at the barrier (in both CTAs of a pair) when the matrix instructions issued so far have completed.
 template <int CG>
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
@@ -170,6 +180,10 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint
 __host__ __device__ inline uint32_t mma_idesc(int m, int n, bool bf16, bool a_mn, bool b_mn) {
     return 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (a_mn ? 1u : 0u) << 15 | (b_mn ? 1u : 0u) << 16 |
            (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
+}
+// The same for signed 8-bit integers (type 1) and 32-bit integer accumulators (type 2); both operands' reduction index is contiguous.
+__host__ __device__ inline uint32_t mma_idesc_i8(int m, int n) {
+    return 2u << 4 | 1u << 7 | 1u << 10 | (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
 }
 
 }  // namespace sc
