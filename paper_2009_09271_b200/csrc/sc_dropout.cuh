@@ -5,8 +5,8 @@
 // the reciprocal of the probability that the bits really give, so that the mean stays the input's.  The gradient is the same
 // call on the gradient.
 #pragma once
-#include "sc_checkpoint.cuh"
 #include "sc_common.cuh"
+#include "sc_rows.cuh"
 
 namespace sc {
 
@@ -30,29 +30,77 @@ __device__ __forceinline__ void drop8(const Drop& d, uint64_t row, uint32_t c0, 
     }
 }
 
+// The same from any column, before the row's first as well: the elements of other rows may come out as anything.
+__device__ __forceinline__ void drop8_any(const Drop& d, uint64_t row, int c0, float f[8]) {
+    const uint64_t at = row * d.groups + (uint64_t)(int64_t)(c0 >> 2);
+    const uint32_t by = 16 * (c0 & 3);
+    uint64_t w[2] = {mix64(d.key, at), mix64(d.key, at + 1)};
+    if (by) {
+        const uint64_t next = mix64(d.key, at + 2);
+        w[0] = w[0] >> by | w[1] << (64 - by);
+        w[1] = w[1] >> by | next << (64 - by);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t bits = (uint32_t)(w[i >> 2] >> (16 * (i & 3))) & 0xFFFFu;
+        f[i] = bits >= d.cut ? f[i] * d.scale : 0.0f;
+    }
+}
+template <bool WIDE>
+__device__ __forceinline__ void drop_pairs(const Drop& d, uint64_t row, int c0, Pair v[4]) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { const float2 p = both(v[i]); f[2 * i] = p.x; f[2 * i + 1] = p.y; }
+    if constexpr (WIDE) drop8(d, row, (uint32_t)c0, f);
+    else drop8_any(d, row, c0, f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pair(f[2 * i], f[2 * i + 1]);
+}
+
+// y = residual + dropout(x), eight elements a thread and item, several items in flight.
 struct DropArgs {
-    uint64_t ldx, ldr, ldy;
-    uint32_t grain_x, grain_r, grain_y;
+    InRows x, residual;
+    OutRows y;
+    Phase phase;
     Drop drop;
 };
-
-// y = residual + dropout(x): one pass, eight elements a thread and item.
-template <typename T>
-__global__ void __launch_bounds__(CKPT_THREADS) dropout_kernel(const T* x, const T* residual, T* y, ItemWalk w, DropArgs a) {
+constexpr int DROP_UNROLL = 4;
+template <typename T, bool RESIDUAL, bool WIDE>
+__global__ void __launch_bounds__(CKPT_THREADS) dropout_kernel(ItemWalk w, DropArgs a) {
     wait_for_predecessor();
     release_successor();
     const uint64_t first = (uint64_t)blockIdx.x * CKPT_THREADS + threadIdx.x, stride = (uint64_t)gridDim.x * CKPT_THREADS;
+    const int cols = (int)w.cols;
     ItemAt at(w, first);
-    for (uint64_t i = first; i < w.total; i += stride, at.next(w)) {
-        const uint32_t c0 = at.item * 8;
-        float f[8], r[8];
-        to_floats(load8(x + at.row * a.ldx, c0, w.cols, a.grain_x), f);
-        if (residual) to_floats(load8(residual + at.row * a.ldr, c0, w.cols, a.grain_r), r);
-        if (a.drop.cut) drop8(a.drop, at.row, c0, f);
-        if (residual)
+    for (uint64_t base = first; base < w.total; base += stride * DROP_UNROLL) {
+        Raw8<T> in[DROP_UNROLL], res[DROP_UNROLL];
+        ItemAt from = at;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] += r[k];
-        store8(y + at.row * a.ldy, c0, w.cols, a.grain_y, f);
+        for (int u = 0; u < DROP_UNROLL; ++u) {
+            if (base + u * stride < w.total) {
+                const int c0 = chunk_col(at.item, row_shift<WIDE>(a.phase, at.row), w.cols);
+                in[u] = row_load8<T, WIDE>(a.x, at.row, c0, cols);
+                if (RESIDUAL) res[u] = row_load8<T, WIDE>(a.residual, at.row, c0, cols);
+            }
+            at.next(w);
+        }
+#pragma unroll
+        for (int u = 0; u < DROP_UNROLL; ++u) {
+            if (base + u * stride < w.total) {
+                const int c0 = chunk_col(from.item, row_shift<WIDE>(a.phase, from.row), w.cols);
+                Pair v[4];
+                to_pairs(in[u], v);
+                if (a.drop.cut) drop_pairs<WIDE>(a.drop, from.row, c0, v);
+                if constexpr (RESIDUAL) {
+                    Pair r[4];
+                    to_pairs(res[u], r);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = v[k] + r[k];
+                }
+                row_store8<T, WIDE>(a.y, from.row, c0, cols, v);
+            }
+            from.next(w);
+        }
     }
 }
 

@@ -1,4 +1,5 @@
 // Host side of 8-bit rows, the root-mean-square norm and dropout, declared in include/sparsecomm.h.
+#include <atomic>
 #include <cmath>
 
 #include "sc_layer_host.cuh"
@@ -6,16 +7,14 @@
 
 namespace {
 
-// Items of eight elements, and the distances that a grid of `item_grid` CTAs walks in.
-uint32_t item_grid(const sc_ctx* c, uint64_t total) {
-    return (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(total, CKPT_THREADS), (uint64_t)c->sm_count * 8));
-}
-ItemWalk item_walk(const sc_ctx* c, size_t rows, size_t cols) {
+// The walk of a grid over `items` items a row, and the grid: enough CTAs for every SM, no more than have work.
+ItemWalk item_walk(const sc_ctx* c, size_t rows, size_t cols, uint64_t items, uint32_t& grid) {
     ItemWalk w{};
     w.cols = (uint32_t)cols;
-    w.items = (uint32_t)ceil_div(cols, 8);
+    w.items = (uint32_t)items;
     w.total = (uint64_t)rows * w.items;
-    const uint64_t stride = (uint64_t)item_grid(c, w.total) * CKPT_THREADS;
+    grid = (uint32_t)std::max<uint64_t>(1, std::min<uint64_t>(ceil_div(w.total, CKPT_THREADS), (uint64_t)c->sm_count * 8));
+    const uint64_t stride = (uint64_t)grid * CKPT_THREADS;
     w.stride_rows = stride / w.items;
     w.stride_items = (uint32_t)(stride % w.items);
     return w;
@@ -23,6 +22,20 @@ ItemWalk item_walk(const sc_ctx* c, size_t rows, size_t cols) {
 uint32_t row_grid(const sc_ctx* c, size_t rows) { return (uint32_t)std::min<uint64_t>(rows, (uint64_t)c->sm_count * 8); }
 
 inline uint32_t grain16(const void* p, size_t rows, size_t ld) { return grain_of(p, rows > 1 ? ld : 0, 2, 8); }
+
+// The shifts of a matrix's rows, and whether another's are the same (a matrix that is not there has any).
+Phase phase_of(const void* p, size_t rows, size_t ld, size_t elem) {
+    return Phase{(uint32_t)(reinterpret_cast<uintptr_t>(p) / elem) & 7u, rows > 1 ? (uint32_t)ld & 7u : 0u};
+}
+bool in_phase(const Phase& phase, const void* p, size_t rows, size_t ld, size_t elem) {
+    const Phase own = phase_of(p, rows, ld, elem);
+    return !p || (own.first == phase.first && own.ld == phase.ld);
+}
+InRows in_rows(const Phase& phase, const void* p, size_t rows, size_t cols, size_t ld, size_t elem = 2) {
+    return InRows{p, ld, (uint64_t)(rows - 1) * (rows > 1 ? ld : 0) + cols, in_phase(phase, p, rows, ld, elem)};
+}
+OutRows out_rows(const Phase& phase, void* p, size_t rows, size_t ld, size_t elem = 2) { return OutRows{p, ld, in_phase(phase, p, rows, ld, elem)}; }
+inline bool unshifted(const Phase& phase, size_t cols) { return phase.first == 0 && phase.ld == 0 && cols % 8 == 0; }
 
 // The cut that p stands for; false where p is no probability.
 bool drop_of(double p, uint64_t seed, size_t cols, Drop& d) {
@@ -35,7 +48,70 @@ bool drop_of(double p, uint64_t seed, size_t cols, Drop& d) {
 }
 inline bool eps_ok(float eps) { return eps >= 0.0f && eps <= 3.402823466e38f; }
 
-// Column sums of the norm's gradient: runs of rows as for the activation's gradient.
+// Runs f(team, elements / 8 a thread) for the threads that hold a row of `cols` elements, shifted by up to 7; false where it is too long for
+// them.
+template <typename F>
+bool with_team(size_t cols, F&& f) {
+    using std::integral_constant;
+#define SC_TEAM(TEAM, V) if (cols <= (size_t)TEAM * V * 8) { f(integral_constant<int, TEAM>(), integral_constant<int, V>()); return true; }
+    SC_TEAM(32, 1) SC_TEAM(32, 2) SC_TEAM(32, 4) SC_TEAM(128, 2) SC_TEAM(128, 4) SC_TEAM(256, 4) SC_TEAM(512, 4) SC_TEAM(1024, 4)
+#undef SC_TEAM
+    return false;
+}
+inline uint32_t team_grid(int team, size_t rows) { return (uint32_t)(team == 32 ? ceil_div(rows, 8) : rows); }
+inline int team_threads(int team) { return team == 32 ? 256 : team; }
+
+template <typename T>
+void run_quantize(sc_ctx* c, const QuantizeArgs& a, float* scales, cudaStream_t st) {
+    const bool wide = unshifted(a.phase, a.cols) && a.q.vec;
+    const bool held = with_team(wide ? a.cols : a.cols + 7ull, [&](auto team, auto v) {
+        constexpr int TEAM = decltype(team)::value, V = decltype(v)::value;
+        if (wide) launch(quantize_rows_kernel<T, TEAM, V, true>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
+        else launch(quantize_rows_kernel<T, TEAM, V, false>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
+    });
+    if (!held) launch(quantize_kernel<T>, row_grid(c, a.rows), NORM_THREADS, 0, 1, st, a, scales);
+}
+
+template <typename T>
+void run_dequantize(sc_ctx* c, const void* q, size_t ldq, const float* scales, size_t rows, size_t cols, void* out, size_t ldo, cudaStream_t st) {
+    uint32_t grid = 0;
+    const uint32_t grain_x = grain_of(out, rows > 1 ? ldo : 0, sizeof(T), 16), grain_q = grain_of(q, rows > 1 ? ldq : 0, 1, 16);
+    if (cols % 16 == 0 && grain_q >= 16 && grain_x * sizeof(T) >= 32) {
+        const ItemWalk w = item_walk(c, rows, cols, cols / 16, grid);
+        launch(dequantize_kernel<T>, grid, CKPT_THREADS, 0, 1, st, static_cast<const uint8_t*>(q), ldq, scales, w, static_cast<T*>(out), ldo);
+    } else {
+        const Phase phase = phase_of(out, rows, ldo, sizeof(T));
+        const ItemWalk w = item_walk(c, rows, cols, ceil_div(cols + 7, 8), grid);
+        launch(dequantize_any_kernel<T>, grid, CKPT_THREADS, 0, 1, st, in_rows(phase, q, rows, cols, ldq, 1), scales, w, phase, out_rows(phase, out, rows, ldo, sizeof(T)));
+    }
+}
+
+template <typename T>
+void run_dropout(sc_ctx* c, size_t rows, size_t cols, const DropArgs& a, cudaStream_t st) {
+    uint32_t grid = 0;
+    const bool wide = unshifted(a.phase, cols) && a.residual.vec && a.y.vec;
+    const ItemWalk w = item_walk(c, rows, cols, ceil_div(wide ? cols : cols + 7, 8), grid);
+#define SC_DROPOUT(RESIDUAL, WIDE) launch(dropout_kernel<T, RESIDUAL, WIDE>, grid, CKPT_THREADS, 0, 1, st, w, a)
+    if (a.residual.p) { if (wide) SC_DROPOUT(true, true); else SC_DROPOUT(true, false); }
+    else if (wide) SC_DROPOUT(false, true);
+    else SC_DROPOUT(false, false);
+#undef SC_DROPOUT
+}
+
+template <typename T, bool DROP>
+void run_norm(sc_ctx* c, const NormArgs& a, float* scales, cudaStream_t st) {
+    const bool wide = unshifted(a.phase, a.cols) && a.residual.vec && a.gamma.vec && a.h.vec && a.y.vec && a.q.vec;
+    const bool held = with_team(wide ? a.cols : a.cols + 7ull, [&](auto team, auto v) {
+        constexpr int TEAM = decltype(team)::value, V = decltype(v)::value;
+        if (wide) launch(rms_norm_rows_kernel<T, TEAM, V, DROP, true>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
+        else launch(rms_norm_rows_kernel<T, TEAM, V, DROP, false>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
+    });
+    if (!held) launch(rms_norm_kernel<T>, row_grid(c, a.rows), NORM_THREADS, 0, 1, st, a, scales);
+}
+
+constexpr uint32_t RING_BYTES = 208 * 1024;          // shared memory for the stages of the norm gradient's rings on an SM
+
+// Column sums of the gradient of rows too long for a ring: runs of rows as for the activation's gradient.
 struct StripPlan { uint32_t strips, runs, run_rows; size_t partial, stats; };
 StripPlan strip_plan(const sc_ctx* c, size_t rows, size_t cols) {
     StripPlan p{};
@@ -46,6 +122,76 @@ StripPlan strip_plan(const sc_ctx* c, size_t rows, size_t cols) {
     p.partial = p.runs > 1 ? ((size_t)p.runs * cols * sizeof(float) + 255) & ~(size_t)255 : 0;
     p.stats = rows * sizeof(float2);
     return p;
+}
+
+
+// Shared memory of the ring kernels: all of a CTA's, once per build and device.
+template <typename T, int TEAM, int V, bool DROP>
+int ring_ready(const sc_ctx* c) {
+    static std::atomic<uint64_t> ready{0};
+    const uint64_t bit = c->device < 64 ? 1ull << c->device : 0;
+    if (!(ready.load(std::memory_order_relaxed) & bit)) {
+        SC_CUDA(cudaFuncSetAttribute(norm_grad_ring_kernel<T, TEAM, V, DROP>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES));
+        ready.fetch_or(bit, std::memory_order_relaxed);
+    }
+    return SC_OK;
+}
+
+template <typename T, int TEAM, int V, bool DROP>
+int launch_norm_grad(sc_ctx* c, NormGradArgs a, bool wide, float* dgamma, cudaStream_t st) {
+    constexpr uint32_t TEAMS = TEAM == 32 ? 8 : 1, FIT = TEAM == 32 ? 2 : 512 / TEAM;      // teams a CTA, CTAs an SM by their registers
+    NormRing ring{};
+    uint32_t per_sm = FIT;
+    if (wide) {
+        // as many stages as leave room for every CTA that fits otherwise, two at least
+        ring.row_bytes = a.cols * 2; ring.operands = a.residual.p ? 3 : 2;
+        const uint32_t stage = TEAMS * ring.row_bytes * ring.operands;
+        ring.stages = std::min(RING_MOST_STAGES, std::max(2u, RING_BYTES / FIT / stage));
+        per_sm = std::max(1u, std::min(FIT, RING_BYTES / (ring.stages * stage)));
+    }
+    uint32_t grid = (uint32_t)std::min<uint64_t>(ceil_div(a.rows, TEAMS), (uint64_t)c->sm_count * per_sm);
+    if (grid < ceil_div(a.rows, TEAMS) && grid >= 8) grid &= ~7u;                          // a team's rows are a multiple of 8 apart
+    a.part_ld = ((uint64_t)a.cols + 7) & ~7ull;
+    float* partial = nullptr;
+    if (dgamma) {
+        if (const int rc = layer_scratch(c, grid * a.part_ld * sizeof(float), st)) return rc;
+        partial = reinterpret_cast<float*>(c->d_layer + TICKET_BYTES);
+    }
+    if (wide) {
+        if (const int rc = ring_ready<T, TEAM, V, DROP>(c)) return rc;
+        Launch l(c, KIND_RMS_NORM_GRAD, st);
+        launch(norm_grad_ring_kernel<T, TEAM, V, DROP>, grid, TEAMS * TEAM, ring.stages * ring.row_bytes * ring.operands * TEAMS, 1, st, a, ring, partial, c->d_status);
+    } else {
+        Launch l(c, KIND_RMS_NORM_GRAD, st);
+        launch(norm_grad_rows_kernel<T, TEAM, V, DROP>, grid, TEAMS * TEAM, 0, 1, st, a, partial);
+    }
+    if (dgamma) {
+        Launch l(c, KIND_RMS_NORM_GRAD, st);
+        launch(norm_join_kernel, (uint32_t)ceil_div(a.cols, 32), 256, 0, 1, st, partial, grid, a.part_ld, a.cols, dgamma, a.accumulate);
+    }
+    return SC_OK;
+}
+
+template <typename T>
+int run_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) {
+    const bool wide = unshifted(a.phase, a.cols) && a.h.vec && a.gamma.vec && a.residual.vec && a.dh.vec && a.dx.vec, drop = a.drop.cut && a.dx.p;
+    const uint64_t held = wide ? a.cols : a.cols + 7ull;
+#define SC_TEAM(TEAM, V) \
+    if (held <= TEAM * V * 8) return drop ? launch_norm_grad<T, TEAM, V, true>(c, a, wide, dgamma, st) : launch_norm_grad<T, TEAM, V, false>(c, a, wide, dgamma, st);
+    SC_TEAM(32, 1) SC_TEAM(32, 2) SC_TEAM(32, 4) SC_TEAM(128, 2) SC_TEAM(256, 2) SC_TEAM(256, 4) SC_TEAM(512, 4)
+#undef SC_TEAM
+    const StripPlan plan = strip_plan(c, a.rows, a.cols);
+    if (const int rc = layer_scratch(c, plan.partial + plan.stats, st)) return rc;
+    a.runs = plan.runs; a.run_rows = plan.run_rows;
+    float* partial = reinterpret_cast<float*>(c->d_layer + TICKET_BYTES);
+    float2* stats = reinterpret_cast<float2*>(c->d_layer + TICKET_BYTES + plan.partial);
+    {
+        Launch l(c, KIND_RMS_NORM_GRAD, st);
+        launch(norm_stats_kernel<T>, row_grid(c, a.rows), NORM_THREADS, 0, 1, st, a, stats);
+    }
+    Launch l(c, KIND_RMS_NORM_GRAD, st);
+    launch(norm_strips_kernel<T>, dim3(plan.strips, plan.runs), CKPT_THREADS, 0, 1, st, a, stats, partial, reinterpret_cast<uint32_t*>(c->d_layer), dgamma);
+    return SC_OK;
 }
 
 }  // namespace
@@ -62,16 +208,16 @@ int sc_quantize(sc_ctx* ctx, int type, const void* x, size_t ldx, size_t rows, s
     DeviceGuard guard(ctx->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     QuantizeArgs a{};
-    a.rows = rows; a.ldx = ldx; a.ldq = ldq; a.cols = (uint32_t)cols;
+    a.rows = rows; a.cols = (uint32_t)cols;
     a.grain_x = grain_of(x, rows > 1 ? ldx : 0, type_bytes(type), 8);
     a.grain_q = grain_of(q, rows > 1 ? ldq : 0, 1, 8);
-    uint8_t* qb = reinterpret_cast<uint8_t*>(q);
+    a.phase = phase_of(x, rows, ldx, type_bytes(type));
+    a.x = in_rows(a.phase, x, rows, cols, ldx, type_bytes(type));
+    a.q = out_rows(a.phase, q, rows, ldq, 1);
     Launch l(ctx, KIND_QUANTIZE, st);
-#define SC_QUANTIZE(T) launch(quantize_kernel<T>, row_grid(ctx, rows), NORM_THREADS, 0, 1, st, static_cast<const T*>(x), a, qb, scales)
-    if (type == SC_BF16) SC_QUANTIZE(__nv_bfloat16);
-    else if (type == SC_F16) SC_QUANTIZE(__half);
-    else SC_QUANTIZE(float);
-#undef SC_QUANTIZE
+    if (type == SC_BF16) run_quantize<__nv_bfloat16>(ctx, a, scales, st);
+    else if (type == SC_F16) run_quantize<__half>(ctx, a, scales, st);
+    else run_quantize<float>(ctx, a, scales, st);
     SC_CUDA(cudaGetLastError());
     return SC_OK;
 }
@@ -86,16 +232,10 @@ int sc_dequantize(sc_ctx* ctx, int type, const int8_t* q, size_t ldq, const floa
     if (!scales || !aligned(scales, 4)) return SC_ERR_INVALID;
     DeviceGuard guard(ctx->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    ItemWalk w = item_walk(ctx, rows, cols);
-    w.grain_x = grain_of(out, rows > 1 ? ldo : 0, type_bytes(type), 8);
-    w.grain_q = grain_of(q, rows > 1 ? ldq : 0, 1, 8);
-    const uint8_t* qb = reinterpret_cast<const uint8_t*>(q);
     Launch l(ctx, KIND_DEQUANTIZE, st);
-#define SC_DEQUANTIZE(T) launch(dequantize_kernel<T>, item_grid(ctx, w.total), CKPT_THREADS, 0, 1, st, qb, ldq, scales, w, static_cast<T*>(out), ldo)
-    if (type == SC_BF16) SC_DEQUANTIZE(__nv_bfloat16);
-    else if (type == SC_F16) SC_DEQUANTIZE(__half);
-    else SC_DEQUANTIZE(float);
-#undef SC_DEQUANTIZE
+    if (type == SC_BF16) run_dequantize<__nv_bfloat16>(ctx, q, ldq, scales, rows, cols, out, ldo, st);
+    else if (type == SC_F16) run_dequantize<__half>(ctx, q, ldq, scales, rows, cols, out, ldo, st);
+    else run_dequantize<float>(ctx, q, ldq, scales, rows, cols, out, ldo, st);
     SC_CUDA(cudaGetLastError());
     return SC_OK;
 }
@@ -112,15 +252,11 @@ int sc_dropout(sc_ctx* ctx, int type, const void* x, size_t ldx, const void* res
     if (rows == 0 || cols == 0) return SC_OK;
     DeviceGuard guard(ctx->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const ItemWalk w = item_walk(ctx, rows, cols);
-    a.ldx = ldx; a.ldr = ldr; a.ldy = ldy;
-    a.grain_x = grain16(x, rows, ldx); a.grain_r = grain16(residual, rows, ldr); a.grain_y = grain16(y, rows, ldy);
+    a.phase = phase_of(x, rows, ldx, 2);
+    a.x = in_rows(a.phase, x, rows, cols, ldx); a.residual = in_rows(a.phase, residual, rows, cols, ldr); a.y = out_rows(a.phase, y, rows, ldy);
     Launch l(ctx, KIND_DROPOUT, st);
-#define SC_DROPOUT(T) launch(dropout_kernel<T>, item_grid(ctx, w.total), CKPT_THREADS, 0, 1, st, static_cast<const T*>(x), static_cast<const T*>(residual), \
-                             static_cast<T*>(y), w, a)
-    if (type == SC_BF16) SC_DROPOUT(__nv_bfloat16);
-    else SC_DROPOUT(__half);
-#undef SC_DROPOUT
+    if (type == SC_BF16) run_dropout<__nv_bfloat16>(ctx, rows, cols, a, st);
+    else run_dropout<__half>(ctx, rows, cols, a, st);
     SC_CUDA(cudaGetLastError());
     return SC_OK;
 }
@@ -141,17 +277,18 @@ int sc_rms_norm(sc_ctx* ctx, int type, const void* x, size_t ldx, const void* re
     if (!gamma || !aligned(gamma, 2) || !aligned(scales, 4) || (q == nullptr) != (scales == nullptr) || (!y && !q)) return SC_ERR_INVALID;
     DeviceGuard guard(ctx->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    a.rows = rows; a.ldx = ldx; a.ldr = ldr; a.ldh = ldh; a.ldy = ldy; a.ldq = ldq; a.cols = (uint32_t)cols;
+    a.rows = rows; a.cols = (uint32_t)cols;
     a.grain_x = grain16(x, rows, ldx); a.grain_r = grain16(residual, rows, ldr); a.grain_g = grain_of(gamma, 0, 2, 8);
     a.grain_h = grain16(h, rows, ldh); a.grain_y = grain16(y, rows, ldy); a.grain_q = grain_of(q, rows > 1 ? ldq : 0, 1, 8);
     a.eps = eps; a.mean = 1.0f / (float)cols;
-    uint8_t* qb = reinterpret_cast<uint8_t*>(q);
+    a.phase = phase_of(x, rows, ldx, 2);
+    a.x = in_rows(a.phase, x, rows, cols, ldx); a.residual = in_rows(a.phase, residual, rows, cols, ldr);
+    a.gamma = InRows{gamma, 0, cols, aligned(gamma, 16)};
+    a.h = out_rows(a.phase, h, rows, ldh); a.y = out_rows(a.phase, y, rows, ldy); a.q = out_rows(a.phase, q, rows, ldq, 1);
     Launch l(ctx, KIND_RMS_NORM, st);
-#define SC_NORM(T) launch(rms_norm_kernel<T>, row_grid(ctx, rows), NORM_THREADS, 0, 1, st, static_cast<const T*>(x), static_cast<const T*>(residual), \
-                          static_cast<const T*>(gamma), a, static_cast<T*>(h), static_cast<T*>(y), qb, scales)
-    if (type == SC_BF16) SC_NORM(__nv_bfloat16);
-    else SC_NORM(__half);
-#undef SC_NORM
+    if (type == SC_BF16) { if (a.drop.cut) run_norm<__nv_bfloat16, true>(ctx, a, scales, st); else run_norm<__nv_bfloat16, false>(ctx, a, scales, st); }
+    else if (a.drop.cut) run_norm<__half, true>(ctx, a, scales, st);
+    else run_norm<__half, false>(ctx, a, scales, st);
     SC_CUDA(cudaGetLastError());
     return SC_OK;
 }
@@ -177,31 +314,16 @@ int sc_rms_norm_grad(sc_ctx* ctx, int type, const void* dy, size_t lddy, const v
         return SC_OK;
     }
     if (!gamma || !aligned(gamma, 2) || (!dh && !dx && !dgamma)) return SC_ERR_INVALID;
-    const StripPlan plan = strip_plan(ctx, rows, cols);
-    if (const int rc = layer_scratch(ctx, plan.partial + plan.stats, st)) return rc;
-    a.rows = rows; a.lddy = lddy; a.ldh = ldh; a.ldr = ldr; a.lddh = lddh; a.lddx = lddx; a.cols = (uint32_t)cols;
+    a.rows = rows; a.cols = (uint32_t)cols;
     a.grain_y = grain16(dy, rows, lddy); a.grain_h = grain16(h, rows, ldh); a.grain_g = grain_of(gamma, 0, 2, 8);
     a.grain_r = grain16(residual, rows, ldr); a.grain_dh = grain16(dh, rows, lddh); a.grain_dx = grain16(dx, rows, lddx);
-    a.runs = plan.runs; a.run_rows = plan.run_rows; a.accumulate = accumulate ? 1u : 0u;
-    a.eps = eps; a.mean = 1.0f / (float)cols;
-    float* partial = reinterpret_cast<float*>(ctx->d_layer + TICKET_BYTES);
-    float2* stats = reinterpret_cast<float2*>(ctx->d_layer + TICKET_BYTES + plan.partial);
-    uint32_t* tickets = reinterpret_cast<uint32_t*>(ctx->d_layer);
-    const dim3 grid(plan.strips, plan.runs);
-#define SC_NORM_GRAD(T)                                                                                                                        \
-    do {                                                                                                                                       \
-        const T *dyp = static_cast<const T*>(dy), *hp = static_cast<const T*>(h), *gp = static_cast<const T*>(gamma);                          \
-        {                                                                                                                                      \
-            Launch l(ctx, KIND_RMS_NORM_GRAD, st);                                                                                             \
-            launch(norm_stats_kernel<T>, row_grid(ctx, rows), NORM_THREADS, 0, 1, st, dyp, hp, gp, a, stats);                                  \
-        }                                                                                                                                      \
-        Launch l(ctx, KIND_RMS_NORM_GRAD, st);                                                                                                 \
-        launch(norm_strips_kernel<T>, grid, CKPT_THREADS, 0, 1, st, dyp, hp, gp, static_cast<const T*>(residual), a, stats, static_cast<T*>(dh), \
-               static_cast<T*>(dx), partial, tickets, dgamma);                                                                                 \
-    } while (0)
-    if (type == SC_BF16) SC_NORM_GRAD(__nv_bfloat16);
-    else SC_NORM_GRAD(__half);
-#undef SC_NORM_GRAD
+    a.accumulate = accumulate ? 1u : 0u; a.eps = eps; a.mean = 1.0f / (float)cols;
+    a.phase = phase_of(dy, rows, lddy, 2);
+    a.dy = in_rows(a.phase, dy, rows, cols, lddy); a.h = in_rows(a.phase, h, rows, cols, ldh); a.residual = in_rows(a.phase, residual, rows, cols, ldr);
+    a.gamma = InRows{gamma, 0, cols, aligned(gamma, 16)};
+    a.dh = out_rows(a.phase, dh, rows, lddh); a.dx = out_rows(a.phase, dx, rows, lddx);
+    const int rc = type == SC_BF16 ? run_norm_grad<__nv_bfloat16>(ctx, a, dgamma, st) : run_norm_grad<__half>(ctx, a, dgamma, st);
+    if (rc) return rc;
     SC_CUDA(cudaGetLastError());
     return SC_OK;
 }

@@ -7,6 +7,7 @@
 #pragma once
 #include "sc_checkpoint.cuh"
 #include "sc_dropout.cuh"
+#include "sc_tcgen05.cuh"
 
 namespace sc {
 
@@ -63,19 +64,49 @@ __device__ __forceinline__ void block_reduce(float& v, float& u, float (*slots)[
     for (uint32_t w = 0; w < warps; ++w) { v += slots[w][0]; u += slots[w][1]; }
 }
 
+// The same over a team, the threads that share a row: a warp, or a whole CTA that makes one reduction.
+template <int TEAM>
+__device__ __forceinline__ void team_reduce(float& v, uint32_t& m, float2* slots) {
+    v = warp_sum(v);
+    m = __reduce_max_sync(0xFFFFFFFFu, m);
+    if constexpr (TEAM > 32) {
+        if ((threadIdx.x & 31u) == 0) slots[threadIdx.x >> 5] = make_float2(v, __uint_as_float(m));
+        __syncthreads();
+        v = 0.0f;
+        m = 0u;
+#pragma unroll
+        for (int w = 0; w < TEAM / 32; ++w) { v += slots[w].x; m = max(m, __float_as_uint(slots[w].y)); }
+    }
+}
+
+__device__ __forceinline__ uint2 row_bytes8(const Pair v[4], float inv) {
+    if (inv == 0.0f) return make_uint2(0u, 0u);
+    uint32_t b[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = both(v[i] * pair(inv));          // a paired addition here would be joined with it, without the rounding between
+        b[2 * i] = __float_as_uint(__fadd_rn(f.x, 12582912.0f)) & 0xFFu;
+        b[2 * i + 1] = __float_as_uint(__fadd_rn(f.y, 12582912.0f)) & 0xFFu;
+    }
+    return ckpt_join8(b);
+}
 struct QuantizeArgs {
-    uint64_t rows, ldx, ldq;
+    uint64_t rows;
+    InRows x;
+    OutRows q;
     uint32_t cols, grain_x, grain_q;
+    Phase phase;
 };
 
 // A CTA a row, read twice: once for its largest magnitude, once for its bytes.
 template <typename T>
-__global__ void __launch_bounds__(NORM_THREADS) quantize_kernel(const T* x, QuantizeArgs a, uint8_t* q, float* scales) {
+__global__ void __launch_bounds__(NORM_THREADS) quantize_kernel(QuantizeArgs a, float* scales) {
     __shared__ float slots[NORM_THREADS / 32][2];
     wait_for_predecessor();
     release_successor();
     for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const T* from = x + row * a.ldx;
+        const T* from = static_cast<const T*>(a.x.p) + row * a.x.ld;
+        uint8_t* to = static_cast<uint8_t*>(a.q.p) + row * a.q.ld;
         uint32_t m = 0u;
         float none = 0.0f;
         for (uint32_t c0 = threadIdx.x * 8; c0 < a.cols; c0 += NORM_THREADS * 8) m = max(m, abs_max8(load8(from, c0, a.cols, a.grain_x)));
@@ -84,27 +115,130 @@ __global__ void __launch_bounds__(NORM_THREADS) quantize_kernel(const T* x, Quan
         for (uint32_t c0 = threadIdx.x * 8; c0 < a.cols; c0 += NORM_THREADS * 8) {
             float f[8];
             to_floats(load8(from, c0, a.cols, a.grain_x), f);
-            store_q8(q + row * a.ldq + c0, c0, a.cols, a.grain_q, row_bytes8(f, s.inv));
+            store_q8(to + c0, c0, a.cols, a.grain_q, row_bytes8(f, s.inv));
         }
         if (threadIdx.x == 0) scales[row] = s.scale;
     }
 }
 
-// The values of 8-bit rows, eight elements a thread and item.
+// The same with the row in registers, V times eight elements a thread, read once.
+template <typename T, int TEAM, int V, bool WIDE>
+__global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM) quantize_rows_kernel(QuantizeArgs a, float* scales) {
+    constexpr int TEAMS = TEAM == 32 ? 8 : 1;
+    __shared__ float2 slots[TEAM / 32];
+    wait_for_predecessor();
+    release_successor();
+    const uint32_t t = TEAM == 32 ? threadIdx.x & 31u : threadIdx.x;
+    const uint64_t row = (uint64_t)blockIdx.x * TEAMS + (TEAM == 32 ? threadIdx.x >> 5 : 0u);
+    if (row >= a.rows) return;
+    const int c0 = (int)(t * 8) - row_shift<WIDE>(a.phase, row), cols = (int)a.cols;
+    Raw8<T> raw[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) raw[j] = row_load8<T, WIDE>(a.x, row, c0 + j * TEAM * 8, cols);
+    uint32_t m = 0u;
+    float none = 0.0f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) m = max(m, abs_max8(raw[j]));
+    team_reduce<TEAM>(none, m, slots);
+    const RowScale s = row_scale(m);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        Pair v[4];
+        to_pairs(raw[j], v);
+        row_store_bytes8<WIDE>(a.q, row, c0 + j * TEAM * 8, cols, row_bytes8(v, s.inv));
+    }
+    if (t == 0) scales[row] = s.scale;
+}
+
+// The values of 8-bit rows, sixteen elements a thread and item, several items in flight.  For rows a multiple of 16 long whose bytes
+// take 16-byte accesses and whose values take 32-byte ones.
+constexpr int DEQUANTIZE_UNROLL = 4;
 template <typename T>
 __global__ void __launch_bounds__(CKPT_THREADS) dequantize_kernel(const uint8_t* q, uint64_t ldq, const float* scales, ItemWalk w, T* out, uint64_t ldo) {
     wait_for_predecessor();
     release_successor();
     const uint64_t first = (uint64_t)blockIdx.x * CKPT_THREADS + threadIdx.x, stride = (uint64_t)gridDim.x * CKPT_THREADS;
     ItemAt at(w, first);
-    for (uint64_t i = first; i < w.total; i += stride, at.next(w)) {
-        const uint32_t c0 = at.item * 8;
-        const uint2 b = load_q8(q + at.row * ldq, c0, w.cols, w.grain_q);
-        const float s = scales[at.row];
-        float f[8];
+    for (uint64_t base = first; base < w.total; base += stride * DEQUANTIZE_UNROLL) {
+        uint4 raw[DEQUANTIZE_UNROLL];
+        float s[DEQUANTIZE_UNROLL];
+        ItemAt from = at;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) f[k] = (float)(int8_t)((k < 4 ? b.x : b.y) >> (8 * (k & 3))) * s;
-        store8(out + at.row * ldo, c0, w.cols, w.grain_x, f);
+        for (int u = 0; u < DEQUANTIZE_UNROLL; ++u) {
+            if (base + u * stride < w.total) {
+                raw[u] = load_stream16(q + at.row * ldq + at.item * 16);
+                s[u] = scales[at.row];
+            }
+            at.next(w);
+        }
+#pragma unroll
+        for (int u = 0; u < DEQUANTIZE_UNROLL; ++u) {
+            if (base + u * stride < w.total) {
+                const uint32_t b[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+                T* to = out + from.row * ldo + from.item * 16;
+                uint4 o[sizeof(T)];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    // a byte's value plus 128 as the low mantissa byte of 2^23; the difference and the product are exact but for the last rounding
+                    const uint32_t v = b[k] ^ 0x80808080u;
+                    float f[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) f[i] = (__uint_as_float(__byte_perm(v, 0x4B000000u, 0x7440 + i)) - 8388736.0f) * s[u];
+                    if constexpr (sizeof(T) == 4) {
+                        o[k] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+                    } else {
+                        uint32_t* p = reinterpret_cast<uint32_t*>(o) + 2 * k;
+                        p[0] = Elem<T>::pack(f[0], f[1]);
+                        p[1] = Elem<T>::pack(f[2], f[3]);
+                    }
+                }
+                store32(to, o[0], o[1]);
+                if constexpr (sizeof(T) == 4) store32(to + 8, o[2], o[3]);
+            }
+            from.next(w);
+        }
+    }
+}
+
+// The same for other rows, in chunks of eight.
+template <typename T>
+__global__ void __launch_bounds__(CKPT_THREADS) dequantize_any_kernel(InRows q, const float* scales, ItemWalk w, Phase phase, OutRows out) {
+    wait_for_predecessor();
+    release_successor();
+    const uint64_t first = (uint64_t)blockIdx.x * CKPT_THREADS + threadIdx.x, stride = (uint64_t)gridDim.x * CKPT_THREADS;
+    const int cols = (int)w.cols;
+    ItemAt at(w, first);
+    for (uint64_t base = first; base < w.total; base += stride * DEQUANTIZE_UNROLL) {
+        uint2 raw[DEQUANTIZE_UNROLL];
+        float s[DEQUANTIZE_UNROLL];
+        ItemAt from = at;
+#pragma unroll
+        for (int u = 0; u < DEQUANTIZE_UNROLL; ++u) {
+            if (base + u * stride < w.total) {
+                raw[u] = row_load_bytes8<false>(q, at.row, chunk_col(at.item, row_shift<false>(phase, at.row), w.cols), cols);
+                s[u] = scales[at.row];
+            }
+            at.next(w);
+        }
+#pragma unroll
+        for (int u = 0; u < DEQUANTIZE_UNROLL; ++u) {
+            if (base + u * stride < w.total) {
+                const int c0 = chunk_col(from.item, row_shift<false>(phase, from.row), w.cols);
+                float f[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    f[i] = (__uint_as_float(__byte_perm((i < 4 ? raw[u].x : raw[u].y) ^ 0x80808080u, 0x4B000000u, 0x7440 + (i & 3))) - 8388736.0f) * s[u];
+                if constexpr (sizeof(T) == 2) {
+                    const Pair v[4] = {pair(f[0], f[1]), pair(f[2], f[3]), pair(f[4], f[5]), pair(f[6], f[7])};
+                    row_store8<T, false>(out, from.row, c0, cols, v);
+                } else {
+                    T* to = static_cast<T*>(out.p) + from.row * out.ld;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) if ((uint32_t)c0 + i < (uint32_t)cols) to[c0 + i] = f[i];
+                }
+            }
+            from.next(w);
+        }
     }
 }
 
@@ -112,9 +246,12 @@ __global__ void __launch_bounds__(CKPT_THREADS) dequantize_kernel(const uint8_t*
 // the norm
 // ---------------------------------------------------------------------------
 struct NormArgs {
-    uint64_t rows, ldx, ldr, ldh, ldy, ldq;
+    uint64_t rows;
+    InRows x, residual, gamma;
+    OutRows h, y, q;
     uint32_t cols, grain_x, grain_r, grain_g, grain_h, grain_y, grain_q;
     float eps, mean;           // mean: 1 / cols
+    Phase phase;
     Drop drop;
 };
 
@@ -125,30 +262,30 @@ __device__ __forceinline__ float rms_inverse(float sum, float mean, float eps) {
 
 // h of 8 columns in fp32; zero past the end.
 template <typename T>
-__device__ __forceinline__ void norm_input8(const T* x, const T* residual, const NormArgs& a, uint64_t row, uint32_t c0, float f[8]) {
-    to_floats(load8(x + row * a.ldx, c0, a.cols, a.grain_x), f);
+__device__ __forceinline__ void norm_input8(const NormArgs& a, uint64_t row, uint32_t c0, float f[8]) {
+    to_floats(load8(static_cast<const T*>(a.x.p) + row * a.x.ld, c0, a.cols, a.grain_x), f);
     if (a.drop.cut) drop8(a.drop, row, c0, f);
-    if (residual) {
+    if (a.residual.p) {
         float r[8];
-        to_floats(load8(residual + row * a.ldr, c0, a.cols, a.grain_r), r);
+        to_floats(load8(static_cast<const T*>(a.residual.p) + row * a.residual.ld, c0, a.cols, a.grain_r), r);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] += r[i];
     }
 }
 
-// A CTA a row, its inputs read twice.  max |h gamma| times r is max |y|, so one pass gives both statistics.
+// A CTA a row, its inputs read twice, for rows of any length.  max |h gamma| times r is max |y|, so one pass gives both statistics.
 template <typename T>
-__global__ void __launch_bounds__(NORM_THREADS) rms_norm_kernel(const T* x, const T* residual, const T* gamma, NormArgs a, T* h, T* y, uint8_t* q,
-                                                                float* scales) {
+__global__ void __launch_bounds__(NORM_THREADS) rms_norm_kernel(NormArgs a, float* scales) {
     __shared__ float slots[NORM_THREADS / 32][2];
     wait_for_predecessor();
     release_successor();
+    const T* gamma = static_cast<const T*>(a.gamma.p);
     for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         float sum = 0.0f;
         uint32_t m = 0u;
         for (uint32_t c0 = threadIdx.x * 8; c0 < a.cols; c0 += NORM_THREADS * 8) {
             float f[8], g[8];
-            norm_input8(x, residual, a, row, c0, f);
+            norm_input8<T>(a, row, c0, f);
             to_floats(load8(gamma, c0, a.cols, a.grain_g), g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -161,38 +298,366 @@ __global__ void __launch_bounds__(NORM_THREADS) rms_norm_kernel(const T* x, cons
         const RowScale s = row_scale(__float_as_uint(__uint_as_float(m) * r) & 0x7FFFFFFFu);
         for (uint32_t c0 = threadIdx.x * 8; c0 < a.cols; c0 += NORM_THREADS * 8) {
             float f[8], g[8];
-            norm_input8(x, residual, a, row, c0, f);
+            norm_input8<T>(a, row, c0, f);
             to_floats(load8(gamma, c0, a.cols, a.grain_g), g);
-            if (h) store8(h + row * a.ldh, c0, a.cols, a.grain_h, f);
+            if (a.h.p) store8(static_cast<T*>(a.h.p) + row * a.h.ld, c0, a.cols, a.grain_h, f);
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = f[i] * r * g[i];
-            if (y) store8(y + row * a.ldy, c0, a.cols, a.grain_y, f);
-            if (q) store_q8(q + row * a.ldq + c0, c0, a.cols, a.grain_q, row_bytes8(f, s.inv));
+            if (a.y.p) store8(static_cast<T*>(a.y.p) + row * a.y.ld, c0, a.cols, a.grain_y, f);
+            if (a.q.p) store_q8(static_cast<uint8_t*>(a.q.p) + row * a.q.ld + c0, c0, a.cols, a.grain_q, row_bytes8(f, s.inv));
         }
-        if (q && threadIdx.x == 0) scales[row] = s.scale;
+        if (a.q.p && threadIdx.x == 0) scales[row] = s.scale;
     }
 }
 
+// The same with the row in registers, V times eight elements a thread, and its inputs read once.
+template <typename T, int TEAM, int V, bool DROP, bool WIDE>
+__global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 512 && WIDE ? 2 : 1) rms_norm_rows_kernel(NormArgs a, float* scales) {
+    constexpr int TEAMS = TEAM == 32 ? 8 : 1;
+    // teams of many threads have no registers left for gamma and read it again
+    constexpr bool AGAIN = TEAM >= 512;
+    __shared__ float2 slots[TEAM / 32];
+    wait_for_predecessor();
+    release_successor();
+    const uint32_t t = TEAM == 32 ? threadIdx.x & 31u : threadIdx.x;
+    const uint64_t row = (uint64_t)blockIdx.x * TEAMS + (TEAM == 32 ? threadIdx.x >> 5 : 0u);
+    if (row >= a.rows) return;
+    const int first = (int)(t * 8) - row_shift<WIDE>(a.phase, row), cols = (int)a.cols;
+    Raw8<T> in[V], res[V], g[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        in[j] = row_load8<T, WIDE>(a.x, row, first + j * TEAM * 8, cols);
+        if (a.residual.p) res[j] = row_load8<T, WIDE>(a.residual, row, first + j * TEAM * 8, cols);
+    }
+    if constexpr (!AGAIN)
+#pragma unroll
+        for (int j = 0; j < V; ++j) g[j] = row_load8_across<T, WIDE>(a.gamma, first + j * TEAM * 8, cols);
+    Pair v[V][4], sums = pair(0.0f);
+    uint32_t m = 0u;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int c0 = first + j * TEAM * 8;
+        to_pairs(in[j], v[j]);
+        if constexpr (DROP) drop_pairs<WIDE>(a.drop, row, c0, v[j]);
+        if (a.residual.p) {
+            Pair r[4];
+            to_pairs(res[j], r);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[j][i] = v[j][i] + r[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums = fma2(v[j][i], v[j][i], sums);       // zeros outside the row, dropped or not
+        if (a.q.p) {
+            Pair w[4];
+            to_pairs(AGAIN ? row_load8_across<T, WIDE>(a.gamma, c0, cols) : g[j], w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = both(v[j][i] * w[i]);
+                m = max(max(m, __float_as_uint(f.x) & 0x7FFFFFFFu), __float_as_uint(f.y) & 0x7FFFFFFFu);
+            }
+        }
+    }
+    const float2 two = both(sums);
+    float sum = two.x + two.y;
+    team_reduce<TEAM>(sum, m, slots);
+    const float r = rms_inverse(sum, a.mean, a.eps);
+    const RowScale s = row_scale(__float_as_uint(__uint_as_float(m) * r) & 0x7FFFFFFFu);
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const int c0 = first + j * TEAM * 8;
+        if (a.h.p) row_store8<T, WIDE>(a.h, row, c0, cols, v[j]);
+        Pair w[4];
+        to_pairs(AGAIN ? row_load8_across<T, WIDE>(a.gamma, c0, cols) : g[j], w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[j][i] = v[j][i] * pair(r) * w[i];
+        if (a.y.p) row_store8<T, WIDE>(a.y, row, c0, cols, v[j]);
+        if (a.q.p) row_store_bytes8<WIDE>(a.q, row, c0, cols, row_bytes8(v[j], s.inv));
+    }
+    if (a.q.p && t == 0) scales[row] = s.scale;
+}
+
 struct NormGradArgs {
-    uint64_t rows, lddy, ldh, ldr, lddh, lddx;
+    uint64_t rows;
+    InRows dy, h, gamma, residual;
+    OutRows dh, dx;
     uint32_t cols, grain_y, grain_h, grain_g, grain_r, grain_dh, grain_dx;
     uint32_t runs, run_rows, accumulate;
+    uint64_t part_ld;          // floats between two partial rows of column sums
     float eps, mean;
+    Phase phase;
     Drop drop;
 };
 
+// What a team of threads makes of eight columns of a row once its statistics are known: dh and dx, and the column sums' terms.
+template <typename T, bool DROP, bool WIDE>
+__device__ __forceinline__ void norm_grad8(const NormGradArgs& a, uint64_t row, int c0, float r, float mean_gu, const Pair d[4], const Pair f[4],
+                                           const Pair g[4], Pair e[4], Pair sum[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const Pair u = f[i] * pair(r);
+        sum[i] = fma2(d[i], u, sum[i]);
+        e[i] = fma2(pair(r), fma2(u, pair(-mean_gu), d[i] * g[i]), e[i]);
+    }
+    if (a.dh.p) row_store8<T, WIDE>(a.dh, row, c0, (int)a.cols, e);
+    if (!a.dx.p) return;
+    if constexpr (DROP) drop_pairs<WIDE>(a.drop, row, c0, e);
+    row_store8<T, WIDE>(a.dx, row, c0, (int)a.cols, e);
+}
+
+// Sums of h^2 and g h over eight columns.
+__device__ __forceinline__ void norm_grad_stats8(const Pair d[4], const Pair f[4], const Pair g[4], Pair& sum, Pair& dot) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        sum = fma2(f[i], f[i], sum);
+        dot = fma2(d[i] * g[i], f[i], dot);
+    }
+}
+template <int TEAM>
+__device__ __forceinline__ void team_reduce(float& v, float& u, float2* slots) {
+    v = warp_sum(v);
+    u = warp_sum(u);
+    if constexpr (TEAM > 32) {
+        if ((threadIdx.x & 31u) == 0) slots[threadIdx.x >> 5] = make_float2(v, u);
+        __syncthreads();
+        v = u = 0.0f;
+#pragma unroll
+        for (int w = 0; w < TEAM / 32; ++w) { v += slots[w].x; u += slots[w].y; }
+    }
+}
+
+// A CTA's column sums to its partial row; those of eight warps are joined in order first, 256 columns at a time.
+template <int TEAM, int V, bool WIDE>
+__device__ __forceinline__ void norm_leave_sums(const Pair (&sum)[V][4], uint32_t t, uint32_t team, int shift, uint32_t cols, float* partial) {
+    if constexpr (TEAM == 32) {
+        __shared__ float join[8][264];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = both(sum[j][i]);
+                const int c = (int)(t * 8) + 2 * i - (WIDE ? 0 : shift);
+                if (WIDE || c >= 0) join[team][c] = f.x;
+                if (WIDE || c + 1 >= 0) join[team][c + 1] = f.y;
+            }
+            // a shifted row's last columns here are its next eight's first
+            if (!WIDE && j + 1 < V && t == 0)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = both(sum[j + 1 < V ? j + 1 : j][i]);
+                    join[team][256 - shift + 2 * i] = f.x;                 // up to 263
+                    join[team][256 - shift + 2 * i + 1] = f.y;
+                }
+            __syncthreads();
+            float total = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) total += join[w][threadIdx.x];
+            if (j * 256 + threadIdx.x < cols) partial[j * 256 + threadIdx.x] = total;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int c0 = (int)((j * TEAM + t) * 8) - (WIDE ? 0 : shift);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = both(sum[j][i]);
+                if ((uint32_t)(c0 + 2 * i) < cols) partial[c0 + 2 * i] = f.x;
+                if ((uint32_t)(c0 + 2 * i + 1) < cols) partial[c0 + 2 * i + 1] = f.y;
+            }
+        }
+    }
+}
+
+// A team a row, V times eight elements a thread, from registers; teams walk the rows with their columns' sums in registers and leave one
+// partial row of sums a CTA.  Their steps are multiples of 8 rows, so that all of a team's rows have the same shift and the same columns.
+template <typename T, int TEAM, int V, bool DROP>
+__global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 1) norm_grad_rows_kernel(NormGradArgs a, float* partial) {
+    constexpr int TEAMS = TEAM == 32 ? 8 : 1;
+    __shared__ float2 slots[2][TEAM / 32];
+    wait_for_predecessor();
+    release_successor();
+    const uint32_t t = TEAM == 32 ? threadIdx.x & 31u : threadIdx.x, team = TEAM == 32 ? threadIdx.x >> 5 : 0u;
+    const uint64_t first = (uint64_t)blockIdx.x * TEAMS + team;
+    const int shift = row_shift<false>(a.phase, first), from = (int)(t * 8) - shift, cols = (int)a.cols;
+    Raw8<T> gr[V];
+    Pair sum[V][4];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        gr[j] = row_load8_across<T, false>(a.gamma, from + j * TEAM * 8, cols);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[j][i] = pair(0.0f);
+    }
+    uint32_t turn = 0;
+    for (uint64_t row = first; row < a.rows; row += (uint64_t)gridDim.x * TEAMS, turn ^= 1u) {
+        Raw8<T> dr[V], hr[V], er[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            dr[j] = row_load8<T, false>(a.dy, row, from + j * TEAM * 8, cols);
+            hr[j] = row_load8<T, false>(a.h, row, from + j * TEAM * 8, cols);
+            if (a.residual.p) er[j] = row_load8<T, false>(a.residual, row, from + j * TEAM * 8, cols);
+        }
+        Pair ss = pair(0.0f), dd = pair(0.0f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            Pair d[4], f[4], g[4];
+            to_pairs(dr[j], d); to_pairs(hr[j], f); to_pairs(gr[j], g);
+            norm_grad_stats8(d, f, g, ss, dd);
+        }
+        const float2 s2 = both(ss), d2 = both(dd);
+        float square = s2.x + s2.y, dot = d2.x + d2.y;
+        team_reduce<TEAM>(square, dot, slots[turn]);
+        const float r = rms_inverse(square, a.mean, a.eps), mean_gu = dot * r * a.mean;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            Pair d[4], f[4], g[4], e[4];
+            to_pairs(dr[j], d); to_pairs(hr[j], f); to_pairs(gr[j], g);
+            if (a.residual.p) to_pairs(er[j], e);
+            else
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] = pair(0.0f);
+            norm_grad8<T, DROP, false>(a, row, from + j * TEAM * 8, r, mean_gu, d, f, g, e, sum[j]);
+        }
+    }
+    if (!partial) return;
+    norm_leave_sums<TEAM, V, false>(sum, t, team, shift, a.cols, partial + (uint64_t)blockIdx.x * a.part_ld);
+}
+
+// The same for rows that take 16-byte accesses, from a ring of shared-memory stages that bulk copies fill ahead of use: loads are in
+// flight while a row is reduced and written, and its operands are read from there twice instead of being kept in registers.  A
+// warp has a ring of its own; a larger team fills a stage again after the next row's barrier, which every thread reaches done with it.
+struct NormRing { uint32_t stages, row_bytes, operands; };
+constexpr uint32_t RING_MOST_STAGES = 8;
+template <typename T, int TEAM, int V, bool DROP>
+__global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 512 / TEAM) norm_grad_ring_kernel(NormGradArgs a, NormRing ring, float* partial,
+                                                                                                              int* status) {
+    constexpr int TEAMS = TEAM == 32 ? 8 : 1;
+    extern __shared__ __align__(128) uint8_t raw[];
+    __shared__ __align__(8) unsigned long long bars[TEAMS * RING_MOST_STAGES];
+    __shared__ float2 slots[2][TEAM / 32];
+    const uint32_t t = TEAM == 32 ? threadIdx.x & 31u : threadIdx.x, team = TEAM == 32 ? threadIdx.x >> 5 : 0u;
+    const uint32_t stage_bytes = ring.operands * ring.row_bytes;
+    const uint8_t* own = raw + team * ring.stages * stage_bytes;
+    const uint32_t base = smem_addr(own), full = smem_addr(bars + team * RING_MOST_STAGES);
+    if (t == 0) {
+        for (uint32_t s = 0; s < ring.stages; ++s) mbar_init(full + 8 * s, 1);
+        mbar_init_fence();
+    }
+    __syncthreads();
+    wait_for_predecessor();
+    release_successor();
+    const uint64_t first = (uint64_t)blockIdx.x * TEAMS + team, step = (uint64_t)gridDim.x * TEAMS;
+    const uint32_t mine = first < a.rows ? (uint32_t)((a.rows - first + step - 1) / step) : 0u;
+    const auto fill = [&](uint32_t n) {                                // row number n of this team
+        const uint64_t row = first + n * step;
+        const uint32_t s = n % ring.stages, bar = full + 8 * s, to = base + s * stage_bytes;
+        mbar_expect_tx(bar, stage_bytes);
+        bulk_load(to, static_cast<const T*>(a.dy.p) + row * a.dy.ld, ring.row_bytes, bar);
+        bulk_load(to + ring.row_bytes, static_cast<const T*>(a.h.p) + row * a.h.ld, ring.row_bytes, bar);
+        if (a.residual.p) bulk_load(to + 2 * ring.row_bytes, static_cast<const T*>(a.residual.p) + row * a.residual.ld, ring.row_bytes, bar);
+    };
+    uint32_t filled = 0;
+    if (t == 0)
+        for (; filled < mine && filled < ring.stages; ++filled) fill(filled);
+    Raw8<T> gr[V];
+    Pair sum[V][4];
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        gr[j] = row_load8<T, true>(a.gamma, 0, (int)((j * TEAM + t) * 8), (int)a.cols);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[j][i] = pair(0.0f);
+    }
+    uint32_t stage = 0, phase = 0;
+    bool ok = true;
+    for (uint32_t n = 0; n < mine; ++n) {
+        const uint64_t row = first + n * step;
+        const uint8_t* at = own + stage * stage_bytes;
+        const auto operand = [&](uint32_t which, uint32_t c0, Pair v[4]) {
+            Raw8<T> x{};
+            if (c0 < a.cols) x.v = *reinterpret_cast<const uint4*>(at + which * ring.row_bytes + c0 * 2);
+            to_pairs(x, v);
+        };
+        ok = mbar_wait(full + 8 * stage, phase);
+        Pair ss = pair(0.0f), dd = pair(0.0f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            Pair d[4], f[4], g[4];
+            operand(0, (j * TEAM + t) * 8, d);
+            operand(1, (j * TEAM + t) * 8, f);
+            to_pairs(gr[j], g);
+            norm_grad_stats8(d, f, g, ss, dd);
+        }
+        const float2 s2 = both(ss), d2 = both(dd);
+        float square = warp_sum(s2.x + s2.y), dot = warp_sum(d2.x + d2.y);
+        if constexpr (TEAM == 32) {
+            if (!(ok = __all_sync(0xFFFFFFFFu, ok))) break;            // the wait ran out: the team leaves together
+        } else {
+            float2* slot = slots[n & 1u];
+            if ((t & 31u) == 0) slot[t >> 5] = make_float2(square, dot);
+            if (!(ok = __syncthreads_and(ok))) break;
+            if (t == 0 && n > 0 && filled < mine) fill(filled++);
+            square = dot = 0.0f;
+#pragma unroll
+            for (int w = 0; w < TEAM / 32; ++w) { square += slot[w].x; dot += slot[w].y; }
+        }
+        const float r = rms_inverse(square, a.mean, a.eps), mean_gu = dot * r * a.mean;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const uint32_t c0 = (j * TEAM + t) * 8;
+            Pair d[4], f[4], g[4], e[4];
+            operand(0, c0, d);
+            operand(1, c0, f);
+            to_pairs(gr[j], g);
+            if (a.residual.p) operand(2, c0, e);
+            else
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] = pair(0.0f);
+            norm_grad8<T, DROP, true>(a, row, (int)c0, r, mean_gu, d, f, g, e, sum[j]);
+        }
+        if constexpr (TEAM == 32) {
+            __syncwarp();
+            if (t == 0 && filled < mine) fill(filled++);
+        }
+        if (++stage == ring.stages) { stage = 0; phase ^= 1u; }
+    }
+    if (!ok && t == 0) {                                               // copies in flight land before the CTA ends
+        atomicCAS(status, 0, ST_TIMEOUT);
+        for (uint32_t n = filled > ring.stages ? filled - ring.stages : 0; n < filled; ++n) mbar_wait(full + 8 * (n % ring.stages), (n / ring.stages) & 1u);
+    }
+    if (!partial) return;
+    norm_leave_sums<TEAM, V, true>(sum, t, team, 0, a.cols, partial + (uint64_t)blockIdx.x * a.part_ld);
+}
+
+// Column sums from the CTAs' partial rows: 32 columns a CTA, every eighth row a thread, joined in order.
+static __global__ void __launch_bounds__(256) norm_join_kernel(const float* partial, uint32_t parts, uint64_t part_ld, uint32_t cols, float* dgamma, uint32_t accumulate) {
+    __shared__ float join[8][32];
+    wait_for_predecessor();
+    release_successor();
+    const uint32_t tx = threadIdx.x & 31u, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
+    float total = 0.0f;
+    if (c < cols)
+#pragma unroll 8
+        for (uint32_t i = ty; i < parts; i += 8) total += load_l2(&partial[i * part_ld + c]);
+    join[ty][tx] = total;
+    __syncthreads();
+    if (ty || c >= cols) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) total += join[i][tx];
+    dgamma[c] = accumulate ? dgamma[c] + total : total;
+}
+
 // Each row's r and mean(g u).
 template <typename T>
-__global__ void __launch_bounds__(NORM_THREADS) norm_stats_kernel(const T* dy, const T* h, const T* gamma, NormGradArgs a, float2* stats) {
+__global__ void __launch_bounds__(NORM_THREADS) norm_stats_kernel(NormGradArgs a, float2* stats) {
     __shared__ float slots[NORM_THREADS / 32][2];
     wait_for_predecessor();
     release_successor();
+    const T *dy = static_cast<const T*>(a.dy.p), *h = static_cast<const T*>(a.h.p), *gamma = static_cast<const T*>(a.gamma.p);
     for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         float sum = 0.0f, dot = 0.0f;
         for (uint32_t c0 = threadIdx.x * 8; c0 < a.cols; c0 += NORM_THREADS * 8) {
             float d[8], f[8], g[8];
-            to_floats(load8(dy + row * a.lddy, c0, a.cols, a.grain_y), d);
-            to_floats(load8(h + row * a.ldh, c0, a.cols, a.grain_h), f);
+            to_floats(load8(dy + row * a.dy.ld, c0, a.cols, a.grain_y), d);
+            to_floats(load8(h + row * a.h.ld, c0, a.cols, a.grain_h), f);
             to_floats(load8(gamma, c0, a.cols, a.grain_g), g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -209,10 +674,12 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_stats_kernel(const T* dy, c
 // The rest, element by element: a CTA owns a strip of 256 columns and a run of rows, as the activation's gradient does, and leaves the
 // column sums the same way: over its row lanes in shared memory, over the runs by the strip's last CTA, in order.
 template <typename T>
-__global__ void __launch_bounds__(CKPT_THREADS) norm_strips_kernel(const T* dy, const T* h, const T* gamma, const T* residual, NormGradArgs a,
-                                                                   const float2* stats, T* dh, T* dx, float* partial, uint32_t* tickets, float* dgamma) {
+__global__ void __launch_bounds__(CKPT_THREADS) norm_strips_kernel(NormGradArgs a, const float2* stats, float* partial, uint32_t* tickets, float* dgamma) {
     wait_for_predecessor();
     release_successor();
+    const T *dy = static_cast<const T*>(a.dy.p), *h = static_cast<const T*>(a.h.p), *gamma = static_cast<const T*>(a.gamma.p);
+    const T* residual = static_cast<const T*>(a.residual.p);
+    T *dh = static_cast<T*>(a.dh.p), *dx = static_cast<T*>(a.dx.p);
     const uint32_t tx = threadIdx.x & 31u, ty = threadIdx.x >> 5;
     const uint32_t c0 = blockIdx.x * GRAD_COLS + tx * 8;
     const uint64_t first = (uint64_t)blockIdx.y * a.run_rows, end = min(first + a.run_rows, a.rows);
@@ -221,9 +688,9 @@ __global__ void __launch_bounds__(CKPT_THREADS) norm_strips_kernel(const T* dy, 
         to_floats(load8(gamma, c0, a.cols, a.grain_g), g);
         for (uint64_t row = first + ty; row < end; row += GRAD_LANES) {
             float d[8], f[8], e[8] = {};
-            to_floats(load8(dy + row * a.lddy, c0, a.cols, a.grain_y), d);
-            to_floats(load8(h + row * a.ldh, c0, a.cols, a.grain_h), f);
-            if (residual) to_floats(load8(residual + row * a.ldr, c0, a.cols, a.grain_r), e);
+            to_floats(load8(dy + row * a.dy.ld, c0, a.cols, a.grain_y), d);
+            to_floats(load8(h + row * a.h.ld, c0, a.cols, a.grain_h), f);
+            if (residual) to_floats(load8(residual + row * a.residual.ld, c0, a.cols, a.grain_r), e);
             const float2 s = stats[row];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -231,10 +698,10 @@ __global__ void __launch_bounds__(CKPT_THREADS) norm_strips_kernel(const T* dy, 
                 sum[i] = fmaf(d[i], u, sum[i]);
                 e[i] = fmaf(s.x, fmaf(-u, s.y, d[i] * g[i]), e[i]);
             }
-            if (dh) store8(dh + row * a.lddh, c0, a.cols, a.grain_dh, e);
+            if (dh) store8(dh + row * a.dh.ld, c0, a.cols, a.grain_dh, e);
             if (dx) {
                 if (a.drop.cut) drop8(a.drop, row, c0, e);
-                store8(dx + row * a.lddx, c0, a.cols, a.grain_dx, e);
+                store8(dx + row * a.dx.ld, c0, a.cols, a.grain_dx, e);
             }
         }
     }

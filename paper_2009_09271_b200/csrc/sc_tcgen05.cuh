@@ -1,4 +1,4 @@
-// Thin wrappers of the sm_100a instructions that the layer products use: mbarriers, TMA tile loads, tcgen05.
+// Thin wrappers of the sm_100a instructions that the layer operators use: mbarriers, TMA loads and stores, tcgen05.
 #pragma once
 #include <cstdint>
 #include <cuda.h>
@@ -79,6 +79,12 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* m, 
     else
         asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+
+// A run of bytes into this CTA's shared memory: both addresses and the size are multiples of 16.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
 // Tile stores from shared memory; the issuing thread's group of copies.
