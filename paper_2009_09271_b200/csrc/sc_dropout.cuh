@@ -79,8 +79,8 @@ __global__ void __launch_bounds__(CKPT_THREADS) dropout_kernel(ItemWalk w, DropA
         for (int u = 0; u < DROP_UNROLL; ++u) {
             if (base + u * stride < w.total) {
                 const int c0 = chunk_col(at.item, row_shift<WIDE>(a.phase, at.row), w.cols);
-                in[u] = row_load8<T, WIDE>(a.x, at.row, c0, cols);
-                if (RESIDUAL) res[u] = row_load8<T, WIDE>(a.residual, at.row, c0, cols);
+                in[u] = row_load8<T, WIDE>(row_in<T, WIDE>(a.x, at.row, cols), c0, cols);
+                if (RESIDUAL) res[u] = row_load8<T, WIDE>(row_in<T, WIDE>(a.residual, at.row, cols), c0, cols);
             }
             at.next(w);
         }

@@ -54,7 +54,7 @@ template <typename F>
 bool with_team(size_t cols, F&& f) {
     using std::integral_constant;
 #define SC_TEAM(TEAM, V) if (cols <= (size_t)TEAM * V * 8) { f(integral_constant<int, TEAM>(), integral_constant<int, V>()); return true; }
-    SC_TEAM(32, 1) SC_TEAM(32, 2) SC_TEAM(32, 4) SC_TEAM(128, 2) SC_TEAM(128, 4) SC_TEAM(256, 4) SC_TEAM(512, 4) SC_TEAM(1024, 4)
+    SC_TEAM(32, 1) SC_TEAM(32, 2) SC_TEAM(32, 4) SC_TEAM(128, 2) SC_TEAM(256, 2) SC_TEAM(256, 4) SC_TEAM(512, 4) SC_TEAM(1024, 4)
 #undef SC_TEAM
     return false;
 }

@@ -36,6 +36,12 @@ __device__ __forceinline__ uint2 row_bytes8(const float v[8], float inv) {
     return ckpt_join8(b);
 }
 
+// The largest of three magnitudes; NaN if one of them is.
+__device__ __forceinline__ float abs_max(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
@@ -85,8 +91,8 @@ __device__ __forceinline__ uint2 row_bytes8(const Pair v[4], float inv) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 f = both(v[i] * pair(inv));          // a paired addition here would be joined with it, without the rounding between
-        b[2 * i] = __float_as_uint(__fadd_rn(f.x, 12582912.0f)) & 0xFFu;
-        b[2 * i + 1] = __float_as_uint(__fadd_rn(f.y, 12582912.0f)) & 0xFFu;
+        b[2 * i] = __float_as_uint(__fadd_rn(f.x, 12582912.0f));             // its low byte
+        b[2 * i + 1] = __float_as_uint(__fadd_rn(f.y, 12582912.0f));
     }
     return ckpt_join8(b);
 }
@@ -132,13 +138,17 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM) quantize_rows_kernel(
     const uint64_t row = (uint64_t)blockIdx.x * TEAMS + (TEAM == 32 ? threadIdx.x >> 5 : 0u);
     if (row >= a.rows) return;
     const int c0 = (int)(t * 8) - row_shift<WIDE>(a.phase, row), cols = (int)a.cols;
+    const RowIn<T> from = row_in<T, WIDE>(a.x, row, cols);
     Raw8<T> raw[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) raw[j] = row_load8<T, WIDE>(a.x, row, c0 + j * TEAM * 8, cols);
+    for (int j = 0; j < V; ++j) raw[j] = row_load8<T, WIDE>(from, c0 + j * TEAM * 8, cols);
     uint32_t m = 0u;
     float none = 0.0f;
 #pragma unroll
-    for (int j = 0; j < V; ++j) m = max(m, abs_max8(raw[j]));
+    for (int j = 0; j < V; ++j) {
+        row_keep8<T, WIDE>(raw[j], c0 + j * TEAM * 8, cols);
+        m = max(m, abs_max8(raw[j]));
+    }
     team_reduce<TEAM>(none, m, slots);
     const RowScale s = row_scale(m);
 #pragma unroll
@@ -255,9 +265,10 @@ struct NormArgs {
     Drop drop;
 };
 
-// (mean of squares + eps)^(-1/2).  Squares that leave fp32's range make it NaN rather than 0: the row is lost and says so.
+// (mean of squares + eps)^(-1/2), the approximate root after one step of Newton's method.  Squares that leave fp32's range make it NaN rather than 0: the row is lost and says so.
 __device__ __forceinline__ float rms_inverse(float sum, float mean, float eps) {
-    return sum <= 3.402823466e38f ? 1.0f / sqrtf(fmaf(sum, mean, eps)) : __uint_as_float(0x7FFFFFFFu);
+    const float v = fmaf(sum, mean, eps), r = rsqrtf(v);
+    return sum <= 3.402823466e38f ? r * fmaf(-0.5f * v * r, r, 1.5f) : __uint_as_float(0x7FFFFFFFu);
 }
 
 // h of 8 columns in fp32; zero past the end.
@@ -310,12 +321,12 @@ __global__ void __launch_bounds__(NORM_THREADS) rms_norm_kernel(NormArgs a, floa
     }
 }
 
-// The same with the row in registers, V times eight elements a thread, and its inputs read once.
+// The same with the row in registers, V times eight elements a thread, and its inputs read once.  h leaves before the reduction; what stays
+// for after it is h gamma, of which y is a multiple.
 template <typename T, int TEAM, int V, bool DROP, bool WIDE>
-__global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 512 && WIDE ? 2 : 1) rms_norm_rows_kernel(NormArgs a, float* scales) {
+__global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 3 : TEAM == 1024 ? 1 : TEAM >= 256 && V == 4 ? 1024 / TEAM - (DROP && TEAM == 256) : 1024 / TEAM)
+rms_norm_rows_kernel(NormArgs a, float* scales) {
     constexpr int TEAMS = TEAM == 32 ? 8 : 1;
-    // teams of many threads have no registers left for gamma and read it again
-    constexpr bool AGAIN = TEAM >= 512;
     __shared__ float2 slots[TEAM / 32];
     wait_for_predecessor();
     release_successor();
@@ -323,57 +334,65 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 512 && WIDE ?
     const uint64_t row = (uint64_t)blockIdx.x * TEAMS + (TEAM == 32 ? threadIdx.x >> 5 : 0u);
     if (row >= a.rows) return;
     const int first = (int)(t * 8) - row_shift<WIDE>(a.phase, row), cols = (int)a.cols;
+    const RowIn<T> xr = row_in<T, WIDE>(a.x, row, cols), rr = row_in<T, WIDE>(a.residual, row, cols);
     Raw8<T> in[V], res[V], g[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        in[j] = row_load8<T, WIDE>(a.x, row, first + j * TEAM * 8, cols);
-        if (a.residual.p) res[j] = row_load8<T, WIDE>(a.residual, row, first + j * TEAM * 8, cols);
+        in[j] = row_load8<T, WIDE>(xr, first + j * TEAM * 8, cols);
+        if (a.residual.p) res[j] = row_load8<T, WIDE>(rr, first + j * TEAM * 8, cols);
     }
-    if constexpr (!AGAIN)
 #pragma unroll
-        for (int j = 0; j < V; ++j) g[j] = row_load8_across<T, WIDE>(a.gamma, first + j * TEAM * 8, cols);
+    for (int j = 0; j < V; ++j) g[j] = across_load8<T, WIDE>(a.gamma, first + j * TEAM * 8, cols);
     Pair v[V][4], sums = pair(0.0f);
-    uint32_t m = 0u;
+    float top = 0.0f;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const int c0 = first + j * TEAM * 8;
+        row_keep8<T, WIDE>(in[j], c0, cols);
         to_pairs(in[j], v[j]);
         if constexpr (DROP) drop_pairs<WIDE>(a.drop, row, c0, v[j]);
         if (a.residual.p) {
             Pair r[4];
+            row_keep8<T, WIDE>(res[j], c0, cols);
             to_pairs(res[j], r);
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[j][i] = v[j][i] + r[i];
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) sums = fma2(v[j][i], v[j][i], sums);       // zeros outside the row, dropped or not
+        if (a.h.p) row_store8<T, WIDE>(a.h, row, c0, cols, v[j]);
+        Pair w[4];
+        to_pairs(across_join8<T, WIDE>(a.gamma, g[j], c0, cols), w);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[j][i] = v[j][i] * w[i];
         if (a.q.p) {
-            Pair w[4];
-            to_pairs(AGAIN ? row_load8_across<T, WIDE>(a.gamma, c0, cols) : g[j], w);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float2 f = both(v[j][i] * w[i]);
-                m = max(max(m, __float_as_uint(f.x) & 0x7FFFFFFFu), __float_as_uint(f.y) & 0x7FFFFFFFu);
+                const float2 f = both(v[j][i]);
+                top = abs_max(top, f.x, f.y);
             }
         }
     }
     const float2 two = both(sums);
     float sum = two.x + two.y;
+    uint32_t m = __float_as_uint(top);
     team_reduce<TEAM>(sum, m, slots);
     const float r = rms_inverse(sum, a.mean, a.eps);
-    const RowScale s = row_scale(__float_as_uint(__uint_as_float(m) * r) & 0x7FFFFFFFu);
+    if (a.q.p) {
+        const RowScale s = row_scale(__float_as_uint(__uint_as_float(m) * r) & 0x7FFFFFFFu);
+        const float by = s.inv * r;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const int c0 = first + j * TEAM * 8;
-        if (a.h.p) row_store8<T, WIDE>(a.h, row, c0, cols, v[j]);
-        Pair w[4];
-        to_pairs(AGAIN ? row_load8_across<T, WIDE>(a.gamma, c0, cols) : g[j], w);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[j][i] = v[j][i] * pair(r) * w[i];
-        if (a.y.p) row_store8<T, WIDE>(a.y, row, c0, cols, v[j]);
-        if (a.q.p) row_store_bytes8<WIDE>(a.q, row, c0, cols, row_bytes8(v[j], s.inv));
+        for (int j = 0; j < V; ++j) row_store_bytes8<WIDE>(a.q, row, first + j * TEAM * 8, cols, row_bytes8(v[j], s.inv == 0.0f ? 0.0f : by));
+        if (t == 0) scales[row] = s.scale;
     }
-    if (a.q.p && t == 0) scales[row] = s.scale;
+    if (a.y.p) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[j][i] = v[j][i] * pair(r);
+            row_store8<T, WIDE>(a.y, row, first + j * TEAM * 8, cols, v[j]);
+        }
+    }
 }
 
 struct NormGradArgs {
@@ -483,23 +502,28 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 1) n
     Pair sum[V][4];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        gr[j] = row_load8_across<T, false>(a.gamma, from + j * TEAM * 8, cols);
+        gr[j] = across_load8<T, false>(a.gamma, from + j * TEAM * 8, cols);
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[j][i] = pair(0.0f);
     }
+#pragma unroll
+    for (int j = 0; j < V; ++j) gr[j] = across_join8<T, false>(a.gamma, gr[j], from + j * TEAM * 8, cols);
     uint32_t turn = 0;
     for (uint64_t row = first; row < a.rows; row += (uint64_t)gridDim.x * TEAMS, turn ^= 1u) {
+        const RowIn<T> dyr = row_in<T, false>(a.dy, row, cols), hrow = row_in<T, false>(a.h, row, cols), rr = row_in<T, false>(a.residual, row, cols);
         Raw8<T> dr[V], hr[V], er[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            dr[j] = row_load8<T, false>(a.dy, row, from + j * TEAM * 8, cols);
-            hr[j] = row_load8<T, false>(a.h, row, from + j * TEAM * 8, cols);
-            if (a.residual.p) er[j] = row_load8<T, false>(a.residual, row, from + j * TEAM * 8, cols);
+            dr[j] = row_load8<T, false>(dyr, from + j * TEAM * 8, cols);
+            hr[j] = row_load8<T, false>(hrow, from + j * TEAM * 8, cols);
+            if (a.residual.p) er[j] = row_load8<T, false>(rr, from + j * TEAM * 8, cols);
         }
         Pair ss = pair(0.0f), dd = pair(0.0f);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             Pair d[4], f[4], g[4];
+            row_keep8<T, false>(dr[j], from + j * TEAM * 8, cols);
+            row_keep8<T, false>(hr[j], from + j * TEAM * 8, cols);
             to_pairs(dr[j], d); to_pairs(hr[j], f); to_pairs(gr[j], g);
             norm_grad_stats8(d, f, g, ss, dd);
         }
@@ -547,22 +571,24 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 512 
     release_successor();
     const uint64_t first = (uint64_t)blockIdx.x * TEAMS + team, step = (uint64_t)gridDim.x * TEAMS;
     const uint32_t mine = first < a.rows ? (uint32_t)((a.rows - first + step - 1) / step) : 0u;
-    const auto fill = [&](uint32_t n) {                                // row number n of this team
-        const uint64_t row = first + n * step;
-        const uint32_t s = n % ring.stages, bar = full + 8 * s, to = base + s * stage_bytes;
+    uint32_t filled = 0, fill_stage = 0;
+    const auto fill = [&] {                                            // this team's next row
+        const uint64_t row = first + filled * step;
+        const uint32_t bar = full + 8 * fill_stage, to = base + fill_stage * stage_bytes;
         mbar_expect_tx(bar, stage_bytes);
         bulk_load(to, static_cast<const T*>(a.dy.p) + row * a.dy.ld, ring.row_bytes, bar);
         bulk_load(to + ring.row_bytes, static_cast<const T*>(a.h.p) + row * a.h.ld, ring.row_bytes, bar);
         if (a.residual.p) bulk_load(to + 2 * ring.row_bytes, static_cast<const T*>(a.residual.p) + row * a.residual.ld, ring.row_bytes, bar);
+        ++filled;
+        if (++fill_stage == ring.stages) fill_stage = 0;
     };
-    uint32_t filled = 0;
     if (t == 0)
-        for (; filled < mine && filled < ring.stages; ++filled) fill(filled);
+        while (filled < mine && filled < ring.stages) fill();
     Raw8<T> gr[V];
     Pair sum[V][4];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        gr[j] = row_load8<T, true>(a.gamma, 0, (int)((j * TEAM + t) * 8), (int)a.cols);
+        gr[j] = across_load8<T, true>(a.gamma, (int)((j * TEAM + t) * 8), (int)a.cols);
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[j][i] = pair(0.0f);
     }
@@ -572,14 +598,15 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 512 
         const uint64_t row = first + n * step;
         const uint8_t* at = own + stage * stage_bytes;
         const auto operand = [&](uint32_t which, uint32_t c0, Pair v[4]) {
-            Raw8<T> x{};
-            if (c0 < a.cols) x.v = *reinterpret_cast<const uint4*>(at + which * ring.row_bytes + c0 * 2);
+            Raw8<T> x;
+            x.v = *reinterpret_cast<const uint4*>(at + which * ring.row_bytes + c0 * 2);
             to_pairs(x, v);
         };
         ok = mbar_wait(full + 8 * stage, phase);
         Pair ss = pair(0.0f), dd = pair(0.0f);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
+            if ((j * TEAM + t) * 8 >= a.cols) break;
             Pair d[4], f[4], g[4];
             operand(0, (j * TEAM + t) * 8, d);
             operand(1, (j * TEAM + t) * 8, f);
@@ -594,7 +621,7 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 512 
             float2* slot = slots[n & 1u];
             if ((t & 31u) == 0) slot[t >> 5] = make_float2(square, dot);
             if (!(ok = __syncthreads_and(ok))) break;
-            if (t == 0 && n > 0 && filled < mine) fill(filled++);
+            if (t == 0 && n > 0 && filled < mine) fill();
             square = dot = 0.0f;
 #pragma unroll
             for (int w = 0; w < TEAM / 32; ++w) { square += slot[w].x; dot += slot[w].y; }
@@ -603,6 +630,7 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 512 
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const uint32_t c0 = (j * TEAM + t) * 8;
+            if (c0 >= a.cols) break;
             Pair d[4], f[4], g[4], e[4];
             operand(0, c0, d);
             operand(1, c0, f);
@@ -615,7 +643,7 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 512 
         }
         if constexpr (TEAM == 32) {
             __syncwarp();
-            if (t == 0 && filled < mine) fill(filled++);
+            if (t == 0 && filled < mine) fill();
         }
         if (++stage == ring.stages) { stage = 0; phase ^= 1u; }
     }

@@ -709,6 +709,152 @@ __global__ void __launch_bounds__(WN * WK * 32) product_tokens_kernel(const T* x
     with_activation(ep.act, [&](auto act) { epilogue8<T, PRODUCT_FORWARD, decltype(act)::value>(ep, m, c0, bias, f); });
 }
 
+// The end of a product of 8-bit integers for a few tokens: lane 4 m + j of a warp joins the WK parts of token m0 + m's eight sums from 8 j.
+template <typename T, int WK, int TOKENS, int COLS>
+__device__ __forceinline__ void tokens_out(const Epilogue& ep, const int (&part)[WK][TOKENS][COLS], uint32_t m0) {
+    const uint32_t lane = threadIdx.x & 31u, m = m0 + (lane >> 2), j = (lane & 3u) * 8;
+    const bool own = m < TOKENS && j < COLS;
+    const uint32_t c0 = own ? blockIdx.x * COLS + j : ep.cols;
+    float f[8] = {}, bias[8], scales[8];
+    if (own)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            int v = 0;
+#pragma unroll
+            for (int s = 0; s < WK; ++s) v += part[s][m][j + i];
+            f[i] = __int_as_float(v);
+        }
+    load_bias<T, PRODUCT_FORWARD>(ep, c0, bias);
+    load_col_scales<PRODUCT_QUANTIZED>(ep, c0, scales);
+    scale8<PRODUCT_QUANTIZED>(ep, m, scales, f);
+    with_activation(ep.act, [&](auto act) { epilogue8<T, PRODUCT_FORWARD, decltype(act)::value>(ep, m, c0, bias, f); });
+}
+
+// The same on 8-bit integers, for one and two tokens: sixteen weights a lane and access, four products an instruction, exact sums.  Rows are
+// 16-byte aligned and a multiple of 16 long.
+template <typename T, int TOKENS, int WN>
+__global__ void __launch_bounds__(WN * 4 * 32, WN == 2 ? 4 : 1) quantized_tokens_kernel(const uint8_t* x, uint64_t ldx, const uint8_t* w, uint64_t ldw, uint32_t K, Epilogue ep) {
+    constexpr int ROWS = 4, WK = 4, COLS = ROWS * WN;
+    wait_for_predecessor();
+    release_successor();
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, wn = warp / WK, wk = warp % WK;
+    const uint32_t n0 = blockIdx.x * COLS + wn * ROWS, tokens = (uint32_t)ep.rows;
+    int acc[ROWS][TOKENS] = {};
+#pragma unroll 2
+    for (uint32_t k = (wk * 32 + lane) * 16; k < K; k += 16 * 32 * WK) {
+        uint4 rw[ROWS], rx[TOKENS];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) rw[r] = n0 + r < ep.cols ? load_stream16(w + (uint64_t)(n0 + r) * ldw + k) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int m = 0; m < TOKENS; ++m) rx[m] = m < tokens ? *reinterpret_cast<const uint4*>(x + m * ldx + k) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int m = 0; m < TOKENS; ++m)
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                acc[r][m] = __dp4a((int)rw[r].x, (int)rx[m].x, acc[r][m]);
+                acc[r][m] = __dp4a((int)rw[r].y, (int)rx[m].y, acc[r][m]);
+                acc[r][m] = __dp4a((int)rw[r].z, (int)rx[m].z, acc[r][m]);
+                acc[r][m] = __dp4a((int)rw[r].w, (int)rx[m].w, acc[r][m]);
+            }
+    }
+    __shared__ int part[WK][TOKENS][COLS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int m = 0; m < TOKENS; ++m) {
+            const int v = __reduce_add_sync(0xFFFFFFFFu, acc[r][m]);
+            if (lane == 0) part[wk][m][wn * ROWS + r] = v;
+        }
+    __syncthreads();
+    if (warp == 0) tokens_out<T, WK, TOKENS, COLS>(ep, part, 0u);
+}
+
+// The same for up to 32 tokens.  The weights' bytes are everything, and the bytes are multiplied as fp16 numbers, which
+// hold them exactly, by warp-wide matrix instructions of 16 x 8 x 16: those for bytes run at a fiftieth of their rate here (4.5 us per eight
+// tokens at 4096 x 4096), dot products of four bytes take 1 us a token.  fp32 sums of integers are exact up to 2^24; they become integers
+// every 256 terms (at most 2^22).  A warp owns 16 rows of W and walks its share of the reduction, 64 terms a step; a lane loads 16 bytes of
+// two rows and of one token in eight: the order of a sum's terms is free, so that its own bytes serve as its columns of both
+// operands.  WK warps split a row and join their integers in shared memory; WN = 2 puts 32 outputs, a
+// checkpoint group, in one CTA.
+__device__ __forceinline__ void mma_halves(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Four bytes as two pairs of fp16: a byte's value plus 128 as the low mantissa bits of 1024, less 1152.
+__device__ __forceinline__ uint2 byte_halves(uint32_t bytes) {
+    const uint32_t u = bytes ^ 0x80808080u;
+    const __half2 off = __half2half2(__ushort_as_half(0x6480u));
+    uint2 r = make_uint2(__byte_perm(u, 0x64646464u, 0x4140), __byte_perm(u, 0x64646464u, 0x4342));
+    __half2 lo = *reinterpret_cast<__half2*>(&r.x), hi = *reinterpret_cast<__half2*>(&r.y);
+    lo = __hsub2(lo, off);
+    hi = __hsub2(hi, off);
+    return make_uint2(*reinterpret_cast<uint32_t*>(&lo), *reinterpret_cast<uint32_t*>(&hi));
+}
+constexpr int TOKENS_WK = 8;
+template <typename T, int EIGHTS, int WN>
+__global__ void __launch_bounds__(WN * TOKENS_WK * 32, EIGHTS == 1 && WN == 1 ? 3 : 2 / WN) quantized_eights_kernel(const uint8_t* x, uint64_t ldx, const uint8_t* w, uint64_t ldw, uint32_t K, Epilogue ep) {
+    constexpr int COLS = 16 * WN, WK = TOKENS_WK, UNROLL = EIGHTS < 4 ? 2 : 1;
+    __shared__ int part[WK][8 * EIGHTS][COLS];
+    wait_for_predecessor();
+    release_successor();
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, wn = warp / WK, wk = warp % WK, g = lane >> 2, t = lane & 3u;
+    const uint32_t n0 = blockIdx.x * COLS + wn * 16 + g, tokens = (uint32_t)ep.rows;
+    const uint8_t *w0 = w + (uint64_t)n0 * ldw, *w1 = w0 + 8 * ldw;
+    const bool in0 = n0 < ep.cols, in1 = n0 + 8 < ep.cols;
+    const auto fetch = [&](bool in, const uint8_t* row, uint32_t k) {
+        return in && k < K ? load_stream16(row + k) : make_uint4(0u, 0u, 0u, 0u);
+    };
+    int acc[EIGHTS][4] = {};
+    struct Step { uint4 a0, a1, b[EIGHTS]; };
+    const auto load = [&](Step (&s)[UNROLL], uint32_t k0) {
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const uint32_t k = k0 + u * WK * 64 + t * 16;
+            s[u].a0 = fetch(in0, w0, k);
+            s[u].a1 = fetch(in1, w1, k);
+#pragma unroll
+            for (int e = 0; e < EIGHTS; ++e) s[u].b[e] = 8 * e + g < tokens && k < K ? *reinterpret_cast<const uint4*>(x + (8 * e + g) * ldx + k) : make_uint4(0u, 0u, 0u, 0u);
+        }
+    };
+    const auto work = [&](const Step (&s)[UNROLL]) {
+        float sum[EIGHTS][4] = {};
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const uint32_t a0[4] = {s[u].a0.x, s[u].a0.y, s[u].a0.z, s[u].a0.w}, a1[4] = {s[u].a1.x, s[u].a1.y, s[u].a1.z, s[u].a1.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint2 h0 = byte_halves(a0[i]), h1 = byte_halves(a1[i]);
+#pragma unroll
+                for (int e = 0; e < EIGHTS; ++e) {
+                    const uint4 b = s[u].b[e];
+                    const uint2 v = byte_halves(i == 0 ? b.x : i == 1 ? b.y : i == 2 ? b.z : b.w);
+                    mma_halves(sum[e], h0.x, h1.x, h0.y, h1.y, v.x, v.y);
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < EIGHTS; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[e][i] += __float2int_rn(sum[e][i]);
+    };
+    constexpr uint32_t STRIDE = WK * 64 * UNROLL;
+    Step one[UNROLL], two[UNROLL];
+    load(one, wk * 64);
+    for (uint32_t k0 = wk * 64; k0 < K; k0 += 2 * STRIDE) {
+        load(two, k0 + STRIDE);
+        work(one);
+        load(one, k0 + 2 * STRIDE);
+        work(two);
+    }
+#pragma unroll
+    for (int e = 0; e < EIGHTS; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) part[wk][8 * e + 2 * t + (i & 1)][wn * 16 + g + 8 * (i >> 1)] = acc[e][i];
+    __syncthreads();
+    if (warp >= EIGHTS) return;
+    tokens_out<T, WK, 8 * EIGHTS, COLS>(ep, part, warp * 8);
+}
+
 // ---------------------------------------------------------------------------
 // Weight gradient of a few tokens
 // ---------------------------------------------------------------------------

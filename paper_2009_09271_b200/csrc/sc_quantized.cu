@@ -5,10 +5,41 @@ namespace {
 
 constexpr uint64_t MAX_TERMS = 131071;        // products of up to 2^14 that a 32-bit integer sum holds: 131071 2^14 < 2^31
 
+template <typename T, int TOKENS>
+void run_tokens(const Stored& x, const Stored& w, const Epilogue& ep, cudaStream_t st) {
+    const uint8_t *xp = static_cast<const uint8_t*>(x.p), *wp = static_cast<const uint8_t*>(w.p);
+    const uint32_t K = (uint32_t)x.cols;
+    if (ep.q) launch(quantized_tokens_kernel<T, TOKENS, 8>, (uint32_t)ceil_div(ep.cols, 32), 8 * 4 * 32, 0, 1, st, xp, x.ld, wp, w.ld, K, ep);
+    else launch(quantized_tokens_kernel<T, TOKENS, 2>, (uint32_t)ceil_div(ep.cols, 8), 2 * 4 * 32, 0, 1, st, xp, x.ld, wp, w.ld, K, ep);
+}
+template <typename T, int EIGHTS>
+void run_eights(const Stored& x, const Stored& w, const Epilogue& ep, cudaStream_t st) {
+    const uint8_t *xp = static_cast<const uint8_t*>(x.p), *wp = static_cast<const uint8_t*>(w.p);
+    const uint32_t K = (uint32_t)x.cols;
+    if (ep.q) launch(quantized_eights_kernel<T, EIGHTS, 2>, (uint32_t)ceil_div(ep.cols, 32), 2 * TOKENS_WK * 32, 0, 1, st, xp, x.ld, wp, w.ld, K, ep);
+    else launch(quantized_eights_kernel<T, EIGHTS, 1>, (uint32_t)ceil_div(ep.cols, 16), TOKENS_WK * 32, 0, 1, st, xp, x.ld, wp, w.ld, K, ep);
+}
+
+// What the kernels without tiles take: rows that are 16-byte aligned and a multiple of 16 long.  Up to 8 tokens they are ahead of the tiles or
+// even with them (8 x 4096 x 4096: 7.7 against 10.5 us, 8 x 16384 x 4096 18.2 against 20.3, 8 x 4096 x 16384 19.3 against 17.8), up to 32
+// while the weights are few (32 x 4096 x 4096 11.0 against 11.9, 16 x 16384 x 4096 26 against 20).
+bool few_tokens(const Stored& x, const Stored& w) {
+    return tma_ready(x) && tma_ready(w) && x.cols % 16 == 0 && (x.rows <= 8 || (x.rows <= 32 && w.rows * w.cols <= (32u << 20)));
+}
+
 template <typename T>
 int run(sc_ctx* c, int type, const Stored& x, const Stored& w, const Epilogue& ep, cudaStream_t st) {
     // an empty sum has nothing to scale: the forward product's epilogue alone
     if (x.cols == 0) return run_product<T, PRODUCT_FORWARD>(c, KIND_LINEAR_QUANTIZED, type, x, w, 0, ep, 0, st);
+    if (!c->layer_force_bn && few_tokens(x, w)) {
+        Launch l(c, KIND_LINEAR_QUANTIZED, st);
+        if (ep.rows == 1) run_tokens<T, 1>(x, w, ep, st);
+        else if (ep.rows == 2) run_tokens<T, 2>(x, w, ep, st);
+        else if (ep.rows <= 8) run_eights<T, 1>(x, w, ep, st);
+        else if (ep.rows <= 16) run_eights<T, 2>(x, w, ep, st);
+        else run_eights<T, 4>(x, w, ep, st);
+        return SC_OK;
+    }
     return run_product<T, PRODUCT_QUANTIZED>(c, KIND_LINEAR_QUANTIZED, type, x, w, x.cols, ep, 0, st);
 }
 
