@@ -290,6 +290,8 @@ class Context:
         _check(lib.sc_create(ctypes.byref(self._h), max_n, max_W, max_segments), "sc_create")
         self._layer, self._handle = _layer_calls(lib), self._h.value
         self._device = torch.cuda.current_device()
+        # the compiled caller's functions that take tensors; without it the binding's own checks and calls do
+        self._direct = self._layer if self._layer is not lib else None
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h:
@@ -536,6 +538,10 @@ class Context:
 
     def sc_quantize(self, x, q, scales, stream=None) -> None:
         """q, scales <- the 8-bit rows of x [rows, cols] (bfloat16, float16 or float32)."""
+        if self._direct is not None:
+            code = self._direct.quantize(self._handle, self._device, x, q, scales, self._queue(stream))
+            if code is not None:
+                return _check(code, "sc_quantize") if code else None
         kind = _layer_type(x, "x", f32=True)
         rows, cols = x.shape
         ldx = _matrix(x, rows, cols, x.dtype, "x")
@@ -545,6 +551,10 @@ class Context:
 
     def sc_dequantize(self, q, scales, out, stream=None) -> None:
         """out [rows, cols] <- the values of 8-bit rows."""
+        if self._direct is not None:
+            code = self._direct.dequantize(self._handle, self._device, q, scales, out, self._queue(stream))
+            if code is not None:
+                return _check(code, "sc_dequantize") if code else None
         kind = _layer_type(out, "out", f32=True)
         rows, cols = out.shape
         ldo = _matrix(out, rows, cols, out.dtype, "out")
@@ -555,6 +565,10 @@ class Context:
     def sc_linear_quantized(self, act: int, x, x_scales, w, w_scales, y, bias=None, residual=None, q=None, scales=None, stream=None) -> None:
         """y [M, N] <- act(z) + residual, z = (x W^T) x_scales w_scales + bias with 8-bit rows x [M, K] and w [N, K]; q, scales <- the
         checkpoint of z."""
+        if self._direct is not None:
+            code = self._direct.linear_quantized(self._handle, self._device, act, x, x_scales, w, w_scales, y, bias, residual, q, scales, self._queue(stream))
+            if code is not None:
+                return _check(code, "sc_linear_quantized") if code else None
         kind = _layer_type(y, "y")
         M, N = y.shape
         ldy = _matrix(y, M, N, y.dtype, "y")
@@ -576,6 +590,10 @@ class Context:
     def sc_dropout(self, x, y, p: float, seed: int, residual=None, stream=None) -> None:
         """y <- residual + dropout(x): each element kept with probability 1 - p and scaled by its reciprocal, by the mask that (seed, row,
         column) give.  The gradient is the same call on dy, without a residual.  y may be x or residual."""
+        if self._direct is not None:
+            code = self._direct.dropout(self._handle, self._device, x, y, p, seed, residual, self._queue(stream))
+            if code is not None:
+                return _check(code, "sc_dropout") if code else None
         kind = _layer_type(x, "x")
         rows, cols = x.shape
         ldx = _matrix(x, rows, cols, x.dtype, "x")
@@ -587,6 +605,10 @@ class Context:
 
     def sc_rms_norm(self, x, gamma, eps: float, y=None, q=None, scales=None, residual=None, h=None, p: float = 0.0, seed: int = 0, stream=None) -> None:
         """h <- residual + dropout(x; p, seed); y, or its 8-bit rows q and scales, or both <- h / sqrt(mean(h^2) + eps) * gamma."""
+        if self._direct is not None:
+            code = self._direct.rms_norm(self._handle, self._device, x, gamma, eps, y, q, scales, residual, h, p, seed, self._queue(stream))
+            if code is not None:
+                return _check(code, "sc_rms_norm") if code else None
         kind = _layer_type(x, "x")
         rows, cols = x.shape
         dtype = x.dtype
@@ -606,6 +628,10 @@ class Context:
     def sc_rms_norm_grad(self, dy, h, gamma, eps: float, dh=None, dgamma=None, residual=None, dx=None, p: float = 0.0, seed: int = 0,
                          accumulate: bool = False, stream=None) -> None:
         """dh <- residual + the norm's gradient at h; dx <- dropout(dh; p, seed); dgamma <- (dgamma +) column sums of dy h / rms(h), float32."""
+        if self._direct is not None:
+            code = self._direct.rms_norm_grad(self._handle, self._device, dy, h, gamma, eps, dh, dgamma, residual, dx, p, seed, accumulate, self._queue(stream))
+            if code is not None:
+                return _check(code, "sc_rms_norm_grad") if code else None
         kind = _layer_type(dy, "dy")
         rows, cols = dy.shape
         dtype = dy.dtype

@@ -1,6 +1,7 @@
 """Builds libsparsecomm.so (the C-ABI library of sm_100a kernels) in-tree with nvcc."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -12,14 +13,14 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparsecomm.so")
 SOURCES = ["sc_api.cu", "sc_layer.cu", "sc_norm.cu", "sc_quantized.cu"]
-# the layer operators' calls without ctypes; the binding does without where Python's headers are not installed
-CALLS_SOURCE = os.path.join(CSRC, "sc_calls.c")
+# the layer operators' calls without ctypes; the binding does without where Python's or torch's headers are not installed
+CALLS_SOURCE = os.path.join(CSRC, "sc_calls.cpp")
 CALLS = os.path.join(HERE, "_sc_calls" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
 
 def _dependencies():
     """Every file under csrc/ plus the public header."""
-    deps = [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith((".cu", ".cuh", ".h", ".c"))]
+    deps = [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith((".cu", ".cuh", ".h", ".cpp"))]
     deps.append(os.path.join(HERE, "..", "include", "sparsecomm.h"))
     deps.append(os.path.abspath(__file__))
     return deps
@@ -45,12 +46,25 @@ def _python_headers() -> str:
     return sysconfig.get_paths()["include"]
 
 
-def _cc():
-    return shutil.which("gcc") or shutil.which("cc")
+def _torch_home() -> str:
+    spec = importlib.util.find_spec("torch")
+    return os.path.dirname(spec.origin) if spec and spec.origin else ""
+
+
+def _cxx():
+    return shutil.which("g++") or shutil.which("c++")
 
 
 def _calls_wanted() -> bool:
-    return os.path.exists(os.path.join(_python_headers(), "Python.h")) and _cc() is not None
+    return (os.path.exists(os.path.join(_python_headers(), "Python.h")) and _cxx() is not None
+            and os.path.exists(os.path.join(_torch_home(), "include", "torch", "csrc", "autograd", "python_variable.h")))
+
+
+def _calls_command() -> list:
+    home = _torch_home()
+    include, lib = os.path.join(home, "include"), os.path.join(home, "lib")
+    return [_cxx(), "-O2", "-std=c++17", "-shared", "-fPIC", "-I", _python_headers(), "-I", include, "-I", os.path.join(include, "torch", "csrc", "api", "include"),
+            "-o", CALLS, CALLS_SOURCE, "-L", lib, "-lc10", "-ltorch_cpu", "-ltorch_python"]
 
 
 def _caller_is_current() -> bool:
@@ -91,10 +105,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
             if link.returncode != 0:
                 failed = "nvcc failed linking libsparsecomm.so"
         if not failed and _calls_wanted():
-            made = subprocess.run([_cc(), "-O2", "-shared", "-fPIC", "-I", _python_headers(), "-o", CALLS, CALLS_SOURCE], capture_output=True, text=True)
+            made = subprocess.run(_calls_command(), capture_output=True, text=True)
             said.append(made.stdout + made.stderr)
             if made.returncode != 0:
-                failed = f"the C compiler failed building {os.path.basename(CALLS)}"
+                failed = f"the C++ compiler failed building {os.path.basename(CALLS)}"
     if failed or verbose:
         sys.stderr.write("".join(said))
     if failed:
