@@ -30,14 +30,21 @@ struct Epilogue {
     uint32_t scales_by4;       // block_rows: four neighbouring scales of a row go out in one access
     const float* row_scale;    // 8-bit product: a scale for each row and each column of the result
     const float* col_scale;
+    uint32_t scales_by16;      // col_scale is 16-byte aligned
 };
 
 // 8-bit product: the scales of 8 columns, zero past the end, and a row's sums (by their bits) times both scales.
 template <int MODE>
 __device__ __forceinline__ void load_col_scales(const Epilogue& ep, uint32_t c0, float s[8]) {
-    if constexpr (MODE == PRODUCT_QUANTIZED)
+    if constexpr (MODE == PRODUCT_QUANTIZED) {
+        if (ep.scales_by16 && c0 + 8 <= ep.cols) {
+            const float4 a = *reinterpret_cast<const float4*>(ep.col_scale + c0), b = *reinterpret_cast<const float4*>(ep.col_scale + c0 + 4);
+            s[0] = a.x; s[1] = a.y; s[2] = a.z; s[3] = a.w; s[4] = b.x; s[5] = b.y; s[6] = b.z; s[7] = b.w;
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] = c0 + i < ep.cols ? ep.col_scale[c0 + i] : 0.0f;
+            for (int i = 0; i < 8; ++i) s[i] = c0 + i < ep.cols ? ep.col_scale[c0 + i] : 0.0f;
+        }
+    }
 }
 template <int MODE>
 __device__ __forceinline__ void scale8(const Epilogue& ep, uint64_t row, const float s[8], float v[8]) {
@@ -192,14 +199,15 @@ __device__ __forceinline__ void load_bias(const Epilogue& ep, uint32_t c0, float
 constexpr int TC_ROWS = 128, TC_STEP = 64, TC_THREADS = 384, TC_EPI_WARPS = 8, TC_CHUNK = 6;
 constexpr int TC_LEAST_REGS = 160;             // 160 x 384 >= 56 x 128 + 208 x 256, for builds that shift registers
 constexpr uint32_t TC_SMEM_LIMIT = 232448;
+constexpr uint32_t TC_COLUMN_BYTES = 32 * 4 + 32 * 2;      // a warp's block: the scales of its columns, and their bias
 
 template <int BN, int CG>
 struct TcShape {
     static constexpr int B_ROWS = BN / CG;
     static constexpr uint32_t A_BYTES = TC_ROWS * TC_STEP * 2, B_BYTES = B_ROWS * TC_STEP * 2, STAGE = A_BYTES + B_BYTES;
-    static constexpr uint32_t STAGING = TC_EPI_WARPS * 32 * 32 * 4;
-    static constexpr int STAGES = (TC_SMEM_LIMIT - 1024 - 256 - STAGING) / STAGE > 8 ? 8 : (TC_SMEM_LIMIT - 1024 - 256 - STAGING) / STAGE;
-    static constexpr uint32_t SMEM = STAGES * STAGE + STAGING + 1024 + 256;
+    static constexpr uint32_t STAGING = TC_EPI_WARPS * 32 * 32 * 4, COLUMNS = TC_EPI_WARPS * TC_COLUMN_BYTES, REST = 1024 + 256 + STAGING + COLUMNS;
+    static constexpr int STAGES = (TC_SMEM_LIMIT - REST) / STAGE > 8 ? 8 : (TC_SMEM_LIMIT - REST) / STAGE;
+    static constexpr uint32_t SMEM = STAGES * STAGE + REST;
     static constexpr uint32_t TMEM_COLS = 2 * BN;
 };
 
@@ -307,23 +315,49 @@ __device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcAr
 // One 32 x 32 block of a 16-bit result, thread t holding row t from TMEM to the end: a checkpoint group is one thread's own, its
 // bytes go out as one sector, and the result leaves by TMA from a 2 KB buffer of 64-byte rows (64-byte swizzle), two of
 // which take turns.  About a third of the instructions of block_out, which serves rows of other alignments.
+// What its columns have in common, one lane a column: fetched while the block before is worked on (the first one while the sums are awaited),
+// handed to the block's threads through shared memory.  Read from HBM's side by every thread, bias and scales were half of the
+// epilogue: 8192 x 8192 x 1024 in 8 bits took 111 us, 78 without a bias.
+struct BlockColumn { float scale; uint16_t bias; };
+template <int PRODUCT>
+__device__ __forceinline__ BlockColumn block_column(const Epilogue& ep, uint32_t col) {
+    BlockColumn c{0.0f, 0};
+    if constexpr (epilogue_of(PRODUCT) == PRODUCT_FORWARD) {
+        if (col < ep.cols) {
+            if constexpr (PRODUCT == PRODUCT_QUANTIZED) c.scale = ep.col_scale[col];
+            if (ep.bias) c.bias = static_cast<const uint16_t*>(ep.bias)[col];
+        }
+    }
+    return c;
+}
+template <int PRODUCT>
+__device__ __forceinline__ void block_columns(const BlockColumn& c, uint32_t at) {
+    if constexpr (epilogue_of(PRODUCT) == PRODUCT_FORWARD) {
+        const uint32_t lane = threadIdx.x & 31u;
+        __syncwarp();                                       // the block before has read its own
+        if constexpr (PRODUCT == PRODUCT_QUANTIZED) asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + lane * 4), "f"(c.scale) : "memory");
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(at + 128 + lane * 2), "h"(c.bias) : "memory");
+        __syncwarp();
+    }
+}
+
 template <typename T, int PRODUCT, int ACT>
-__device__ __forceinline__ void block_rows(const CUtensorMap* map_out, const Epilogue& ep, uint32_t buffer, const uint32_t (&v)[32], uint64_t row0,
-                                           uint32_t col0, uint32_t& scale4) {
+__device__ __forceinline__ void block_rows(const CUtensorMap* map_out, const Epilogue& ep, uint32_t buffer, uint32_t columns, float row_scale, const uint32_t (&v)[32],
+                                           uint64_t row0, uint32_t col0, uint32_t& scale4) {
     const uint32_t lane = threadIdx.x & 31u;
     const uint64_t row = row0 + lane;
     const bool in = row < ep.rows && col0 < ep.cols, whole = col0 + 32 <= ep.cols;
     constexpr int MODE = epilogue_of(PRODUCT);
     Pair z[16];
     if constexpr (PRODUCT == PRODUCT_QUANTIZED) {
-        const Pair r = pair(row < ep.rows ? ep.row_scale[row] : 0.0f);
+        const Pair r = pair(row_scale);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float s[8];
-            load_col_scales<PRODUCT>(ep, col0 + 8 * j, s);
+        for (int j = 0; j < 8; ++j) {
+            float s[4];
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(s[0]), "=f"(s[1]), "=f"(s[2]), "=f"(s[3]) : "r"(columns + 16 * j) : "memory");
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                z[4 * j + i] = pair((float)(int32_t)v[8 * j + 2 * i], (float)(int32_t)v[8 * j + 2 * i + 1]) * r * pair(s[2 * i], s[2 * i + 1]);
+            for (int i = 0; i < 2; ++i)
+                z[2 * j + i] = pair((float)(int32_t)v[4 * j + 2 * i], (float)(int32_t)v[4 * j + 2 * i + 1]) * r * pair(s[2 * i], s[2 * i + 1]);
         }
     } else {
 #pragma unroll
@@ -333,10 +367,13 @@ __device__ __forceinline__ void block_rows(const CUtensorMap* map_out, const Epi
         if (ep.bias) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                float b[8];
-                load_bias<T, MODE>(ep, col0 + 8 * j, b);
+                uint32_t b[4];
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]) : "r"(columns + 128 + 16 * j) : "memory");
 #pragma unroll
-                for (int i = 0; i < 4; ++i) z[4 * j + i] = z[4 * j + i] + pair(b[2 * i], b[2 * i + 1]);
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = Elem<T>::unpack(b[i]);
+                    z[4 * j + i] = z[4 * j + i] + pair(f.x, f.y);
+                }
             }
         }
         if (ep.q) {
@@ -453,7 +490,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
     const uint32_t base = (smem_addr(raw) + 1023u) & ~1023u;
     const uint32_t staging = base + S::STAGES * S::STAGE;
     const uint32_t bars = staging + S::STAGING;
-    const uint32_t full = bars, empty = bars + 8 * S::STAGES, tfull = empty + 8 * S::STAGES, tempty = tfull + 16, slot = tempty + 16;
+    const uint32_t full = bars, empty = bars + 8 * S::STAGES, tfull = empty + 8 * S::STAGES, tempty = tfull + 16, slot = tempty + 16, column_base = bars + 256;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
     const uint32_t first = blockIdx.x / CG, step = gridDim.x / CG;
@@ -600,6 +637,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
 #pragma unroll
                 for (int c = 0; c < BN / 64; ++c) block_out<T, MODE>(&map_out, a, ep, stage_addr, sum[c], row0, col0 + c * 32, split);
             } else {
+                BlockColumn column{0.0f, 0};
+                float row_scale = 0.0f;
+                if (a.rows_form) {
+                    column = block_column<MODE>(ep, col0 + lane);
+                    if constexpr (MODE == PRODUCT_QUANTIZED) row_scale = row0 + lane < ep.rows ? ep.row_scale[row0 + lane] : 0.0f;
+                }
                 if (!(ok = warp_wait(tfull + 8 * acc, acc_phase))) break;
                 __syncwarp();
                 tcgen05_fence_after();
@@ -615,8 +658,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                         if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_rank(tempty + 8 * acc, 0) : tempty + 8 * acc);
                     }
                     if (a.rows_form) {
+                        const uint32_t columns = column_base + e * TC_COLUMN_BYTES;
+                        block_columns<MODE>(column, columns);
+                        if (c + 32 < BN / 2) column = block_column<MODE>(ep, col0 + c + 32 + lane);
                         with_activation(ep.act, [&](auto act) {
-                            block_rows<T, MODE, decltype(act)::value>(&map_out, ep, stage_addr + turn, v, row0, col0 + c, scale4);
+                            block_rows<T, MODE, decltype(act)::value>(&map_out, ep, stage_addr + turn, columns, row_scale, v, row0, col0 + c, scale4);
                         });
                         turn ^= 2048u;                      // the two buffers take turns from block to block, whatever the tile
                     } else

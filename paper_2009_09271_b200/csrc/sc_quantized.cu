@@ -65,7 +65,7 @@ int sc_linear_quantized(sc_ctx* ctx, int type, int act, const int8_t* x, size_t 
     Epilogue ep{};
     ep.bias = bias; ep.residual = residual; ep.ldr = ldr; ep.out = y; ep.ldo = ldy; ep.rows = M; ep.cols = (uint32_t)N;
     ep.q = reinterpret_cast<uint8_t*>(q); ep.scales = scales; ep.groups = (uint32_t)ckpt_groups(N); ep.act = act;
-    ep.row_scale = x_scales; ep.col_scale = w_scales;
+    ep.row_scale = x_scales; ep.col_scale = w_scales; ep.scales_by16 = aligned(w_scales, 16);
     ep.grain_out = grain_of(y, M > 1 ? ldy : 0, 2, 8); ep.grain_res = grain_of(residual, M > 1 ? ldr : 0, 2, 8);
     ep.grain_q = grain_of(q, M > 1 ? N : 0, 1, 32); ep.grain_bias = grain_of(bias, 0, 2, 8);
     const Stored xs{x, M, K, ldx, 1}, ws{w, N, K, ldw, 1};
