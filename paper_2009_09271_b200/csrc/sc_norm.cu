@@ -137,12 +137,13 @@ int ring_ready(const sc_ctx* c) {
     return SC_OK;
 }
 
-template <typename T, int TEAM, int V, bool DROP>
-int launch_norm_grad(sc_ctx* c, NormGradArgs a, bool wide, float* dgamma, cudaStream_t st) {
-    constexpr uint32_t TEAMS = TEAM == 32 ? 8 : 1, FIT = TEAM == 32 ? 2 : 512 / TEAM;      // teams a CTA, CTAs an SM by their registers
+template <typename T, int TEAM, int V, bool DROP, bool RING>
+int launch_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) {
+    // teams a CTA, CTAs an SM by their registers
+    constexpr uint32_t TEAMS = RING ? (TEAM == 32 ? 8 : 1) : grad_teams(TEAM), FIT = TEAM == 32 ? 2 : 512 / TEAM / (RING ? 1 : TEAMS);
     NormRing ring{};
     uint32_t per_sm = FIT;
-    if (wide) {
+    if constexpr (RING) {
         // as many stages as leave room for every CTA that fits otherwise, two at least
         ring.row_bytes = a.cols * 2; ring.operands = a.residual.p ? 3 : 2;
         const uint32_t stage = TEAMS * ring.row_bytes * ring.operands;
@@ -157,7 +158,7 @@ int launch_norm_grad(sc_ctx* c, NormGradArgs a, bool wide, float* dgamma, cudaSt
         if (const int rc = layer_scratch(c, grid * a.part_ld * sizeof(float), st)) return rc;
         partial = reinterpret_cast<float*>(c->d_layer + TICKET_BYTES);
     }
-    if (wide) {
+    if constexpr (RING) {
         if (const int rc = ring_ready<T, TEAM, V, DROP>(c)) return rc;
         Launch l(c, KIND_RMS_NORM_GRAD, st);
         launch(norm_grad_ring_kernel<T, TEAM, V, DROP>, grid, TEAMS * TEAM, ring.stages * ring.row_bytes * ring.operands * TEAMS, 1, st, a, ring, partial, c->d_status);
@@ -167,7 +168,7 @@ int launch_norm_grad(sc_ctx* c, NormGradArgs a, bool wide, float* dgamma, cudaSt
     }
     if (dgamma) {
         Launch l(c, KIND_RMS_NORM_GRAD, st);
-        launch(norm_join_kernel, (uint32_t)ceil_div(a.cols, 32), 256, 0, 1, st, partial, grid, a.part_ld, a.cols, dgamma, a.accumulate);
+        launch(norm_join_kernel, (uint32_t)ceil_div(a.cols, 32), JOIN_LANES * 32, 0, 1, st, partial, grid, a.part_ld, a.cols, dgamma, a.accumulate);
     }
     return SC_OK;
 }
@@ -175,10 +176,12 @@ int launch_norm_grad(sc_ctx* c, NormGradArgs a, bool wide, float* dgamma, cudaSt
 template <typename T>
 int run_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) {
     const bool wide = unshifted(a.phase, a.cols) && a.h.vec && a.gamma.vec && a.residual.vec && a.dh.vec && a.dx.vec, drop = a.drop.cut && a.dx.p;
-    const uint64_t held = wide ? a.cols : a.cols + 7ull;
-#define SC_TEAM(TEAM, V) \
-    if (held <= TEAM * V * 8) return drop ? launch_norm_grad<T, TEAM, V, true>(c, a, wide, dgamma, st) : launch_norm_grad<T, TEAM, V, false>(c, a, wide, dgamma, st);
-    SC_TEAM(32, 1) SC_TEAM(32, 2) SC_TEAM(32, 4) SC_TEAM(128, 2) SC_TEAM(256, 2) SC_TEAM(256, 4) SC_TEAM(512, 4)
+    // rows in registers want fewer elements a thread than rows in shared memory
+#define SC_TEAM(TEAM, V, RING) \
+    if (wide == RING && a.cols + (RING ? 0ull : 7ull) <= TEAM * V * 8) \
+        return drop ? launch_norm_grad<T, TEAM, V, true, RING>(c, a, dgamma, st) : launch_norm_grad<T, TEAM, V, false, RING>(c, a, dgamma, st);
+    SC_TEAM(32, 1, true) SC_TEAM(32, 2, true) SC_TEAM(32, 4, true) SC_TEAM(128, 2, true) SC_TEAM(256, 2, true) SC_TEAM(256, 4, true) SC_TEAM(512, 4, true)
+    SC_TEAM(32, 1, false) SC_TEAM(32, 2, false) SC_TEAM(128, 1, false) SC_TEAM(128, 2, false) SC_TEAM(256, 2, false) SC_TEAM(512, 2, false) SC_TEAM(512, 4, false)
 #undef SC_TEAM
     const StripPlan plan = strip_plan(c, a.rows, a.cols);
     if (const int rc = layer_scratch(c, plan.partial + plan.stats, st)) return rc;

@@ -432,23 +432,24 @@ __device__ __forceinline__ void norm_grad_stats8(const Pair d[4], const Pair f[4
     }
 }
 template <int TEAM>
-__device__ __forceinline__ void team_reduce(float& v, float& u, float2* slots) {
+__device__ __forceinline__ void team_reduce(float& v, float& u, float2* slots, uint32_t team) {
     v = warp_sum(v);
     u = warp_sum(u);
     if constexpr (TEAM > 32) {
-        if ((threadIdx.x & 31u) == 0) slots[threadIdx.x >> 5] = make_float2(v, u);
-        __syncthreads();
+        if ((threadIdx.x & 31u) == 0) slots[(threadIdx.x % TEAM) >> 5] = make_float2(v, u);
+        asm volatile("bar.sync %0, %1;" ::"r"(1u + team), "n"(TEAM) : "memory");      // the team's own barrier
         v = u = 0.0f;
 #pragma unroll
         for (int w = 0; w < TEAM / 32; ++w) { v += slots[w].x; u += slots[w].y; }
     }
 }
 
-// A CTA's column sums to its partial row; those of eight warps are joined in order first, 256 columns at a time.
-template <int TEAM, int V, bool WIDE>
+// A CTA's column sums to its partial row; those of several teams are joined in order first, 8 columns a thread at a time.
+template <int TEAM, int TEAMS, int V, bool WIDE>
 __device__ __forceinline__ void norm_leave_sums(const Pair (&sum)[V][4], uint32_t t, uint32_t team, int shift, uint32_t cols, float* partial) {
-    if constexpr (TEAM == 32) {
-        __shared__ float join[8][264];
+    if constexpr (TEAMS > 1) {
+        constexpr uint32_t WIDTH = TEAM * 8;
+        __shared__ float join[TEAMS][WIDTH + 8];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             __syncthreads();
@@ -464,14 +465,17 @@ __device__ __forceinline__ void norm_leave_sums(const Pair (&sum)[V][4], uint32_
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float2 f = both(sum[j + 1 < V ? j + 1 : j][i]);
-                    join[team][256 - shift + 2 * i] = f.x;                 // up to 263
-                    join[team][256 - shift + 2 * i + 1] = f.y;
+                    join[team][WIDTH - shift + 2 * i] = f.x;               // up to WIDTH + 7
+                    join[team][WIDTH - shift + 2 * i + 1] = f.y;
                 }
             __syncthreads();
-            float total = 0.0f;
 #pragma unroll
-            for (int w = 0; w < 8; ++w) total += join[w][threadIdx.x];
-            if (j * 256 + threadIdx.x < cols) partial[j * 256 + threadIdx.x] = total;
+            for (uint32_t c = threadIdx.x; c < WIDTH; c += TEAMS * TEAM) {
+                float total = 0.0f;
+#pragma unroll
+                for (int w = 0; w < TEAMS; ++w) total += join[w][c];
+                if (j * WIDTH + c < cols) partial[j * WIDTH + c] = total;
+            }
         }
     } else {
 #pragma unroll
@@ -488,14 +492,16 @@ __device__ __forceinline__ void norm_leave_sums(const Pair (&sum)[V][4], uint32_
 }
 
 // A team a row, V times eight elements a thread, from registers; teams walk the rows with their columns' sums in registers and leave one
-// partial row of sums a CTA.  Their steps are multiples of 8 rows, so that all of a team's rows have the same shift and the same columns.
+// partial row of sums a CTA, so that few CTAs of several teams leave little to join.  Their steps are multiples of 8 rows: all of a team's rows
+// have the same shift and the same columns.
+constexpr int grad_teams(int team) { return team == 32 ? 8 : team == 128 ? 4 : 1; }
 template <typename T, int TEAM, int V, bool DROP>
-__global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 1) norm_grad_rows_kernel(NormGradArgs a, float* partial) {
-    constexpr int TEAMS = TEAM == 32 ? 8 : 1;
-    __shared__ float2 slots[2][TEAM / 32];
+__global__ void __launch_bounds__(grad_teams(TEAM) * TEAM, TEAM == 32 ? 2 : 1) norm_grad_rows_kernel(NormGradArgs a, float* partial) {
+    constexpr int TEAMS = TEAM == 32 ? 8 : TEAM == 128 ? 4 : 1;
+    __shared__ float2 slots[2][TEAMS][TEAM / 32];
     wait_for_predecessor();
     release_successor();
-    const uint32_t t = TEAM == 32 ? threadIdx.x & 31u : threadIdx.x, team = TEAM == 32 ? threadIdx.x >> 5 : 0u;
+    const uint32_t t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
     const uint64_t first = (uint64_t)blockIdx.x * TEAMS + team;
     const int shift = row_shift<false>(a.phase, first), from = (int)(t * 8) - shift, cols = (int)a.cols;
     Raw8<T> gr[V];
@@ -529,7 +535,7 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 1) n
         }
         const float2 s2 = both(ss), d2 = both(dd);
         float square = s2.x + s2.y, dot = d2.x + d2.y;
-        team_reduce<TEAM>(square, dot, slots[turn]);
+        team_reduce<TEAM>(square, dot, slots[turn][team], team);
         const float r = rms_inverse(square, a.mean, a.eps), mean_gu = dot * r * a.mean;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
@@ -543,7 +549,7 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 1) n
         }
     }
     if (!partial) return;
-    norm_leave_sums<TEAM, V, false>(sum, t, team, shift, a.cols, partial + (uint64_t)blockIdx.x * a.part_ld);
+    norm_leave_sums<TEAM, TEAMS, V, false>(sum, t, team, shift, a.cols, partial + (uint64_t)blockIdx.x * a.part_ld);
 }
 
 // The same for rows that take 16-byte accesses, from a ring of shared-memory stages that bulk copies fill ahead of use: loads are in
@@ -652,25 +658,28 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 512 
         for (uint32_t n = filled > ring.stages ? filled - ring.stages : 0; n < filled; ++n) mbar_wait(full + 8 * (n % ring.stages), (n / ring.stages) & 1u);
     }
     if (!partial) return;
-    norm_leave_sums<TEAM, V, true>(sum, t, team, 0, a.cols, partial + (uint64_t)blockIdx.x * a.part_ld);
+    norm_leave_sums<TEAM, TEAMS, V, true>(sum, t, team, 0, a.cols, partial + (uint64_t)blockIdx.x * a.part_ld);
 }
 
-// Column sums from the CTAs' partial rows: 32 columns a CTA, every eighth row a thread, joined in order.
-static __global__ void __launch_bounds__(256) norm_join_kernel(const float* partial, uint32_t parts, uint64_t part_ld, uint32_t cols, float* dgamma, uint32_t accumulate) {
-    __shared__ float join[8][32];
+// Column sums from the CTAs' partial rows: 32 columns a CTA, one of JOIN_LANES rows a thread, joined in order.
+constexpr int JOIN_LANES = 32;
+static __global__ void __launch_bounds__(JOIN_LANES * 32) norm_join_kernel(const float* partial, uint32_t parts, uint64_t part_ld, uint32_t cols, float* dgamma,
+                                                                           uint32_t accumulate) {
+    __shared__ float join[JOIN_LANES][33];
     wait_for_predecessor();
     release_successor();
     const uint32_t tx = threadIdx.x & 31u, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
     float total = 0.0f;
     if (c < cols)
 #pragma unroll 8
-        for (uint32_t i = ty; i < parts; i += 8) total += load_l2(&partial[i * part_ld + c]);
+        for (uint32_t i = ty; i < parts; i += JOIN_LANES) total += load_l2(&partial[i * part_ld + c]);
     join[ty][tx] = total;
     __syncthreads();
-    if (ty || c >= cols) return;
-#pragma unroll
-    for (int i = 1; i < 8; ++i) total += join[i][tx];
-    dgamma[c] = accumulate ? dgamma[c] + total : total;
+    total = warp_sum(join[tx][ty]);                          // a warp a column
+    if (tx == 0 && blockIdx.x * 32 + ty < cols) {
+        float* to = dgamma + blockIdx.x * 32 + ty;
+        *to = accumulate ? *to + total : total;
+    }
 }
 
 // Each row's r and mean(g u).
