@@ -126,30 +126,27 @@ StripPlan strip_plan(const sc_ctx* c, size_t rows, size_t cols) {
 
 
 // Shared memory of the ring kernels: all of a CTA's, once per build and device.
-template <typename T, int TEAM, int V, bool DROP>
+template <typename T, int TEAM, int V, bool DROP, bool WIDE>
 int ring_ready(const sc_ctx* c) {
     static std::atomic<uint64_t> ready{0};
     const uint64_t bit = c->device < 64 ? 1ull << c->device : 0;
     if (!(ready.load(std::memory_order_relaxed) & bit)) {
-        SC_CUDA(cudaFuncSetAttribute(norm_grad_ring_kernel<T, TEAM, V, DROP>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES));
+        SC_CUDA(cudaFuncSetAttribute(norm_grad_ring_kernel<T, TEAM, V, DROP, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES));
         ready.fetch_or(bit, std::memory_order_relaxed);
     }
     return SC_OK;
 }
 
-template <typename T, int TEAM, int V, bool DROP, bool RING>
+template <typename T, int TEAM, int V, bool DROP, bool WIDE>
 int launch_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) {
-    // teams a CTA, CTAs an SM by their registers
-    constexpr uint32_t TEAMS = RING ? (TEAM == 32 ? 8 : 1) : grad_teams(TEAM), FIT = TEAM == 32 ? 2 : 512 / TEAM / (RING ? 1 : TEAMS);
+    constexpr uint32_t TEAMS = ring_teams(TEAM, V), FIT = ring_ctas(TEAM, V);
+    // as many stages as leave room for every CTA that fits otherwise, two at least
     NormRing ring{};
-    uint32_t per_sm = FIT;
-    if constexpr (RING) {
-        // as many stages as leave room for every CTA that fits otherwise, two at least
-        ring.row_bytes = a.cols * 2; ring.operands = a.residual.p ? 3 : 2;
-        const uint32_t stage = TEAMS * ring.row_bytes * ring.operands;
-        ring.stages = std::min(RING_MOST_STAGES, std::max(2u, RING_BYTES / FIT / stage));
-        per_sm = std::max(1u, std::min(FIT, RING_BYTES / (ring.stages * stage)));
-    }
+    ring.row_bytes = 16 * (uint32_t)ceil_div(WIDE ? a.cols : a.cols + 7ull, 8); ring.operands = a.residual.p ? 3 : 2;
+    ring.guard = std::min({a.dy.ld, a.h.ld, a.residual.p ? a.residual.ld : a.h.ld}) >= 7 ? 1 : 7;
+    const uint32_t stage = TEAMS * ring.row_bytes * ring.operands;
+    ring.stages = std::min(RING_MOST_STAGES, std::max(2u, RING_BYTES / FIT / stage));
+    const uint32_t per_sm = std::max(1u, std::min(FIT, RING_BYTES / (ring.stages * stage)));
     uint32_t grid = (uint32_t)std::min<uint64_t>(ceil_div(a.rows, TEAMS), (uint64_t)c->sm_count * per_sm);
     if (grid < ceil_div(a.rows, TEAMS) && grid >= 8) grid &= ~7u;                          // a team's rows are a multiple of 8 apart
     a.part_ld = ((uint64_t)a.cols + 7) & ~7ull;
@@ -158,13 +155,10 @@ int launch_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) 
         if (const int rc = layer_scratch(c, grid * a.part_ld * sizeof(float), st)) return rc;
         partial = reinterpret_cast<float*>(c->d_layer + TICKET_BYTES);
     }
-    if constexpr (RING) {
-        if (const int rc = ring_ready<T, TEAM, V, DROP>(c)) return rc;
+    if (const int rc = ring_ready<T, TEAM, V, DROP, WIDE>(c)) return rc;
+    {
         Launch l(c, KIND_RMS_NORM_GRAD, st);
-        launch(norm_grad_ring_kernel<T, TEAM, V, DROP>, grid, TEAMS * TEAM, ring.stages * ring.row_bytes * ring.operands * TEAMS, 1, st, a, ring, partial, c->d_status);
-    } else {
-        Launch l(c, KIND_RMS_NORM_GRAD, st);
-        launch(norm_grad_rows_kernel<T, TEAM, V, DROP>, grid, TEAMS * TEAM, 0, 1, st, a, partial);
+        launch(norm_grad_ring_kernel<T, TEAM, V, DROP, WIDE>, grid, TEAMS * TEAM, ring.stages * stage, 1, st, a, ring, partial, c->d_status);
     }
     if (dgamma) {
         Launch l(c, KIND_RMS_NORM_GRAD, st);
@@ -176,13 +170,21 @@ int launch_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) 
 template <typename T>
 int run_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) {
     const bool wide = unshifted(a.phase, a.cols) && a.h.vec && a.gamma.vec && a.residual.vec && a.dh.vec && a.dx.vec, drop = a.drop.cut && a.dx.p;
-    // rows in registers want fewer elements a thread than rows in shared memory
-#define SC_TEAM(TEAM, V, RING) \
-    if (wide == RING && a.cols + (RING ? 0ull : 7ull) <= TEAM * V * 8) \
-        return drop ? launch_norm_grad<T, TEAM, V, true, RING>(c, a, dgamma, st) : launch_norm_grad<T, TEAM, V, false, RING>(c, a, dgamma, st);
-    SC_TEAM(32, 1, true) SC_TEAM(32, 2, true) SC_TEAM(32, 4, true) SC_TEAM(128, 2, true) SC_TEAM(256, 2, true) SC_TEAM(256, 4, true) SC_TEAM(512, 4, true)
-    SC_TEAM(32, 1, false) SC_TEAM(32, 2, false) SC_TEAM(128, 1, false) SC_TEAM(128, 2, false) SC_TEAM(256, 2, false) SC_TEAM(512, 2, false) SC_TEAM(512, 4, false)
+    const bool ringed = a.h.vec && a.residual.vec;                 // results of another phase leave in single elements
+    const uint64_t held = wide ? a.cols : a.cols + 7ull;
+#define SC_TEAM(TEAM, V) \
+    if (ringed && held <= TEAM * V * 8) { \
+        if (wide) return drop ? launch_norm_grad<T, TEAM, V, true, true>(c, a, dgamma, st) : launch_norm_grad<T, TEAM, V, false, true>(c, a, dgamma, st); \
+        return drop ? launch_norm_grad<T, TEAM, V, true, false>(c, a, dgamma, st) : launch_norm_grad<T, TEAM, V, false, false>(c, a, dgamma, st); \
+    }
+    SC_TEAM(32, 1) SC_TEAM(32, 2)
+    // A handful of shifted rows is over sooner with a chunk a thread, whose code is fetched cold (509 x 1001: 6.5 against 8.9 us); many rows
+    // are not (16384 x 1001: 50 against 36), nor are rows without shifts (2048 x 1024: 9.5 against 8.2).
+    if (ringed && !wide && held <= 1024 && a.rows <= 4ull * c->sm_count)
+        return drop ? launch_norm_grad<T, 128, 1, true, false>(c, a, dgamma, st) : launch_norm_grad<T, 128, 1, false, false>(c, a, dgamma, st);
+    SC_TEAM(32, 4) SC_TEAM(128, 2) SC_TEAM(256, 2) SC_TEAM(256, 4) SC_TEAM(512, 4)
 #undef SC_TEAM
+    // rows too long for a ring's stages, or inputs of several phases
     const StripPlan plan = strip_plan(c, a.rows, a.cols);
     if (const int rc = layer_scratch(c, plan.partial + plan.stats, st)) return rc;
     a.runs = plan.runs; a.run_rows = plan.run_rows;

@@ -431,19 +431,6 @@ __device__ __forceinline__ void norm_grad_stats8(const Pair d[4], const Pair f[4
         dot = fma2(d[i] * g[i], f[i], dot);
     }
 }
-template <int TEAM>
-__device__ __forceinline__ void team_reduce(float& v, float& u, float2* slots, uint32_t team) {
-    v = warp_sum(v);
-    u = warp_sum(u);
-    if constexpr (TEAM > 32) {
-        if ((threadIdx.x & 31u) == 0) slots[(threadIdx.x % TEAM) >> 5] = make_float2(v, u);
-        asm volatile("bar.sync %0, %1;" ::"r"(1u + team), "n"(TEAM) : "memory");      // the team's own barrier
-        v = u = 0.0f;
-#pragma unroll
-        for (int w = 0; w < TEAM / 32; ++w) { v += slots[w].x; u += slots[w].y; }
-    }
-}
-
 // A CTA's column sums to its partial row; those of several teams are joined in order first, 8 columns a thread at a time.
 template <int TEAM, int TEAMS, int V, bool WIDE>
 __device__ __forceinline__ void norm_leave_sums(const Pair (&sum)[V][4], uint32_t t, uint32_t team, int shift, uint32_t cols, float* partial) {
@@ -491,80 +478,32 @@ __device__ __forceinline__ void norm_leave_sums(const Pair (&sum)[V][4], uint32_
     }
 }
 
-// A team a row, V times eight elements a thread, from registers; teams walk the rows with their columns' sums in registers and leave one
-// partial row of sums a CTA, so that few CTAs of several teams leave little to join.  Their steps are multiples of 8 rows: all of a team's rows
-// have the same shift and the same columns.
-constexpr int grad_teams(int team) { return team == 32 ? 8 : team == 128 ? 4 : 1; }
-template <typename T, int TEAM, int V, bool DROP>
-__global__ void __launch_bounds__(grad_teams(TEAM) * TEAM, TEAM == 32 ? 2 : 1) norm_grad_rows_kernel(NormGradArgs a, float* partial) {
-    constexpr int TEAMS = TEAM == 32 ? 8 : TEAM == 128 ? 4 : 1;
-    __shared__ float2 slots[2][TEAMS][TEAM / 32];
-    wait_for_predecessor();
-    release_successor();
-    const uint32_t t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-    const uint64_t first = (uint64_t)blockIdx.x * TEAMS + team;
-    const int shift = row_shift<false>(a.phase, first), from = (int)(t * 8) - shift, cols = (int)a.cols;
-    Raw8<T> gr[V];
-    Pair sum[V][4];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        gr[j] = across_load8<T, false>(a.gamma, from + j * TEAM * 8, cols);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum[j][i] = pair(0.0f);
-    }
-#pragma unroll
-    for (int j = 0; j < V; ++j) gr[j] = across_join8<T, false>(a.gamma, gr[j], from + j * TEAM * 8, cols);
-    uint32_t turn = 0;
-    for (uint64_t row = first; row < a.rows; row += (uint64_t)gridDim.x * TEAMS, turn ^= 1u) {
-        const RowIn<T> dyr = row_in<T, false>(a.dy, row, cols), hrow = row_in<T, false>(a.h, row, cols), rr = row_in<T, false>(a.residual, row, cols);
-        Raw8<T> dr[V], hr[V], er[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            dr[j] = row_load8<T, false>(dyr, from + j * TEAM * 8, cols);
-            hr[j] = row_load8<T, false>(hrow, from + j * TEAM * 8, cols);
-            if (a.residual.p) er[j] = row_load8<T, false>(rr, from + j * TEAM * 8, cols);
-        }
-        Pair ss = pair(0.0f), dd = pair(0.0f);
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            Pair d[4], f[4], g[4];
-            row_keep8<T, false>(dr[j], from + j * TEAM * 8, cols);
-            row_keep8<T, false>(hr[j], from + j * TEAM * 8, cols);
-            to_pairs(dr[j], d); to_pairs(hr[j], f); to_pairs(gr[j], g);
-            norm_grad_stats8(d, f, g, ss, dd);
-        }
-        const float2 s2 = both(ss), d2 = both(dd);
-        float square = s2.x + s2.y, dot = d2.x + d2.y;
-        team_reduce<TEAM>(square, dot, slots[turn][team], team);
-        const float r = rms_inverse(square, a.mean, a.eps), mean_gu = dot * r * a.mean;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            Pair d[4], f[4], g[4], e[4];
-            to_pairs(dr[j], d); to_pairs(hr[j], f); to_pairs(gr[j], g);
-            if (a.residual.p) to_pairs(er[j], e);
-            else
-#pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] = pair(0.0f);
-            norm_grad8<T, DROP, false>(a, row, from + j * TEAM * 8, r, mean_gu, d, f, g, e, sum[j]);
-        }
-    }
-    if (!partial) return;
-    norm_leave_sums<TEAM, TEAMS, V, false>(sum, t, team, shift, a.cols, partial + (uint64_t)blockIdx.x * a.part_ld);
-}
-
-// The same for rows that take 16-byte accesses, from a ring of shared-memory stages that bulk copies fill ahead of use: loads are in
-// flight while a row is reduced and written, and its operands are read from there twice instead of being kept in registers.  A
-// warp has a ring of its own; a larger team fills a stage again after the next row's barrier, which every thread reaches done with it.
-struct NormRing { uint32_t stages, row_bytes, operands; };
+// A team a row, V times eight elements a thread, for inputs of one phase, from a ring of shared-memory stages that bulk copies fill
+// ahead of use: loads are in flight while a row is reduced and written, and its operands are read from there twice instead of being
+// kept in registers.  Teams walk the rows with their columns' sums in registers and leave one partial row of sums a CTA; their steps are
+// multiples of 8 rows, so that all of a team's rows have the same shift and the same columns.  A warp has a ring of its own; a larger team
+// fills a stage again after the next row's barrier, which every thread reaches done with it.
+// row_bytes: of a stage's place for one operand; guard: rows at the matrix's ends whose chunks reach beyond it
+struct NormRing { uint32_t stages, row_bytes, operands, guard; };
 constexpr uint32_t RING_MOST_STAGES = 8;
-template <typename T, int TEAM, int V, bool DROP>
-__global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 512 / TEAM) norm_grad_ring_kernel(NormGradArgs a, NormRing ring, float* partial,
-                                                                                                              int* status) {
-    constexpr int TEAMS = TEAM == 32 ? 8 : 1;
+// Teams a CTA, and CTAs an SM: 16 warps of up to 128 registers a thread.
+__host__ __device__ constexpr int ring_teams(int team, int v) { return team == 32 ? 8 : team == 128 && v == 1 ? 4 : 1; }
+__host__ __device__ constexpr int ring_ctas(int team, int v) { return 512 / (team * ring_teams(team, v)); }
+// A team's barrier; whether all of its threads say yes.
+template <int TEAM>
+__device__ __forceinline__ bool team_and(bool yes, uint32_t team) {
+    uint32_t all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred.aligned q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(all) : "r"((uint32_t)yes), "r"(team + 1), "n"(TEAM) : "memory");
+    return all != 0;
+}
+template <typename T, int TEAM, int V, bool DROP, bool WIDE>
+__global__ void __launch_bounds__(ring_teams(TEAM, V) * TEAM, ring_ctas(TEAM, V)) norm_grad_ring_kernel(NormGradArgs a, NormRing ring, float* partial, int* status) {
+    constexpr int TEAMS = ring_teams(TEAM, V);
     extern __shared__ __align__(128) uint8_t raw[];
     __shared__ __align__(8) unsigned long long bars[TEAMS * RING_MOST_STAGES];
-    __shared__ float2 slots[2][TEAM / 32];
-    const uint32_t t = TEAM == 32 ? threadIdx.x & 31u : threadIdx.x, team = TEAM == 32 ? threadIdx.x >> 5 : 0u;
+    __shared__ float2 slots[2][TEAMS][TEAM / 32];
+    const uint32_t t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
     const uint32_t stage_bytes = ring.operands * ring.row_bytes;
     const uint8_t* own = raw + team * ring.stages * stage_bytes;
     const uint32_t base = smem_addr(own), full = smem_addr(bars + team * RING_MOST_STAGES);
@@ -578,13 +517,26 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 512 
     const uint64_t first = (uint64_t)blockIdx.x * TEAMS + team, step = (uint64_t)gridDim.x * TEAMS;
     const uint32_t mine = first < a.rows ? (uint32_t)((a.rows - first + step - 1) / step) : 0u;
     uint32_t filled = 0, fill_stage = 0;
+    const int shift = row_shift<WIDE>(a.phase, first), cols = (int)a.cols;
+    const uint32_t chunks = (a.cols + (uint32_t)shift + 7) / 8;
+    // What of a row's chunks is copied: of the matrix's first and last rows not the ones that reach beyond it.
+    struct Part { uint32_t from, to; };
+    const auto part_of = [&](uint64_t row) {
+        if constexpr (WIDE) return Part{0u, chunks};
+        return Part{shift && row < ring.guard ? 1u : 0u, (cols + shift) % 8 && row + ring.guard >= a.rows ? chunks - 1 : chunks};
+    };
     const auto fill = [&] {                                            // this team's next row
         const uint64_t row = first + filled * step;
-        const uint32_t bar = full + 8 * fill_stage, to = base + fill_stage * stage_bytes;
-        mbar_expect_tx(bar, stage_bytes);
-        bulk_load(to, static_cast<const T*>(a.dy.p) + row * a.dy.ld, ring.row_bytes, bar);
-        bulk_load(to + ring.row_bytes, static_cast<const T*>(a.h.p) + row * a.h.ld, ring.row_bytes, bar);
-        if (a.residual.p) bulk_load(to + 2 * ring.row_bytes, static_cast<const T*>(a.residual.p) + row * a.residual.ld, ring.row_bytes, bar);
+        const uint32_t bar = full + 8 * fill_stage;
+        const Part p = part_of(row);
+        const uint32_t bytes = p.to > p.from ? 16 * (p.to - p.from) : 0u, to = base + fill_stage * stage_bytes + 16 * p.from;
+        const int64_t at = 8 * (int64_t)p.from - shift;
+        mbar_expect_tx(bar, bytes * ring.operands);
+        if (bytes) {
+            bulk_load(to, static_cast<const T*>(a.dy.p) + row * a.dy.ld + at, bytes, bar);
+            bulk_load(to + ring.row_bytes, static_cast<const T*>(a.h.p) + row * a.h.ld + at, bytes, bar);
+            if (a.residual.p) bulk_load(to + 2 * ring.row_bytes, static_cast<const T*>(a.residual.p) + row * a.residual.ld + at, bytes, bar);
+        }
         ++filled;
         if (++fill_stage == ring.stages) fill_stage = 0;
     };
@@ -594,28 +546,37 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 512 
     Pair sum[V][4];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        gr[j] = across_load8<T, true>(a.gamma, (int)((j * TEAM + t) * 8), (int)a.cols);
+        gr[j] = across_load8<T, WIDE>(a.gamma, (int)((j * TEAM + t) * 8) - shift, cols);
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[j][i] = pair(0.0f);
     }
+#pragma unroll
+    for (int j = 0; j < V; ++j) gr[j] = across_join8<T, WIDE>(a.gamma, gr[j], (int)((j * TEAM + t) * 8) - shift, cols);
     uint32_t stage = 0, phase = 0;
     bool ok = true;
     for (uint32_t n = 0; n < mine; ++n) {
         const uint64_t row = first + n * step;
         const uint8_t* at = own + stage * stage_bytes;
-        const auto operand = [&](uint32_t which, uint32_t c0, Pair v[4]) {
+        const Part part = part_of(row);
+        // a chunk from its place, or, where it was not copied, from memory
+        const auto operand = [&](int which, const InRows& m, uint32_t chunk) {
             Raw8<T> x;
-            x.v = *reinterpret_cast<const uint4*>(at + which * ring.row_bytes + c0 * 2);
-            to_pairs(x, v);
+            x.v = *reinterpret_cast<const uint4*>(at + which * ring.row_bytes + chunk * 16);
+            if constexpr (!WIDE)
+                if (chunk < part.from || chunk >= part.to)
+                    x.v = load_some(static_cast<const uint16_t*>(m.p) + row * m.ld, (int)(chunk * 8) - shift, cols);
+            return x;
         };
         ok = mbar_wait(full + 8 * stage, phase);
         Pair ss = pair(0.0f), dd = pair(0.0f);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            if ((j * TEAM + t) * 8 >= a.cols) break;
+            if (j * TEAM + t >= chunks) break;
             Pair d[4], f[4], g[4];
-            operand(0, (j * TEAM + t) * 8, d);
-            operand(1, (j * TEAM + t) * 8, f);
+            Raw8<T> dr = operand(0, a.dy, j * TEAM + t), hr = operand(1, a.h, j * TEAM + t);
+            row_keep8<T, WIDE>(dr, (int)((j * TEAM + t) * 8) - shift, cols);
+            row_keep8<T, WIDE>(hr, (int)((j * TEAM + t) * 8) - shift, cols);
+            to_pairs(dr, d); to_pairs(hr, f);
             to_pairs(gr[j], g);
             norm_grad_stats8(d, f, g, ss, dd);
         }
@@ -624,9 +585,9 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 512 
         if constexpr (TEAM == 32) {
             if (!(ok = __all_sync(0xFFFFFFFFu, ok))) break;            // the wait ran out: the team leaves together
         } else {
-            float2* slot = slots[n & 1u];
+            float2* slot = slots[n & 1u][team];
             if ((t & 31u) == 0) slot[t >> 5] = make_float2(square, dot);
-            if (!(ok = __syncthreads_and(ok))) break;
+            if (!(ok = team_and<TEAM>(ok, team))) break;
             if (t == 0 && n > 0 && filled < mine) fill();
             square = dot = 0.0f;
 #pragma unroll
@@ -635,17 +596,15 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 512 
         const float r = rms_inverse(square, a.mean, a.eps), mean_gu = dot * r * a.mean;
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const uint32_t c0 = (j * TEAM + t) * 8;
-            if (c0 >= a.cols) break;
+            const uint32_t chunk = j * TEAM + t;
+            if (chunk >= chunks) break;
             Pair d[4], f[4], g[4], e[4];
-            operand(0, c0, d);
-            operand(1, c0, f);
-            to_pairs(gr[j], g);
-            if (a.residual.p) operand(2, c0, e);
+            to_pairs(operand(0, a.dy, chunk), d); to_pairs(operand(1, a.h, chunk), f); to_pairs(gr[j], g);
+            if (a.residual.p) to_pairs(operand(2, a.residual, chunk), e);
             else
 #pragma unroll
                 for (int i = 0; i < 4; ++i) e[i] = pair(0.0f);
-            norm_grad8<T, DROP, true>(a, row, (int)c0, r, mean_gu, d, f, g, e, sum[j]);
+            norm_grad8<T, DROP, WIDE>(a, row, (int)(chunk * 8) - shift, r, mean_gu, d, f, g, e, sum[j]);
         }
         if constexpr (TEAM == 32) {
             __syncwarp();
@@ -658,7 +617,7 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 2 : 512 
         for (uint32_t n = filled > ring.stages ? filled - ring.stages : 0; n < filled; ++n) mbar_wait(full + 8 * (n % ring.stages), (n / ring.stages) & 1u);
     }
     if (!partial) return;
-    norm_leave_sums<TEAM, TEAMS, V, true>(sum, t, team, 0, a.cols, partial + (uint64_t)blockIdx.x * a.part_ld);
+    norm_leave_sums<TEAM, TEAMS, V, WIDE>(sum, t, team, shift, a.cols, partial + (uint64_t)blockIdx.x * a.part_ld);
 }
 
 // Column sums from the CTAs' partial rows: 32 columns a CTA, one of JOIN_LANES rows a thread, joined in order.
