@@ -48,26 +48,28 @@ bool drop_of(double p, uint64_t seed, size_t cols, Drop& d) {
 }
 inline bool eps_ok(float eps) { return eps >= 0.0f && eps <= 3.402823466e38f; }
 
-// Runs f(team, elements / 8 a thread) for the threads that hold a row of `cols` elements, shifted by up to 7; false where it is too long for
-// them.
-template <typename F>
+// Runs f(team, elements / 8 a thread, wide) for the threads that hold a row of `cols` elements, and up to 7 more where rows are shifted; false
+// where it is too long for them.
+template <bool WIDE, typename F>
 bool with_team(size_t cols, F&& f) {
     using std::integral_constant;
-#define SC_TEAM(TEAM, V) if (cols <= (size_t)TEAM * V * 8) { f(integral_constant<int, TEAM>(), integral_constant<int, V>()); return true; }
+#define SC_TEAM(TEAM, V) \
+    if (cols + (WIDE ? 0 : 7) <= (size_t)TEAM * V * 8) { f(integral_constant<int, TEAM>(), integral_constant<int, V>(), integral_constant<bool, WIDE>()); return true; }
     SC_TEAM(32, 1) SC_TEAM(32, 2) SC_TEAM(32, 4) SC_TEAM(128, 2) SC_TEAM(256, 2) SC_TEAM(256, 4) SC_TEAM(512, 4) SC_TEAM(1024, 4)
 #undef SC_TEAM
     return false;
 }
+template <typename F>
+bool with_team(bool wide, size_t cols, F&& f) { return wide ? with_team<true>(cols, f) : with_team<false>(cols, f); }
 inline uint32_t team_grid(int team, size_t rows) { return (uint32_t)(team == 32 ? ceil_div(rows, 8) : rows); }
 inline int team_threads(int team) { return team == 32 ? 256 : team; }
 
 template <typename T>
 void run_quantize(sc_ctx* c, const QuantizeArgs& a, float* scales, cudaStream_t st) {
     const bool wide = unshifted(a.phase, a.cols) && a.q.vec;
-    const bool held = with_team(wide ? a.cols : a.cols + 7ull, [&](auto team, auto v) {
-        constexpr int TEAM = decltype(team)::value, V = decltype(v)::value;
-        if (wide) launch(quantize_rows_kernel<T, TEAM, V, true>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
-        else launch(quantize_rows_kernel<T, TEAM, V, false>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
+    const bool held = with_team(wide, a.cols, [&](auto team, auto v, auto whole) {
+        constexpr int TEAM = decltype(team)::value;
+        launch(quantize_rows_kernel<T, TEAM, decltype(v)::value, decltype(whole)::value>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
     });
     if (!held) launch(quantize_kernel<T>, row_grid(c, a.rows), NORM_THREADS, 0, 1, st, a, scales);
 }
@@ -101,10 +103,14 @@ void run_dropout(sc_ctx* c, size_t rows, size_t cols, const DropArgs& a, cudaStr
 template <typename T, bool DROP>
 void run_norm(sc_ctx* c, const NormArgs& a, float* scales, cudaStream_t st) {
     const bool wide = unshifted(a.phase, a.cols) && a.residual.vec && a.gamma.vec && a.h.vec && a.y.vec && a.q.vec;
-    const bool held = with_team(wide ? a.cols : a.cols + 7ull, [&](auto team, auto v) {
-        constexpr int TEAM = decltype(team)::value, V = decltype(v)::value;
-        if (wide) launch(rms_norm_rows_kernel<T, TEAM, V, DROP, true>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
-        else launch(rms_norm_rows_kernel<T, TEAM, V, DROP, false>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
+    // shifted rows carry more code a chunk: 16384 x 1001 takes 27.6 us with one chunk a thread, 31.0 with four; 64 x 1001 2.2 and 4.3
+    if (!wide && a.cols + 7ull > 512 && a.cols + 7ull <= 1024) {
+        launch(rms_norm_rows_kernel<T, 128, 1, DROP, false>, team_grid(128, a.rows), team_threads(128), 0, 1, st, a, scales);
+        return;
+    }
+    const bool held = with_team(wide, a.cols, [&](auto team, auto v, auto whole) {
+        constexpr int TEAM = decltype(team)::value;
+        launch(rms_norm_rows_kernel<T, TEAM, decltype(v)::value, DROP, decltype(whole)::value>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
     });
     if (!held) launch(rms_norm_kernel<T>, row_grid(c, a.rows), NORM_THREADS, 0, 1, st, a, scales);
 }
