@@ -48,28 +48,28 @@ bool drop_of(double p, uint64_t seed, size_t cols, Drop& d) {
 }
 inline bool eps_ok(float eps) { return eps >= 0.0f && eps <= 3.402823466e38f; }
 
-// Runs f(team, elements / 8 a thread, wide) for the threads that hold a row of `cols` elements, and up to 7 more where rows are shifted; false
-// where it is too long for them.
-template <bool WIDE, typename F>
-bool with_team(size_t cols, F&& f) {
+// Runs f(team, elements / 8 a thread) for the threads that hold a row of `held` elements; false where it is too long for them.  `held` is
+// the row and, where the first operand's rows are shifted, 7 more: how a row is shared out, and with it the order of its sums, does
+// not depend on where the results or the other operands lie.
+template <typename F>
+bool with_team(size_t held, F&& f) {
     using std::integral_constant;
-#define SC_TEAM(TEAM, V) \
-    if (cols + (WIDE ? 0 : 7) <= (size_t)TEAM * V * 8) { f(integral_constant<int, TEAM>(), integral_constant<int, V>(), integral_constant<bool, WIDE>()); return true; }
+#define SC_TEAM(TEAM, V) if (held <= (size_t)TEAM * V * 8) { f(integral_constant<int, TEAM>(), integral_constant<int, V>()); return true; }
     SC_TEAM(32, 1) SC_TEAM(32, 2) SC_TEAM(32, 4) SC_TEAM(128, 2) SC_TEAM(256, 2) SC_TEAM(256, 4) SC_TEAM(512, 4) SC_TEAM(1024, 4)
 #undef SC_TEAM
     return false;
 }
-template <typename F>
-bool with_team(bool wide, size_t cols, F&& f) { return wide ? with_team<true>(cols, f) : with_team<false>(cols, f); }
+inline uint64_t held_of(const Phase& phase, uint64_t cols) { return unshifted(phase, cols) ? cols : cols + 7; }
 inline uint32_t team_grid(int team, size_t rows) { return (uint32_t)(team == 32 ? ceil_div(rows, 8) : rows); }
 inline int team_threads(int team) { return team == 32 ? 256 : team; }
 
 template <typename T>
 void run_quantize(sc_ctx* c, const QuantizeArgs& a, float* scales, cudaStream_t st) {
     const bool wide = unshifted(a.phase, a.cols) && a.q.vec;
-    const bool held = with_team(wide, a.cols, [&](auto team, auto v, auto whole) {
-        constexpr int TEAM = decltype(team)::value;
-        launch(quantize_rows_kernel<T, TEAM, decltype(v)::value, decltype(whole)::value>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
+    const bool held = with_team(held_of(a.phase, a.cols), [&](auto team, auto v) {
+        constexpr int TEAM = decltype(team)::value, V = decltype(v)::value;
+        if (wide) launch(quantize_rows_kernel<T, TEAM, V, true>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
+        else launch(quantize_rows_kernel<T, TEAM, V, false>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
     });
     if (!held) launch(quantize_kernel<T>, row_grid(c, a.rows), NORM_THREADS, 0, 1, st, a, scales);
 }
@@ -103,14 +103,16 @@ void run_dropout(sc_ctx* c, size_t rows, size_t cols, const DropArgs& a, cudaStr
 template <typename T, bool DROP>
 void run_norm(sc_ctx* c, const NormArgs& a, float* scales, cudaStream_t st) {
     const bool wide = unshifted(a.phase, a.cols) && a.residual.vec && a.gamma.vec && a.h.vec && a.y.vec && a.q.vec;
+    const uint64_t elements = held_of(a.phase, a.cols);
     // shifted rows carry more code a chunk: 16384 x 1001 takes 27.6 us with one chunk a thread, 31.0 with four; 64 x 1001 2.2 and 4.3
-    if (!wide && a.cols + 7ull > 512 && a.cols + 7ull <= 1024) {
+    if (elements > a.cols && elements > 512 && elements <= 1024) {
         launch(rms_norm_rows_kernel<T, 128, 1, DROP, false>, team_grid(128, a.rows), team_threads(128), 0, 1, st, a, scales);
         return;
     }
-    const bool held = with_team(wide, a.cols, [&](auto team, auto v, auto whole) {
-        constexpr int TEAM = decltype(team)::value;
-        launch(rms_norm_rows_kernel<T, TEAM, decltype(v)::value, DROP, decltype(whole)::value>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
+    const bool held = with_team(elements, [&](auto team, auto v) {
+        constexpr int TEAM = decltype(team)::value, V = decltype(v)::value;
+        if (wide) launch(rms_norm_rows_kernel<T, TEAM, V, DROP, true>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
+        else launch(rms_norm_rows_kernel<T, TEAM, V, DROP, false>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
     });
     if (!held) launch(rms_norm_kernel<T>, row_grid(c, a.rows), NORM_THREADS, 0, 1, st, a, scales);
 }
@@ -148,7 +150,7 @@ int launch_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) 
     constexpr uint32_t TEAMS = ring_teams(TEAM, V), FIT = ring_ctas(TEAM, V);
     // as many stages as leave room for every CTA that fits otherwise, two at least
     NormRing ring{};
-    ring.row_bytes = 16 * (uint32_t)ceil_div(WIDE ? a.cols : a.cols + 7ull, 8); ring.operands = a.residual.p ? 3 : 2;
+    ring.row_bytes = 16 * (uint32_t)ceil_div(held_of(a.phase, a.cols), 8); ring.operands = a.residual.p ? 3 : 2;
     ring.guard = std::min({a.dy.ld, a.h.ld, a.residual.p ? a.residual.ld : a.h.ld}) >= 7 ? 1 : 7;
     const uint32_t stage = TEAMS * ring.row_bytes * ring.operands;
     ring.stages = std::min(RING_MOST_STAGES, std::max(2u, RING_BYTES / FIT / stage));
@@ -177,7 +179,7 @@ template <typename T>
 int run_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) {
     const bool wide = unshifted(a.phase, a.cols) && a.h.vec && a.gamma.vec && a.residual.vec && a.dh.vec && a.dx.vec, drop = a.drop.cut && a.dx.p;
     const bool ringed = a.h.vec && a.residual.vec;                 // results of another phase leave in single elements
-    const uint64_t held = wide ? a.cols : a.cols + 7ull;
+    const uint64_t held = held_of(a.phase, a.cols);
 #define SC_TEAM(TEAM, V) \
     if (ringed && held <= TEAM * V * 8) { \
         if (wide) return drop ? launch_norm_grad<T, TEAM, V, true, true>(c, a, dgamma, st) : launch_norm_grad<T, TEAM, V, false, true>(c, a, dgamma, st); \
@@ -186,7 +188,7 @@ int run_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) {
     SC_TEAM(32, 1) SC_TEAM(32, 2)
     // A handful of shifted rows is over sooner with a chunk a thread, whose code is fetched cold (509 x 1001: 6.5 against 8.9 us); many rows
     // are not (16384 x 1001: 50 against 36), nor are rows without shifts (2048 x 1024: 9.5 against 8.2).
-    if (ringed && !wide && held <= 1024 && a.rows <= 4ull * c->sm_count)
+    if (ringed && held > a.cols && held <= 1024 && a.rows <= 4ull * c->sm_count)
         return drop ? launch_norm_grad<T, 128, 1, true, false>(c, a, dgamma, st) : launch_norm_grad<T, 128, 1, false, false>(c, a, dgamma, st);
     SC_TEAM(32, 4) SC_TEAM(128, 2) SC_TEAM(256, 2) SC_TEAM(256, 4) SC_TEAM(512, 4)
 #undef SC_TEAM

@@ -297,3 +297,76 @@ def test_refusals(ctx):
         with pytest.raises((TypeError, ValueError, sc.SparseCommError)):
             call()
     assert ctx.launch_count == launches
+
+
+@pytest.mark.parametrize("rows,cols", [(9, 264), (40, 1001), (300, 1000), (5, 2050), (3, 4099), (1, 9)])
+@pytest.mark.parametrize("which", ["x", "residual", "gamma", "out", "8 bits"])
+def test_rows_of_several_alignments(ctx, rows, cols, which):
+    """One operand lies apart from the others: the results are those of dense ones, bit for bit where only a result lies apart."""
+    x, r, gamma, g = inputs(torch.bfloat16, rows, cols)
+    new = lambda t=x.dtype: torch.zeros(rows, cols, device="cuda").to(t)  # noqa: E731
+    apart = lambda t: strided(t, 3, 5)  # noqa: E731
+    want = {"h": new(), "y": new(), "q": new(torch.int8), "scales": torch.empty(rows, device="cuda")}
+    ctx.sc_rms_norm(x, gamma, EPS, residual=r, p=0.3, seed=5, **want)
+    given = {"h": new(), "y": new(), "q": new(torch.int8), "scales": torch.empty(rows, device="cuda")}
+    if which == "out":
+        given["h"], given["y"] = apart(given["h"]), strided(given["y"], 1, 2)
+    if which == "8 bits":
+        given["q"] = apart(given["q"])
+    xs, rs = (apart(x) if which == "x" else x), (apart(r) if which == "residual" else r)
+    gs = strided(gamma.view(1, -1), 0, 3).view(-1) if which == "gamma" else gamma
+    ctx.sc_rms_norm(xs, gs, EPS, residual=rs, p=0.3, seed=5, **given)
+    wh, wy = norm64(x, r, gamma, EPS, 5, 0.3)
+    assert torch.equal(given["h"], want["h"])                          # elementwise: no sums
+    assert bool(((given["y"].double() - want["y"].double()).abs() <= wy.abs() * (2.0 ** -7 + depth(cols) * 2.0 ** -23) + 1e-30).all())
+    if which in ("out", "8 bits"):
+        assert all(torch.equal(given[k], want[k]) for k in want)
+    assert int((given["q"].int() - want["q"].int()).abs().max()) <= 1
+
+    dy = (normal(g, rows, cols) * 0.1).to(x.dtype)
+    outs = [{"dh": new(), "dx": new(), "dgamma": torch.empty(cols, device="cuda")} for _ in range(2)]
+    ctx.sc_rms_norm_grad(dy, x, gamma, EPS, residual=r, p=0.3, seed=5, **outs[0])
+    if which == "out":
+        outs[1]["dh"], outs[1]["dx"] = apart(outs[1]["dh"]), strided(outs[1]["dx"], 1, 2)
+    ctx.sc_rms_norm_grad(apart(dy) if which == "8 bits" else dy, xs, gs, EPS, residual=rs, p=0.3, seed=5, **outs[1])
+    (dh, dg), (dh_slack, dg_slack) = norm_grad64(dy, x, gamma, EPS, r)
+    for o in outs:
+        assert_close(o["dh"], dh, dh_slack, x.dtype, "dh")
+        assert_close(o["dgamma"], dg, dg_slack, torch.float32, "dgamma")
+        assert_close(o["dx"], dropped64(dh, 5, 0.3), dropped64(dh_slack + dh.abs() * 2.0 ** -23, 5, 0.3), x.dtype, "dx")
+
+    y, z = new(), apart(new())
+    ctx.sc_dropout(x, y, 0.3, 5, residual=r)
+    ctx.sc_dropout(xs, z if which == "out" else y.clone().copy_(y), 0.3, 5, residual=rs)
+    if which == "out":
+        assert torch.equal(z, y)
+
+
+@pytest.mark.parametrize("cols", [1, 2, 5, 6, 7, 9, 15])
+@pytest.mark.parametrize("rows", [1, 2, 3, 8, 9, 40])
+def test_short_rows_and_their_neighbours(ctx, rows, cols):
+    """Rows shorter than an access: what lies before, between and behind them is neither read nor written."""
+    for dtype in TYPES:
+        check_norm(ctx, dtype, rows, cols, True, 0.3, 0, 1)
+        check_grad(ctx, dtype, rows, cols, True, 0.3, 0, 3)
+        x, r, gamma, _ = inputs(dtype, rows, cols, 3, 5)
+        store = torch.full((rows * (cols + 3) + 40,), float("nan"), device="cuda").to(dtype)
+
+        def among_nan(t):
+            v = store.clone()[5:5 + rows * (cols + 3)].view(rows, cols + 3)[:, :cols]
+            v.copy_(t)
+            return v
+
+        a, b = among_nan(x), among_nan(r)
+        y, h, z = (among_nan(torch.zeros_like(x)) for _ in range(3))
+        ctx.sc_rms_norm(a, gamma, EPS, y=y, h=h, residual=b, p=0.3, seed=2)
+        want_h, want_y = torch.empty(rows, cols, dtype=dtype, device="cuda"), torch.empty(rows, cols, dtype=dtype, device="cuda")
+        ctx.sc_rms_norm(x.contiguous(), gamma, EPS, y=want_y, h=want_h, residual=r.contiguous(), p=0.3, seed=2)
+        assert torch.equal(h, want_h) and bool(torch.isfinite(y).all())
+        ctx.sc_dropout(a, z, 0.3, 2, residual=b)
+        assert torch.equal(z, want_h)
+        for t in (y, h, z):                                             # the rest of the storage is as it was
+            whole = t.as_strided((rows * (cols + 3) + 40 - 5,), (1,), 5)
+            outside = torch.ones(whole.shape, dtype=torch.bool, device="cuda")
+            outside[:rows * (cols + 3)].view(rows, cols + 3)[:, :cols] = False
+            assert bool(torch.isnan(whole[outside]).all())

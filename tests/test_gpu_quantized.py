@@ -271,3 +271,42 @@ def test_refusals(ctx):
         with pytest.raises((TypeError, ValueError, sc.SparseCommError)):
             call()
     assert ctx.launch_count == launches
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 8, 9, 16, 17, 32, 33])
+@pytest.mark.parametrize("N,K", [(1, 16), (15, 48), (40, 1024), (1000, 80), (33, 4112)])
+def test_few_tokens(ctx, M, N, K):
+    ctx.sc_debug_layer_tiles()
+    before = ctx.launch_count
+    check_linear(ctx, torch.bfloat16, "gelu", M, N, K, True, True, False)
+    assert ctx.launch_count - before == 1 or M == 33                    # no copies, no join
+    check_linear(ctx, torch.float16, "none", M, N, K, False, False, True, 16, 16)
+
+
+def test_sums_of_few_tokens_are_exact_at_their_largest(ctx):
+    """A multiple of 16 near the largest sum, which these sizes' kernels take; the result is the exact sum rounded once to 24 bits and once to 8."""
+    K = 131056
+    ones = torch.ones(64, device="cuda")
+    for M in (1, 2, 5, 12, 30):
+        for a, b in ((127, 127), (-128, -128), (-128, 127)):
+            x, w = torch.full((M, K), a, dtype=torch.int8, device="cuda"), torch.full((37, K), b, dtype=torch.int8, device="cuda")
+            x[:, 5], w[:, K - 3] = 1, 1
+            y = torch.empty(M, 37, dtype=torch.bfloat16, device="cuda")
+            ctx.sc_linear_quantized(sc.SC_ACT_NONE, x, ones[:M], w, ones[:37], y)
+            assert bool((y == torch.tensor(float(a * b * (K - 2) + b + a)).to(torch.bfloat16)).all())
+
+
+def test_sums_of_few_tokens_term_by_term(ctx):
+    """Large sums that cancel: every single term is seen in the result."""
+    K = 4096
+    g = rng(3)
+    x = torch.randint(-128, 128, (32, K), generator=g, device="cuda").to(torch.int8)
+    w = torch.randint(-128, 128, (64, K // 2), generator=g, device="cuda").to(torch.int8)
+    w = torch.cat((w, torch.where(w == -128, 127, -w).to(torch.int8)), 1)
+    x = torch.cat((x[:, :K // 2], x[:, :K // 2]), 1)
+    exact = x.double() @ w.double().t()                                 # small: only where w was -128 the halves differ
+    ones = torch.ones(64, device="cuda")
+    for M in (1, 2, 6, 16, 32):
+        y = torch.empty(M, 64, dtype=torch.float16, device="cuda")
+        ctx.sc_linear_quantized(sc.SC_ACT_NONE, x[:M], ones[:M], w, ones, y)
+        assert torch.equal(y, exact[:M].to(torch.float16))
