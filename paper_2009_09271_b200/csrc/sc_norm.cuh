@@ -350,7 +350,7 @@ rms_norm_rows_kernel(NormArgs a, float* scales) {
         const int c0 = first + j * TEAM * 8;
         row_keep8<T, WIDE>(in[j], c0, cols);
         to_pairs(in[j], v[j]);
-        if constexpr (DROP) drop_pairs<WIDE>(a.drop, row, c0, v[j]);
+        if constexpr (DROP) drop_pairs<WIDE>(a.drop, drop_row(a.drop, row), c0, v[j]);
         if (a.residual.p) {
             Pair r[4];
             row_keep8<T, WIDE>(res[j], c0, cols);
@@ -419,7 +419,7 @@ __device__ __forceinline__ void norm_grad8(const NormGradArgs& a, uint64_t row, 
     }
     if (a.dh.p) row_store8<T, WIDE>(a.dh, row, c0, (int)a.cols, e);
     if (!a.dx.p) return;
-    if constexpr (DROP) drop_pairs<WIDE>(a.drop, row, c0, e);
+    if constexpr (DROP) drop_pairs<WIDE>(a.drop, drop_row(a.drop, row), c0, e);
     row_store8<T, WIDE>(a.dx, row, c0, (int)a.cols, e);
 }
 
