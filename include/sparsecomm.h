@@ -286,9 +286,10 @@ int sc_linear_grad_weight(sc_ctx* ctx, int type, const void* dz, size_t lddz, co
  * operators': types SC_BF16 and SC_F16, matrices as rows ld apart, fp32 inside and one rounding at the end, empty sizes allowed,
  * sc_layer_reserve(rows, cols, cols) for a call's workspace.
  *
- * 8-bit rows of a matrix: q int8, and scales, one fp32 a row.  With m the row's largest magnitude the scale is m / 127 (at most the largest
- * number whose 127-fold is finite) and q = rint(v * (127 * (1 / m))), each operation rounded to fp32, ties to even; the value is q * scale.  Rows with m < 2^-100 have
- * scale 0 and q = 0.  A row with an element that is not finite has scale NaN and q = 0, so that all that reads it is NaN.
+ * 8-bit rows of a matrix: q int8, and scales, one fp32 a row.  With m the row's largest magnitude the scale is m / 127 (at most the
+ * largest number whose 127-fold is finite) and q = rint(v * (127 * (1 / m))), each operation rounded to fp32, ties to even; the value is
+ * q * scale.  Rows with m < 2^-100 have scale 0 and q = 0.  A row with an element that is not finite has scale NaN and q = 0, so that
+ * all that reads it is NaN.
  * --------------------------------------------------------------------------------------------------------- */
 
 /* 8-bit rows of x (SC_F32 too), a token's or an output channel's; and their values, rounded to `type`. */
@@ -296,9 +297,9 @@ int sc_quantize(sc_ctx* ctx, int type, const void* x, size_t ldx, size_t rows, s
 int sc_dequantize(sc_ctx* ctx, int type, const int8_t* q, size_t ldq, const float* scales, size_t rows, size_t cols, void* out, size_t ldo,
                   void* stream);
 
-/* sc_linear on 8-bit rows of x [M, K] and W [N, K]: z[m, n] = (sum_k x[m, k] w[n, k]) * x_scales[m] * w_scales[n] + bias[n],
- * y = act(z) + residual, the checkpoint of z on request.  The sums are exact integers, so no result depends on the order of their terms;
- * K < 131072 (SC_ERR_RANGE).  Its gradients are the layer operators': sc_linear_grad_input with W in 16 bits, and
+/* sc_linear on 8-bit rows of x [M, K] and W [N, K], ldx and ldw bytes apart:
+ * z[m, n] = (sum_k x[m, k] w[n, k]) * x_scales[m] * w_scales[n] + bias[n], y = act(z) + residual, the checkpoint of z on request; y may be
+ * residual (same ld).  The sums are exact integers, so no result depends on the order of their terms; K < 131072 (SC_ERR_RANGE).  Its gradients are the layer operators': sc_linear_grad_input with W in 16 bits, and
  * sc_linear_grad_weight with x from sc_dequantize (the rounding to 8 bits is passed straight through). */
 int sc_linear_quantized(sc_ctx* ctx, int type, int act, const int8_t* x, size_t ldx, const float* x_scales, const int8_t* w, size_t ldw,
                         const float* w_scales, const void* bias, const void* residual, size_t ldr, size_t M, size_t N, size_t K, void* y, size_t ldy,

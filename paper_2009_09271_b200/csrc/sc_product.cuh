@@ -777,7 +777,8 @@ __device__ __forceinline__ void tokens_out(const Epilogue& ep, const int (&part)
 }
 
 // The same on 8-bit integers, for one and two tokens: sixteen weights a lane and access, four products an instruction, exact sums.  Rows are
-// 16-byte aligned and a multiple of 16 long.
+// 16-byte aligned and a multiple of 16 long.  1 x 4096 x 4096 takes 5.2 us, 1 x 4096 x 16384 12.5 (5.4 TB/s): the weights' bytes, and 2 us that
+// every launch takes.
 template <typename T, int TOKENS, int WN>
 __global__ void __launch_bounds__(WN * 4 * 32, WN == 2 ? 4 : 1) quantized_tokens_kernel(const uint8_t* x, uint64_t ldx, const uint8_t* w, uint64_t ldw, uint32_t K, Epilogue ep) {
     constexpr int ROWS = 4, WK = 4, COLS = ROWS * WN;
@@ -818,7 +819,7 @@ __global__ void __launch_bounds__(WN * 4 * 32, WN == 2 ? 4 : 1) quantized_tokens
 // The same for up to 32 tokens.  The weights' bytes are everything, and the bytes are multiplied as fp16 numbers, which
 // hold them exactly, by warp-wide matrix instructions of 16 x 8 x 16: those for bytes run at a fiftieth of their rate here (4.5 us per eight
 // tokens at 4096 x 4096), dot products of four bytes take 1 us a token.  fp32 sums of integers are exact up to 2^24; they become integers
-// every 256 terms (at most 2^22).  A warp owns 16 rows of W and walks its share of the reduction, 64 terms a step; a lane loads 16 bytes of
+// every 128 terms (at most 2^21).  A warp owns 16 rows of W and walks its share of the reduction, 64 terms a step; a lane loads 16 bytes of
 // two rows and of one token in eight: the order of a sum's terms is free, so that its own bytes serve as its columns of both
 // operands.  WK warps split a row and join their integers in shared memory; WN = 2 puts 32 outputs, a
 // checkpoint group, in one CTA.
