@@ -382,10 +382,18 @@ rms_norm_rows_kernel(NormArgs a, float* scales) {
     float sum = two.x + two.y;
     uint32_t m = __float_as_uint(top);
     team_reduce<TEAM>(sum, m, slots);
-    const float r = rms_inverse(sum, a.mean, a.eps);
+    float r = rms_inverse(sum, a.mean, a.eps);
     if (a.q.p) {
         const RowScale s = row_scale(__float_as_uint(__uint_as_float(m) * r) & 0x7FFFFFFFu);
-        const float by = s.inv * r;
+        float by = s.inv * r;
+        if (by > 3.402823466e38f) {                          // h gamma next to fp32's smallest numbers: its multiple first, bytes of that
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[j][i] = v[j][i] * pair(r);
+            r = 1.0f;
+            by = s.inv;
+        }
 #pragma unroll
         for (int j = 0; j < V; ++j) row_store_bytes8<WIDE>(a.q, row, first + j * TEAM * 8, cols, row_bytes8(v[j], s.inv == 0.0f ? 0.0f : by));
         if (t == 0) scales[row] = s.scale;

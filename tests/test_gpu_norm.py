@@ -129,6 +129,24 @@ def test_norm_of_small_and_large_rows(ctx, scale):
         check_norm(ctx, torch.bfloat16, 4, 1000, False, 0.0, x=(x.float() * scale).to(torch.bfloat16), eps=0.0)
 
 
+@pytest.mark.parametrize("cols", [40, 1001, 4096, 20000])
+def test_norm_to_8_bits_where_h_gamma_is_next_to_the_smallest_numbers(ctx, cols):
+    """The largest h gamma is 2^-121.6, and 127 over it no fp32 number; the row itself is around 2^-72.  Elements of 2^-6 and more of the largest
+    are normal numbers, the others are off by 2^-150, 2^-28 of the largest, at most."""
+    g = rng(cols)
+    x = torch.randint(-80, 81, (3, cols), generator=g, device="cuda").to(torch.bfloat16) * 2.0 ** -56
+    x[:, 0], x[:, 1] = 80 * 2.0 ** -56, 0.0
+    gamma = torch.full((cols,), 2.0 ** -72, device="cuda", dtype=torch.bfloat16)
+    _, wy = norm64(x, None, gamma, 0.0)
+    y, q, only, scales = torch.empty_like(x), torch.empty_like(x, dtype=torch.int8), torch.empty_like(x, dtype=torch.int8), torch.empty(3, device="cuda")
+    ctx.sc_rms_norm(x, gamma, 0.0, q=only, scales=scales)
+    ctx.sc_rms_norm(x, gamma, 0.0, y=y, q=q, scales=scales)
+    assert torch.equal(q, only) and bool((q[:, 0] == 127).all()) and bool((q[:, 1] == 0).all())
+    slack, step = wy.abs() * depth(cols) * 2.0 ** -24 + wy.abs().amax(1, keepdim=True) * 2.0 ** -28, scales.double()[:, None]
+    assert bool(((q.double() * step - wy).abs() <= step * 0.5 + slack + 127 * step * 2.0 ** -22).all())
+    assert_close(y, wy, slack, torch.bfloat16, "y")
+
+
 # -- backward --------------------------------------------------------------------------------------------------------
 def check_grad(ctx, dtype, rows, cols, residual, p, extra=0, offset=0, eps=EPS):
     h, r, gamma, g = inputs(dtype, rows, cols, extra, offset)
