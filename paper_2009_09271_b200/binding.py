@@ -276,6 +276,12 @@ def _layer_calls(lib):
     return _calls
 
 
+def _tensor_calls(calls):
+    """The compiled caller's functions that take tensors, where it was built for this torch; without them (None) the binding's own checks do."""
+    built_for = getattr(calls, "torch_version", None)
+    return calls if built_for is not None and torch.__version__.split("+")[0] == built_for.split("+")[0] else None
+
+
 class Context:
     """Owns an sc_ctx (scratch memory on the current CUDA device)."""
 
@@ -290,8 +296,7 @@ class Context:
         _check(lib.sc_create(ctypes.byref(self._h), max_n, max_W, max_segments), "sc_create")
         self._layer, self._handle = _layer_calls(lib), self._h.value
         self._device = torch.cuda.current_device()
-        # the compiled caller's functions that take tensors; without it the binding's own checks and calls do
-        self._direct = self._layer if self._layer is not lib else None
+        self._direct = _tensor_calls(self._layer)
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h:
@@ -589,7 +594,7 @@ class Context:
 
     def sc_dropout(self, x, y, p: float, seed: int, residual=None, stream=None) -> None:
         """y <- residual + dropout(x): each element kept with probability 1 - p and scaled by its reciprocal, by the mask that (seed, row,
-        column) give.  The gradient is the same call on dy, without a residual.  y may be x or residual."""
+        column) give.  The gradient is the same call on dy, without a residual.  y may be x or residual.  A captured call keeps its seed."""
         if self._direct is not None:
             code = self._direct.dropout(self._handle, self._device, x, y, p, seed, residual, self._queue(stream))
             if code is not None:

@@ -6,6 +6,7 @@
 // needs 0.4 us to look at a matrix, and a norm has seven.  It checks what the binding checks and calls the library; for any argument
 // that it does not take as it is, it returns None, and the binding's own checks say what is wrong.
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/version.h>
 
 #include "../../include/sparsecomm.h"
 
@@ -369,4 +370,9 @@ static PyMethodDef methods[] = {METHOD("bind", bind),
                                 METHOD("rms_norm_grad", rms_norm_grad),
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_sc_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
-PyMODINIT_FUNC PyInit__sc_calls(void) { return PyModule_Create(&definition); }
+PyMODINIT_FUNC PyInit__sc_calls(void) {
+    PyObject* m = PyModule_Create(&definition);
+    // the tensors' layout is that of the headers it was built with: the binding compares
+    if (m && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) < 0) Py_CLEAR(m);
+    return m;
+}

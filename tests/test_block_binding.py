@@ -49,6 +49,18 @@ def test_null_context_and_wrong_arguments(name, args):
                 getattr(calls, name)(*bad)
 
 
+def test_tensors_are_taken_by_a_caller_built_for_this_torch_only():
+    import types
+    here = torch.__version__.split("+")[0]
+    calls = binding._layer_calls(sc.load_library())
+    if hasattr(calls, "bind"):
+        assert calls.torch_version.split("+")[0] == here and binding._tensor_calls(calls) is calls
+    for built_for, taken in ((here, True), (here + "+cu1", True), ("1.0.0", False), (here + "1", False)):
+        fake = types.SimpleNamespace(torch_version=built_for)
+        assert binding._tensor_calls(fake) is (fake if taken else None)
+    assert binding._tensor_calls(types.SimpleNamespace()) is None and binding._tensor_calls(object()) is None
+
+
 def test_kept_mask_is_the_oracles_generator():
     for seed, rows, cols, p in ((0, 3, 7, 0.5), (2 ** 64 - 5, 2, 8, 0.1), (12345, 1, 1, 0.9)):
         mask, scale = kept_mask(seed, rows, cols, p)
