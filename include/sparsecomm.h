@@ -246,8 +246,8 @@ int sc_layer_reserve(sc_ctx* ctx, size_t M, size_t N, size_t K);
 
 /* Instrumentation for tests: later products of this context run in tiles of rows x cols outputs (256 x 256, 128 x 256, 128 x 128 or
  * 128 x 64), their sums cut into `parts` (1 to 64), instead of what the library chooses for the size; 0, 0, 0 restores its choice.  Products
- * of up to 128 rows take no 256-row tiles, sums no more parts than blocks of 64 terms or 64 MB of partial sums allow, and the few
- * tokens that are served without tiles still are.  Host-side state, no device work. */
+ * of up to 128 rows take no 256-row tiles, sums no more parts than blocks of 64 terms (128 in 8 bits) or 64 MB of partial sums allow, and
+ * the few tokens that 16-bit products serve without tiles still are.  Host-side state, no device work. */
 int sc_debug_layer_tiles(sc_ctx* ctx, int rows, int cols, int parts);
 
 /* Checkpoint of x, and the values of a checkpoint (rounded to `type` where the checkpoint was made from another). */
@@ -299,8 +299,9 @@ int sc_dequantize(sc_ctx* ctx, int type, const int8_t* q, size_t ldq, const floa
 
 /* sc_linear on 8-bit rows of x [M, K] and W [N, K], ldx and ldw bytes apart:
  * z[m, n] = (sum_k x[m, k] w[n, k]) * x_scales[m] * w_scales[n] + bias[n], y = act(z) + residual, the checkpoint of z on request; y may be
- * residual (same ld).  The sums are exact integers, so no result depends on the order of their terms; K < 131072 (SC_ERR_RANGE).  Its gradients are the layer operators': sc_linear_grad_input with W in 16 bits, and
- * sc_linear_grad_weight with x from sc_dequantize (the rounding to 8 bits is passed straight through). */
+ * residual (same ld).  The sums are exact integers, so no result depends on the order of their terms; K < 131072 (SC_ERR_RANGE).  Its
+ * gradients are the layer operators': sc_linear_grad_input with W in 16 bits, and sc_linear_grad_weight with x from sc_dequantize (the
+ * rounding to 8 bits is passed straight through). */
 int sc_linear_quantized(sc_ctx* ctx, int type, int act, const int8_t* x, size_t ldx, const float* x_scales, const int8_t* w, size_t ldw,
                         const float* w_scales, const void* bias, const void* residual, size_t ldr, size_t M, size_t N, size_t K, void* y, size_t ldy,
                         int8_t* q, uint8_t* scales, void* stream);
@@ -308,14 +309,15 @@ int sc_linear_quantized(sc_ctx* ctx, int type, int act, const int8_t* x, size_t 
 /* Dropout with probability p in [0, 1]: y = residual + (kept ? x * 65536 / (65536 - t) : 0), t = rint(65536 p); residual may be NULL.
  * The mask is not stored but drawn from (seed, row, column): with key = mix64(seed, 0x64726F70) and mix64 the generator of the seeded
  * schemes, the four elements of a row from column 4 j share the 64 bits of mix64(key, row * ceil(cols / 4) + j), 16 bits each, the lowest first;
- * an element is kept where its bits are at least t.  Its gradient is the same call, without a residual, on dy.  y may be x or residual
- * (same ld). */
+ * an element is kept where its bits are at least t.  Its gradient is the same call, without a residual, on dy.  A captured call keeps
+ * its seed from replay to replay.  y may be x or residual (same ld). */
 int sc_dropout(sc_ctx* ctx, int type, const void* x, size_t ldx, const void* residual, size_t ldr, double p, uint64_t seed, size_t rows, size_t cols,
                void* y, size_t ldy, void* stream);
 
 /* h = residual + dropout(x; p, seed), r = (mean of the row's h^2 + eps)^(-1/2), y = h r gamma; gamma[cols] is of the type, residual may be
  * NULL, p = 0 drops nothing.  y is written in 16 bits, as 8-bit rows (q and scales), or both; h on request (NULL: not written).  y and q are
- * made from the fp32 h.  Squares are summed in fp32: a row whose sum is not finite gives NaN.  h and y may be x or residual (same ld), each another. */
+ * made from the fp32 h.  Squares are summed in fp32: a row whose sum is not finite gives NaN; h gamma is formed before it is multiplied by
+ * r, and has to stay within fp32's range.  h and y may be x or residual (same ld), each another. */
 int sc_rms_norm(sc_ctx* ctx, int type, const void* x, size_t ldx, const void* residual, size_t ldr, const void* gamma, float eps, double p, uint64_t seed,
                 size_t rows, size_t cols, void* h, size_t ldh, void* y, size_t ldy, int8_t* q, size_t ldq, float* scales, void* stream);
 
