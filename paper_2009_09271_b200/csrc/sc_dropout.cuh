@@ -32,8 +32,7 @@ __device__ __forceinline__ void drop4(const Drop& d, uint64_t word, Pair v[2]) {
     v[0] = pair((lo & 0xFFFFu) >= d.cut ? a.x * d.scale : 0.0f, (lo >> 16) >= d.cut ? a.y * d.scale : 0.0f);
     v[1] = pair((hi & 0xFFFFu) >= d.cut ? b.x * d.scale : 0.0f, (hi >> 16) >= d.cut ? b.y * d.scale : 0.0f);
 }
-// Eight elements from column c0 of the row whose words begin at `base`.  Where c0 is no multiple of 4 they lie across three words; the elements
-// of other rows may come out as anything.
+// Eight elements from column c0 of the row whose words begin at `base`.  Where c0 is no multiple of 4 they lie across three words.
 template <bool WIDE>
 __device__ __forceinline__ void drop_pairs(const Drop& d, uint64_t base, int c0, Pair v[4]) {
     const uint64_t z = base + (uint64_t)(int64_t)(c0 >> 2) * GENERATOR_STEP;
@@ -46,6 +45,11 @@ __device__ __forceinline__ void drop_pairs(const Drop& d, uint64_t base, int c0,
     }
     drop4(d, w[0], v);
     drop4(d, w[1], v + 2);
+}
+// The element of column c alone.
+__device__ __forceinline__ float drop1(const Drop& d, uint64_t base, int c, float v) {
+    const uint64_t word = mix64(base + (uint64_t)(c >> 2) * GENERATOR_STEP, 0);
+    return ((uint32_t)(word >> (16 * (c & 3))) & 0xFFFFu) >= d.cut ? v * d.scale : 0.0f;
 }
 __device__ __forceinline__ void drop8(const Drop& d, uint64_t row, uint32_t c0, float f[8]) {
     Pair v[4];
@@ -76,32 +80,43 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM) dropout_kernel(DropAr
     const uint32_t t = TEAM == 32 ? threadIdx.x & 31u : threadIdx.x;
     const uint64_t row = (uint64_t)blockIdx.x * TEAMS + (TEAM == 32 ? threadIdx.x >> 5 : 0u);
     if (row >= a.rows) return;
-    const int shift = row_shift<WIDE>(a.phase, row), cols = (int)a.cols;
-    const uint32_t chunks = (uint32_t)(((uint64_t)a.cols + shift + 7) / 8);
-    const RowIn<T> xr = row_in<T, WIDE>(a.x, row, cols), rr = row_in<T, WIDE>(a.residual, row, cols);
+    const RowCut cut = row_cut<WIDE>(a.phase, row, a.cols);
+    const T *x = row_of<T>(a.x, row), *res = row_of<T>(a.residual, row);
+    T* y = row_of<T>(a.y, row);
     const uint64_t base = drop_row(a.drop, row);
-    for (uint32_t first = blockIdx.y * (TEAM * V) + t; first < chunks; first += gridDim.y * (TEAM * V)) {
-        Raw8<T> in[V], res[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c0 = chunk_col(first + j * TEAM, shift, a.cols);
-            in[j] = row_load8<T, WIDE>(xr, c0, cols);
-            if (RESIDUAL) res[j] = row_load8<T, WIDE>(rr, c0, cols);
+    if (!WIDE && blockIdx.y == 0 && last_warp<TEAM>(t)) {                  // the ends
+        const int c = end_col(cut, a.cols, t & 31u);
+        if (c >= 0) {
+            float f = element(x[c]);
+            if (a.drop.cut) f = drop1(a.drop, base, c, f);
+            if (RESIDUAL) f += element(res[c]);
+            y[c] = rounded<T>(f);
         }
+    }
+    for (uint32_t first = blockIdx.y * (TEAM * V) + t; first < cut.whole; first += gridDim.y * (TEAM * V)) {
+        Raw8<T> in[V], add[V];
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c0 = chunk_col(first + j * TEAM, shift, a.cols);
-            Pair v[4];
-            to_pairs(in[j], v);
-            if (a.drop.cut) drop_pairs<WIDE>(a.drop, base, c0, v);
-            if constexpr (RESIDUAL) {
-                Pair r[4];
-                to_pairs(res[j], r);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = v[k] + r[k];
+        for (int j = 0; j < V; ++j)
+            if (first + j * TEAM < cut.whole) {
+                const int c = cut.lead + (int)(first + j * TEAM) * 8;
+                in[j] = chunk_load8<T, WIDE>(a.x, x, c);
+                if (RESIDUAL) add[j] = chunk_load8<T, WIDE>(a.residual, res, c);
             }
-            row_store8<T, WIDE>(a.y, row, c0, cols, v);
-        }
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (first + j * TEAM < cut.whole) {
+                const int c = cut.lead + (int)(first + j * TEAM) * 8;
+                Pair v[4];
+                to_pairs(in[j], v);
+                if (a.drop.cut) drop_pairs<WIDE>(a.drop, base, c, v);
+                if constexpr (RESIDUAL) {
+                    Pair r[4];
+                    to_pairs(add[j], r);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = v[k] + r[k];
+                }
+                chunk_store8<T, WIDE>(a.y, y, c, v);
+            }
     }
 }
 

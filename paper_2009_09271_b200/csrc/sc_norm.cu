@@ -33,9 +33,7 @@ bool in_phase(const Phase& phase, const void* p, size_t rows, size_t ld, size_t 
     const Phase own = phase_of(p, rows, ld, elem);
     return !p || (own.first == phase.first && own.ld == phase.ld);
 }
-InRows in_rows(const Phase& phase, const void* p, size_t rows, size_t cols, size_t ld, size_t elem = 2) {
-    return InRows{p, ld, (uint64_t)(rows - 1) * (rows > 1 ? ld : 0) + cols, in_phase(phase, p, rows, ld, elem)};
-}
+InRows in_rows(const Phase& phase, const void* p, size_t rows, size_t ld, size_t elem = 2) { return InRows{p, ld, in_phase(phase, p, rows, ld, elem)}; }
 OutRows out_rows(const Phase& phase, void* p, size_t rows, size_t ld, size_t elem = 2) { return OutRows{p, ld, in_phase(phase, p, rows, ld, elem)}; }
 inline bool unshifted(const Phase& phase, size_t cols) { return phase.first == 0 && phase.ld == 0 && cols % 8 == 0; }
 
@@ -50,25 +48,24 @@ bool drop_of(double p, uint64_t seed, size_t cols, Drop& d) {
 }
 inline bool eps_ok(float eps) { return eps >= 0.0f && eps <= 3.402823466e38f; }
 
-// Runs f(team, elements / 8 a thread) for the threads that hold a row of `held` elements; false where it is too long for them.  `held` is
-// the row and, where the first operand's rows are shifted, 7 more: how a row is shared out, and with it the order of its sums, does
-// not depend on where the results or the other operands lie.
+// Runs f(team, elements / 8 a thread) for the threads that hold a row's chunks of eight; false where it is too long for them.  How a row
+// is shared out, and with it the order of its sums, depends on its length and on how the first operand's rows are cut, not on where the results
+// or the other operands lie.
 template <typename F>
-bool with_team(size_t held, F&& f) {
+bool with_team(uint64_t chunks, F&& f) {
     using std::integral_constant;
-#define SC_TEAM(TEAM, V) if (held <= (size_t)TEAM * V * 8) { f(integral_constant<int, TEAM>(), integral_constant<int, V>()); return true; }
+#define SC_TEAM(TEAM, V) if (chunks <= (uint64_t)TEAM * V) { f(integral_constant<int, TEAM>(), integral_constant<int, V>()); return true; }
     SC_TEAM(32, 1) SC_TEAM(32, 2) SC_TEAM(32, 4) SC_TEAM(128, 2) SC_TEAM(256, 2) SC_TEAM(256, 4) SC_TEAM(512, 4) SC_TEAM(1024, 4)
 #undef SC_TEAM
     return false;
 }
-inline uint64_t held_of(const Phase& phase, uint64_t cols) { return unshifted(phase, cols) ? cols : cols + 7; }
 inline uint32_t team_grid(int team, size_t rows) { return (uint32_t)(team == 32 ? ceil_div(rows, 8) : rows); }
 inline int team_threads(int team) { return team == 32 ? 256 : team; }
 
 template <typename T>
 void run_quantize(sc_ctx* c, const QuantizeArgs& a, float* scales, cudaStream_t st) {
     const bool wide = unshifted(a.phase, a.cols) && a.q.vec;
-    const bool held = with_team(held_of(a.phase, a.cols), [&](auto team, auto v) {
+    const bool held = with_team(a.cols / 8, [&](auto team, auto v) {
         constexpr int TEAM = decltype(team)::value, V = decltype(v)::value;
         if (wide) launch(quantize_rows_kernel<T, TEAM, V, true>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
         else launch(quantize_rows_kernel<T, TEAM, V, false>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
@@ -85,16 +82,29 @@ void run_dequantize(sc_ctx* c, const void* q, size_t ldq, const float* scales, s
         const ItemWalk w = item_walk(c, rows, cols, cols / 16, grid, DEQUANTIZE_UNROLL);
         launch(dequantize_kernel<T>, grid, CKPT_THREADS, 0, 1, st, static_cast<const uint8_t*>(q), ldq, scales, w, static_cast<T*>(out), ldo);
     } else {
-        const Phase phase = phase_of(out, rows, ldo, sizeof(T));
-        const ItemWalk w = item_walk(c, rows, cols, ceil_div(cols + 7, 8), grid);
-        launch(dequantize_any_kernel<T>, grid, CKPT_THREADS, 0, 1, st, in_rows(phase, q, rows, cols, ldq, 1), scales, w, phase, out_rows(phase, out, rows, ldo, sizeof(T)));
+        DequantizeArgs a{};
+        a.rows = rows; a.cols = (uint32_t)cols; a.scales = scales;
+        a.phase = phase_of(out, rows, ldo, sizeof(T));
+        a.q = in_rows(a.phase, q, rows, ldq, 1); a.out = out_rows(a.phase, out, rows, ldo, sizeof(T));
+        const uint64_t chunks = std::max(a.cols / 8, 1u);
+        const auto start = [&](auto team, auto v) {
+            constexpr int TEAM = decltype(team)::value, V = decltype(v)::value;
+            launch(dequantize_rows_kernel<T, TEAM, V>, dim3(team_grid(TEAM, rows), (uint32_t)std::min<uint64_t>(ceil_div(chunks, TEAM * V), 65535)), team_threads(TEAM), 0, 1, st, a);
+        };
+        using std::integral_constant;
+        if (chunks <= 32) start(integral_constant<int, 32>(), integral_constant<int, 1>());
+        else if (chunks <= 64) start(integral_constant<int, 32>(), integral_constant<int, 2>());
+        else if (chunks <= 128 && rows > 16ull * c->sm_count) start(integral_constant<int, 32>(), integral_constant<int, 4>());
+        else if (chunks <= 128) start(integral_constant<int, 128>(), integral_constant<int, 1>());
+        else if (chunks <= 256) start(integral_constant<int, 128>(), integral_constant<int, 2>());
+        else start(integral_constant<int, 256>(), integral_constant<int, 2>());
     }
 }
 
 template <typename T>
 void run_dropout(const sc_ctx* c, const DropArgs& a, cudaStream_t st) {
     const bool wide = unshifted(a.phase, a.cols) && a.residual.vec && a.y.vec;
-    const uint64_t chunks = ceil_div(held_of(a.phase, a.cols), 8);
+    const uint64_t chunks = std::max(a.cols / 8, 1u);
     const auto start = [&](auto team, auto v) {
         constexpr int TEAM = decltype(team)::value, V = decltype(v)::value;
         const dim3 grid(team_grid(TEAM, a.rows), (uint32_t)std::min<uint64_t>(ceil_div(chunks, TEAM * V), 65535));
@@ -118,13 +128,13 @@ void run_dropout(const sc_ctx* c, const DropArgs& a, cudaStream_t st) {
 template <typename T, bool DROP>
 void run_norm(sc_ctx* c, const NormArgs& a, float* scales, cudaStream_t st) {
     const bool wide = unshifted(a.phase, a.cols) && a.residual.vec && a.gamma.vec && a.h.vec && a.y.vec && a.q.vec;
-    const uint64_t elements = held_of(a.phase, a.cols);
+    const uint64_t chunks = a.cols / 8;
     // shifted rows carry more code a chunk: 16384 x 1001 takes 27.6 us with one chunk a thread, 31.0 with four; 64 x 1001 2.2 and 4.3
-    if (elements > a.cols && elements > 512 && elements <= 1024) {
+    if (!unshifted(a.phase, a.cols) && chunks > 64 && chunks <= 128) {
         launch(rms_norm_rows_kernel<T, 128, 1, DROP, false>, team_grid(128, a.rows), team_threads(128), 0, 1, st, a, scales);
         return;
     }
-    const bool held = with_team(elements, [&](auto team, auto v) {
+    const bool held = with_team(chunks, [&](auto team, auto v) {
         constexpr int TEAM = decltype(team)::value, V = decltype(v)::value;
         if (wide) launch(rms_norm_rows_kernel<T, TEAM, V, DROP, true>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
         else launch(rms_norm_rows_kernel<T, TEAM, V, DROP, false>, team_grid(TEAM, a.rows), team_threads(TEAM), 0, 1, st, a, scales);
@@ -165,8 +175,7 @@ int launch_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) 
     constexpr uint32_t TEAMS = ring_teams(TEAM, V), FIT = ring_ctas(TEAM, V);
     // as many stages as leave room for every CTA that fits otherwise, two at least
     NormRing ring{};
-    ring.row_bytes = 16 * (uint32_t)ceil_div(held_of(a.phase, a.cols), 8); ring.operands = a.residual.p ? 3 : 2;
-    ring.guard = std::min({a.dy.ld, a.h.ld, a.residual.p ? a.residual.ld : a.h.ld}) >= 7 ? 1 : 7;
+    ring.row_bytes = 16 * (a.cols / 8 + !WIDE); ring.operands = a.residual.p ? 3 : 2;
     const uint32_t stage = TEAMS * ring.row_bytes * ring.operands;
     ring.stages = std::min(RING_MOST_STAGES, std::max(2u, RING_BYTES / FIT / stage));
     const uint32_t per_sm = std::max(1u, std::min(FIT, RING_BYTES / (ring.stages * stage)));
@@ -194,16 +203,16 @@ template <typename T>
 int run_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) {
     const bool wide = unshifted(a.phase, a.cols) && a.h.vec && a.gamma.vec && a.residual.vec && a.dh.vec && a.dx.vec, drop = a.drop.cut && a.dx.p;
     const bool ringed = a.h.vec && a.residual.vec;                 // results of another phase leave in single elements
-    const uint64_t held = held_of(a.phase, a.cols);
+    const uint32_t chunks = a.cols / 8;
 #define SC_TEAM(TEAM, V) \
-    if (ringed && held <= TEAM * V * 8) { \
+    if (ringed && chunks <= TEAM * V) { \
         if (wide) return drop ? launch_norm_grad<T, TEAM, V, true, true>(c, a, dgamma, st) : launch_norm_grad<T, TEAM, V, false, true>(c, a, dgamma, st); \
         return drop ? launch_norm_grad<T, TEAM, V, true, false>(c, a, dgamma, st) : launch_norm_grad<T, TEAM, V, false, false>(c, a, dgamma, st); \
     }
     SC_TEAM(32, 1) SC_TEAM(32, 2)
     // A handful of shifted rows is over sooner with a chunk a thread, whose code is fetched cold (509 x 1001: 6.5 against 8.9 us); many rows
     // are not (16384 x 1001: 50 against 36), nor are rows without shifts (2048 x 1024: 9.5 against 8.2).
-    if (ringed && held > a.cols && held <= 1024 && a.rows <= 4ull * c->sm_count)
+    if (ringed && !unshifted(a.phase, a.cols) && chunks <= 128 && a.rows <= 4ull * c->sm_count)
         return drop ? launch_norm_grad<T, 128, 1, true, false>(c, a, dgamma, st) : launch_norm_grad<T, 128, 1, false, false>(c, a, dgamma, st);
     SC_TEAM(32, 4) SC_TEAM(128, 2) SC_TEAM(256, 2) SC_TEAM(256, 4) SC_TEAM(512, 4)
 #undef SC_TEAM
@@ -240,7 +249,7 @@ int sc_quantize(sc_ctx* ctx, int type, const void* x, size_t ldx, size_t rows, s
     a.grain_x = grain_of(x, rows > 1 ? ldx : 0, type_bytes(type), 8);
     a.grain_q = grain_of(q, rows > 1 ? ldq : 0, 1, 8);
     a.phase = phase_of(x, rows, ldx, type_bytes(type));
-    a.x = in_rows(a.phase, x, rows, cols, ldx, type_bytes(type));
+    a.x = in_rows(a.phase, x, rows, ldx, type_bytes(type));
     a.q = out_rows(a.phase, q, rows, ldq, 1);
     Launch l(ctx, KIND_QUANTIZE, st);
     if (type == SC_BF16) run_quantize<__nv_bfloat16>(ctx, a, scales, st);
@@ -282,7 +291,7 @@ int sc_dropout(sc_ctx* ctx, int type, const void* x, size_t ldx, const void* res
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     a.rows = rows; a.cols = (uint32_t)cols;
     a.phase = phase_of(x, rows, ldx, 2);
-    a.x = in_rows(a.phase, x, rows, cols, ldx); a.residual = in_rows(a.phase, residual, rows, cols, ldr); a.y = out_rows(a.phase, y, rows, ldy);
+    a.x = in_rows(a.phase, x, rows, ldx); a.residual = in_rows(a.phase, residual, rows, ldr); a.y = out_rows(a.phase, y, rows, ldy);
     Launch l(ctx, KIND_DROPOUT, st);
     if (type == SC_BF16) run_dropout<__nv_bfloat16>(ctx, a, st);
     else run_dropout<__half>(ctx, a, st);
@@ -311,8 +320,8 @@ int sc_rms_norm(sc_ctx* ctx, int type, const void* x, size_t ldx, const void* re
     a.grain_h = grain16(h, rows, ldh); a.grain_y = grain16(y, rows, ldy); a.grain_q = grain_of(q, rows > 1 ? ldq : 0, 1, 8);
     a.eps = eps; a.mean = 1.0f / (float)cols;
     a.phase = phase_of(x, rows, ldx, 2);
-    a.x = in_rows(a.phase, x, rows, cols, ldx); a.residual = in_rows(a.phase, residual, rows, cols, ldr);
-    a.gamma = InRows{gamma, 0, cols, aligned(gamma, 16)};
+    a.x = in_rows(a.phase, x, rows, ldx); a.residual = in_rows(a.phase, residual, rows, ldr);
+    a.gamma = InRows{gamma, 0, aligned(gamma, 16)};
     a.h = out_rows(a.phase, h, rows, ldh); a.y = out_rows(a.phase, y, rows, ldy); a.q = out_rows(a.phase, q, rows, ldq, 1);
     Launch l(ctx, KIND_RMS_NORM, st);
     if (type == SC_BF16) { if (a.drop.cut) run_norm<__nv_bfloat16, true>(ctx, a, scales, st); else run_norm<__nv_bfloat16, false>(ctx, a, scales, st); }
@@ -348,8 +357,8 @@ int sc_rms_norm_grad(sc_ctx* ctx, int type, const void* dy, size_t lddy, const v
     a.grain_r = grain16(residual, rows, ldr); a.grain_dh = grain16(dh, rows, lddh); a.grain_dx = grain16(dx, rows, lddx);
     a.accumulate = accumulate ? 1u : 0u; a.eps = eps; a.mean = 1.0f / (float)cols;
     a.phase = phase_of(dy, rows, lddy, 2);
-    a.dy = in_rows(a.phase, dy, rows, cols, lddy); a.h = in_rows(a.phase, h, rows, cols, ldh); a.residual = in_rows(a.phase, residual, rows, cols, ldr);
-    a.gamma = InRows{gamma, 0, cols, aligned(gamma, 16)};
+    a.dy = in_rows(a.phase, dy, rows, lddy); a.h = in_rows(a.phase, h, rows, ldh); a.residual = in_rows(a.phase, residual, rows, ldr);
+    a.gamma = InRows{gamma, 0, aligned(gamma, 16)};
     a.dh = out_rows(a.phase, dh, rows, lddh); a.dx = out_rows(a.phase, dx, rows, lddx);
     const int rc = type == SC_BF16 ? run_norm_grad<__nv_bfloat16>(ctx, a, dgamma, st) : run_norm_grad<__half>(ctx, a, dgamma, st);
     if (rc) return rc;

@@ -96,6 +96,7 @@ __device__ __forceinline__ uint2 row_bytes8(const Pair v[4], float inv) {
     }
     return ckpt_join8(b);
 }
+__device__ __forceinline__ uint8_t row_byte(float v, float inv) { return inv == 0.0f ? 0 : (uint8_t)__float_as_uint(__fadd_rn(__fmul_rn(v, inv), 12582912.0f)); }
 struct QuantizeArgs {
     uint64_t rows;
     InRows x;
@@ -138,26 +139,28 @@ __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM) quantize_rows_kernel(
     const uint32_t t = TEAM == 32 ? threadIdx.x & 31u : threadIdx.x;
     const uint64_t row = (uint64_t)blockIdx.x * TEAMS + (TEAM == 32 ? threadIdx.x >> 5 : 0u);
     if (row >= a.rows) return;
-    const int c0 = (int)(t * 8) - row_shift<WIDE>(a.phase, row), cols = (int)a.cols;
-    const RowIn<T> from = row_in<T, WIDE>(a.x, row, cols);
+    const RowCut cut = row_cut<WIDE>(a.phase, row, a.cols);
+    const T* from = row_of<T>(a.x, row);
+    uint8_t* to = row_of<uint8_t>(a.q, row);
+    const int ec = !WIDE && last_warp<TEAM>(t) ? end_col(cut, a.cols, t & 31u) : -1;        // the ends are the last warp's
     Raw8<T> raw[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) raw[j] = row_load8<T, WIDE>(from, c0 + j * TEAM * 8, cols);
-    uint32_t m = 0u;
+    for (int j = 0; j < V; ++j) raw[j] = j * TEAM + t < cut.whole ? chunk_load8<T, WIDE>(a.x, from, cut.lead + (int)(j * TEAM + t) * 8) : Raw8<T>{};
+    const float end = ec >= 0 ? element(from[ec]) : 0.0f;
+    uint32_t m = WIDE ? 0u : __float_as_uint(end) & 0x7FFFFFFFu;
     float none = 0.0f;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        row_keep8<T, WIDE>(raw[j], c0 + j * TEAM * 8, cols);
-        m = max(m, abs_max8(raw[j]));
-    }
+    for (int j = 0; j < V; ++j) m = max(m, abs_max8(raw[j]));
     team_reduce<TEAM>(none, m, slots);
     const RowScale s = row_scale(m);
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        Pair v[4];
-        to_pairs(raw[j], v);
-        row_store_bytes8<WIDE>(a.q, row, c0 + j * TEAM * 8, cols, row_bytes8(v, s.inv));
-    }
+    for (int j = 0; j < V; ++j)
+        if (j * TEAM + t < cut.whole) {
+            Pair v[4];
+            to_pairs(raw[j], v);
+            chunk_store_bytes8<WIDE>(a.q, to, cut.lead + (int)(j * TEAM + t) * 8, row_bytes8(v, s.inv));
+        }
+    if (ec >= 0) to[ec] = row_byte(end, s.inv);
     if (t == 0) scales[row] = s.scale;
 }
 
@@ -211,45 +214,52 @@ __global__ void __launch_bounds__(CKPT_THREADS) dequantize_kernel(const uint8_t*
     }
 }
 
-// The same for other rows, in chunks of eight.
-template <typename T>
-__global__ void __launch_bounds__(CKPT_THREADS) dequantize_any_kernel(InRows q, const float* scales, ItemWalk w, Phase phase, OutRows out) {
+// The same for other rows: a team of threads a row, or with blockIdx.y a part of one, V times eight elements a thread at a time.
+struct DequantizeArgs {
+    uint64_t rows;
+    InRows q;
+    OutRows out;
+    const float* scales;
+    uint32_t cols;
+    Phase phase;
+};
+template <typename T, int TEAM, int V>
+__global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM) dequantize_rows_kernel(DequantizeArgs a) {
+    constexpr int TEAMS = TEAM == 32 ? 8 : 1;
     wait_for_predecessor();
     release_successor();
-    const uint64_t first = (uint64_t)blockIdx.x * CKPT_THREADS + threadIdx.x, stride = (uint64_t)gridDim.x * CKPT_THREADS;
-    const int cols = (int)w.cols;
-    ItemAt at(w, first);
-    for (uint64_t base = first; base < w.total; base += stride * DEQUANTIZE_UNROLL) {
-        uint2 raw[DEQUANTIZE_UNROLL];
-        float s[DEQUANTIZE_UNROLL];
-        ItemAt from = at;
+    const uint32_t t = TEAM == 32 ? threadIdx.x & 31u : threadIdx.x;
+    const uint64_t row = (uint64_t)blockIdx.x * TEAMS + (TEAM == 32 ? threadIdx.x >> 5 : 0u);
+    if (row >= a.rows) return;
+    const RowCut cut = row_cut<false>(a.phase, row, a.cols);
+    const uint8_t* q = row_of<uint8_t>(a.q, row);
+    T* out = row_of<T>(a.out, row);
+    const float s = a.scales[row];
+    if (blockIdx.y == 0 && last_warp<TEAM>(t)) {                           // the ends
+        const int c = end_col(cut, a.cols, t & 31u);
+        if (c >= 0) out[c] = rounded<T>((float)(int8_t)q[c] * s);
+    }
+    for (uint32_t first = blockIdx.y * (TEAM * V) + t; first < cut.whole; first += gridDim.y * (TEAM * V)) {
+        uint2 raw[V];
 #pragma unroll
-        for (int u = 0; u < DEQUANTIZE_UNROLL; ++u) {
-            if (base + u * stride < w.total) {
-                raw[u] = row_load_bytes8<false>(q, at.row, chunk_col(at.item, row_shift<false>(phase, at.row), w.cols), cols);
-                s[u] = scales[at.row];
-            }
-            at.next(w);
-        }
+        for (int j = 0; j < V; ++j)
+            if (first + j * TEAM < cut.whole) raw[j] = chunk_load_bytes8(a.q, q, cut.lead + (int)(first + j * TEAM) * 8);
 #pragma unroll
-        for (int u = 0; u < DEQUANTIZE_UNROLL; ++u) {
-            if (base + u * stride < w.total) {
-                const int c0 = chunk_col(from.item, row_shift<false>(phase, from.row), w.cols);
+        for (int j = 0; j < V; ++j)
+            if (first + j * TEAM < cut.whole) {
+                const int c = cut.lead + (int)(first + j * TEAM) * 8;
                 float f[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    f[i] = (__uint_as_float(__byte_perm((i < 4 ? raw[u].x : raw[u].y) ^ 0x80808080u, 0x4B000000u, 0x7440 + (i & 3))) - 8388736.0f) * s[u];
+                    f[i] = (__uint_as_float(__byte_perm((i < 4 ? raw[j].x : raw[j].y) ^ 0x80808080u, 0x4B000000u, 0x7440 + (i & 3))) - 8388736.0f) * s;
                 if constexpr (sizeof(T) == 2) {
                     const Pair v[4] = {pair(f[0], f[1]), pair(f[2], f[3]), pair(f[4], f[5]), pair(f[6], f[7])};
-                    row_store8<T, false>(out, from.row, c0, cols, v);
+                    chunk_store8<T, false>(a.out, out, c, v);
                 } else {
-                    T* to = static_cast<T*>(out.p) + from.row * out.ld;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) if ((uint32_t)c0 + i < (uint32_t)cols) to[c0 + i] = f[i];
+                    *reinterpret_cast<float4*>(out + c) = make_float4(f[0], f[1], f[2], f[3]);
+                    *reinterpret_cast<float4*>(out + c + 4) = make_float4(f[4], f[5], f[6], f[7]);
                 }
             }
-            from.next(w);
-        }
     }
 }
 
@@ -329,7 +339,7 @@ __global__ void __launch_bounds__(NORM_THREADS) rms_norm_kernel(NormArgs a, floa
 // has in flight.  With gamma kept in its own type and h stored after the reduction the 8-bit form took 212 us.  Rows of 16384 and more
 // leave room for two CTAs an SM and one (8192 x 16384 162 us, 2000 x 20000 68).  One token of 4096 takes 1.9 us.
 template <typename T, int TEAM, int V, bool DROP, bool WIDE>
-__global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 3 : TEAM == 1024 ? 1 : TEAM >= 256 && V == 4 ? 1024 / TEAM - (DROP && TEAM == 256) : 1024 / TEAM)
+__global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 3 : TEAM == 1024 ? 1 : TEAM >= 256 && V == 4 ? 1024 / TEAM - (DROP && TEAM == 256) : V == 2 && WIDE && !DROP ? 1536 / TEAM : 1024 / TEAM)
 rms_norm_rows_kernel(NormArgs a, float* scales) {
     constexpr int TEAMS = TEAM == 32 ? 8 : 1;
     __shared__ float2 slots[TEAM / 32];
@@ -338,36 +348,46 @@ rms_norm_rows_kernel(NormArgs a, float* scales) {
     const uint32_t t = TEAM == 32 ? threadIdx.x & 31u : threadIdx.x;
     const uint64_t row = (uint64_t)blockIdx.x * TEAMS + (TEAM == 32 ? threadIdx.x >> 5 : 0u);
     if (row >= a.rows) return;
-    const int first = (int)(t * 8) - row_shift<WIDE>(a.phase, row), cols = (int)a.cols;
-    const RowIn<T> xr = row_in<T, WIDE>(a.x, row, cols), rr = row_in<T, WIDE>(a.residual, row, cols);
+    const RowCut cut = row_cut<WIDE>(a.phase, row, a.cols);
+    const int first = cut.lead + (int)t * 8, cols = (int)a.cols;
+    const int ec = !WIDE && last_warp<TEAM>(t) ? end_col(cut, a.cols, t & 31u) : -1;        // the ends are the last warp's
+    const T *x = row_of<T>(a.x, row), *add = row_of<T>(a.residual, row);
     Raw8<T> in[V], res[V], g[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        in[j] = row_load8<T, WIDE>(xr, first + j * TEAM * 8, cols);
-        if (a.residual.p) res[j] = row_load8<T, WIDE>(rr, first + j * TEAM * 8, cols);
+        in[j] = j * TEAM + t < cut.whole ? chunk_load8<T, WIDE>(a.x, x, first + j * TEAM * 8) : Raw8<T>{};
+        if (a.residual.p) res[j] = j * TEAM + t < cut.whole ? chunk_load8<T, WIDE>(a.residual, add, first + j * TEAM * 8) : Raw8<T>{};
+    }
+    T ends[3] = {};
+    if (ec >= 0) {
+        ends[0] = x[ec];
+        if (a.residual.p) ends[1] = add[ec];
+        ends[2] = static_cast<const T*>(a.gamma.p)[ec];
     }
 #pragma unroll
-    for (int j = 0; j < V; ++j) g[j] = across_load8<T, WIDE>(a.gamma, first + j * TEAM * 8, cols);
+    for (int j = 0; j < V; ++j) g[j] = j * TEAM + t < cut.whole ? across_load8<T, WIDE>(a.gamma, first + j * TEAM * 8, cols) : Raw8<T>{};
     Pair v[V][4], sums = pair(0.0f);
     float top = 0.0f;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
         const int c0 = first + j * TEAM * 8;
-        row_keep8<T, WIDE>(in[j], c0, cols);
+        const bool own = j * TEAM + t < cut.whole;
         to_pairs(in[j], v[j]);
         if constexpr (DROP) drop_pairs<WIDE>(a.drop, drop_row(a.drop, row), c0, v[j]);
         if (a.residual.p) {
             Pair r[4];
-            row_keep8<T, WIDE>(res[j], c0, cols);
             to_pairs(res[j], r);
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[j][i] = v[j][i] + r[i];
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) sums = fma2(v[j][i], v[j][i], sums);       // zeros outside the row, dropped or not
-        if (a.h.p) row_store8<T, WIDE>(a.h, row, c0, cols, v[j]);
+        if (a.h.p && own) chunk_store8<T, WIDE>(a.h, row_of<T>(a.h, row), c0, v[j]);
         Pair w[4];
-        to_pairs(across_join8<T, WIDE>(a.gamma, g[j], c0, cols), w);
+        if (WIDE || own) to_pairs(across_join8<T, WIDE>(a.gamma, g[j], c0, cols), w);
+        else
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = pair(0.0f);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[j][i] = v[j][i] * w[i];
         if (a.q.p) {
@@ -379,7 +399,16 @@ rms_norm_rows_kernel(NormArgs a, float* scales) {
         }
     }
     const float2 two = both(sums);
-    float sum = two.x + two.y;
+    float sum = two.x + two.y, end = 0.0f;
+    if (!WIDE && ec >= 0) {
+        end = element(ends[0]);
+        if constexpr (DROP) end = drop1(a.drop, drop_row(a.drop, row), ec, end);
+        if (a.residual.p) end += element(ends[1]);
+        sum = fmaf(end, end, sum);
+        if (a.h.p) row_of<T>(a.h, row)[ec] = rounded<T>(end);
+        end *= element(ends[2]);
+        top = abs_max(top, end, end);
+    }
     uint32_t m = __float_as_uint(top);
     team_reduce<TEAM>(sum, m, slots);
     float r = rms_inverse(sum, a.mean, a.eps);
@@ -391,20 +420,27 @@ rms_norm_rows_kernel(NormArgs a, float* scales) {
             for (int j = 0; j < V; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[j][i] = v[j][i] * pair(r);
+            end *= r;
             r = 1.0f;
             by = s.inv;
         }
+        if (s.inv == 0.0f) by = 0.0f;
+        uint8_t* q = row_of<uint8_t>(a.q, row);
 #pragma unroll
-        for (int j = 0; j < V; ++j) row_store_bytes8<WIDE>(a.q, row, first + j * TEAM * 8, cols, row_bytes8(v[j], s.inv == 0.0f ? 0.0f : by));
+        for (int j = 0; j < V; ++j)
+            if (j * TEAM + t < cut.whole) chunk_store_bytes8<WIDE>(a.q, q, first + j * TEAM * 8, row_bytes8(v[j], by));
+        if (ec >= 0) q[ec] = row_byte(end, by);
         if (t == 0) scales[row] = s.scale;
     }
     if (a.y.p) {
+        T* y = row_of<T>(a.y, row);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[j][i] = v[j][i] * pair(r);
-            row_store8<T, WIDE>(a.y, row, first + j * TEAM * 8, cols, v[j]);
+            if (j * TEAM + t < cut.whole) chunk_store8<T, WIDE>(a.y, y, first + j * TEAM * 8, v[j]);
         }
+        if (ec >= 0) y[ec] = rounded<T>(end * r);
     }
 }
 
@@ -422,7 +458,7 @@ struct NormGradArgs {
 
 // What a team of threads makes of eight columns of a row once its statistics are known: dh and dx, and the column sums' terms.
 template <typename T, bool DROP, bool WIDE>
-__device__ __forceinline__ void norm_grad8(const NormGradArgs& a, uint64_t row, int c0, float r, float mean_gu, const Pair d[4], const Pair f[4],
+__device__ __forceinline__ void norm_grad8(const NormGradArgs& a, uint64_t row, int c, float r, float mean_gu, const Pair d[4], const Pair f[4],
                                            const Pair g[4], Pair e[4], Pair sum[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -430,10 +466,10 @@ __device__ __forceinline__ void norm_grad8(const NormGradArgs& a, uint64_t row, 
         sum[i] = fma2(d[i], u, sum[i]);
         e[i] = fma2(pair(r), fma2(u, pair(-mean_gu), d[i] * g[i]), e[i]);
     }
-    if (a.dh.p) row_store8<T, WIDE>(a.dh, row, c0, (int)a.cols, e);
+    if (a.dh.p) chunk_store8<T, WIDE>(a.dh, row_of<T>(a.dh, row), c, e);
     if (!a.dx.p) return;
-    if constexpr (DROP) drop_pairs<WIDE>(a.drop, drop_row(a.drop, row), c0, e);
-    row_store8<T, WIDE>(a.dx, row, c0, (int)a.cols, e);
+    if constexpr (DROP) drop_pairs<WIDE>(a.drop, drop_row(a.drop, row), c, e);
+    chunk_store8<T, WIDE>(a.dx, row_of<T>(a.dx, row), c, e);
 }
 
 // Sums of h^2 and g h over eight columns.
@@ -444,51 +480,21 @@ __device__ __forceinline__ void norm_grad_stats8(const Pair d[4], const Pair f[4
         dot = fma2(d[i] * g[i], f[i], dot);
     }
 }
-// A CTA's column sums to its partial row; those of several teams are joined in order first, 8 columns a thread at a time.
-template <int TEAM, int TEAMS, int V, bool WIDE>
-__device__ __forceinline__ void norm_leave_sums(const Pair (&sum)[V][4], uint32_t t, uint32_t team, int shift, uint32_t cols, float* partial) {
-    if constexpr (TEAMS > 1) {
-        constexpr uint32_t WIDTH = TEAM * 8;
-        __shared__ float join[TEAMS][WIDTH + 8];
+// A team's column sums to `to`: its threads' chunks, and the ends.
+template <int TEAM, int V>
+__device__ __forceinline__ void norm_leave_sums(const Pair (&sum)[V][4], float end, int ec, uint32_t t, const RowCut& cut, float* to) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            __syncthreads();
+    for (int j = 0; j < V; ++j) {
+        if (j * TEAM + t >= cut.whole) break;
+        float* at = to + cut.lead + (j * TEAM + t) * 8;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = both(sum[j][i]);
-                const int c = (int)(t * 8) + 2 * i - (WIDE ? 0 : shift);
-                if (WIDE || c >= 0) join[team][c] = f.x;
-                if (WIDE || c + 1 >= 0) join[team][c + 1] = f.y;
-            }
-            // a shifted row's last columns here are its next eight's first
-            if (!WIDE && j + 1 < V && t == 0)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 f = both(sum[j + 1 < V ? j + 1 : j][i]);
-                    join[team][WIDTH - shift + 2 * i] = f.x;               // up to WIDTH + 7
-                    join[team][WIDTH - shift + 2 * i + 1] = f.y;
-                }
-            __syncthreads();
-#pragma unroll
-            for (uint32_t c = threadIdx.x; c < WIDTH; c += TEAMS * TEAM) {
-                float total = 0.0f;
-#pragma unroll
-                for (int w = 0; w < TEAMS; ++w) total += join[w][c];
-                if (j * WIDTH + c < cols) partial[j * WIDTH + c] = total;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int c0 = (int)((j * TEAM + t) * 8) - (WIDE ? 0 : shift);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = both(sum[j][i]);
-                if ((uint32_t)(c0 + 2 * i) < cols) partial[c0 + 2 * i] = f.x;
-                if ((uint32_t)(c0 + 2 * i + 1) < cols) partial[c0 + 2 * i + 1] = f.y;
-            }
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = both(sum[j][i]);
+            at[2 * i] = f.x;
+            at[2 * i + 1] = f.y;
         }
     }
+    if (ec >= 0) to[ec] = end;
 }
 
 // A team a row, V times eight elements a thread, for inputs of one phase, from a ring of shared-memory stages that bulk copies fill
@@ -499,8 +505,8 @@ __device__ __forceinline__ void norm_leave_sums(const Pair (&sum)[V][4], uint32_
 // Bound by HBM at 2048 columns and more: 16384 x 8192 bf16 with residual in 168 us (6.4 TB/s, 0.98 of the copy rate), with dx through dropout
 // 225 (0.91: the generator's products, at half the multiply-add rate).  Narrower rows spend issue slots instead: 65536 x 1024 0.89, 262144 x
 // 256 0.71.  Read twice from HBM by two kernels, statistics and strips, 16384 x 8192 with dropout took 316 us.
-// row_bytes: of a stage's place for one operand; guard: rows at the matrix's ends whose chunks reach beyond it
-struct NormRing { uint32_t stages, row_bytes, operands, guard; };
+// row_bytes: of a stage's place for one operand, sixteen at least more than a row's chunks
+struct NormRing { uint32_t stages, row_bytes, operands; };
 constexpr uint32_t RING_MOST_STAGES = 8;
 // Teams a CTA, and CTAs an SM: 16 warps of up to 128 registers a thread.
 __host__ __device__ constexpr int ring_teams(int team, int v) { return team == 32 ? 8 : team == 128 && v == 1 ? 4 : 1; }
@@ -533,71 +539,76 @@ __global__ void __launch_bounds__(ring_teams(TEAM, V) * TEAM, ring_ctas(TEAM, V)
     const uint64_t first = (uint64_t)blockIdx.x * TEAMS + team, step = (uint64_t)gridDim.x * TEAMS;
     const uint32_t mine = first < a.rows ? (uint32_t)((a.rows - first + step - 1) / step) : 0u;
     uint32_t filled = 0, fill_stage = 0;
-    const int shift = row_shift<WIDE>(a.phase, first), cols = (int)a.cols;
-    const uint32_t chunks = (a.cols + (uint32_t)shift + 7) / 8;
-    // What of a row's chunks is copied: of the matrix's first and last rows not the ones that reach beyond it.
-    struct Part { uint32_t from, to; };
-    const auto part_of = [&](uint64_t row) {
-        if constexpr (WIDE) return Part{0u, chunks};
-        return Part{shift && row < ring.guard ? 1u : 0u, (cols + shift) % 8 && row + ring.guard >= a.rows ? chunks - 1 : chunks};
-    };
+    const RowCut cut = row_cut<WIDE>(a.phase, first, a.cols);
+    const int cols = (int)a.cols;
     const auto fill = [&] {                                            // this team's next row
         const uint64_t row = first + filled * step;
-        const uint32_t bar = full + 8 * fill_stage;
-        const Part p = part_of(row);
-        const uint32_t bytes = p.to > p.from ? 16 * (p.to - p.from) : 0u, to = base + fill_stage * stage_bytes + 16 * p.from;
-        const int64_t at = 8 * (int64_t)p.from - shift;
+        const uint32_t bar = full + 8 * fill_stage, bytes = 16 * cut.whole, to = base + fill_stage * stage_bytes;
         mbar_expect_tx(bar, bytes * ring.operands);
         if (bytes) {
-            bulk_load(to, static_cast<const T*>(a.dy.p) + row * a.dy.ld + at, bytes, bar);
-            bulk_load(to + ring.row_bytes, static_cast<const T*>(a.h.p) + row * a.h.ld + at, bytes, bar);
-            if (a.residual.p) bulk_load(to + 2 * ring.row_bytes, static_cast<const T*>(a.residual.p) + row * a.residual.ld + at, bytes, bar);
+            bulk_load(to, row_of<T>(a.dy, row) + cut.lead, bytes, bar);
+            bulk_load(to + ring.row_bytes, row_of<T>(a.h, row) + cut.lead, bytes, bar);
+            if (a.residual.p) bulk_load(to + 2 * ring.row_bytes, row_of<T>(a.residual, row) + cut.lead, bytes, bar);
         }
         ++filled;
         if (++fill_stage == ring.stages) fill_stage = 0;
     };
     if (t == 0)
         while (filled < mine && filled < ring.stages) fill();
+    // the ends are the last warp's, loaded a row ahead
+    const int ec = !WIDE && last_warp<TEAM>(t) ? end_col(cut, a.cols, t & 31u) : -1;
+    T ends[3] = {};
+    const auto ahead = [&](uint64_t row) {
+        ends[0] = row_of<T>(a.dy, row)[ec];
+        ends[1] = row_of<T>(a.h, row)[ec];
+        if (a.residual.p) ends[2] = row_of<T>(a.residual, row)[ec];
+    };
+    float end_gamma = 0.0f, end_sum = 0.0f;
+    if (ec >= 0) {
+        end_gamma = element(static_cast<const T*>(a.gamma.p)[ec]);
+        if (mine) ahead(first);
+    }
     Raw8<T> gr[V];
     Pair sum[V][4];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        gr[j] = across_load8<T, WIDE>(a.gamma, (int)((j * TEAM + t) * 8) - shift, cols);
+        gr[j] = j * TEAM + t < cut.whole ? across_load8<T, WIDE>(a.gamma, cut.lead + (int)(j * TEAM + t) * 8, cols) : Raw8<T>{};
 #pragma unroll
         for (int i = 0; i < 4; ++i) sum[j][i] = pair(0.0f);
     }
 #pragma unroll
-    for (int j = 0; j < V; ++j) gr[j] = across_join8<T, WIDE>(a.gamma, gr[j], (int)((j * TEAM + t) * 8) - shift, cols);
+    for (int j = 0; j < V; ++j)
+        if (j * TEAM + t < cut.whole) gr[j] = across_join8<T, WIDE>(a.gamma, gr[j], cut.lead + (int)(j * TEAM + t) * 8, cols);
     uint32_t stage = 0, phase = 0;
     bool ok = true;
     for (uint32_t n = 0; n < mine; ++n) {
         const uint64_t row = first + n * step;
         const uint8_t* at = own + stage * stage_bytes;
-        const Part part = part_of(row);
-        // a chunk from its place, or, where it was not copied, from memory
-        const auto operand = [&](int which, const InRows& m, uint32_t chunk) {
+        const auto operand = [&](int which, uint32_t chunk) {
             Raw8<T> x;
             x.v = *reinterpret_cast<const uint4*>(at + which * ring.row_bytes + chunk * 16);
-            if constexpr (!WIDE)
-                if (chunk < part.from || chunk >= part.to)
-                    x.v = load_some(static_cast<const uint16_t*>(m.p) + row * m.ld, (int)(chunk * 8) - shift, cols);
             return x;
         };
+        const float end_d = element(ends[0]), end_f = element(ends[1]), end_e = element(ends[2]);
+        if (ec >= 0 && n + 1 < mine) ahead(row + step);
         ok = mbar_wait(full + 8 * stage, phase);
         Pair ss = pair(0.0f), dd = pair(0.0f);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            if (j * TEAM + t >= chunks) break;
+            if (j * TEAM + t >= cut.whole) break;
             Pair d[4], f[4], g[4];
-            Raw8<T> dr = operand(0, a.dy, j * TEAM + t), hr = operand(1, a.h, j * TEAM + t);
-            row_keep8<T, WIDE>(dr, (int)((j * TEAM + t) * 8) - shift, cols);
-            row_keep8<T, WIDE>(hr, (int)((j * TEAM + t) * 8) - shift, cols);
-            to_pairs(dr, d); to_pairs(hr, f);
+            to_pairs(operand(0, j * TEAM + t), d); to_pairs(operand(1, j * TEAM + t), f);
             to_pairs(gr[j], g);
             norm_grad_stats8(d, f, g, ss, dd);
         }
         const float2 s2 = both(ss), d2 = both(dd);
-        float square = warp_sum(s2.x + s2.y), dot = warp_sum(d2.x + d2.y);
+        float square = s2.x + s2.y, dot = d2.x + d2.y;
+        if constexpr (!WIDE) {                                         // zeros where there is none
+            square = fmaf(end_f, end_f, square);
+            dot = fmaf(end_d * end_gamma, end_f, dot);
+        }
+        square = warp_sum(square);
+        dot = warp_sum(dot);
         if constexpr (TEAM == 32) {
             if (!(ok = __all_sync(0xFFFFFFFFu, ok))) break;            // the wait ran out: the team leaves together
         } else {
@@ -613,14 +624,24 @@ __global__ void __launch_bounds__(ring_teams(TEAM, V) * TEAM, ring_ctas(TEAM, V)
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const uint32_t chunk = j * TEAM + t;
-            if (chunk >= chunks) break;
+            if (chunk >= cut.whole) break;
             Pair d[4], f[4], g[4], e[4];
-            to_pairs(operand(0, a.dy, chunk), d); to_pairs(operand(1, a.h, chunk), f); to_pairs(gr[j], g);
-            if (a.residual.p) to_pairs(operand(2, a.residual, chunk), e);
+            to_pairs(operand(0, chunk), d); to_pairs(operand(1, chunk), f); to_pairs(gr[j], g);
+            if (a.residual.p) to_pairs(operand(2, chunk), e);
             else
 #pragma unroll
                 for (int i = 0; i < 4; ++i) e[i] = pair(0.0f);
-            norm_grad8<T, DROP, WIDE>(a, row, (int)(chunk * 8) - shift, r, mean_gu, d, f, g, e, sum[j]);
+            norm_grad8<T, DROP, WIDE>(a, row, cut.lead + (int)chunk * 8, r, mean_gu, d, f, g, e, sum[j]);
+        }
+        if (!WIDE && ec >= 0) {
+            const float u = end_f * r;
+            end_sum = fmaf(end_d, u, end_sum);
+            float e = fmaf(r, fmaf(u, -mean_gu, end_d * end_gamma), end_e);
+            if (a.dh.p) row_of<T>(a.dh, row)[ec] = rounded<T>(e);
+            if (a.dx.p) {
+                if constexpr (DROP) e = drop1(a.drop, drop_row(a.drop, row), ec, e);
+                row_of<T>(a.dx, row)[ec] = rounded<T>(e);
+            }
         }
         if constexpr (TEAM == 32) {
             __syncwarp();
@@ -633,7 +654,20 @@ __global__ void __launch_bounds__(ring_teams(TEAM, V) * TEAM, ring_ctas(TEAM, V)
         for (uint32_t n = filled > ring.stages ? filled - ring.stages : 0; n < filled; ++n) mbar_wait(full + 8 * (n % ring.stages), (n / ring.stages) & 1u);
     }
     if (!partial) return;
-    norm_leave_sums<TEAM, TEAMS, V, WIDE>(sum, t, team, shift, a.cols, partial + (uint64_t)blockIdx.x * a.part_ld);
+    partial += (uint64_t)blockIdx.x * a.part_ld;
+    if constexpr (TEAMS == 1) {
+        norm_leave_sums<TEAM, V>(sum, end_sum, ec, t, cut, partial);
+    } else {                                                           // the teams' sums in the stages' place, added in order
+        __syncthreads();
+        norm_leave_sums<TEAM, V>(sum, end_sum, ec, t, cut, reinterpret_cast<float*>(raw + team * ring.stages * stage_bytes));
+        __syncthreads();
+        for (uint32_t c = threadIdx.x; c < a.cols; c += TEAMS * TEAM) {
+            float total = 0.0f;
+#pragma unroll
+            for (int w = 0; w < TEAMS; ++w) total += reinterpret_cast<const float*>(raw + w * ring.stages * stage_bytes)[c];
+            partial[c] = total;
+        }
+    }
 }
 
 // Column sums from the CTAs' partial rows: 32 columns a CTA, one of JOIN_LANES rows a thread, joined in order.  3 us, most of it the second launch.

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import paper_2009_09271_b200 as sc
-from block_util import SALT_DROPOUT, depth, dropped64, kept_mask, mix64, norm64, norm_grad64
+from block_util import SALT_DROPOUT, depth, dropped64, kept_mask, mix64, norm64, norm_grad64, rows_in_8_bits
 from layer_util import assert_close, strided
 
 pytestmark = pytest.mark.gpu
@@ -388,3 +388,27 @@ def test_short_rows_and_their_neighbours(ctx, rows, cols):
             outside = torch.ones(whole.shape, dtype=torch.bool, device="cuda")
             outside[:rows * (cols + 3)].view(rows, cols + 3)[:, :cols] = False
             assert bool(torch.isnan(whole[outside]).all())
+
+
+# -- rows as long as a kernel's threads hold, and their ends ----------------------------------------------------------------
+LONGEST = [(9, 255), (9, 263), (9, 519), (9, 1031), (2500, 1031), (5, 2055), (5, 4103), (3, 8199), (2, 16391), (2, 16399), (1, 32775), (1, 32776)]
+
+
+@pytest.mark.parametrize("extra,offset", [(0, 0), (3, 1)])
+@pytest.mark.parametrize("rows,cols", LONGEST)
+def test_longest_rows_of_each_kernel(ctx, rows, cols, extra, offset):
+    check_norm(ctx, torch.bfloat16, rows, cols, True, 0.25, extra, offset)
+    check_grad(ctx, torch.float16, rows, cols, True, 0.25, extra, offset)
+    g = rng(cols)
+    x = strided(normal(g, rows, cols).bfloat16(), extra, offset)
+    y = strided(torch.zeros(rows, cols, device="cuda").bfloat16(), extra, offset)
+    ctx.sc_dropout(x, y, 0.3, 11)
+    mask, scale = kept_mask(11, rows, cols, 0.3)
+    want = torch.where(mask.cuda(), x.float() * np.float32(scale), torch.zeros((), device="cuda")).bfloat16()
+    assert torch.equal(y, want)
+    q, scales = strided(torch.zeros(rows, cols, device="cuda").to(torch.int8), extra, offset), torch.empty(rows, device="cuda")
+    ctx.sc_quantize(x, q, scales)
+    wq, ws = rows_in_8_bits(x)
+    assert torch.equal(q.cpu(), wq) and torch.equal(scales.cpu(), ws)
+    ctx.sc_dequantize(q, scales, y)
+    assert torch.equal(y, (q.float() * scales[:, None]).bfloat16())
