@@ -94,6 +94,7 @@ void run_dequantize(sc_ctx* c, const void* q, size_t ldq, const float* scales, s
         using std::integral_constant;
         if (chunks <= 32) start(integral_constant<int, 32>(), integral_constant<int, 1>());
         else if (chunks <= 64) start(integral_constant<int, 32>(), integral_constant<int, 2>());
+        // a warp a row once there are rows for every warp (16384 x 1001: 10.2 against 17.9 us), a chunk a thread for fewer (300 x 1001: 1.7 against 1.8)
         else if (chunks <= 128 && rows > 16ull * c->sm_count) start(integral_constant<int, 32>(), integral_constant<int, 4>());
         else if (chunks <= 128) start(integral_constant<int, 128>(), integral_constant<int, 1>());
         else if (chunks <= 256) start(integral_constant<int, 128>(), integral_constant<int, 2>());
@@ -117,8 +118,9 @@ void run_dropout(const sc_ctx* c, const DropArgs& a, cudaStream_t st) {
     using std::integral_constant;
     if (chunks <= 32) start(integral_constant<int, 32>(), integral_constant<int, 1>());
     else if (chunks <= 64) start(integral_constant<int, 32>(), integral_constant<int, 2>());
-    // a warp a row once there are rows for every warp (65536 x 1024 without a residual 46 against 69 us), a chunk a thread for fewer (77 x 1001: 1.9 against 3.3)
-    else if (chunks <= 128 && a.rows > 16ull * c->sm_count) start(integral_constant<int, 32>(), integral_constant<int, 4>());
+    // a warp a row once there are rows for every warp (65536 x 1024 without a residual 46 against 69 us), a chunk a thread for fewer (509 x 1024:
+    // 1.7 against 2.2) and for cut rows (8000 x 1001: 11.8 against 14.1)
+    else if (chunks <= 128 && unshifted(a.phase, a.cols) && a.rows > 16ull * c->sm_count) start(integral_constant<int, 32>(), integral_constant<int, 4>());
     else if (chunks <= 128) start(integral_constant<int, 128>(), integral_constant<int, 1>());
     else if (chunks <= 256) start(integral_constant<int, 128>(), integral_constant<int, 2>());
     else if (chunks <= 512 || a.residual.p) start(integral_constant<int, 256>(), integral_constant<int, 2>());
@@ -129,7 +131,7 @@ template <typename T, bool DROP>
 void run_norm(sc_ctx* c, const NormArgs& a, float* scales, cudaStream_t st) {
     const bool wide = unshifted(a.phase, a.cols) && a.residual.vec && a.gamma.vec && a.h.vec && a.y.vec && a.q.vec;
     const uint64_t chunks = a.cols / 8;
-    // shifted rows carry more code a chunk: 16384 x 1001 takes 27.6 us with one chunk a thread, 31.0 with four; 64 x 1001 2.2 and 4.3
+    // cut rows carry more code a chunk: 16384 x 1001 takes 25.7 us with one chunk a thread, 29.6 with four; 64 x 1001 2.1 and 3.9
     if (!unshifted(a.phase, a.cols) && chunks > 64 && chunks <= 128) {
         launch(rms_norm_rows_kernel<T, 128, 1, DROP, false>, team_grid(128, a.rows), team_threads(128), 0, 1, st, a, scales);
         return;
@@ -210,9 +212,10 @@ int run_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) {
         return drop ? launch_norm_grad<T, TEAM, V, true, false>(c, a, dgamma, st) : launch_norm_grad<T, TEAM, V, false, false>(c, a, dgamma, st); \
     }
     SC_TEAM(32, 1) SC_TEAM(32, 2)
-    // A handful of shifted rows is over sooner with a chunk a thread, whose code is fetched cold (509 x 1001: 6.5 against 8.9 us); many rows
-    // are not (16384 x 1001: 50 against 36), nor are rows without shifts (2048 x 1024: 9.5 against 8.2).
-    if (ringed && !unshifted(a.phase, a.cols) && chunks <= 128 && a.rows <= 4ull * c->sm_count)
+    // Up to some thousand cut rows are over sooner with a chunk a thread, whose code is fetched cold (509 x 1001: 6.1 against 7.9 us, 2000 x 1001
+    // 11.0 against 12.9); more are not (4000 x 1001: 16.4 against 16.3, 16384 x 1001 42 against 31), nor are rows without ends (2048 x 1024:
+    // 9.5 against 8.2).
+    if (ringed && !unshifted(a.phase, a.cols) && chunks <= 128 && a.rows <= 16ull * c->sm_count)
         return drop ? launch_norm_grad<T, 128, 1, true, false>(c, a, dgamma, st) : launch_norm_grad<T, 128, 1, false, false>(c, a, dgamma, st);
     SC_TEAM(32, 4) SC_TEAM(128, 2) SC_TEAM(256, 2) SC_TEAM(256, 4) SC_TEAM(512, 4)
 #undef SC_TEAM
