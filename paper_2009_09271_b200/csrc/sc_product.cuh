@@ -235,7 +235,7 @@ __device__ __forceinline__ void tile_at(const TcArgs& a, uint32_t t, uint32_t& t
 // makes both directions free of bank conflicts.
 template <typename T, int MODE>
 __device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcArgs& a, const Epilogue& ep, uint32_t stage_addr, const uint32_t (&v)[32], uint64_t row0, uint32_t col0,
-                                          uint32_t split) {
+                                          uint32_t split, uint32_t columns, float row_scale) {
     const uint32_t lane = threadIdx.x & 31u;
     if (a.tma_out) {                       // the last block's copy has left the buffer
         if (lane == 0) tma_store_wait_read();
@@ -290,9 +290,18 @@ __device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcAr
         }
     } else {
         constexpr int NEXT = epilogue_of(MODE);
-        float bias[8], scales[8];
-        load_bias<T, NEXT>(ep, c0, bias);
-        load_col_scales<MODE>(ep, c0, scales);
+        float bias[8] = {}, scales[8];
+        if constexpr (NEXT == PRODUCT_FORWARD) {                  // what block_columns left
+            uint32_t b[4];
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]) : "r"(columns + 128 + (lane & 3u) * 16) : "memory");
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { const float2 f = Elem<T>::unpack(b[i]); bias[2 * i] = f.x; bias[2 * i + 1] = f.y; }
+        }
+        if constexpr (MODE == PRODUCT_QUANTIZED)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(scales[4 * i]), "=f"(scales[4 * i + 1]), "=f"(scales[4 * i + 2]), "=f"(scales[4 * i + 3])
+                             : "r"(columns + (lane & 3u) * 32 + 16 * i) : "memory");
         const bool narrow = ep.grain_out == 1 || (NEXT == PRODUCT_FORWARD && ep.q && ep.grain_q == 1);
         with_activation(ep.act, [&](auto act) {
 #pragma unroll 1                                              // little code: it is fetched cold in a small call
@@ -300,7 +309,11 @@ __device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcAr
                 float f[8];
                 const uint64_t row = fetch(i, f);
                 if (narrow) __syncwarp();                     // the row's four lanes have read it
-                scale8<MODE>(ep, row, scales, f);
+                if constexpr (MODE == PRODUCT_QUANTIZED) {
+                    const float r = __shfl_sync(0xFFFFFFFFu, row_scale, (lane >> 2) + 8 * i);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] = (float)__float_as_int(f[j]) * r * scales[j];
+                }
                 epilogue8<T, NEXT, decltype(act)::value>(ep, row, c0, bias, f, narrow ? stage_addr + (uint32_t)(row - row0) * 128 : 0u);
             }
         });
@@ -635,11 +648,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                 }
                 if (!ok) break;
 #pragma unroll
-                for (int c = 0; c < BN / 64; ++c) block_out<T, MODE>(&map_out, a, ep, stage_addr, sum[c], row0, col0 + c * 32, split);
+                for (int c = 0; c < BN / 64; ++c) block_out<T, MODE>(&map_out, a, ep, stage_addr, sum[c], row0, col0 + c * 32, split, 0u, 0.0f);
             } else {
                 BlockColumn column{0.0f, 0};
                 float row_scale = 0.0f;
-                if (a.rows_form) {
+                if (!a.tma_out) {
                     column = block_column<MODE>(ep, col0 + lane);
                     if constexpr (MODE == PRODUCT_QUANTIZED) row_scale = row0 + lane < ep.rows ? ep.row_scale[row0 + lane] : 0.0f;
                 }
@@ -657,16 +670,18 @@ __global__ void __launch_bounds__(TC_THREADS, 1) product_kernel(const __grid_con
                         __syncwarp();
                         if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_rank(tempty + 8 * acc, 0) : tempty + 8 * acc);
                     }
-                    if (a.rows_form) {
-                        const uint32_t columns = column_base + e * TC_COLUMN_BYTES;
+                    const uint32_t columns = column_base + e * TC_COLUMN_BYTES;
+                    if (!a.tma_out) {
                         block_columns<MODE>(column, columns);
                         if (c + 32 < BN / 2) column = block_column<MODE>(ep, col0 + c + 32 + lane);
+                    }
+                    if (a.rows_form) {
                         with_activation(ep.act, [&](auto act) {
                             block_rows<T, MODE, decltype(act)::value>(&map_out, ep, stage_addr + turn, columns, row_scale, v, row0, col0 + c, scale4);
                         });
                         turn ^= 2048u;                      // the two buffers take turns from block to block, whatever the tile
                     } else
-                        block_out<T, MODE>(&map_out, a, ep, stage_addr, v, row0, col0 + c, split);
+                        block_out<T, MODE>(&map_out, a, ep, stage_addr, v, row0, col0 + c, split, columns, row_scale);
                 }
                 if ((acc ^= 1u) == 0) acc_phase ^= 1u;
             }
@@ -1053,19 +1068,60 @@ __device__ __forceinline__ void layout_rows(const LayoutArgs& a, uint32_t block,
         }
     }
 }
-// The same for bytes, to rows a multiple of 16 apart: 16 bytes a thread, read in runs of the rows' alignment.
-__device__ __forceinline__ void layout_byte_rows(const LayoutArgs& a, uint32_t block, uint32_t blocks) {
-    const uint8_t* src = reinterpret_cast<const uint8_t*>(a.src);
-    uint8_t* dst = reinterpret_cast<uint8_t*>(a.dst);
-    const uint32_t chunks = a.ldd / 16;
-    for (uint64_t i = (uint64_t)block * 256 + threadIdx.x; i < a.rows * chunks; i += (uint64_t)blocks * 256) {
-        const uint64_t row = i / chunks;
-        const uint32_t c0 = (uint32_t)(i - row * chunks) * 16;
-        const uint8_t* p = src + row * a.ld + c0;
-        uint2 v[2];
+// Sixteen bytes from p, zeros where they are not the matrix's, which lies from `begin` to `end`.
+static __device__ __noinline__ uint4 load_bytes16(const uint8_t* p, const uint8_t* begin, const uint8_t* end) {
+    uint32_t w[4] = {};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) v[h] = c0 + 8 * h < a.cols ? load_q_narrow(p + 8 * h, a.cols - c0 - 8 * h, a.grain) : make_uint2(0u, 0u);
-        *reinterpret_cast<uint4*>(dst + row * a.ldd + c0) = make_uint4(v[0].x, v[0].y, v[1].x, v[1].y);
+    for (int i = 0; i < 16; ++i)
+        if (p + i >= begin && p + i < end) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// The same for bytes, to rows a multiple of 16 apart, a warp 128 runs of 16 bytes of a row at a time: each is cut out of the two aligned
+// accesses that it lies across, by a shift that a row's runs share.  8192 x 4097 and 16384 x 4097 in 38 us (5.3 TB/s); in runs of the rows' alignment and one thread a run it took 61.
+constexpr uint32_t LAYOUT_RUNS = 128;
+__device__ __forceinline__ void layout_byte_rows(const LayoutArgs& a, uint32_t block, uint32_t blocks) {
+    const uint8_t *src = reinterpret_cast<const uint8_t*>(a.src), *end = src + (a.rows - 1) * a.ld + a.cols;
+    uint8_t* dst = reinterpret_cast<uint8_t*>(a.dst);
+    const uint32_t lane = threadIdx.x & 31u, runs = (a.cols + 15) / 16, parts = (runs + LAYOUT_RUNS - 1) / LAYOUT_RUNS;
+    for (uint64_t unit = (uint64_t)block * 8 + (threadIdx.x >> 5); unit < a.rows * parts; unit += (uint64_t)blocks * 8) {
+        const uint64_t row = unit / parts;
+        const uint32_t run0 = (uint32_t)(unit - row * parts) * LAYOUT_RUNS + lane;
+        const uint8_t* from = src + row * a.ld;
+        const uint32_t by = (uint32_t)(reinterpret_cast<uintptr_t>(from) & 15u);
+        uint4 first[LAYOUT_RUNS / 32], second[LAYOUT_RUNS / 32];
+#pragma unroll
+        for (uint32_t j = 0; j < LAYOUT_RUNS / 32; ++j) {
+            const uint32_t run = run0 + 32 * j;
+            const uint8_t* p = from + (uint64_t)run * 16 - by;
+            first[j] = second[j] = make_uint4(0u, 0u, 0u, 0u);
+            if (run >= runs) continue;
+            if (p >= src && p + 16 <= end) first[j] = *reinterpret_cast<const uint4*>(p);
+            else first[j] = load_bytes16(p, src, end);
+            if (by == 0) continue;
+            if (p + 32 <= end) second[j] = *reinterpret_cast<const uint4*>(p + 16);
+            else second[j] = load_bytes16(p + 16, src, end);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < LAYOUT_RUNS / 32; ++j) {
+            const uint32_t run = run0 + 32 * j, c0 = run * 16;
+            if (run >= runs) continue;
+            uint32_t w[8] = {first[j].x, first[j].y, first[j].z, first[j].w, second[j].x, second[j].y, second[j].z, second[j].w};
+            if (by & 8)
+#pragma unroll
+                for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+            if (by & 4)
+#pragma unroll
+                for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 8 * (by & 3));
+            if (c0 + 16 > a.cols)                              // zeros behind the row
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    const uint32_t n = c0 + 4 * i < a.cols ? min(a.cols - c0 - 4 * i, 4u) : 0u;
+                    w[i] &= n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
+                }
+            *reinterpret_cast<uint4*>(dst + row * a.ldd + c0) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
     }
 }
 // One or both operands of a product: blockIdx.y chooses.

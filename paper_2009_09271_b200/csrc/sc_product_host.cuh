@@ -18,8 +18,12 @@ struct Stored {
 
 inline uint64_t round8(uint64_t n) { return (n + 7) & ~7ull; }
 inline bool tma_ready(const Stored& m) { return aligned(m.p, 16) && m.ld * m.elem % 16 == 0; }
-// A copy's rows are 16-byte aligned: elements between them, and its bytes.
-inline uint64_t layout_ld(const Stored& m) { return m.elem == 1 ? (m.cols + 15) & ~15ull : round8(m.cols); }
+// A copy's rows are 16-byte aligned: elements between them, and its bytes.  Long rows of bytes start on whole cache lines: with tiles' rows
+// across two of them 8192 x 16384 x 4097 took 443 us instead of 340.
+inline uint64_t layout_ld(const Stored& m) {
+    const uint64_t to = m.cols >= 128 ? 128 : 16;
+    return m.elem == 1 ? (m.cols + to - 1) & ~(to - 1) : round8(m.cols);
+}
 inline size_t layout_bytes(const Stored& m) { return (m.rows * layout_ld(m) * m.elem + 255) & ~(size_t)255; }
 inline size_t layout_bytes(uint64_t rows, uint64_t cols) { return (rows * round8(cols) * 2 + 255) & ~(size_t)255; }
 
@@ -150,7 +154,7 @@ int run_product(sc_ctx* c, int kind, int type, Stored A, Stored B, uint64_t red,
         const uint32_t ldd = (uint32_t)layout_ld(*m);
         copies[ncopies++] = LayoutArgs{static_cast<const uint16_t*>(m->p), reinterpret_cast<uint16_t*>(at), m->ld, m->rows, (uint32_t)m->cols, ldd,
                                        std::min(4u, grain_of(m->p, m->rows > 1 ? m->ld : 0, m->elem, 8))};
-        work = std::max(work, m->rows * (ldd * m->elem / 16));
+        work = std::max(work, m->elem == 1 ? m->rows * ceil_div(m->cols, 16 * LAYOUT_RUNS) * 32 : m->rows * (ldd / 8));
         m->p = at; m->ld = ldd;
         at += layout_bytes(*m);
     }

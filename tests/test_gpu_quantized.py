@@ -310,3 +310,15 @@ def test_sums_of_few_tokens_term_by_term(ctx):
         y = torch.empty(M, 64, dtype=torch.float16, device="cuda")
         ctx.sc_linear_quantized(sc.SC_ACT_NONE, x[:M], ones[:M], w, ones, y)
         assert torch.equal(y, exact[:M].to(torch.float16))
+
+
+@pytest.mark.parametrize("offset", [0, 1, 7, 15])
+@pytest.mark.parametrize("M,N,K", [(9, 40, 127), (9, 40, 129), (1, 33, 2047), (40, 1, 2049), (33, 65, 4097), (3, 20, 131071)])
+def test_rows_of_bytes_at_any_alignment(ctx, M, N, K, offset):
+    """The operands' copies: rows that begin anywhere in 16 bytes, among bytes that are not theirs, of one and of several runs a warp."""
+    ctx.sc_debug_layer_tiles()
+    g = rng(K + offset)
+    x, w = (strided(torch.randint(-127, 128, (r, K), generator=g, device="cuda").to(torch.int8), 5 if offset else 0, offset) for r in (M, N))
+    y, ones = torch.empty(M, N, device="cuda", dtype=torch.bfloat16), [torch.ones(n, device="cuda") for n in (M, N)]
+    ctx.sc_linear_quantized(sc.ACTIVATIONS["none"], x, ones[0], w, ones[1], y)
+    assert torch.equal(y, (x.double() @ w.double().T).float().bfloat16())
