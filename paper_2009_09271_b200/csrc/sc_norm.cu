@@ -7,14 +7,13 @@
 
 namespace {
 
-// The walk of a grid over `items` items a row, and the grid: up to eight CTAs an SM that go on, or, with `round`, as many as give each thread
-// one round of so many items.
-ItemWalk item_walk(const sc_ctx* c, size_t rows, size_t cols, uint64_t items, uint32_t& grid, int round = 0) {
+// The walk of a grid over `items` items a row, and the grid: eight CTAs an SM, or as many as give each thread one round of so many items.
+ItemWalk item_walk(const sc_ctx* c, size_t rows, size_t cols, uint64_t items, uint32_t& grid, int round) {
     ItemWalk w{};
     w.cols = (uint32_t)cols;
     w.items = (uint32_t)items;
     w.total = (uint64_t)rows * w.items;
-    const uint64_t few = std::min<uint64_t>(ceil_div(w.total, CKPT_THREADS), (uint64_t)c->sm_count * 8), one = round ? ceil_div(w.total, (uint64_t)CKPT_THREADS * round) : 1;
+    const uint64_t few = std::min<uint64_t>(ceil_div(w.total, CKPT_THREADS), (uint64_t)c->sm_count * 8), one = ceil_div(w.total, (uint64_t)CKPT_THREADS * round);
     grid = (uint32_t)std::min<uint64_t>(std::max(few, one), 1u << 30);
     const uint64_t stride = (uint64_t)grid * CKPT_THREADS;
     w.stride_rows = stride / w.items;
@@ -204,7 +203,7 @@ int launch_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) 
 template <typename T>
 int run_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) {
     const bool wide = unshifted(a.phase, a.cols) && a.h.vec && a.gamma.vec && a.residual.vec && a.dh.vec && a.dx.vec, drop = a.drop.cut && a.dx.p;
-    const bool ringed = a.h.vec && a.residual.vec;                 // results of another phase leave in single elements
+    const bool ringed = a.h.vec && a.residual.vec;                 // results of another cut leave in single elements
     const uint32_t chunks = a.cols / 8;
 #define SC_TEAM(TEAM, V) \
     if (ringed && chunks <= TEAM * V) { \

@@ -337,7 +337,8 @@ __global__ void __launch_bounds__(NORM_THREADS) rms_norm_kernel(NormArgs a, floa
 // for after it is h gamma, of which y is a multiple.  Bound by HBM: 16384 x 8192 bf16 with residual in 158 us (6.8 TB/s, 1.04 of the copy
 // rate), to 8 bits 138 us, with dropout 166 and 160 (0.99, 0.90).  A row of 8192 in 256 threads: what is kept decides how many rows an SM
 // has in flight.  With gamma kept in its own type and h stored after the reduction the 8-bit form took 212 us.  Rows of 16384 and more
-// leave room for two CTAs an SM and one (8192 x 16384 162 us, 2000 x 20000 68).  One token of 4096 takes 1.9 us.
+// leave room for two CTAs an SM and one (8192 x 16384 162 us, 2000 x 20000 68).  Held to 40 registers rows of 4096 without a residual take 46.6
+// us instead of 48.4.  Rows with ends: 16384 x 4097 97 us (0.85), 16384 x 1001 25.7 (0.78).  One token of 4096 takes 1.9 us.
 template <typename T, int TEAM, int V, bool DROP, bool WIDE>
 __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 3 : TEAM == 1024 ? 1 : TEAM >= 256 && V == 4 ? 1024 / TEAM - (DROP && TEAM == 256) : V == 2 && WIDE && !DROP ? 1536 / TEAM : 1024 / TEAM)
 rms_norm_rows_kernel(NormArgs a, float* scales) {
@@ -500,12 +501,13 @@ __device__ __forceinline__ void norm_leave_sums(const Pair (&sum)[V][4], float e
 // A team a row, V times eight elements a thread, for inputs of one phase, from a ring of shared-memory stages that bulk copies fill
 // ahead of use: loads are in flight while a row is reduced and written, and its operands are read from there twice instead of being
 // kept in registers.  Teams walk the rows with their columns' sums in registers and leave one partial row of sums a CTA; their steps are
-// multiples of 8 rows, so that all of a team's rows have the same shift and the same columns.  A warp has a ring of its own; a larger team
+// multiples of 8 rows, so that all of a team's rows have the same cut and the same columns.  A warp has a ring of its own; a larger team
 // fills a stage again after the next row's barrier, which every thread reaches done with it.
 // Bound by HBM at 2048 columns and more: 16384 x 8192 bf16 with residual in 168 us (6.4 TB/s, 0.98 of the copy rate), with dx through dropout
 // 225 (0.91: the generator's products, at half the multiply-add rate).  Narrower rows spend issue slots instead: 65536 x 1024 0.89, 262144 x
 // 256 0.71.  Read twice from HBM by two kernels, statistics and strips, 16384 x 8192 with dropout took 316 us.
-// row_bytes: of a stage's place for one operand, sixteen at least more than a row's chunks
+// 16384 x 4097 takes 89 us (0.92), 16384 x 1001 31 (0.64).
+// row_bytes: of a stage's place for one operand, a row's chunks and, where rows have ends, sixteen more
 struct NormRing { uint32_t stages, row_bytes, operands; };
 constexpr uint32_t RING_MOST_STAGES = 8;
 // Teams a CTA, and CTAs an SM: 16 warps of up to 128 registers a thread.

@@ -412,3 +412,29 @@ def test_longest_rows_of_each_kernel(ctx, rows, cols, extra, offset):
     assert torch.equal(q.cpu(), wq) and torch.equal(scales.cpu(), ws)
     ctx.sc_dequantize(q, scales, y)
     assert torch.equal(y, (q.float() * scales[:, None]).bfloat16())
+
+
+def test_one_row_as_long_as_sizes_go(ctx):
+    """2^31 - 1 columns that begin off a boundary: both ends, and the middle, of dropout and of 8-bit rows there and back."""
+    cols = 2 ** 31 - 1
+    base = torch.empty(cols + 1, device="cuda", dtype=torch.bfloat16).normal_(generator=rng(1))
+    x, y = base[1:].view(1, cols), torch.zeros(cols + 1, device="cuda", dtype=torch.bfloat16)
+    y[0] = 7.0
+    places = [slice(c, c + 4096) for c in (0, 2 ** 30 - 2048, cols - 4096 - cols % 4)] + [slice(cols - cols % 4 - 4, cols)]
+    ctx.sc_dropout(x, y[1:].view(1, cols), 0.5, 3)
+    assert float(y[0]) == 7.0
+    key = mix64(3, SALT_DROPOUT)
+    for s in places:
+        words = mix64(key, np.arange(s.start // 4, -(-s.stop // 4), dtype=np.uint64))
+        bits = np.stack([(words >> np.uint64(16 * i)) & np.uint64(0xFFFF) for i in range(4)], 1).reshape(-1)[:s.stop - s.start]
+        kept = torch.from_numpy(bits >= np.uint64(32768)).cuda()
+        assert torch.equal(y[1:][s], torch.where(kept, x[0, s] * 2, torch.zeros_like(x[0, s])))
+    q, scales = torch.zeros(1, cols, device="cuda", dtype=torch.int8), torch.empty(1, device="cuda")
+    ctx.sc_quantize(x, q, scales)
+    top = torch.maximum(x.max(), -x.min()).float()
+    assert float(scales) == float(top / torch.full_like(top, 127.0))
+    ctx.sc_dequantize(q, scales, y[1:].view(1, cols))
+    for s in places:
+        want = torch.round(x[0, s].float() * (127 * (1 / top)))
+        assert torch.equal(q[0, s].float(), want)
+        assert torch.equal(y[1:][s], (want * scales).bfloat16())
