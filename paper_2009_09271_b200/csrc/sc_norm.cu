@@ -24,7 +24,7 @@ uint32_t row_grid(const sc_ctx* c, size_t rows) { return (uint32_t)std::min<uint
 
 inline uint32_t grain16(const void* p, size_t rows, size_t ld) { return grain_of(p, rows > 1 ? ld : 0, 2, 8); }
 
-// The shifts of a matrix's rows, and whether another's are the same (a matrix that is not there has any).
+// How a matrix's rows are cut, and whether another's are cut the same (one that is not there is).
 Phase phase_of(const void* p, size_t rows, size_t ld, size_t elem) {
     return Phase{(uint32_t)(reinterpret_cast<uintptr_t>(p) / elem) & 7u, rows > 1 ? (uint32_t)ld & 7u : 0u};
 }

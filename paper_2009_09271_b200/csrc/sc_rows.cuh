@@ -4,13 +4,13 @@
 // ends, up to seven elements before the first boundary and up to seven after the last, which one warp handles one element a lane.
 // Matrices of one odd width have the same cut in the same row, so all of them move in whole accesses; one whose rows are cut elsewhere
 // has its chunks moved in single elements.  WIDE is the case without ends: every row starts on a boundary and is a multiple of 8 long.
-// With checks for the ends at each chunk instead, rows of 4097 took 1.3 to 1.9 times as long as rows of 4096.
+// With checks for the ends at each chunk instead, rows of 4097 took 1.5 to 2.6 times as long as rows of 4096; now it is 1.1 to 1.3.
 #pragma once
 #include "sc_checkpoint.cuh"
 
 namespace sc {
 
-// A matrix to read.  `vec`: its rows have the shifts of the phase (and are 16-byte accesses).
+// A matrix to read.  `vec`: its rows are cut as the phase says (and chunks are 16-byte accesses).
 struct InRows {
     const void* p;
     uint64_t ld;
