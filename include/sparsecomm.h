@@ -314,9 +314,10 @@ int sc_linear_quantized(sc_ctx* ctx, int type, int act, const int8_t* x, size_t 
 int sc_dropout(sc_ctx* ctx, int type, const void* x, size_t ldx, const void* residual, size_t ldr, double p, uint64_t seed, size_t rows, size_t cols,
                void* y, size_t ldy, void* stream);
 
-/* h = residual + dropout(x; p, seed), r = (mean of the row's h^2 + eps)^(-1/2), y = h r gamma; gamma[cols] is of the type, residual may be
- * NULL, p = 0 drops nothing.  y is written in 16 bits, as 8-bit rows (q and scales), or both; h on request (NULL: not written).  y and q are
- * made from the fp32 h.  Squares are summed in fp32: a row whose sum is not finite gives NaN; h gamma is formed before it is multiplied by
+/* h = residual + dropout(x; p, seed), r = (mean of the row's h^2 + eps)^(-1/2), y = (h gamma) r; gamma[cols] is of the type, residual may be
+ * NULL, p = 0 drops nothing.  y is written in 16 bits, as 8-bit rows (q and scales), or both; h on request (NULL: not written).  y is
+ * made from the fp32 h in two products, each rounded to fp32, and q and scales are the 8-bit rows of that y before its own rounding to 16
+ * bits.  Squares are summed in fp32: a row whose sum is not finite gives NaN; h gamma is formed before it is multiplied by
  * r, and has to stay within fp32's range.  h and y may be x or residual (same ld), each another. */
 int sc_rms_norm(sc_ctx* ctx, int type, const void* x, size_t ldx, const void* residual, size_t ldr, const void* gamma, float eps, double p, uint64_t seed,
                 size_t rows, size_t cols, void* h, size_t ldh, void* y, size_t ldy, int8_t* q, size_t ldq, float* scales, void* stream);

@@ -1,9 +1,10 @@
 // Rows in 8 bits with one scale each, and the root-mean-square norm with the residual's addition, forward and backward.
 //
 //   8-bit rows   m = max |v|, s = m / 127, q = rint(v i), i = 127 (1 / m), every product and quotient rounded to fp32
-//   forward      h = residual + dropout(x),  r = (mean(h^2) + eps)^(-1/2),  y = h r gamma, in 16 bits or as 8-bit rows
+//   forward      h = residual + dropout(x),  r = (mean(h^2) + eps)^(-1/2),  y = (h gamma) r, in 16 bits or as 8-bit rows
 //   backward     g = gamma dy,  u = h r,  dh = residual + r (g - u mean(g u)),  dx = dropout(dh),  dgamma = column sums of dy u
-// A row's sums and its largest magnitude are fp32; y is made from the fp32 h, before that is rounded to its type.
+// A row's sums and its largest magnitude are fp32; y is made from the fp32 h, before that is rounded to its type, and the 8-bit rows are
+// those of the fp32 y.
 #pragma once
 #include "sc_checkpoint.cuh"
 #include "sc_dropout.cuh"
@@ -325,7 +326,7 @@ __global__ void __launch_bounds__(NORM_THREADS) rms_norm_kernel(NormArgs a, floa
             to_floats(load8(gamma, c0, a.cols, a.grain_g), g);
             if (a.h.p) store8(static_cast<T*>(a.h.p) + row * a.h.ld, c0, a.cols, a.grain_h, f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = f[i] * r * g[i];
+            for (int i = 0; i < 8; ++i) f[i] = f[i] * g[i] * r;
             if (a.y.p) store8(static_cast<T*>(a.y.p) + row * a.y.ld, c0, a.cols, a.grain_y, f);
             if (a.q.p) store_q8(static_cast<uint8_t*>(a.q.p) + row * a.q.ld + c0, c0, a.cols, a.grain_q, row_bytes8(f, s.inv));
         }
@@ -412,36 +413,28 @@ rms_norm_rows_kernel(NormArgs a, float* scales) {
     }
     uint32_t m = __float_as_uint(top);
     team_reduce<TEAM>(sum, m, slots);
-    float r = rms_inverse(sum, a.mean, a.eps);
+    // y, in place of h gamma: rounding keeps the order of magnitudes, so the largest h gamma times r is the largest y
+    const float r = rms_inverse(sum, a.mean, a.eps);
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[j][i] = v[j][i] * pair(r);
+    end *= r;
     if (a.q.p) {
         const RowScale s = row_scale(__float_as_uint(__uint_as_float(m) * r) & 0x7FFFFFFFu);
-        float by = s.inv * r;
-        if (by > 3.402823466e38f) {                          // h gamma next to fp32's smallest numbers: its multiple first, bytes of that
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[j][i] = v[j][i] * pair(r);
-            end *= r;
-            r = 1.0f;
-            by = s.inv;
-        }
-        if (s.inv == 0.0f) by = 0.0f;
         uint8_t* q = row_of<uint8_t>(a.q, row);
 #pragma unroll
         for (int j = 0; j < V; ++j)
-            if (j * TEAM + t < cut.whole) chunk_store_bytes8<WIDE>(a.q, q, first + j * TEAM * 8, row_bytes8(v[j], by));
-        if (ec >= 0) q[ec] = row_byte(end, by);
+            if (j * TEAM + t < cut.whole) chunk_store_bytes8<WIDE>(a.q, q, first + j * TEAM * 8, row_bytes8(v[j], s.inv));
+        if (ec >= 0) q[ec] = row_byte(end, s.inv);
         if (t == 0) scales[row] = s.scale;
     }
     if (a.y.p) {
         T* y = row_of<T>(a.y, row);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[j][i] = v[j][i] * pair(r);
+        for (int j = 0; j < V; ++j)
             if (j * TEAM + t < cut.whole) chunk_store8<T, WIDE>(a.y, y, first + j * TEAM * 8, v[j]);
-        }
-        if (ec >= 0) y[ec] = rounded<T>(end * r);
+        if (ec >= 0) y[ec] = rounded<T>(end);
     }
 }
 
