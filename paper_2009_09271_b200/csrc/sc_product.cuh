@@ -33,7 +33,7 @@ struct Epilogue {
     uint32_t scales_by16;      // col_scale is 16-byte aligned
 };
 
-// 8-bit product: the scales of 8 columns, zero past the end, and a row's sums (by their bits) times both scales.
+// 8-bit product: the scales of 8 columns, zero past the end.
 template <int MODE>
 __device__ __forceinline__ void load_col_scales(const Epilogue& ep, uint32_t c0, float s[8]) {
     if constexpr (MODE == PRODUCT_QUANTIZED) {
@@ -46,17 +46,29 @@ __device__ __forceinline__ void load_col_scales(const Epilogue& ep, uint32_t c0,
         }
     }
 }
+// A row's scale in two factors, the second one 2^64 where the scale is larger than that, else 1: a sum times the first and the column's scale leaves
+// fp32's range only where the result does.  (Sum, row, column in this order, with the whole scale, overflowed half-way for rows beyond 2^97.)
+// The second is multiplied exactly, with the bias's addition: three roundings in all, the same ones on every path.
+struct RowFactors { float first, second; };
+__device__ __forceinline__ RowFactors row_factors(float scale) {
+    const bool far = fabsf(scale) > 18446744073709551616.0f;
+    return {far ? scale * 5.4210108624275222e-20f : scale, far ? 18446744073709551616.0f : 1.0f};
+}
+__device__ __forceinline__ float scaled(float sum_bits, RowFactors r, float col_scale, float bias) {
+    return __fmaf_rn(__fmul_rn(__fmul_rn((float)__float_as_int(sum_bits), r.first), col_scale), r.second, bias);
+}
+// 8-bit product: a row's eight sums (by their bits) to z.
 template <int MODE>
-__device__ __forceinline__ void scale8(const Epilogue& ep, uint64_t row, const float s[8], float v[8]) {
+__device__ __forceinline__ void scale8(const Epilogue& ep, uint64_t row, const float s[8], const float bias[8], float v[8]) {
     if constexpr (MODE == PRODUCT_QUANTIZED) {
-        const float r = row < ep.rows ? ep.row_scale[row] : 0.0f;
+        const RowFactors r = row_factors(row < ep.rows ? ep.row_scale[row] : 0.0f);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)__float_as_int(v[i]) * r * s[i];
+        for (int i = 0; i < 8; ++i) v[i] = scaled(v[i], r, s[i], bias[i]);
     }
 }
 
 // What follows the product for 8 columns from c0 of one row.  All 32 lanes of a warp call it; four neighbouring lanes hold
-// 32 consecutive columns of one row, from a multiple of 32, so they share a checkpoint group.  `bias`: of these columns.
+// 32 consecutive columns of one row, from a multiple of 32, so they share a checkpoint group.  `bias`: of these columns, null where v has it.
 // `slot`: 0, or the row's 128 bytes of shared memory, where the 16-bit result and the checkpoint's bytes (from byte 64) are
 // left for rows_out instead of being written to rows that take narrow accesses only.
 template <typename T, int MODE, int ACT>
@@ -75,8 +87,10 @@ __device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint
         float res[8] = {};
         if (in && ep.residual) to_floats(load8(static_cast<const T*>(ep.residual) + row * ep.ldr, c0, ep.cols, ep.grain_res), res);
         if constexpr (MODE == PRODUCT_FORWARD) {
+            if (bias) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += bias[i];
+                for (int i = 0; i < 8; ++i) v[i] += bias[i];
+            }
             if (ep.q) {
                 uint32_t m = 0;                         // columns past the end hold zeros: no product, no bias
 #pragma unroll
@@ -310,11 +324,11 @@ __device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcAr
                 const uint64_t row = fetch(i, f);
                 if (narrow) __syncwarp();                     // the row's four lanes have read it
                 if constexpr (MODE == PRODUCT_QUANTIZED) {
-                    const float r = __shfl_sync(0xFFFFFFFFu, row_scale, (lane >> 2) + 8 * i);
+                    const RowFactors r = row_factors(__shfl_sync(0xFFFFFFFFu, row_scale, (lane >> 2) + 8 * i));
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) f[j] = (float)__float_as_int(f[j]) * r * scales[j];
+                    for (int j = 0; j < 8; ++j) f[j] = scaled(f[j], r, scales[j], bias[j]);
                 }
-                epilogue8<T, NEXT, decltype(act)::value>(ep, row, c0, bias, f, narrow ? stage_addr + (uint32_t)(row - row0) * 128 : 0u);
+                epilogue8<T, NEXT, decltype(act)::value>(ep, row, c0, MODE == PRODUCT_QUANTIZED ? nullptr : bias, f, narrow ? stage_addr + (uint32_t)(row - row0) * 128 : 0u);
             }
         });
         if (narrow) {
@@ -363,21 +377,26 @@ __device__ __forceinline__ void block_rows(const CUtensorMap* map_out, const Epi
     constexpr int MODE = epilogue_of(PRODUCT);
     Pair z[16];
     if constexpr (PRODUCT == PRODUCT_QUANTIZED) {
-        const Pair r = pair(row_scale);
+        const RowFactors r = row_factors(row_scale);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float s[4];
+            uint32_t b[2];
             asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(s[0]), "=f"(s[1]), "=f"(s[2]), "=f"(s[3]) : "r"(columns + 16 * j) : "memory");
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(b[0]), "=r"(b[1]) : "r"(columns + 128 + 8 * j) : "memory");
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                z[2 * j + i] = pair((float)(int32_t)v[4 * j + 2 * i], (float)(int32_t)v[4 * j + 2 * i + 1]) * r * pair(s[2 * i], s[2 * i + 1]);
+            for (int i = 0; i < 2; ++i) {
+                const float2 f = Elem<T>::unpack(b[i]);                     // zeros without a bias
+                z[2 * j + i] = fma2(pair((float)(int32_t)v[4 * j + 2 * i], (float)(int32_t)v[4 * j + 2 * i + 1]) * pair(r.first) * pair(s[2 * i], s[2 * i + 1]),
+                                    pair(r.second), pair(f.x, f.y));
+            }
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i) z[i] = pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
     }
     if constexpr (MODE == PRODUCT_FORWARD) {
-        if (ep.bias) {
+        if (PRODUCT != PRODUCT_QUANTIZED && ep.bias) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 uint32_t b[4];
@@ -787,8 +806,8 @@ __device__ __forceinline__ void tokens_out(const Epilogue& ep, const int (&part)
         }
     load_bias<T, PRODUCT_FORWARD>(ep, c0, bias);
     load_col_scales<PRODUCT_QUANTIZED>(ep, c0, scales);
-    scale8<PRODUCT_QUANTIZED>(ep, m, scales, f);
-    with_activation(ep.act, [&](auto act) { epilogue8<T, PRODUCT_FORWARD, decltype(act)::value>(ep, m, c0, bias, f); });
+    scale8<PRODUCT_QUANTIZED>(ep, m, scales, bias, f);
+    with_activation(ep.act, [&](auto act) { epilogue8<T, PRODUCT_FORWARD, decltype(act)::value>(ep, m, c0, nullptr, f); });
 }
 
 // The same on 8-bit integers, for one and two tokens: sixteen weights a lane and access, four products an instruction, exact sums.  Rows are
@@ -1032,8 +1051,8 @@ __global__ void __launch_bounds__(256) product_join_kernel(const float* partial,
             float bias[8], scales[8];
             load_bias<T, NEXT>(ep, c0, bias);
             load_col_scales<MODE>(ep, c0, scales);
-            scale8<MODE>(ep, row, scales, f);
-            with_activation(ep.act, [&](auto act) { epilogue8<T, NEXT, decltype(act)::value>(ep, row, c0, bias, f); });
+            scale8<MODE>(ep, row, scales, bias, f);
+            with_activation(ep.act, [&](auto act) { epilogue8<T, NEXT, decltype(act)::value>(ep, row, c0, MODE == PRODUCT_QUANTIZED ? nullptr : bias, f); });
         }
     }
 }
