@@ -299,9 +299,9 @@ int sc_dequantize(sc_ctx* ctx, int type, const int8_t* q, size_t ldq, const floa
 
 /* sc_linear on 8-bit rows of x [M, K] and W [N, K], ldx and ldw bytes apart:
  * z[m, n] = (sum_k x[m, k] w[n, k]) * x_scales[m] * w_scales[n] + bias[n], y = act(z) + residual, the checkpoint of z on request; y may be
- * residual (same ld).  The sums are exact integers, so no result depends on the order of their terms; z is infinite only
- * where the scaled sum is beyond fp32's range, whichever scale is the large one; K < 131072 (SC_ERR_RANGE).  Its
- * gradients are the layer operators': sc_linear_grad_input with W in 16 bits, and sc_linear_grad_weight with x from sc_dequantize (the
+ * residual (same ld).  The sums are exact integers, and what follows them is the same roundings on every path: a result depends on its
+ * row and column alone, not on the number of tokens, on where anything lies, or on how the sum was cut.  z is infinite only
+ * where the scaled sum is beyond fp32's range, whichever scale is the large one; K < 131072 (SC_ERR_RANGE).  Its gradients are the layer operators': sc_linear_grad_input with W in 16 bits, and sc_linear_grad_weight with x from sc_dequantize (the
  * rounding to 8 bits is passed straight through). */
 int sc_linear_quantized(sc_ctx* ctx, int type, int act, const int8_t* x, size_t ldx, const float* x_scales, const int8_t* w, size_t ldw,
                         const float* w_scales, const void* bias, const void* residual, size_t ldr, size_t M, size_t N, size_t K, void* y, size_t ldy,

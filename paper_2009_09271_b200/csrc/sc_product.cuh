@@ -67,14 +67,22 @@ __device__ __forceinline__ void scale8(const Epilogue& ep, uint64_t row, const f
     }
 }
 
+// The 8-bit product's last step, the same on every path: nothing is added where there is no residual (a negative zero stays one), and otherwise
+// in two scalar additions, since a paired one may be joined with the activation's last product, without the rounding between.
+__device__ __forceinline__ Pair plus(Pair y, float lo, float hi) {
+    const float2 f = both(y);
+    return pair(__fadd_rn(f.x, lo), __fadd_rn(f.y, hi));
+}
+
 // What follows the product for 8 columns from c0 of one row.  All 32 lanes of a warp call it; four neighbouring lanes hold
 // 32 consecutive columns of one row, from a multiple of 32, so they share a checkpoint group.  `bias`: of these columns, null where v has it.
 // `slot`: 0, or the row's 128 bytes of shared memory, where the 16-bit result and the checkpoint's bytes (from byte 64) are
 // left for rows_out instead of being written to rows that take narrow accesses only.
 template <typename T, int MODE, int ACT>
 __device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint32_t c0, const float bias[8], float v[8], uint32_t slot = 0) {
+    constexpr int NEXT = epilogue_of(MODE);
     const bool in = row < ep.rows && c0 < ep.cols;
-    if constexpr (MODE == PRODUCT_WEIGHT) {
+    if constexpr (NEXT == PRODUCT_WEIGHT) {
         if (!in) return;
         float* out = static_cast<float*>(ep.out) + row * ep.ldo + c0;
         if (ep.accumulate) {
@@ -86,7 +94,7 @@ __device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint
     } else {
         float res[8] = {};
         if (in && ep.residual) to_floats(load8(static_cast<const T*>(ep.residual) + row * ep.ldr, c0, ep.cols, ep.grain_res), res);
-        if constexpr (MODE == PRODUCT_FORWARD) {
+        if constexpr (NEXT == PRODUCT_FORWARD) {
             if (bias) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] += bias[i];
@@ -108,7 +116,10 @@ __device__ __forceinline__ void epilogue8(const Epilogue& ep, uint64_t row, uint
             if (!in) return;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float2 f = both(activation<ACT>(pair(v[2 * i], v[2 * i + 1])) + pair(res[2 * i], res[2 * i + 1]));
+                Pair y = activation<ACT>(pair(v[2 * i], v[2 * i + 1]));
+                if constexpr (MODE != PRODUCT_QUANTIZED) y = y + pair(res[2 * i], res[2 * i + 1]);
+                else if (ep.residual) y = plus(y, res[2 * i], res[2 * i + 1]);
+                const float2 f = both(y);
                 v[2 * i] = f.x; v[2 * i + 1] = f.y;
             }
         } else {
@@ -328,7 +339,7 @@ __device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcAr
 #pragma unroll
                     for (int j = 0; j < 8; ++j) f[j] = scaled(f[j], r, scales[j], bias[j]);
                 }
-                epilogue8<T, NEXT, decltype(act)::value>(ep, row, c0, MODE == PRODUCT_QUANTIZED ? nullptr : bias, f, narrow ? stage_addr + (uint32_t)(row - row0) * 128 : 0u);
+                epilogue8<T, MODE, decltype(act)::value>(ep, row, c0, MODE == PRODUCT_QUANTIZED ? nullptr : bias, f, narrow ? stage_addr + (uint32_t)(row - row0) * 128 : 0u);
             }
         });
         if (narrow) {
@@ -472,7 +483,9 @@ __device__ __forceinline__ void block_rows(const CUtensorMap* map_out, const Epi
             float r[8];
             to_floats(load8(static_cast<const T*>(ep.residual) + row * ep.ldr, col0 + 8 * j, ep.cols, 8u), r);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[4 * j + i] = z[4 * j + i] + pair(r[2 * i], r[2 * i + 1]);
+            for (int i = 0; i < 4; ++i)
+                if constexpr (PRODUCT == PRODUCT_QUANTIZED) z[4 * j + i] = plus(z[4 * j + i], r[2 * i], r[2 * i + 1]);
+                else z[4 * j + i] = z[4 * j + i] + pair(r[2 * i], r[2 * i + 1]);
         }
     }
     if constexpr (MODE == PRODUCT_INPUT && ACT != SC_ACT_NONE) {
@@ -807,7 +820,7 @@ __device__ __forceinline__ void tokens_out(const Epilogue& ep, const int (&part)
     load_bias<T, PRODUCT_FORWARD>(ep, c0, bias);
     load_col_scales<PRODUCT_QUANTIZED>(ep, c0, scales);
     scale8<PRODUCT_QUANTIZED>(ep, m, scales, bias, f);
-    with_activation(ep.act, [&](auto act) { epilogue8<T, PRODUCT_FORWARD, decltype(act)::value>(ep, m, c0, nullptr, f); });
+    with_activation(ep.act, [&](auto act) { epilogue8<T, PRODUCT_QUANTIZED, decltype(act)::value>(ep, m, c0, nullptr, f); });
 }
 
 // The same on 8-bit integers, for one and two tokens: sixteen weights a lane and access, four products an instruction, exact sums.  Rows are
@@ -1052,7 +1065,7 @@ __global__ void __launch_bounds__(256) product_join_kernel(const float* partial,
             load_bias<T, NEXT>(ep, c0, bias);
             load_col_scales<MODE>(ep, c0, scales);
             scale8<MODE>(ep, row, scales, bias, f);
-            with_activation(ep.act, [&](auto act) { epilogue8<T, NEXT, decltype(act)::value>(ep, row, c0, MODE == PRODUCT_QUANTIZED ? nullptr : bias, f); });
+            with_activation(ep.act, [&](auto act) { epilogue8<T, MODE, decltype(act)::value>(ep, row, c0, MODE == PRODUCT_QUANTIZED ? nullptr : bias, f); });
         }
     }
 }

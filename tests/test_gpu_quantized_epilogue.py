@@ -56,3 +56,38 @@ def test_scales_far_from_one(ctx, M, N, K):
         ctx.sc_linear_quantized(sc.SC_ACT_NONE, torch.zeros_like(x), xs, w, ws, y, bias=bias)
         assert torch.equal(y, bias.expand(M, N))
     ctx.sc_debug_layer_tiles()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("M,N,K", [(1, 40, 64), (2, 136, 272), (7, 64, 400), (30, 72, 400), (150, 264, 400), (300, 513, 1024)])
+def test_every_path_gives_the_same_bits(ctx, dtype, act, M, N, K):
+    """y and the checkpoint of z, zeros' signs among them, with and without bias and residual.  z reaches from where the activations are curved
+    to where they have become 0 or z."""
+    g = torch.Generator(device="cuda").manual_seed(N)
+    x, w = (torch.randint(-127, 128, (r, K), generator=g, device="cuda").to(torch.int8) for r in (M, N))
+    x[-1] = 0 if M > 1 else x[-1]
+    xs = torch.exp2(torch.randint(-14, -4, (M,), generator=g, device="cuda").float()) * (1 + torch.rand(M, generator=g, device="cuda"))
+    ws = torch.rand(N, generator=g, device="cuda") / K ** 0.5
+    ws[3] = -ws[3]
+    bias = torch.randn(N, generator=g, device="cuda").to(dtype)
+    bias[:2] = torch.tensor([0.0, -0.0])
+    residual = torch.randn(M, N, generator=g, device="cuda").to(dtype)
+    residual[:, 1:4] = torch.tensor([0.0, -0.0, 0.0], device="cuda").to(dtype)
+    for b in (None, bias):
+        for r in (None, residual):
+            want, kept = None, None
+            for tile, parts, extra, offset in paths(M, K):
+                ctx.sc_debug_layer_tiles(*tile, parts)
+                for keep in (False, True):
+                    y = strided(torch.zeros(M, N, device="cuda", dtype=dtype), extra, offset)
+                    q, scales = sc.checkpoint_buffers(M, N) if keep else (None, None)
+                    ctx.sc_linear_quantized(sc.ACTIVATIONS[act], x, xs, w, ws, y, bias=b, residual=None if r is None else strided(r, extra, offset), q=q, scales=scales)
+                    y, path = y.contiguous().view(torch.int16), (tile, parts, extra, offset, b is not None, r is not None, keep)
+                    want = y if want is None else want
+                    differing = int((y != want).sum())
+                    assert differing == 0, path
+                    if keep:
+                        kept = (q, scales) if kept is None else kept
+                        assert torch.equal(q, kept[0]) and torch.equal(scales, kept[1]), path
+    ctx.sc_debug_layer_tiles()
