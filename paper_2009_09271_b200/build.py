@@ -13,7 +13,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparsecomm.so")
 SOURCES = ["sc_api.cu", "sc_layer.cu", "sc_norm.cu", "sc_quantized.cu"]
-# the layer operators' calls without ctypes; the binding does without where Python's or torch's headers are not installed
+# the layer operators' calls without ctypes; the binding does without where Python's headers are not installed, and without the calls that
+# take tensors where torch's are not, or do not compile
 CALLS_SOURCE = os.path.join(CSRC, "sc_calls.cpp")
 CALLS = os.path.join(HERE, "_sc_calls" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
@@ -56,15 +57,18 @@ def _cxx():
 
 
 def _calls_wanted() -> bool:
-    return (os.path.exists(os.path.join(_python_headers(), "Python.h")) and _cxx() is not None
-            and os.path.exists(os.path.join(_torch_home(), "include", "torch", "csrc", "autograd", "python_variable.h")))
+    return os.path.exists(os.path.join(_python_headers(), "Python.h")) and _cxx() is not None
 
 
-def _calls_command() -> list:
+def _calls_commands() -> list:
+    """Commands that make the compiled caller, the preferred one first."""
+    plain = [_cxx(), "-O2", "-std=c++17", "-shared", "-fPIC", "-I", _python_headers(), "-o", CALLS, CALLS_SOURCE]
     home = _torch_home()
     include, lib = os.path.join(home, "include"), os.path.join(home, "lib")
-    return [_cxx(), "-O2", "-std=c++17", "-shared", "-fPIC", "-I", _python_headers(), "-I", include, "-I", os.path.join(include, "torch", "csrc", "api", "include"),
-            "-o", CALLS, CALLS_SOURCE, "-L", lib, "-lc10", "-ltorch_cpu", "-ltorch_python"]
+    if not os.path.exists(os.path.join(include, "torch", "csrc", "autograd", "python_variable.h")):
+        return [plain]
+    return [plain + ["-DSC_TENSORS", "-I", include, "-I", os.path.join(include, "torch", "csrc", "api", "include"), "-L", lib, "-lc10", "-ltorch_cpu", "-ltorch_python"],
+            plain]
 
 
 def _caller_is_current() -> bool:
@@ -105,9 +109,12 @@ def build(force: bool = False, verbose: bool = False) -> str:
             if link.returncode != 0:
                 failed = "nvcc failed linking libsparsecomm.so"
         if not failed and _calls_wanted():
-            made = subprocess.run(_calls_command(), capture_output=True, text=True)
-            said.append(made.stdout + made.stderr)
-            if made.returncode != 0:
+            for command in _calls_commands():
+                made = subprocess.run(command, capture_output=True, text=True)
+                said.append(made.stdout + made.stderr)
+                if made.returncode == 0:
+                    break
+            else:
                 failed = f"the C++ compiler failed building {os.path.basename(CALLS)}"
     if failed or verbose:
         sys.stderr.write("".join(said))

@@ -4,9 +4,15 @@
 //
 // The operators around a layer (norm, dropout, 8-bit rows and their product) have a second form that takes the tensors themselves: Python
 // needs 0.4 us to look at a matrix, and a norm has seven.  It checks what the binding checks and calls the library; for any argument
-// that it does not take as it is, it returns None, and the binding's own checks say what is wrong.
+// that it does not take as it is, it returns None, and the binding's own checks say what is wrong.  That form needs torch's headers and is
+// built with SC_TENSORS; the rest needs Python's alone.
+#ifdef SC_TENSORS
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/version.h>
+#else
+#define PY_SSIZE_T_CLEAN
+#include <Python.h>
+#endif
 
 #include "../../include/sparsecomm.h"
 
@@ -135,6 +141,7 @@ static PyObject* bind(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 }
 
 // -- calls that take tensors ---------------------------------------------------------------------------------
+#ifdef SC_TENSORS
 namespace {
 
 // What is wrong with an argument is not said here: the first failed check ends the call, whose answer is None.
@@ -347,6 +354,7 @@ PyObject* rms_norm_grad(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 }  // namespace
+#endif
 
 #define METHOD(name, f) {name, (PyCFunction)(void (*)(void))f, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {METHOD("bind", bind),
@@ -362,17 +370,21 @@ static PyMethodDef methods[] = {METHOD("bind", bind),
                                 METHOD("sc_dropout", sc_dropout_py),
                                 METHOD("sc_rms_norm", sc_rms_norm_py),
                                 METHOD("sc_rms_norm_grad", sc_rms_norm_grad_py),
+#ifdef SC_TENSORS
                                 METHOD("quantize", quantize),
                                 METHOD("dequantize", dequantize),
                                 METHOD("linear_quantized", linear_quantized),
                                 METHOD("dropout", dropout),
                                 METHOD("rms_norm", rms_norm),
                                 METHOD("rms_norm_grad", rms_norm_grad),
+#endif
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_sc_calls", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__sc_calls(void) {
     PyObject* m = PyModule_Create(&definition);
+#ifdef SC_TENSORS
     // the tensors' layout is that of the headers it was built with: the binding compares
     if (m && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) < 0) Py_CLEAR(m);
+#endif
     return m;
 }
