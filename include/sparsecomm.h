@@ -235,7 +235,7 @@ int sc_step_host(sc_ctx* ctx, int scheme, int W, const float* h_grads, float* re
  * relu's slope is 0.  The value q * 2^e is exactly a value of
  * the type, so what reads a checkpoint adds no rounding of its own.
  * --------------------------------------------------------------------------------------------------------- */
-enum { SC_BF16 = 0, SC_F16 = 1, SC_F32 = 2 /* checkpoints only */ };
+enum { SC_BF16 = 0, SC_F16 = 1, SC_F32 = 2 /* checkpoints and 8-bit rows only */ };
 enum { SC_ACT_NONE = 0, SC_ACT_RELU = 1, SC_ACT_GELU = 2 /* z Phi(z) */,
        SC_ACT_GELU_TANH = 3 /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */, SC_ACT_SILU = 4 /* z / (1 + e^-z) */ };
 
@@ -284,7 +284,11 @@ int sc_linear_grad_weight(sc_ctx* ctx, int type, const void* dz, size_t lddz, co
 /* ---------------------------------------------------------------------------------------------------------
  * What stands between two such layers of a residual network, and a linear layer on 8-bit integers.  The conventions are the layer
  * operators': types SC_BF16 and SC_F16, matrices as rows ld apart, fp32 inside and one rounding at the end, empty sizes allowed,
- * sc_layer_reserve(rows, cols, cols) for a call's workspace.
+ * sc_layer_reserve(rows, cols, cols) for a call's workspace (the product's: M, N, K).
+ *
+ * The order in which a row of the norm is summed goes with the row's length and with where the first operand's row begins within 16 bytes;
+ * for the gradient also with whether the other operands' rows begin alike and whether there are more rows than 16 an SM.  The same call
+ * gives the same bits; equal rows at other places, or among another number of rows, may differ in the last bit of their sum.
  *
  * 8-bit rows of a matrix: q int8, and scales, one fp32 a row.  With m the row's largest magnitude the scale is m / 127 (at most the
  * largest number whose 127-fold is finite) and q = rint(v * (127 * (1 / m))), each operation rounded to fp32, ties to even; the value is
@@ -301,7 +305,8 @@ int sc_dequantize(sc_ctx* ctx, int type, const int8_t* q, size_t ldq, const floa
  * z[m, n] = (sum_k x[m, k] w[n, k]) * x_scales[m] * w_scales[n] + bias[n], y = act(z) + residual, the checkpoint of z on request; y may be
  * residual (same ld).  The sums are exact integers, and what follows them is the same roundings on every path: a result depends on its
  * row and column alone, not on the number of tokens, on where anything lies, or on how the sum was cut.  z is infinite only
- * where the scaled sum is beyond fp32's range, whichever scale is the large one; K < 131072 (SC_ERR_RANGE).  Its gradients are the layer operators': sc_linear_grad_input with W in 16 bits, and sc_linear_grad_weight with x from sc_dequantize (the
+ * where the scaled sum is beyond fp32's range, whichever scale is the large one; K < 131072 (SC_ERR_RANGE).  Its gradients are the
+ * layer operators': sc_linear_grad_input with W in 16 bits, and sc_linear_grad_weight with x from sc_dequantize (the
  * rounding to 8 bits is passed straight through). */
 int sc_linear_quantized(sc_ctx* ctx, int type, int act, const int8_t* x, size_t ldx, const float* x_scales, const int8_t* w, size_t ldw,
                         const float* w_scales, const void* bias, const void* residual, size_t ldr, size_t M, size_t N, size_t K, void* y, size_t ldy,
@@ -318,8 +323,8 @@ int sc_dropout(sc_ctx* ctx, int type, const void* x, size_t ldx, const void* res
 /* h = residual + dropout(x; p, seed), r = (mean of the row's h^2 + eps)^(-1/2), y = (h gamma) r; gamma[cols] is of the type, residual may be
  * NULL, p = 0 drops nothing.  y is written in 16 bits, as 8-bit rows (q and scales), or both; h on request (NULL: not written).  y is
  * made from the fp32 h in two products, each rounded to fp32, and q and scales are the 8-bit rows of that y before its own rounding to 16
- * bits.  Squares are summed in fp32: a row whose sum is not finite gives NaN; h gamma is formed before it is multiplied by
- * r, and has to stay within fp32's range.  h and y may be x or residual (same ld), each another. */
+ * bits.  Squares are summed in fp32: a row whose sum is not finite gives NaN, and so does one whose squares add up to 0 where eps is 0;
+ * h gamma is formed before it is multiplied by r, and has to stay within fp32's range.  h and y may be x or residual (same ld), each another. */
 int sc_rms_norm(sc_ctx* ctx, int type, const void* x, size_t ldx, const void* residual, size_t ldr, const void* gamma, float eps, double p, uint64_t seed,
                 size_t rows, size_t cols, void* h, size_t ldh, void* y, size_t ldy, int8_t* q, size_t ldq, float* scales, void* stream);
 

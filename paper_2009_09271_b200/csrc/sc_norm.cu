@@ -213,7 +213,7 @@ int run_norm_grad(sc_ctx* c, NormGradArgs a, float* dgamma, cudaStream_t st) {
     SC_TEAM(32, 1) SC_TEAM(32, 2)
     // Up to some thousand cut rows are over sooner with a chunk a thread, whose code is fetched cold (509 x 1001: 6.1 against 7.9 us, 2000 x 1001
     // 11.0 against 12.9); more are not (4000 x 1001: 16.4 against 16.3, 16384 x 1001 42 against 31), nor are rows without ends (2048 x 1024:
-    // 9.5 against 8.2).
+    // 9.5 against 8.2).  The order of a row's sums goes with the choice.
     if (ringed && !unshifted(a.phase, a.cols) && chunks <= 128 && a.rows <= 16ull * c->sm_count)
         return drop ? launch_norm_grad<T, 128, 1, true, false>(c, a, dgamma, st) : launch_norm_grad<T, 128, 1, false, false>(c, a, dgamma, st);
     SC_TEAM(32, 4) SC_TEAM(128, 2) SC_TEAM(256, 2) SC_TEAM(256, 4) SC_TEAM(512, 4)

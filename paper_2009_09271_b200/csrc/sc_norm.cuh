@@ -335,11 +335,12 @@ __global__ void __launch_bounds__(NORM_THREADS) rms_norm_kernel(NormArgs a, floa
 }
 
 // The same with the row in registers, V times eight elements a thread, and its inputs read once.  h leaves before the reduction; what stays
-// for after it is h gamma, of which y is a multiple.  Bound by HBM: 16384 x 8192 bf16 with residual in 158 us (6.8 TB/s, 1.04 of the copy
-// rate), to 8 bits 138 us, with dropout 166 and 160 (0.99, 0.90).  A row of 8192 in 256 threads: what is kept decides how many rows an SM
-// has in flight.  With gamma kept in its own type and h stored after the reduction the 8-bit form took 212 us.  Rows of 16384 and more
-// leave room for two CTAs an SM and one (8192 x 16384 162 us, 2000 x 20000 68).  Held to 40 registers rows of 4096 without a residual take 46.6
-// us instead of 48.4.  Rows with ends: 16384 x 4097 97 us (0.85), 16384 x 1001 25.7 (0.78).  One token of 4096 takes 1.9 us.
+// for after it is h gamma, which becomes y, and y the bytes.  Bound by HBM: 16384 x 8192 bf16 with residual in 158 us (6.8 TB/s, 1.04 of the copy
+// rate), to 8 bits 139 us, with dropout 166 and 156 (0.99, 0.92).  A row of 8192 in 256 threads: what is kept decides how many rows an SM
+// has in flight, and to 8 bits without residual and h they are too few (16384 x 8192 77 us, 0.80; 16384 x 4096 44, 0.70).  With gamma kept in its own
+// type and h stored after the reduction the 8-bit form took 212 us.  Rows of 16384 and more leave room for two CTAs an SM and one (8192 x 16384
+// 165 us, 2000 x 20000 68).  Held to 40 registers rows of 4096 without a residual take 46.6 us instead of 48.4.  Rows with ends: 16384 x 4097
+// 97 us (0.85), 16384 x 1001 26 (0.77); to 8 bits without residual 75 (0.41) and 23 (0.33).  One token of 4096 takes 1.9 us.
 template <typename T, int TEAM, int V, bool DROP, bool WIDE>
 __global__ void __launch_bounds__(TEAM == 32 ? 256 : TEAM, TEAM == 32 ? 3 : TEAM == 1024 ? 1 : TEAM >= 256 && V == 4 ? 1024 / TEAM - (DROP && TEAM == 256) : V == 2 && WIDE && !DROP ? 1536 / TEAM : 1024 / TEAM)
 rms_norm_rows_kernel(NormArgs a, float* scales) {

@@ -350,10 +350,7 @@ __device__ __forceinline__ void block_out(const CUtensorMap* map_out, const TcAr
     __syncwarp();
 }
 
-// One 32 x 32 block of a 16-bit result, thread t holding row t from TMEM to the end: a checkpoint group is one thread's own, its
-// bytes go out as one sector, and the result leaves by TMA from a 2 KB buffer of 64-byte rows (64-byte swizzle), two of
-// which take turns.  About a third of the instructions of block_out, which serves rows of other alignments.
-// What its columns have in common, one lane a column: fetched while the block before is worked on (the first one while the sums are awaited),
+// What a block's columns have in common, one lane a column: fetched while the block before is worked on (the first one while the sums are awaited),
 // handed to the block's threads through shared memory.  Read from HBM's side by every thread, bias and scales were half of the
 // epilogue: 8192 x 8192 x 1024 in 8 bits took 111 us, 78 without a bias.
 struct BlockColumn { float scale; uint16_t bias; };
@@ -379,6 +376,9 @@ __device__ __forceinline__ void block_columns(const BlockColumn& c, uint32_t at)
     }
 }
 
+// One 32 x 32 block of a 16-bit result, thread t holding row t from TMEM to the end: a checkpoint group is one thread's own, its
+// bytes go out as one sector, and the result leaves by TMA from a 2 KB buffer of 64-byte rows (64-byte swizzle), two of
+// which take turns.  About a third of the instructions of block_out, which serves rows of other alignments.
 template <typename T, int PRODUCT, int ACT>
 __device__ __forceinline__ void block_rows(const CUtensorMap* map_out, const Epilogue& ep, uint32_t buffer, uint32_t columns, float row_scale, const uint32_t (&v)[32],
                                            uint64_t row0, uint32_t col0, uint32_t& scale4) {

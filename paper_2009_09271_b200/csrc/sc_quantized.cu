@@ -20,9 +20,9 @@ void run_eights(const Stored& x, const Stored& w, const Epilogue& ep, cudaStream
     else launch(quantized_eights_kernel<T, EIGHTS, 1>, (uint32_t)ceil_div(ep.cols, 16), TOKENS_WK * 32, 0, 1, st, xp, x.ld, wp, w.ld, K, ep);
 }
 
-// What the kernels without tiles take: rows that are 16-byte aligned and a multiple of 16 long.  Up to 8 tokens they are ahead of the tiles or
-// even with them (8 x 4096 x 4096: 7.7 against 10.5 us, 8 x 16384 x 4096 18.2 against 20.3, 8 x 4096 x 16384 19.3 against 17.8), up to 32
-// while the weights are few (32 x 4096 x 4096 11.0 against 11.9, 16 x 16384 x 4096 26 against 20).
+// What the kernels without tiles take: rows that are 16-byte aligned and a multiple of 16 long.  Up to 8 tokens they are ahead of the tiles
+// (8 x 4096 x 4096: 7.3 against 10.5 us, 8 x 16384 x 4096 19 against 20), but for long sums, where they are up to a tenth behind (8 x 4096 x 16384 19.5 against
+// 17.8), and up to 32 while the weights are few (32 x 4096 x 4096 10.7 against 11.5; 16 x 16384 x 4096 26 against 17).
 bool few_tokens(const Stored& x, const Stored& w) {
     return tma_ready(x) && tma_ready(w) && x.cols % 16 == 0 && (x.rows <= 8 || (x.rows <= 32 && w.rows * w.cols <= (32u << 20)));
 }
