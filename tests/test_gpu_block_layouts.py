@@ -130,3 +130,58 @@ def test_product_keeps_to_its_rows(ctx, M, N, K):
         ctx.sc_linear_quantized(sc.SC_ACT_SILU, a.at, xs, b.at, ws, y.at, residual=c.at, q=q.at.view(M, N), scales=s.at.view(M, -1))
         assert torch.equal(y.at, want) and torch.equal(q.at.view(M, N), kept[0]) and torch.equal(s.at.view(M, -1), kept[1])
         assert y.kept() and q.kept() and s.kept()
+
+
+@pytest.mark.parametrize("M", [1, 7, 30, 300])
+@pytest.mark.parametrize("N,K", [(72, 400), (33, 129)])
+def test_product_onto_its_residual(ctx, M, N, K):
+    g = rng(M + N)
+    x, w = (torch.randint(-127, 128, (n, K), generator=g, device="cuda").to(torch.int8) for n in (M, N))
+    xs, ws = torch.rand(M, generator=g, device="cuda") / 64, torch.rand(N, generator=g, device="cuda") / 64
+    r = torch.randn(M, N, generator=g, device="cuda").bfloat16()
+    want = torch.empty_like(r)
+    ctx.sc_linear_quantized(sc.SC_ACT_GELU, x, xs, w, ws, want, residual=r)
+    for tile, parts in (((0, 0), 0), ((128, 64), 1), ((128, 128), 2), ((256, 256), 1)):
+        ctx.sc_debug_layer_tiles(*tile, parts)
+        for extra, offset in ((0, 0), (2, 2), (3, 1)):
+            y = Placed(M, N, torch.bfloat16, extra, offset, 77, r)
+            ctx.sc_linear_quantized(sc.SC_ACT_GELU, x, xs, w, ws, y.at, residual=y.at)
+            assert torch.equal(y.at, want) and y.kept()
+    ctx.sc_debug_layer_tiles()
+
+
+@pytest.mark.parametrize("cols,ld", [(1000, 2 ** 30 + 8), (1001, 2 ** 30 + 9), (40001, 2 ** 30 + 8)])
+def test_rows_further_apart_than_32_bits_reach(ctx, cols, ld):
+    """Four rows, the last one 3 * 2^30 elements in: norm, gradient, dropout, 8-bit rows and a product, against the same rows close together and alike cut."""
+    rows, g = 4, rng(cols)
+
+    def far(values):
+        t = torch.empty(3 * ld + cols, dtype=values.dtype, device="cuda").as_strided((rows, cols), (ld, 1))
+        t.copy_(values)
+        return t
+
+    near = lambda values: Placed(rows, cols, values.dtype, (ld - cols) % 16, 0, 77, values).at  # noqa: E731
+    x, r, gamma = (torch.randn(*s, generator=g, device="cuda").bfloat16() for s in ((rows, cols), (rows, cols), (cols,)))
+    a, b, c, d = far(x), far(r), far(torch.zeros_like(x)), far(torch.zeros_like(x, dtype=torch.int8))
+    na, nb, want, wq = near(x), near(r), near(torch.zeros_like(x)), near(torch.zeros_like(x, dtype=torch.int8))
+    s, ws = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    ctx.sc_rms_norm(a, gamma, EPS, y=c, q=d, scales=s, residual=b, p=0.2, seed=3)
+    ctx.sc_rms_norm(na, gamma, EPS, y=want, q=wq, scales=ws, residual=nb, p=0.2, seed=3)
+    assert torch.equal(c, want) and torch.equal(d, wq) and torch.equal(s, ws)
+    dgamma, wg = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    ctx.sc_rms_norm_grad(b, a, gamma, EPS, c, dgamma=dgamma, residual=a, p=0.2, seed=3)
+    ctx.sc_rms_norm_grad(nb, na, gamma, EPS, want, dgamma=wg, residual=na, p=0.2, seed=3)
+    assert torch.equal(c, want) and torch.equal(dgamma, wg)
+    ctx.sc_dropout(a, c, 0.3, 4, residual=b)
+    ctx.sc_dropout(na, want, 0.3, 4, residual=nb)
+    assert torch.equal(c, want)
+    ctx.sc_quantize(b, d, s)
+    ctx.sc_dequantize(d, s, c)
+    q, ref = rows_in_8_bits(r)
+    assert torch.equal(d.cpu(), q) and torch.equal(s.cpu(), ref) and torch.equal(c.cpu(), (q.float() * ref[:, None]).bfloat16())
+    w, y = q.cuda(), [torch.empty(rows, rows, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    ctx.sc_linear_quantized(sc.SC_ACT_NONE, d, s, w, s, y[0])
+    ctx.sc_linear_quantized(sc.SC_ACT_NONE, w, s, d, s, y[1])
+    exact = (w.double() @ w.double().t()) * s.double()[:, None] * s.double()
+    for got in y:
+        assert_close(got, exact, exact.abs() * 4 * 2.0 ** -24, torch.bfloat16, "product")
